@@ -390,14 +390,14 @@ def _workspace(c, nbytes):
 def _run_own(c):
     b = _binding()
     if c["op"] == "norm":
-        b.headnorm_rope_fwd(c["q"], c["k"], c["q_gain"], c["k_gain"], c["cos_sin"], c["positions"], c["q_out"], c["k_out"], eps=EPS,
+        b.rmsnorm_rope_fwd(c["q"], c["k"], c["q_gain"], c["k_gain"], c["cos_sin"], c["positions"], c["q_out"], c["k_out"], eps=EPS,
                             interleaved=c["interleaved"])
         return [c["q_out"], c["k_out"]]
     if c["op"] == "norm_bwd":
         ws = c.get("workspace")
         if ws is None:
-            ws = _workspace(c, b.headnorm_rope_bwd_workspace_bytes(c["tokens"], c["q_heads"], c["k_heads"], c["dim"]))
-        b.headnorm_rope_bwd(c["q"], c["k"], c["gq"], c["gk"], c["q_gain"], c["k_gain"], c["cos_sin"], c["positions"], c["q_out"],
+            ws = _workspace(c, b.rmsnorm_rope_bwd_workspace_bytes(c["tokens"], c["q_heads"], c["k_heads"], c["dim"]))
+        b.rmsnorm_rope_bwd(c["q"], c["k"], c["gq"], c["gk"], c["q_gain"], c["k_gain"], c["cos_sin"], c["positions"], c["q_out"],
                             c["k_out"], c["dq_gain"], c["dk_gain"], ws, eps=EPS, interleaved=c["interleaved"])
         return [c["q_out"], c["k_out"], c["dq_gain"], c["dk_gain"]]
     if c["op"] == "append":
