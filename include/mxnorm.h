@@ -71,7 +71,8 @@ typedef enum {
     MXN_ERR_WORKSPACE = 5, /* workspace NULL or smaller than the query says */
     MXN_ERR_CUDA = 6,      /* the CUDA runtime reported an error at launch */
     MXN_ERR_TIMEOUT = 7,   /* a bounded device-side wait ran out (reported by mxn_device_timeouts) */
-    MXN_ERR_TOO_LARGE = 8  /* the problem needs more built-in scratch than the library holds */
+    MXN_ERR_TOO_LARGE = 8, /* the problem needs more built-in scratch than the library holds */
+    MXN_ERR_INDEX = 9      /* an index in device memory was out of range (reported by mxn_device_bad_indices) */
 } mxn_status;
 
 /* Power-of-two rounding of the block scale (Section 3.2: "implementation-defined").
@@ -91,11 +92,11 @@ size_t mxn_scale_bytes(int64_t T, int64_t K, mxn_scale_layout layout);
 
 const char* mxn_status_string(mxn_status s);
 
-/* Diagnostics: the one kernel that waits on asynchronous copies (the backward, which feeds its rows through a ring of
- * shared-memory stages filled by the bulk-copy engine) bounds every wait.  A wait that runs out makes its thread block
+/* Diagnostics: the kernels that wait on asynchronous copies (the backward and the attention over the cache, which feed
+ * themselves through rings of shared-memory stages filled by the copy engines) bound every wait.  A wait that runs out makes its thread block
  * stop and bumps a device-side counter instead of hanging: the block requests no further copies, gives the copies it
  * had already requested a second, shorter bounded wait, writes zeros for its share of the dgain partial sums and
- * returns.  After such an event the dx rows that block had not reached yet are unwritten and dgain lacks that block's
+ * returns (the attention likewise, with the keys read so far).  After such an event the dx rows that block had not reached yet are unwritten and dgain lacks that block's
  * rows: the outputs of the affected launch are incomplete and must be discarded.
  *   mxn_device_timeouts synchronises the device, stores the number of such events since the library was loaded (or
  *   since the last reset) into *count_out and returns MXN_ERR_TIMEOUT when it is non-zero, else MXN_OK.
@@ -304,6 +305,103 @@ mxn_status mxnorm_fwd_host(const void* x_host_bf16, int64_t T, int64_t D, int bl
                            mxn_round round, mxn_scale_layout layout,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
 size_t mxnorm_fwd_host_workspace_bytes(int64_t T, int64_t D, int block, mxn_scale_layout layout);
+
+/* ---- queries, keys and values around attention ---------------------------------------------------------
+ * The entry points below take activations as `heads` heads of `head_dim` bf16 elements a token: the heads of a token are
+ * contiguous, tokens are `stride` elements apart (so that queries, keys and values can be slices of one fused projection).
+ * Pointers are 16-byte aligned, strides multiples of 8 elements and at least heads * head_dim; head_dim is a multiple of 16
+ * up to 256 (mxkv_attention: 64 or 128); at most 4096 heads and 2^31 - 1 tokens.  A head count of 0 leaves its pointers unused.
+ *
+ * Rotation: with rot_dim rotated elements (a multiple of 16, at most head_dim; the others are passed on) element pairs
+ *   MXN_ROPE_HALVES: (i, i + rot_dim/2)      MXN_ROPE_PAIRS: (2i, 2i + 1)      i = 0 .. rot_dim/2 - 1
+ * are turned: (a, b) -> (a cos - b sin, b cos + a sin).  cos_sin is fp32 [table_rows, rot_dim], 16-byte aligned: row p holds
+ * the rot_dim/2 cosines, then the rot_dim/2 sines of position p (usually of p * base^(-2i/rot_dim), computed in binary64).
+ * Products and sums of the rotation are single binary32 operations.
+ *
+ * Indices that live in device memory cannot be refused by the call; the kernels check them.  A position outside the table,
+ * a page number outside the pool, a length shorter than the new tokens: the token or block concerned is left out as stated
+ * at each entry point and a device-side counter is raised, nothing is read or written out of bounds.
+ * mxn_device_bad_indices synchronises the device, stores the counter (since the library was loaded or the last reset) into
+ * *count_out and returns MXN_ERR_INDEX when it is non-zero, else MXN_OK. */
+mxn_status mxn_device_bad_indices(unsigned int* count_out);
+mxn_status mxn_device_bad_indices_reset(void);
+
+typedef enum { MXN_ROPE_HALVES = 0, MXN_ROPE_PAIRS = 1 } mxn_rope;
+
+/* RMS norm of every query and key head, with the position rotation in the same pass.
+ *   normalise == 1: u = x / sqrt(mean(x^2) + eps) * gain over each head (gain_bf16 [head_dim], NULL = ones); a head of
+ *   zeros stays zero for eps = 0.  normalise == 0: u = x (gains must be NULL).
+ *   y = rotation of u by the token's position (cos_sin NULL: y = u); positions int32 [T], NULL = row index.
+ *   Outputs bf16, rounded once; they may be the inputs themselves (same pointer and stride), other overlaps are not allowed.
+ *   A token whose position lies outside the table gets NaN.  Sums in binary32. */
+mxn_status rmsnorm_rope_fwd(const void* q_bf16, int64_t q_stride, int q_heads, const void* k_bf16, int64_t k_stride, int k_heads,
+                            int64_t T, int head_dim, int normalise, const void* q_gain_bf16_or_null,
+                            const void* k_gain_bf16_or_null, float eps, const float* cos_sin_or_null, int64_t table_rows, int rot_dim,
+                            mxn_rope pairing, const int32_t* positions_or_null, void* q_out_bf16, int64_t q_out_stride,
+                            void* k_out_bf16, int64_t k_out_stride, void* cuda_stream);
+
+/* Its gradient, from the forward's inputs (1/rms is computed again, nothing has to be saved).
+ *   du = rotation of grad by the opposite angle;  n = x / rms;  dgain_j = sum over tokens and heads of du_j n_j (fp32
+ *   [head_dim], NULL = not wanted);  h = du * gain;  dx = (h - n mean(h n)) / rms, bf16, may be written over x or over grad
+ *   (same pointer and stride).  normalise == 0: dx = du, the inputs are not read and may be NULL, dgain must be NULL.
+ *   The gradients of the gains are summed in a fixed order through `workspace` (device memory, 16-byte aligned, at least
+ *   rmsnorm_rope_bwd_workspace_bytes(T, ...) bytes, contents irrelevant before and after; NULL when no dgain is wanted).  The
+ *   size does not decrease with T.  Calls that may overlap need workspaces of their own.  T == 0 writes zeros to dgain.
+ *   A token whose position lies outside the table gets NaN and adds nothing to dgain. */
+mxn_status rmsnorm_rope_bwd(const void* q_bf16_or_null, int64_t q_stride, int q_heads, const void* k_bf16_or_null, int64_t k_stride,
+                            int k_heads, const void* grad_q_bf16, int64_t grad_q_stride, const void* grad_k_bf16,
+                            int64_t grad_k_stride, int64_t T, int head_dim, int normalise, const void* q_gain_bf16_or_null,
+                            const void* k_gain_bf16_or_null, float eps, const float* cos_sin_or_null, int64_t table_rows, int rot_dim,
+                            mxn_rope pairing, const int32_t* positions_or_null, void* dq_bf16, int64_t dq_stride, void* dk_bf16,
+                            int64_t dk_stride, float* q_dgain_f32_or_null, float* k_dgain_f32_or_null, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+size_t rmsnorm_rope_bwd_workspace_bytes(int64_t T, int q_heads, int k_heads, int head_dim);
+
+/* The paged cache: pages of page_size tokens (a power of two, 16 .. 256), keys and values apart.
+ *   codes  u8 [num_pages, kv_heads, page_size, head_dim]   E4M3, 16-byte aligned
+ *   scales u8 [num_pages, kv_heads, page_size / block]     E8M0, one for each block of tokens (16, 32 or 64, at most a page)
+ *                                                          of a head;  value = code * 2^(scale - 127)
+ *   page_table int32 [n_seqs, max_pages]: token t of sequence s is in page page_table[s][t / page_size] at t % page_size.
+ * Sequences are packed: rows cu[s] .. cu[s+1] - 1 of the activations belong to sequence s (int32 [n_seqs + 1], rising); rows
+ * before cu[0] and from cu[n_seqs] on are neither read nor written.  kv_lens int32 [n_seqs] counts a sequence's tokens
+ * WITH the new ones, so row cu[s+1] - 1 is token kv_lens[s] - 1 in both entry points below.
+ *
+ * Append: writes the new tokens' keys (rotated by their place in the sequence when cos_sin is given) and values.
+ *   Scale of a block of one head: S = 2^(ceil(log2 absmax) - 8) over its tokens, as in mx_cast; codes = E4M3(x / S).
+ *   A block that holds earlier tokens keeps at least its scale: where the new tokens need more, the earlier codes are rounded
+ *   again on the new scale (exact unless they become subnormal).  Appending the same tokens to the same places again changes
+ *   nothing.  Other tokens' codes and other blocks' scales are left as they were.
+ *   The blocks written must belong to one sequence only (pages shared by sequences are full pages, or are copied first).
+ *   A block whose page is out of range, or whose tokens lie outside the table, is left out; so are all tokens of a sequence
+ *   whose kv_lens is smaller than its number of new tokens. */
+mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16, int64_t v_stride, int64_t n_tokens, int kv_heads,
+                       int head_dim, const int32_t* cu_tokens, int64_t n_seqs, const int32_t* kv_lens, const int32_t* page_table,
+                       int64_t max_pages, int64_t num_pages, int page_size, int block, const float* cos_sin_or_null,
+                       int64_t table_rows, int rot_dim, mxn_rope pairing, void* k_codes_u8, void* k_scales_u8, void* v_codes_u8,
+                       void* v_scales_u8, void* cuda_stream);
+
+/* Attention of new queries over the cache: out = softmax(scale * q k^T) v for each query row and head.
+ *   q, out bf16 [n_tokens, q_heads, head_dim], head_dim 64 or 128; query head i reads key head i / (q_heads / kv_heads).
+ *   The query in row cu_q[s+1] - 1 stands at place kv_lens[s] - 1 of its sequence, the ones before it at the places before.
+ *   causal == 1: it sees the keys up to its own place (causal == 0: all of the sequence); window > 0: of those not more than
+ *   `window` places back, its own included.  A row that sees no key gets zeros and lse = -infinity.
+ *   max_q_len and max_kv_len bound the sequences' new queries and lengths (host values; they shape the launch: queries past
+ *   max_q_len are not computed - their rows may receive undefined values - and keys past max_kv_len are not seen).
+ *   lse_out [n_tokens, q_heads] fp32: the logarithm of the sum of exp(scale q k) over the keys seen.
+ *   Products run on the E4M3 codes with binary32 sums; q enters exactly (elements below 2^-14 of their row's largest: to
+ *   2^-22 of it), the softmax's weights with 8 significant bits, its sums in binary32.
+ *   What stands in the cache behind a sequence's last token, or in pages no visible key is in, has no influence.  A page out of
+ *   range among the visible ones: its keys are left out.
+ *   workspace: device memory, 16-byte aligned, at least mxkv_attention_workspace_bytes(...) bytes for the same sizes (0: none
+ *   needed); contents irrelevant before and after.  Calls that may overlap need workspaces of their own. */
+mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                          const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                          const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                          const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8,
+                          float scale, int causal, int64_t window, void* out_bf16, int64_t out_stride, float* lse_out_or_null,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads,
+                                      int kv_heads, int head_dim);
 
 #ifdef __cplusplus
 }

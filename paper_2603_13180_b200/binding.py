@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libmxnorm.so")
 
 ROUND_RCEIL_POW2, ROUND_FLOOR_OCP, ROUND_RCEIL_MAX = 0, 1, 2
 SCALES_ROWMAJOR, SCALES_SWIZZLE_128x4 = 0, 1
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 OK = 0
 
 EXPORTS = ("mxn_scale_bytes", "mxn_status_string", "mx_cast", "rmsnorm_mxfp8_fwd", "mxnorm_fwd",
@@ -24,7 +25,9 @@ EXPORTS = ("mxn_scale_bytes", "mxn_status_string", "mx_cast", "rmsnorm_mxfp8_fwd
            "mxn_device_timeouts", "mxn_device_timeouts_reset", "mxn_selftest_bounded_wait", "mx_cast_fp4", "rmsnorm_mxfp4_fwd", "mxnorm_mxfp4_fwd",
            "mx_cast_transposed", "rmsnorm_nvfp4_fwd", "mxn_selftest_division", "mxn_selftest_dispatch",
            "mx_cast_e5m2", "mx_cast_transposed_e5m2", "mxnorm_postround_fwd",
-           "mxnorm_add_fwd", "mx_cast_nvfp4")
+           "mxnorm_add_fwd", "mx_cast_nvfp4", "mxn_device_bad_indices", "mxn_device_bad_indices_reset",
+           "rmsnorm_rope_fwd", "rmsnorm_rope_bwd", "rmsnorm_rope_bwd_workspace_bytes", "mxkv_append", "mxkv_attention",
+           "mxkv_attention_workspace_bytes")
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -71,11 +74,26 @@ lib.mx_cast_transposed.argtypes = [_vp, _vp, _i64, _i64, _f32, _vp, _vp, _i32, _
 lib.mxnorm_bwd_noalloc.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _i32, _vp, _vp]
 lib.mxnorm_bwd_noalloc_max_scratch_bytes.argtypes = []
 lib.mxnorm_bwd_noalloc_max_scratch_bytes.restype = _sz
+lib.mxn_device_bad_indices.argtypes = [ctypes.POINTER(ctypes.c_uint)]
+lib.mxn_device_bad_indices_reset.argtypes = []
+lib.rmsnorm_rope_fwd.argtypes = [_vp, _i64, _i32, _vp, _i64, _i32, _i64, _i32, _i32, _vp, _vp, _f32, _vp, _i64, _i32, _i32, _vp,
+                                 _vp, _i64, _vp, _i64, _vp]
+lib.rmsnorm_rope_bwd.argtypes = [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp, _f32, _vp, _i64,
+                                 _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
+lib.rmsnorm_rope_bwd_workspace_bytes.argtypes = [_i64, _i32, _i32, _i32]
+lib.rmsnorm_rope_bwd_workspace_bytes.restype = _sz
+lib.mxkv_append.argtypes = [_vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _i32, _i32,
+                            _vp, _vp, _vp, _vp, _vp]
+lib.mxkv_attention.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp, _vp,
+                               _vp, _f32, _i32, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+lib.mxkv_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i32, _i32, _i32]
+lib.mxkv_attention_workspace_bytes.restype = _sz
 for _name in ("mx_cast", "rmsnorm_mxfp8_fwd", "mxnorm_fwd", "mxnorm_nvfp4_fwd", "mxnorm_bwd", "mxnorm_fwd_host",
               "mxnorm_bwd_noalloc", "mx_cast_fp4", "rmsnorm_mxfp4_fwd", "mxnorm_mxfp4_fwd",
            "mx_cast_transposed", "rmsnorm_nvfp4_fwd", "mxn_selftest_division", "mxn_selftest_dispatch",
            "mx_cast_e5m2", "mx_cast_transposed_e5m2", "mxnorm_postround_fwd",
-           "mxnorm_add_fwd", "mx_cast_nvfp4"):
+           "mxnorm_add_fwd", "mx_cast_nvfp4", "mxn_device_bad_indices", "mxn_device_bad_indices_reset", "rmsnorm_rope_fwd",
+           "rmsnorm_rope_bwd", "mxkv_append", "mxkv_attention"):
     getattr(lib, _name).restype = _i32
 
 
@@ -306,3 +324,181 @@ def mxnorm_add_fwd(x, residual, h_out, codes, scales, rms_est_out=None, p=2, coe
     T, D = x.shape
     _check(lib.mxnorm_add_fwd(_ptr(x), _ptr(residual), T, D, block, p, coef, eps, _ptr(h_out), _ptr(codes), _ptr(scales),
                               _ptr(rms_est_out), layout, _stream(stream)), "mxnorm_add_fwd")
+
+
+# ---- queries, keys and values around attention ----
+
+def device_bad_indices() -> int:
+    """Synchronises the device and returns how many indices in device memory were found out of range (0 = healthy)."""
+    n = ctypes.c_uint(0)
+    st = lib.mxn_device_bad_indices(ctypes.byref(n))
+    if st not in (OK, 9):
+        raise MXNormError(st, "mxn_device_bad_indices")
+    return int(n.value)
+
+
+def device_bad_indices_reset() -> None:
+    """Synchronises the device and sets the count of indices found out of range back to 0."""
+    _check(lib.mxn_device_bad_indices_reset(), "mxn_device_bad_indices_reset")
+
+
+def _on(device, **tensors):
+    """Every tensor lies on `device`, and that is the current one (calls enqueue on the current device)."""
+    if device.type != "cuda":
+        raise ValueError(f"expected CUDA tensors, not tensors on {device}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _heads(t, name, like=None):
+    """(pointer, token stride, heads) of a bf16 [T, heads, dim] tensor whose heads are contiguous; (None, 0, 0) for None."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype is not torch.bfloat16 or t.dim() != 3:
+        raise ValueError(f"{name}: expected a bf16 tensor [tokens, heads, dim]")
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if like is not None and t.shape != like.shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(like.shape)}")
+    return t.data_ptr(), (st if n > 1 else h * d), h
+
+
+def _vec(t, dtype, name, shape=None):
+    """Pointer of a contiguous tensor (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    return t.data_ptr()
+
+
+def _table(cos_sin):
+    """(pointer, rows, rotated elements) of a rotation table fp32 [rows, rot]."""
+    if cos_sin is None:
+        return None, 0, 0
+    if cos_sin.dim() != 2:
+        raise ValueError("cos_sin: expected [positions, rot_dim]")
+    return _vec(cos_sin, torch.float32, "cos_sin"), cos_sin.shape[0], cos_sin.shape[1]
+
+
+def rmsnorm_rope_fwd(q, k, q_gain, k_gain, cos_sin, positions, q_out, k_out, eps=1e-6, interleaved=False, normalise=True,
+                     stream=None):
+    """RMS norm of every head of q [T, Hq, D] and k [T, Hk, D] (k may be None) and rotation by cos_sin [P, rot] (may be None)
+    at int32 positions [T] (None: row index).  q_out / k_out may be q / k themselves."""
+    _on(q.device, k=k, q_gain=q_gain, k_gain=k_gain, cos_sin=cos_sin, positions=positions, q_out=q_out, k_out=k_out)
+    T, _, D = q.shape
+    if k is not None and (k.shape[0] != T or k.shape[2] != D or k_out is None):
+        raise ValueError("k: expected [tokens, heads, dim] with q's tokens and dim, and a k_out")
+    qp, qs, qh = _heads(q, "q")
+    kp, ks, kh = _heads(k, "k")
+    qop, qos, _ = _heads(q_out, "q_out", q)
+    kop, kos, _ = _heads(k_out if k is not None else None, "k_out", k)
+    tp, rows, rot = _table(cos_sin)
+    _check(lib.rmsnorm_rope_fwd(qp, qs, qh, kp, ks, kh, T, D, 1 if normalise else 0, _vec(q_gain, torch.bfloat16, "q_gain", (D,)),
+                                _vec(k_gain, torch.bfloat16, "k_gain", (D,)), eps, tp, rows, rot, 1 if interleaved else 0,
+                                _vec(positions, torch.int32, "positions", (T,)), qop, qos, kop, kos, _stream(stream)),
+           "rmsnorm_rope_fwd")
+
+
+def rmsnorm_rope_bwd_workspace_bytes(T: int, q_heads: int, k_heads: int, dim: int) -> int:
+    return int(lib.rmsnorm_rope_bwd_workspace_bytes(T, q_heads, k_heads, dim))
+
+
+def rmsnorm_rope_bwd(q, k, grad_q, grad_k, q_gain, k_gain, cos_sin, positions, dq, dk, q_dgain=None, k_dgain=None, workspace=None,
+                     eps=1e-6, interleaved=False, normalise=True, stream=None):
+    """Gradient of rmsnorm_rope_fwd: grad_q / grad_k -> dq / dk (and fp32 q_dgain / k_dgain [D]); q and k are the forward's inputs
+    (None with normalise=False, which does not read them)."""
+    _on(grad_q.device, q=q, k=k, grad_k=grad_k, q_gain=q_gain, k_gain=k_gain, cos_sin=cos_sin, positions=positions, dq=dq, dk=dk,
+        q_dgain=q_dgain, k_dgain=k_dgain, workspace=workspace)
+    T, _, D = grad_q.shape
+    if grad_k is not None and (grad_k.shape[0] != T or grad_k.shape[2] != D or dk is None):
+        raise ValueError("grad_k: expected [tokens, heads, dim] with grad_q's tokens and dim, and a dk")
+    if normalise and (q is None or (k is None) != (grad_k is None)):
+        raise ValueError("q / k: the forward's inputs are needed")
+    gqp, gqs, qh = _heads(grad_q, "grad_q")
+    gkp, gks, kh = _heads(grad_k, "grad_k")
+    qp, qs, _ = _heads(q, "q", grad_q)
+    kp, ks, _ = _heads(k if grad_k is not None else None, "k", grad_k)
+    dqp, dqs, _ = _heads(dq, "dq", grad_q)
+    dkp, dks, _ = _heads(dk if grad_k is not None else None, "dk", grad_k)
+    tp, rows, rot = _table(cos_sin)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.rmsnorm_rope_bwd(qp, qs, qh, kp, ks, kh, gqp, gqs, gkp, gks, T, D, 1 if normalise else 0,
+                                _vec(q_gain, torch.bfloat16, "q_gain", (D,)), _vec(k_gain, torch.bfloat16, "k_gain", (D,)), eps, tp,
+                                rows, rot, 1 if interleaved else 0, _vec(positions, torch.int32, "positions", (T,)), dqp, dqs, dkp, dks,
+                                _vec(q_dgain, torch.float32, "q_dgain", (D,)), _vec(k_dgain, torch.float32, "k_dgain", (D,)),
+                                _ptr(workspace), ws_bytes, _stream(stream)), "rmsnorm_rope_bwd")
+
+
+def alloc_kv_cache(num_pages: int, kv_heads: int, page_size: int, dim: int, block: int = 16, device="cuda"):
+    """(k_codes, k_scales, v_codes, v_scales) of an empty paged cache: E4M3 codes [pages, heads, page, dim] and one E8M0 scale for
+    each `block` tokens of a head."""
+    def one():
+        return (torch.zeros((num_pages, kv_heads, page_size, dim), dtype=torch.uint8, device=device),
+                torch.zeros((num_pages, kv_heads, page_size // block), dtype=torch.uint8, device=device))
+    return one() + one()
+
+
+def _cache(k_codes, k_scales, v_codes, v_scales):
+    """(pages, heads, page size, dim, block) of a cache's four tensors and their pointers."""
+    if k_codes.dim() != 4 or k_scales.dim() != 3 or k_scales.shape[2] < 1:
+        raise ValueError("cache: expected codes [pages, heads, page, dim] and scales [pages, heads, page / block]")
+    pages, heads, page, dim = k_codes.shape
+    cs, ss = (pages, heads, page, dim), (pages, heads, k_scales.shape[2])
+    return (pages, heads, page, dim, page // k_scales.shape[2] if page % k_scales.shape[2] == 0 else 0,
+            _vec(k_codes, torch.uint8, "k_codes"), _vec(k_scales, torch.uint8, "k_scales", ss),
+            _vec(v_codes, torch.uint8, "v_codes", cs), _vec(v_scales, torch.uint8, "v_scales", ss))
+
+
+def _sequences(cu, lens, page_table):
+    """(sequences, pages a sequence) and the pointers of the three lists."""
+    if page_table.dim() != 2:
+        raise ValueError("page_table: expected int32 [sequences, pages]")
+    s, width = page_table.shape
+    return (s, width, _vec(cu, torch.int32, "cu", (s + 1,)), _vec(lens, torch.int32, "kv_lens", (s,)),
+            _vec(page_table, torch.int32, "page_table"))
+
+
+def mxkv_append(k, v, cu_tokens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, cos_sin=None, interleaved=False, stream=None):
+    """Writes new tokens' keys (rotated by their place when cos_sin is given) and values [n, H, D] into the paged cache.
+    kv_lens counts the new tokens; rows cu_tokens[s] .. cu_tokens[s+1]-1 are the last ones of sequence s."""
+    _on(k.device, v=v, cu_tokens=cu_tokens, kv_lens=kv_lens, page_table=page_table, k_codes=k_codes, k_scales=k_scales,
+        v_codes=v_codes, v_scales=v_scales, cos_sin=cos_sin)
+    pages, heads, page, dim, block, kc, ks, vc, vs = _cache(k_codes, k_scales, v_codes, v_scales)
+    s, width, cup, lp, pt = _sequences(cu_tokens, kv_lens, page_table)
+    kp, kst, kh = _heads(k, "k")
+    vp, vst, _ = _heads(v, "v", k)
+    if kh != heads or k.shape[2] != dim:
+        raise ValueError("k, v: heads and dim differ from the cache's")
+    tp, rows, rot = _table(cos_sin)
+    _check(lib.mxkv_append(kp, kst, vp, vst, k.shape[0], heads, dim, cup, s, lp, pt, width, pages, page, block, tp, rows, rot,
+                           1 if interleaved else 0, kc, ks, vc, vs, _stream(stream)), "mxkv_append")
+
+
+def mxkv_attention_workspace_bytes(n_tokens: int, n_seqs: int, max_q_len: int, max_kv_len: int, q_heads: int, kv_heads: int, dim: int) -> int:
+    return int(lib.mxkv_attention_workspace_bytes(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, dim))
+
+
+def mxkv_attention(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, causal=True,
+                   window=0, lse=None, workspace=None, stream=None):
+    """Attention of the queries [n, Hq, D] over the paged cache; see mxkv_attention in include/mxnorm.h."""
+    _on(q.device, cu_q=cu_q, kv_lens=kv_lens, page_table=page_table, k_codes=k_codes, k_scales=k_scales, v_codes=v_codes,
+        v_scales=v_scales, out=out, lse=lse, workspace=workspace)
+    pages, heads, page, dim, block, kc, ks, vc, vs = _cache(k_codes, k_scales, v_codes, v_scales)
+    s, width, cup, lp, pt = _sequences(cu_q, kv_lens, page_table)
+    qp, qst, qh = _heads(q, "q")
+    op, ost, _ = _heads(out, "out", q)
+    if q.shape[2] != dim:
+        raise ValueError("q: dim differs from the cache's")
+    n = q.shape[0]
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.mxkv_attention(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
+                              scale, 1 if causal else 0, window, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), _ptr(workspace),
+                              ws_bytes, _stream(stream)), "mxkv_attention")

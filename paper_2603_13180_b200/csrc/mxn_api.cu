@@ -99,21 +99,45 @@ const char* mxn_status_string(mxn_status s)
         case MXN_ERR_CUDA: return "CUDA runtime error at launch";
         case MXN_ERR_TIMEOUT: return "a bounded device-side wait ran out";
         case MXN_ERR_TOO_LARGE: return "the problem needs more built-in scratch than the library holds";
+        case MXN_ERR_INDEX: return "an index held in device memory was out of range";
         default: return "unknown status";
     }
 }
 
 mxn_status mxn_device_timeouts(unsigned int* count_out)
 {
-    unsigned int n = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_timeouts(&n) != cudaSuccess) return MXN_ERR_CUDA;
+    unsigned int n = 0, attn = 0, bad = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_timeouts(&n) != cudaSuccess ||
+        mxn::read_attn_counters(&attn, &bad) != cudaSuccess)
+        return MXN_ERR_CUDA;
+    n += attn;
     if (count_out != nullptr) *count_out = n;
     return n == 0 ? MXN_OK : MXN_ERR_TIMEOUT;
 }
 
 mxn_status mxn_device_timeouts_reset(void)
 {
-    return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_timeouts() == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+    return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_timeouts() == cudaSuccess &&
+                   mxn::reset_attn_timeouts() == cudaSuccess
+               ? MXN_OK : MXN_ERR_CUDA;
+}
+
+mxn_status mxn_device_bad_indices(unsigned int* count_out)
+{
+    unsigned int heads = 0, kv = 0, attn = 0, timeouts = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_heads_bad(&heads) != cudaSuccess ||
+        mxn::read_kv_bad(&kv) != cudaSuccess || mxn::read_attn_counters(&timeouts, &attn) != cudaSuccess)
+        return MXN_ERR_CUDA;
+    const unsigned int n = heads + kv + attn;
+    if (count_out != nullptr) *count_out = n;
+    return n == 0 ? MXN_OK : MXN_ERR_INDEX;
+}
+
+mxn_status mxn_device_bad_indices_reset(void)
+{
+    return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_heads_bad() == cudaSuccess &&
+                   mxn::reset_kv_bad() == cudaSuccess && mxn::reset_attn_bad() == cudaSuccess
+               ? MXN_OK : MXN_ERR_CUDA;
 }
 
 mxn_status mxn_selftest_bounded_wait(unsigned int polls, void* cuda_stream)
@@ -467,6 +491,288 @@ mxn_status mxnorm_fwd_host(const void* x_host_bf16, int64_t T, int64_t D, int bl
                         cudaStreamWaitEvent(user, hp->join, 0) == cudaSuccess;
     if (failed != MXN_OK) return failed;
     return ok && joined ? MXN_OK : MXN_ERR_CUDA;
+}
+
+// ---- queries, keys and values around attention ------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kMaxTokens = 0x7FFFFFFF;   // positions and row counts are 32-bit in device memory
+constexpr int kMaxHeads = 4096;
+
+bool head_dim_supported(int dim) { return dim >= 16 && dim <= 256 && dim % 16 == 0; }
+
+// one operand of `heads` heads of `dim` elements a token: pointer, token stride, alignment of 16 bytes
+mxn_status check_heads(const void* p, int64_t stride, int heads, int dim)
+{
+    if (heads == 0) return MXN_OK;
+    if (p == nullptr) return MXN_ERR_NULL;
+    if (stride < (int64_t)heads * dim) return MXN_ERR_SHAPE;
+    if (misaligned(p, 16) || stride % 8 != 0) return MXN_ERR_ALIGN;
+    return MXN_OK;
+}
+
+mxn_status check_rotation(const float* cos_sin, int64_t table_rows, int rot, int dim, int pairing)
+{
+    if (pairing != MXN_ROPE_HALVES && pairing != MXN_ROPE_PAIRS) return MXN_ERR_ENUM;
+    if (cos_sin == nullptr) return MXN_OK;
+    if (rot < 16 || rot > dim || rot % 16 != 0 || table_rows < 1) return MXN_ERR_SHAPE;
+    return misaligned(cos_sin, 16) ? MXN_ERR_ALIGN : MXN_OK;
+}
+
+mxn_status check_rope(int64_t T, int q_heads, int k_heads, int dim, int normalise, const void* q_gain, const void* k_gain, float eps,
+                      const float* cos_sin, int64_t table_rows, int rot, int pairing, const int32_t* positions)
+{
+    if (T < 0 || T > kMaxTokens || q_heads < 0 || k_heads < 0 || q_heads + k_heads < 1 || q_heads > kMaxHeads || k_heads > kMaxHeads ||
+        !head_dim_supported(dim))
+        return MXN_ERR_SHAPE;
+    if (normalise != 0 && normalise != 1) return MXN_ERR_ENUM;
+    if (!(eps >= 0.0f) || (normalise == 0 && (q_gain != nullptr || k_gain != nullptr))) return MXN_ERR_SHAPE;
+    const mxn_status st = check_rotation(cos_sin, table_rows, rot, dim, pairing);
+    if (st != MXN_OK) return st;
+    if ((q_gain != nullptr && misaligned(q_gain, 16)) || (k_gain != nullptr && misaligned(k_gain, 16)) ||
+        (positions != nullptr && misaligned(positions, 4)))
+        return MXN_ERR_ALIGN;
+    return MXN_OK;
+}
+
+mxn::HeadsParams rope_params(int64_t T, int q_heads, int k_heads, int dim, int normalise, const void* q_gain, const void* k_gain, float eps,
+                             const float* cos_sin, int64_t table_rows, int rot, int pairing, const int32_t* positions)
+{
+    mxn::HeadsParams P{};
+    P.T = T;
+    P.heads[0] = q_heads;
+    P.heads[1] = k_heads;
+    P.dim = dim;
+    P.norm = normalise;
+    P.gain[0] = static_cast<const uint16_t*>(q_gain);
+    P.gain[1] = static_cast<const uint16_t*>(k_gain);
+    P.eps = eps;
+    P.inv_dim = 1.0f / (float)dim;
+    P.cos_sin = cos_sin;
+    P.table_rows = table_rows;
+    P.rot = cos_sin != nullptr ? rot : 0;
+    P.pairs = pairing == MXN_ROPE_PAIRS;
+    P.positions = positions;
+    return P;
+}
+
+mxn_status check_cache(int kv_heads, int dim, int64_t n_seqs, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                       const void* cu, const void* lens, const void* table, const void* kc, const void* ks, const void* vc, const void* vs)
+{
+    if (kv_heads < 1 || kv_heads > kMaxHeads || !head_dim_supported(dim) || n_seqs < 0 || n_seqs > kMaxTokens || max_pages < 1 || num_pages < 1)
+        return MXN_ERR_SHAPE;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return MXN_ERR_SHAPE;
+    if ((block != 16 && block != 32 && block != 64) || block > page_size) return MXN_ERR_SHAPE;
+    if (max_pages > kMaxTokens / page_size || num_pages > kMaxTokens / kv_heads) return MXN_ERR_SHAPE;
+    if (n_seqs == 0) return MXN_OK;
+    if (cu == nullptr || lens == nullptr || table == nullptr || kc == nullptr || ks == nullptr || vc == nullptr || vs == nullptr) return MXN_ERR_NULL;
+    if (misaligned(cu, 4) || misaligned(lens, 4) || misaligned(table, 4) || misaligned(kc, 16) || misaligned(vc, 16)) return MXN_ERR_ALIGN;
+    return MXN_OK;
+}
+
+int log2_of(int v)
+{
+    int n = 0;
+    while ((1 << n) < v) ++n;
+    return n;
+}
+
+bool attention_shape_ok(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads, int kv_heads, int dim)
+{
+    return n_tokens >= 0 && n_tokens <= kMaxTokens && n_seqs >= 0 && n_seqs <= kMaxTokens && max_q_len >= 1 && max_q_len <= kMaxTokens &&
+           max_kv_len >= 0 && max_kv_len <= kMaxTokens - 64 && kv_heads >= 1 && q_heads >= kv_heads && q_heads <= kMaxHeads &&
+           q_heads % kv_heads == 0 && (dim == 64 || dim == 128);
+}
+
+}  // namespace
+
+mxn_status rmsnorm_rope_fwd(const void* q_bf16, int64_t q_stride, int q_heads, const void* k_bf16, int64_t k_stride, int k_heads, int64_t T,
+                            int head_dim, int normalise, const void* q_gain_bf16_or_null, const void* k_gain_bf16_or_null, float eps,
+                            const float* cos_sin_or_null, int64_t table_rows, int rot_dim, mxn_rope pairing, const int32_t* positions_or_null,
+                            void* q_out_bf16, int64_t q_out_stride, void* k_out_bf16, int64_t k_out_stride, void* cuda_stream)
+{
+    mxn_status st = check_rope(T, q_heads, k_heads, head_dim, normalise, q_gain_bf16_or_null, k_gain_bf16_or_null, eps, cos_sin_or_null,
+                               table_rows, rot_dim, pairing, positions_or_null);
+    if (st != MXN_OK || T == 0) return st;
+    if ((st = check_heads(q_bf16, q_stride, q_heads, head_dim)) != MXN_OK || (st = check_heads(k_bf16, k_stride, k_heads, head_dim)) != MXN_OK ||
+        (st = check_heads(q_out_bf16, q_out_stride, q_heads, head_dim)) != MXN_OK ||
+        (st = check_heads(k_out_bf16, k_out_stride, k_heads, head_dim)) != MXN_OK)
+        return st;
+    mxn::HeadsParams P = rope_params(T, q_heads, k_heads, head_dim, normalise, q_gain_bf16_or_null, k_gain_bf16_or_null, eps, cos_sin_or_null,
+                                     table_rows, rot_dim, pairing, positions_or_null);
+    P.x[0] = static_cast<const uint16_t*>(q_bf16);
+    P.x[1] = static_cast<const uint16_t*>(k_bf16);
+    P.x_stride[0] = q_stride;
+    P.x_stride[1] = k_stride;
+    P.y[0] = static_cast<uint16_t*>(q_out_bf16);
+    P.y[1] = static_cast<uint16_t*>(k_out_bf16);
+    P.y_stride[0] = q_out_stride;
+    P.y_stride[1] = k_out_stride;
+    return mxn::launch_rope_fwd(P, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+}
+
+size_t rmsnorm_rope_bwd_workspace_bytes(int64_t T, int q_heads, int k_heads, int head_dim)
+{
+    if (check_rope(T, q_heads, k_heads, head_dim, 1, nullptr, nullptr, 0.0f, nullptr, 0, 0, MXN_ROPE_HALVES, nullptr) != MXN_OK) return 0;
+    return (size_t)mxn::rope_bwd_ctas(T, q_heads, k_heads, head_dim) * head_dim * 4;
+}
+
+mxn_status rmsnorm_rope_bwd(const void* q_bf16_or_null, int64_t q_stride, int q_heads, const void* k_bf16_or_null, int64_t k_stride, int k_heads,
+                            const void* grad_q_bf16, int64_t grad_q_stride, const void* grad_k_bf16, int64_t grad_k_stride, int64_t T,
+                            int head_dim, int normalise, const void* q_gain_bf16_or_null, const void* k_gain_bf16_or_null, float eps,
+                            const float* cos_sin_or_null, int64_t table_rows, int rot_dim, mxn_rope pairing, const int32_t* positions_or_null,
+                            void* dq_bf16, int64_t dq_stride, void* dk_bf16, int64_t dk_stride, float* q_dgain_f32_or_null,
+                            float* k_dgain_f32_or_null, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    mxn_status st = check_rope(T, q_heads, k_heads, head_dim, normalise, q_gain_bf16_or_null, k_gain_bf16_or_null, eps, cos_sin_or_null,
+                               table_rows, rot_dim, pairing, positions_or_null);
+    if (st != MXN_OK) return st;
+    const bool dgain = q_dgain_f32_or_null != nullptr || k_dgain_f32_or_null != nullptr;
+    if (normalise == 0 && dgain) return MXN_ERR_SHAPE;
+    if ((q_dgain_f32_or_null != nullptr && misaligned(q_dgain_f32_or_null, 4)) ||
+        (k_dgain_f32_or_null != nullptr && misaligned(k_dgain_f32_or_null, 4)))
+        return MXN_ERR_ALIGN;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (T == 0) {
+        const size_t bytes = (size_t)head_dim * 4;
+        if ((q_dgain_f32_or_null != nullptr && cudaMemsetAsync(q_dgain_f32_or_null, 0, bytes, s) != cudaSuccess) ||
+            (k_dgain_f32_or_null != nullptr && cudaMemsetAsync(k_dgain_f32_or_null, 0, bytes, s) != cudaSuccess))
+            return MXN_ERR_CUDA;
+        return MXN_OK;
+    }
+    if (normalise != 0 && ((st = check_heads(q_bf16_or_null, q_stride, q_heads, head_dim)) != MXN_OK ||
+                           (st = check_heads(k_bf16_or_null, k_stride, k_heads, head_dim)) != MXN_OK))
+        return st;
+    if ((st = check_heads(grad_q_bf16, grad_q_stride, q_heads, head_dim)) != MXN_OK ||
+        (st = check_heads(grad_k_bf16, grad_k_stride, k_heads, head_dim)) != MXN_OK ||
+        (st = check_heads(dq_bf16, dq_stride, q_heads, head_dim)) != MXN_OK || (st = check_heads(dk_bf16, dk_stride, k_heads, head_dim)) != MXN_OK)
+        return st;
+    if (dgain) {
+        if (workspace == nullptr || workspace_bytes < rmsnorm_rope_bwd_workspace_bytes(T, q_heads, k_heads, head_dim)) return MXN_ERR_WORKSPACE;
+        if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
+    }
+    mxn::HeadsParams P = rope_params(T, q_heads, k_heads, head_dim, normalise, q_gain_bf16_or_null, k_gain_bf16_or_null, eps, cos_sin_or_null,
+                                     table_rows, rot_dim, pairing, positions_or_null);
+    P.x[0] = static_cast<const uint16_t*>(q_bf16_or_null);
+    P.x[1] = static_cast<const uint16_t*>(k_bf16_or_null);
+    P.x_stride[0] = q_stride;
+    P.x_stride[1] = k_stride;
+    P.grad[0] = static_cast<const uint16_t*>(grad_q_bf16);
+    P.grad[1] = static_cast<const uint16_t*>(grad_k_bf16);
+    P.grad_stride[0] = grad_q_stride;
+    P.grad_stride[1] = grad_k_stride;
+    P.y[0] = static_cast<uint16_t*>(dq_bf16);
+    P.y[1] = static_cast<uint16_t*>(dk_bf16);
+    P.y_stride[0] = dq_stride;
+    P.y_stride[1] = dk_stride;
+    P.dgain[0] = q_dgain_f32_or_null;
+    P.dgain[1] = k_dgain_f32_or_null;
+    P.partial = dgain ? static_cast<float*>(workspace) : nullptr;
+    return mxn::launch_rope_bwd(P, s) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+}
+
+mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16, int64_t v_stride, int64_t n_tokens, int kv_heads, int head_dim,
+                       const int32_t* cu_tokens, int64_t n_seqs, const int32_t* kv_lens, const int32_t* page_table, int64_t max_pages,
+                       int64_t num_pages, int page_size, int block, const float* cos_sin_or_null, int64_t table_rows, int rot_dim,
+                       mxn_rope pairing, void* k_codes_u8, void* k_scales_u8, void* v_codes_u8, void* v_scales_u8, void* cuda_stream)
+{
+    mxn_status st = check_cache(kv_heads, head_dim, n_seqs, max_pages, num_pages, page_size, block, cu_tokens, kv_lens, page_table, k_codes_u8,
+                                k_scales_u8, v_codes_u8, v_scales_u8);
+    if (st != MXN_OK) return st;
+    if (n_tokens < 0 || n_tokens > kMaxTokens) return MXN_ERR_SHAPE;
+    if ((st = check_rotation(cos_sin_or_null, table_rows, rot_dim, head_dim, pairing)) != MXN_OK) return st;
+    if (n_tokens == 0 || n_seqs == 0) return MXN_OK;
+    if ((st = check_heads(k_bf16, k_stride, kv_heads, head_dim)) != MXN_OK || (st = check_heads(v_bf16, v_stride, kv_heads, head_dim)) != MXN_OK)
+        return st;
+    mxn::KvAppendParams P{};
+    P.x[0] = static_cast<const uint16_t*>(k_bf16);
+    P.x[1] = static_cast<const uint16_t*>(v_bf16);
+    P.x_stride[0] = k_stride;
+    P.x_stride[1] = v_stride;
+    P.codes[0] = static_cast<uint8_t*>(k_codes_u8);
+    P.codes[1] = static_cast<uint8_t*>(v_codes_u8);
+    P.scales[0] = static_cast<uint8_t*>(k_scales_u8);
+    P.scales[1] = static_cast<uint8_t*>(v_scales_u8);
+    P.cu = cu_tokens;
+    P.lens = kv_lens;
+    P.page_table = page_table;
+    P.cos_sin = cos_sin_or_null;
+    P.n = n_tokens;
+    P.num_pages = num_pages;
+    P.max_pages = max_pages;
+    P.table_rows = table_rows;
+    P.seqs = (int)n_seqs;
+    P.heads = kv_heads;
+    P.dim = head_dim;
+    P.page = page_size;
+    P.block = block;
+    P.rot = rot_dim;
+    P.pairs = pairing == MXN_ROPE_PAIRS;
+    return mxn::launch_kv_append(P, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+}
+
+size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads, int kv_heads,
+                                      int head_dim)
+{
+    if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim) || n_tokens == 0 || n_seqs == 0) return 0;
+    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, q_heads, kv_heads, head_dim).workspace;
+}
+
+mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                          const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                          const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block, const void* k_codes_u8,
+                          const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale, int causal, int64_t window,
+                          void* out_bf16, int64_t out_stride, float* lse_out_or_null, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream)
+{
+    if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim)) return MXN_ERR_SHAPE;
+    mxn_status st = check_cache(kv_heads, head_dim, n_seqs, max_pages, num_pages, page_size, block, cu_q, kv_lens, page_table, k_codes_u8,
+                                k_scales_u8, v_codes_u8, v_scales_u8);
+    if (st != MXN_OK) return st;
+    if (max_kv_len > max_pages * page_size || window < 0 || window > kMaxTokens || !(scale == scale)) return MXN_ERR_SHAPE;
+    if (causal != 0 && causal != 1) return MXN_ERR_ENUM;
+    if (n_tokens == 0 || n_seqs == 0) return MXN_OK;
+    if ((st = check_heads(q_bf16, q_stride, q_heads, head_dim)) != MXN_OK || (st = check_heads(out_bf16, out_stride, q_heads, head_dim)) != MXN_OK)
+        return st;
+    if (lse_out_or_null != nullptr && misaligned(lse_out_or_null, 4)) return MXN_ERR_ALIGN;
+    const mxn::AttnPlan plan = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, causal ? window : 0, q_heads, kv_heads,
+                                                    head_dim);
+    if (plan.ctas > 0x7FFFFFFF || (n_tokens * q_heads + 3) / 4 > 0x7FFFFFFF) return MXN_ERR_SHAPE;
+    if (plan.splits > 1) {
+        if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
+        if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
+    }
+    mxn::AttnParams P{};
+    P.q = static_cast<const uint16_t*>(q_bf16);
+    P.out = static_cast<uint16_t*>(out_bf16);
+    P.lse = lse_out_or_null;
+    P.k_codes = static_cast<const uint8_t*>(k_codes_u8);
+    P.k_scales = static_cast<const uint8_t*>(k_scales_u8);
+    P.v_codes = static_cast<const uint8_t*>(v_codes_u8);
+    P.v_scales = static_cast<const uint8_t*>(v_scales_u8);
+    P.cu_q = cu_q;
+    P.lens = kv_lens;
+    P.page_table = page_table;
+    P.n = n_tokens;
+    P.q_stride = q_stride;
+    P.out_stride = out_stride;
+    P.max_pages = max_pages;
+    P.num_pages = (int)num_pages;
+    P.seqs = (int)n_seqs;
+    P.q_heads = q_heads;
+    P.kv_heads = kv_heads;
+    P.group = q_heads / kv_heads;
+    P.dim = head_dim;
+    P.page = page_size;
+    P.page_shift = log2_of(page_size);
+    P.block_shift = log2_of(block);
+    P.max_q = (int)(max_q_len < n_tokens ? max_q_len : n_tokens);
+    P.max_len = (int)max_kv_len;
+    P.causal = causal;
+    P.window = (int)window;
+    P.scale = scale;
+    return mxn::launch_attention(P, plan, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
 }
 
 }  // extern "C"

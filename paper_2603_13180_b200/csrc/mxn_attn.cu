@@ -1,0 +1,638 @@
+// Attention over the paged 8-bit cache for few query rows: one token a sequence, or a few drafted ones.
+//
+//   s_t = scale * q . k_t,   o = sum_t softmax(s)_t v_t,   k_t = 2^(sk - 127) * code, v_t likewise
+//
+// Every code is read once from HBM, which bounds the call (2 * dim bytes a token and head); the arithmetic runs on the codes
+// as they are.  The tensor cores multiply E4M3 by E4M3 with binary32 sums, so q and the softmax's weights are written as
+// sums of two E4M3 numbers, hi + lo/16.  The product tile has 16 rows and a group of query heads rarely more than eight, so
+// eight query rows fill a tile: row g is hi and row g + 8 lo of the same query row, and one multiplication does both.  The two
+// sums of a query row end in the same thread.  The splits:
+//   q  is scaled by a power of two that brings the row's largest magnitude to [128, 256).  hi is q to 4 significant bits, what
+//      is left of a bf16 value has at most 4 significant bits again: hi + lo/16 IS q, but for elements below 2^-14 of the
+//      row's largest, which keep an absolute error of 2^-22 of it.
+//   p  keeps 8 bits (relative error at most 2^-8, as a bf16 would), or 2^-23 of the largest weight of its tile in absolute terms.
+// The scales of the cache never touch the codes: a key block's scale multiplies the finished product, a value block's is
+// folded into the weight, w_t = 2^(s_t + sv_t - R), with the reference R following the tiles' largest s + sv (an integer,
+// so that the correction of the sums is exact).  The softmax's own sum l keeps a reference of its own and unrounded weights.
+//
+// A CTA of four warps takes `rows` = 8 * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
+// of warps walk over the chunk's tiles of 32 tokens in turn; each group feeds itself through a ring of tiles that the
+// tensor copy engine fills (128-byte swizzle: the two access patterns below are then free of bank conflicts).  Within a tile,
+// a thread reads its operand words with 16-byte loads: the order of the dimensions within a product and of the tokens within a
+// sum is free, and is chosen so that a thread's share is contiguous.  The values' operand wants four tokens of one dimension
+// in a word: a 4 x 4 byte transposition by eight byte permutations.  The weights go from the first product's accumulators to
+// the second product's operand without leaving the thread.
+//
+// Partial results of the chunks go to the workspace as (normalised row, logarithm of its sum) and are joined in a fixed
+// order by a second kernel; with one chunk the row is written at once.
+//
+// Every wait is bounded (see mxn_device_timeouts).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <cmath>
+
+#include "mxn_attn.cuh"
+
+namespace mxn {
+
+namespace {
+
+constexpr int kSMs = 148;
+constexpr int kWarps = 4;
+constexpr int kTile = 32;      // tokens of a tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ unsigned int g_attn_timeouts = 0;
+__device__ unsigned int g_attn_bad = 0;   // pages out of range within a sequence's length
+
+__device__ __forceinline__ void mma_e4m3(float* c, const uint32_t* a, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint2 lds_v2(uint32_t addr)
+{
+    uint2 r;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr));
+    return r;
+}
+// four binary32 -> hi and lo words: hi = E4M3(x), lo = E4M3(16 (x - hi)); |x| <= 256
+__device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_t& lo)
+{
+    // in f16 pairs: 11 bits hold what hi + lo can express, and x - hi is exact
+    const __half2 a = __floats2half2_rn(x0, x1);
+    hi = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(a), __NV_SATFINITE, __NV_E4M3);
+    const __half2 left = __hsub2(a, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3)));
+    lo = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(__hmul2(left, __float2half2_rn(16.0f))), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, uint32_t& hi, uint32_t& lo)
+{
+    uint32_t h0, h1, l0, l1;
+    split2(x0, x1, h0, l0);
+    split2(x2, x3, h1, l1);
+    hi = h0 | (h1 << 16);
+    lo = l0 | (l1 << 16);
+}
+__device__ __forceinline__ float quad_max(float v)
+{
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v)
+{
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+    return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+template <int DIM, int RW, int STAGES>
+struct DecodeShape {
+    static constexpr int kGroups = kWarps / RW;                  // warp groups that share out the tiles
+    static constexpr int kTileBytes = kTile * DIM;               // codes of a tile, keys or values
+    static constexpr int kRingBytes = kGroups * STAGES * 2 * kTileBytes;
+    static constexpr int kRows = 8 * RW;
+    static constexpr int kJoinBytes = kGroups * kRows * (DIM * 4 + 8);
+    static constexpr int kSmem = (kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes) + 1024;
+};
+
+template <int DIM, int RW, int STAGES>
+__global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
+{
+    using Sh = DecodeShape<DIM, RW, STAGES>;
+    constexpr int NT = DIM / 8;      // column tiles of the second product
+    constexpr int KS = DIM / 32;     // steps of the first
+    constexpr int GROUPS = Sh::kGroups;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[2 * GROUPS * STAGES];   // full, then empty
+
+    pdl_prologue();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    const int group = warp / RW, rw = warp % RW;
+    int64_t b = blockIdx.x;
+    const int split = (int)(b % P.splits);
+    b /= P.splits;
+    const int rt = (int)(b % P.row_tiles);
+    b /= P.row_tiles;
+    const int h = (int)(b % P.kv_heads);
+    const int seq = (int)(b / P.kv_heads);
+
+    const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
+    const int len = min(__ldg(P.lens + seq), P.max_len);
+    const int nq = max(0, min(q1 - q0, P.max_q));
+    const int G = P.group, row0 = rt * Sh::kRows, rows = nq * G;
+    if (q0 < 0 || row0 >= rows) return;
+    // keys that any row of this tile sees: [lo, hi)
+    const int shift = len - (q1 - q0);              // position of the sequence's first query
+    const int last = min(rows, row0 + Sh::kRows) - 1;
+    const int hi = max(0, min(len, P.causal ? shift + last / G + 1 : len));
+    const int lo = P.window > 0 ? max(0, shift + row0 / G - P.window + 1) / kTile * kTile : 0;
+    const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
+    const int tiles = (k1 - k0 + kTile - 1) / kTile;
+
+    // this thread's row: its query token, head and place among the outputs
+    const int row = row0 + rw * 8 + g;
+    const bool row_live = row < rows;
+    const int64_t tok = q0 + (row_live ? row / G : 0);
+    const int head = h * G + (row_live ? row % G : 0);
+    const int pos = shift + (row_live ? row / G : nq - 1);
+    const int see_hi = P.causal ? min(pos + 1, len) : len;                     // keys [see_lo, see_hi)
+    const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t ring = base + (uint32_t)group * STAGES * 2 * Sh::kTileBytes;
+    const uint32_t full = smem_u32(bars) + (uint32_t)group * STAGES * 8, empty = full + GROUPS * STAGES * 8;
+    const bool leader = rw == 0 && lane == 0;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < GROUPS * STAGES; ++i) {
+            mbar_init(smem_u32(bars) + 8 * i, 1);
+            mbar_init(smem_u32(bars) + 8 * (GROUPS * STAGES + i), RW);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+
+    // the group's tiles are group, group + GROUPS, ...; tile i of them goes to stage i % STAGES
+    const int mine = tiles > group ? (tiles - group + GROUPS - 1) / GROUPS : 0;
+    const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
+    // a tile has two runs of 16 tokens, each within one page; lanes 0-15 look after the first, 16-31 after the second.
+    // page_at(i): the page of this lane's run of tile i; -1 behind the last token or where the table is out of range
+    const int run = lane >> 4;
+    bool bad_page = false;
+    auto tile_at = [&](int i) { return k0 + (group + i * GROUPS) * kTile; };
+    auto page_at = [&](int i) -> int {
+        const int t = tile_at(i) + 16 * run;
+        if (i >= mine || t >= k1) return -1;
+        const int pg = __ldg(table + (t >> P.page_shift));
+        const bool good = pg >= 0 && pg < P.num_pages;
+        bad_page |= !good;
+        return good ? pg : -1;
+    };
+    const bool two_boxes = P.page < kTile;   // a page of 16 tokens takes two boxes to a tile
+    auto request = [&](int i, int pg) {      // by a whole warp, with page_at(i) in hand
+        const int pg1 = __shfl_sync(0xFFFFFFFFu, pg, 16);
+        if (!leader) return;
+        const int t0 = tile_at(i);
+        const uint32_t dst = ring + (uint32_t)(i % STAGES) * 2 * Sh::kTileBytes, bar = full + 8 * (i % STAGES);
+        const uint32_t box_bytes = two_boxes ? Sh::kTileBytes / 2 : Sh::kTileBytes;
+        const uint32_t bytes = (uint32_t)((pg >= 0) + (two_boxes && pg1 >= 0)) * 2 * box_bytes;
+        if (bytes == 0) {
+            mbar_arrive(bar);
+            return;
+        }
+        mbar_expect_tx(bar, bytes);
+        const int y = t0 & (P.page - 1);
+        if (pg >= 0) {
+            tma_load_codes(dst, &M.k, y, pg * P.kv_heads + h, bar);
+            tma_load_codes(dst + Sh::kTileBytes, &M.v, y, pg * P.kv_heads + h, bar);
+        }
+        if (two_boxes && pg1 >= 0) {
+            tma_load_codes(dst + box_bytes, &M.k, 0, pg1 * P.kv_heads + h, bar);
+            tma_load_codes(dst + Sh::kTileBytes + box_bytes, &M.v, 0, pg1 * P.kv_heads + h, bar);
+        }
+    };
+    // pages of the tiles from the one at hand on: asked for STAGES + 1 tiles ahead
+    int pages[STAGES + 2];
+#pragma unroll
+    for (int d = 0; d < STAGES + 2; ++d) pages[d] = page_at(d);
+    if (rw == 0) {
+#pragma unroll
+        for (int d = 0; d < STAGES; ++d)
+            if (d < mine) request(d, pages[d]);
+    }
+    // scales, one tile ahead: lanes 0 and 16 hold the key scales of the two runs, lanes 1 and 17 the value scales
+    auto scale_at = [&](int i, int pg) -> uint32_t {
+        if ((lane & 15) >= 2 || pg < 0) return 0;
+        const uint8_t* s = lane & 1 ? P.v_scales : P.k_scales;
+        return __ldg(s + ((((int64_t)pg * P.kv_heads + h) << (P.page_shift - P.block_shift)) +
+                          (((tile_at(i) + 16 * run) & (P.page - 1)) >> P.block_shift)));
+    };
+    uint32_t sc_next = scale_at(0, pages[0]);
+
+    // q: the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on, split; the power of two goes to the row's factor
+    uint32_t qa[KS][4];
+    float row_factor;
+    {
+        uint4 w[DIM / 32];
+        const uint16_t* qp = P.q + tok * P.q_stride + (int64_t)head * DIM + c * (DIM / 4);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; ++i) w[i] = row_live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
+        const uint32_t E = __float_as_uint(quad_max(hmax_abs_to_f32(m))) >> 23;
+        const uint32_t Ec = min(max(E, 8u), 254u);
+        const float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);   // 2^(7 - (E - 127))
+        row_factor = P.scale * kLog2e * __uint_as_float((Ec - 7u) << 23);                // ... and its inverse
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t a = u[4 * k + 2 * x], d = u[4 * k + 2 * x + 1];
+                split4(bf16_lo(a) * up, bf16_hi(a) * up, bf16_lo(d) * up, bf16_hi(d) * up, qa[k][2 * x], qa[k][2 * x + 1]);
+            }
+    }
+
+    float acc[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
+    const float kNone = -INFINITY;
+    float m_ref = kNone, l = 0.0f;             // softmax: reference (an integer) and this thread's part of the sum
+    float r_ref = kNone, r_top = kNone;        // second product: reference (an integer) and the largest so far
+    bool ok = true;
+
+    for (int i = 0; i < mine; ++i) {
+        const int st = i % STAGES;
+        const uint32_t ph = (uint32_t)(i / STAGES) & 1u;
+        const int t0 = tile_at(i);
+        const uint32_t sc = sc_next;
+        sc_next = scale_at(i + 1, pages[1]);
+        const float kf0 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)) * row_factor, kf1 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16)) * row_factor;
+        const float sv0 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, sv1 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f;
+        // tokens of the tile that exist and whose page could be read
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && pages[0] >= 0);
+
+        if (!mbar_wait_bounded(full + 8 * st, ph)) {
+            ok = false;
+            break;
+        }
+        const uint32_t kt = ring + (uint32_t)st * 2 * Sh::kTileBytes, vt = kt + Sh::kTileBytes;
+
+        // ---- s = q . k: token 8j + g is column g of column tile j ----
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = 8 * j + g;
+            uint32_t w[2 * KS];
+            if constexpr (DIM == 128) {
+                const uint4 a = lds_v4(kt + r * 128 + (((2 * c) ^ g) << 4)), d = lds_v4(kt + r * 128 + (((2 * c + 1) ^ g) << 4));
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+                w[KS * 2 - 4] = d.x; w[KS * 2 - 3] = d.y; w[KS * 2 - 2] = d.z; w[KS * 2 - 1] = d.w;
+            } else {
+                const uint4 a = lds_v4(kt + r * 64 + ((c ^ ((g >> 1) & 3)) << 4));
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+            }
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) mma_e4m3(d, qa[k], w[2 * k], w[2 * k + 1]);
+            const float f = j < 2 ? kf0 : kf1;
+            s[2 * j] = fmaf(d[2], 0.0625f, d[0]) * f;
+            s[2 * j + 1] = fmaf(d[3], 0.0625f, d[1]) * f;
+        }
+        // ---- what this row may not see ----
+        const bool all = there == 0xFFFFFFFFu && t0 >= see_lo && t0 + kTile <= see_hi;
+        if (!__all_sync(0xFFFFFFFFu, all)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = 8 * (e >> 1) + 2 * c + (e & 1);
+                if (!((there >> t) & 1u) || t0 + t < see_lo || t0 + t >= see_hi) s[e] = kNone;
+            }
+        }
+        // ---- references ----
+        const float top0 = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top1 = fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]));
+        const float top = quad_max(fmaxf(top0, top1));
+        const float utop = ceilf(quad_max(fmaxf(top0 + sv0, top1 + sv1)));
+        if (top > m_ref) {
+            const float n = ceilf(top);
+            l *= ex2(m_ref - n);
+            m_ref = n;
+        }
+        r_top = fmaxf(r_top, utop);
+        // follow the tile's largest: up at once, down when six binades are lost (never 40 below the largest so far, so
+        // that the sums cannot overflow)
+        float r_new = r_ref;
+        if (utop > r_ref) r_new = utop;
+        else if (utop < r_ref - 6.0f && utop > kNone) r_new = fmaxf(utop, r_top - 40.0f);
+        if (__any_sync(0xFFFFFFFFu, r_new != r_ref)) {
+            const float alpha = r_ref == kNone ? 0.0f : ex2(r_ref - r_new);
+            r_ref = r_new;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] *= alpha;
+        }
+        // ---- weights ----
+        const float ms = m_ref == kNone ? 0.0f : m_ref, rs = r_ref == kNone ? 0.0f : r_ref;
+        const float b0 = sv0 + 8.0f - rs, b1 = sv1 + 8.0f - rs;   // largest weight 2^8
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            l += ex2(s[e] - ms);
+            w[e] = ex2(s[e] + (e < 4 ? b0 : b1));
+        }
+        uint32_t pa[4];
+        split4(w[0], w[1], w[2], w[3], pa[0], pa[1]);
+        split4(w[4], w[5], w[6], w[7], pa[2], pa[3]);
+        // ---- o += w v: tokens 2c, 2c+1, 8+2c, 9+2c (then 16 more) of DIM/8 dimensions from g * DIM/8 on ----
+        constexpr int VW = DIM / 32;   // words a thread reads of each token
+        uint32_t v[8][VW];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int r = 8 * (x >> 1) + 2 * c + (x & 1);
+            if constexpr (DIM == 128) {
+                const uint4 a = lds_v4(vt + r * 128 + ((g ^ (r & 7)) << 4));
+                v[x][0] = a.x; v[x][1] = a.y; v[x][VW - 2] = a.z; v[x][VW - 1] = a.w;
+            } else {
+                const uint2 a = lds_v2(vt + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
+                v[x][0] = a.x; v[x][1] = a.y;
+            }
+        }
+        if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token, a NaN among it, must not meet the zero weights
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int t = 8 * (x >> 1) + 2 * c + (x & 1);
+                if (!((there >> t) & 1u))
+#pragma unroll
+                    for (int y = 0; y < VW; ++y) v[x][y] = 0u;
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < VW; ++y) {
+            uint32_t o[2][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t a0 = __byte_perm(v[4 * x][y], v[4 * x + 1][y], 0x5140), a1 = __byte_perm(v[4 * x][y], v[4 * x + 1][y], 0x7362);
+                const uint32_t a2 = __byte_perm(v[4 * x + 2][y], v[4 * x + 3][y], 0x5140), a3 = __byte_perm(v[4 * x + 2][y], v[4 * x + 3][y], 0x7362);
+                o[x][0] = __byte_perm(a0, a2, 0x5410);
+                o[x][1] = __byte_perm(a0, a2, 0x7632);
+                o[x][2] = __byte_perm(a1, a3, 0x5410);
+                o[x][3] = __byte_perm(a1, a3, 0x7632);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mma_e4m3(acc[4 * y + e], pa, o[0][e], o[1][e]);
+        }
+        // ---- hand the stage back ----
+        __syncwarp();
+        if (RW > 1) {
+            if (lane == 0) mbar_arrive(empty + 8 * st);
+            if (rw == 0 && i + STAGES < mine) {
+                if (!mbar_wait_bounded(empty + 8 * st, ph)) {
+                    ok = false;
+                    break;
+                }
+                request(i + STAGES, pages[STAGES]);
+            }
+        } else if (i + STAGES < mine) {
+            request(i + STAGES, pages[STAGES]);
+        }
+#pragma unroll
+        for (int d = 0; d < STAGES + 1; ++d) pages[d] = pages[d + 1];
+        pages[STAGES + 1] = page_at(i + STAGES + 2);
+    }
+    if (!__all_sync(0xFFFFFFFFu, ok)) {
+        // a wait ran out: no further copies are asked for; those in flight get a second, shorter wait before the shared
+        // memory is given up
+        if (lane == 0) atomicAdd(&g_attn_timeouts, 1u);
+        if (leader)
+            for (int st = 0; st < STAGES; ++st) {
+                (void)mbar_wait_bounded(full + 8 * st, 0, 1u << 14);
+                (void)mbar_wait_bounded(full + 8 * st, 1, 1u << 14);
+            }
+    }
+    if (__any_sync(0xFFFFFFFFu, bad_page) && lane == 0) atomicAdd(&g_attn_bad, 1u);
+
+    // ---- join the groups of warps ----
+    l = quad_sum(l);
+    const float ms = m_ref == kNone ? 0.0f : m_ref, rs = r_ref == kNone ? 0.0f : r_ref;
+    const float back = ex2(fminf(fmaxf(rs - 8.0f - ms, -126.0f), 127.0f));
+    constexpr int OUT = DIM / 4;   // dimensions a thread ends with: those from c * OUT on
+    float o[OUT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        o[j] = fmaf(acc[j][2], 0.0625f, acc[j][0]) * back;
+        o[NT + j] = fmaf(acc[j][3], 0.0625f, acc[j][1]) * back;
+    }
+    if (GROUPS > 1) {
+        float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+        float* const stat = sm + GROUPS * Sh::kRows * DIM;
+        __syncthreads();   // every copy has landed and been read
+        if (group != 0) {
+            float* const p = sm + ((int64_t)group * Sh::kRows + rw * 8 + g) * DIM + c * OUT;
+#pragma unroll
+            for (int x = 0; x < OUT / 4; ++x) *reinterpret_cast<float4*>(p + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            if (c == 0) {
+                stat[2 * (group * Sh::kRows + rw * 8 + g)] = m_ref;
+                stat[2 * (group * Sh::kRows + rw * 8 + g) + 1] = l;
+            }
+        }
+        __syncthreads();
+        if (group != 0) return;
+        float m_all = m_ref;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) m_all = fmaxf(m_all, stat[2 * (k * Sh::kRows + rw * 8 + g)]);
+        const float own = m_ref == kNone ? 0.0f : ex2(m_ref - m_all);
+        l *= own;
+#pragma unroll
+        for (int x = 0; x < OUT; ++x) o[x] *= own;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) {
+            const int at = k * Sh::kRows + rw * 8 + g;
+            const float mk = stat[2 * at];
+            if (mk == kNone) continue;
+            const float f = ex2(mk - m_all);
+            l = fmaf(stat[2 * at + 1], f, l);
+            const float* const p = sm + (int64_t)at * DIM + c * OUT;
+#pragma unroll
+            for (int x = 0; x < OUT / 4; ++x) {
+                const float4 a = *reinterpret_cast<const float4*>(p + 4 * x);
+                o[4 * x] = fmaf(a.x, f, o[4 * x]);
+                o[4 * x + 1] = fmaf(a.y, f, o[4 * x + 1]);
+                o[4 * x + 2] = fmaf(a.z, f, o[4 * x + 2]);
+                o[4 * x + 3] = fmaf(a.w, f, o[4 * x + 3]);
+            }
+        }
+        m_ref = m_all;
+    }
+    if (!row_live) return;
+    const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;       // a row that sees nothing: zeros
+    const float lse2 = l > 0.0f ? m_ref + log2f(l) : kNone;
+    if (P.splits == 1) {
+        uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + c * OUT;
+#pragma unroll
+        for (int x = 0; x < OUT / 8; ++x) {
+            const uint32_t r[4] = {pack_bf16(o[8 * x] * inv, o[8 * x + 1] * inv), pack_bf16(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
+                                   pack_bf16(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack_bf16(o[8 * x + 6] * inv, o[8 * x + 7] * inv)};
+            st_v4(y + 8 * x, r);
+        }
+        if (P.lse != nullptr && c == 0) P.lse[tok * P.q_heads + head] = lse2 * kLn2;
+    } else {
+        const int64_t at = (tok * P.q_heads + head) * P.splits + split;
+        if (c == 0) P.part_lse[at] = lse2;
+        if (l > 0.0f) {
+            float* const y = P.part_out + at * DIM + c * OUT;
+#pragma unroll
+            for (int x = 0; x < OUT / 4; ++x)
+                *reinterpret_cast<float4*>(y + 4 * x) = make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
+        }
+    }
+}
+
+// joins the chunks of each row: one warp a row, chunks in order
+template <int DIM>
+__global__ void __launch_bounds__(128) attn_join_kernel(const AttnParams P)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t tok = row / P.q_heads;
+    // rows of no sequence are left as they were
+    if (tok >= min((int64_t)__ldg(P.cu_q + P.seqs), P.n) || tok < __ldg(P.cu_q)) return;
+    const float* const part = P.part_lse + row * P.splits;
+    float top = -INFINITY;
+    for (int i = lane; i < P.splits; i += 32) top = fmaxf(top, part[i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const bool none = top == -INFINITY;
+    constexpr int E = DIM / 32;
+    float sum = 0.0f, acc[E] = {};
+    if (!none) {
+        for (int i = 0; i < P.splits; ++i) {
+            const float li = part[i];
+            if (li == -INFINITY) continue;
+            const float f = ex2(li - top);
+            sum += f;
+            const float* const p = P.part_out + (row * P.splits + i) * DIM + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(p[e], f, acc[e]);
+        }
+    }
+    const float inv = none ? 0.0f : __fdiv_rn(1.0f, sum);
+    uint32_t* const y = reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM + lane * E);
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) y[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    if (P.lse != nullptr && lane == 0) P.lse[row] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+template <class K, class... Args>
+cudaError_t launch(K kernel, int64_t ctas, int threads, int smem, cudaStream_t stream, const Args&... args)
+{
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// the driver's encoder, looked up once per process (nothing of it depends on the device)
+EncodeTiled encoder()
+{
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+bool make_map(CUtensorMap* map, const uint8_t* codes, const AttnParams& P, int box_rows)
+{
+    const EncodeTiled enc = encoder();
+    if (enc == nullptr) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)P.dim, (cuuint64_t)P.page, (cuuint64_t)P.num_pages * (cuuint64_t)P.kv_heads};
+    const cuuint64_t strides[2] = {(cuuint64_t)P.dim, (cuuint64_t)P.dim * (cuuint64_t)P.page};
+    const cuuint32_t box[3] = {(cuuint32_t)P.dim, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               P.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DIM, int RW, int STAGES>
+cudaError_t launch_decode(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
+{
+    return launch(attn_decode_kernel<DIM, RW, STAGES>, ctas, kWarps * 32, DecodeShape<DIM, RW, STAGES>::kSmem, stream, P, M);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+// How the keys are shared out: from sizes alone, so that the workspace can be asked for ahead of the call.
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim)
+{
+    AttnPlan a{};
+    if (max_q > n) max_q = n;
+    const int64_t rows = max_q * (q_heads / kv_heads);
+    a.row_warps = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+    a.row_tiles = ceil_div(rows, 8 * a.row_warps);
+    // enough chunks for four rounds of the CTAs that are resident at a time (sequences differ in length), none
+    // shorter than a tile for every group of warps
+    const int64_t units = seqs * kv_heads * a.row_tiles, least = kTile * (kWarps / a.row_warps);
+    int64_t splits = ceil_div((int64_t)kSMs * (dim == 128 ? 3 : 4) * 4, units);
+    // keys that the rows of a tile can see between them
+    const int64_t tokens = ceil_div(8 * a.row_warps, q_heads / kv_heads) + 1;
+    const int64_t span = window > 0 && window + tokens + kTile < max_len ? window + tokens + kTile : max_len;
+    const int64_t most = ceil_div(max_len, least);   // of the workspace: for any window
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    a.workspace = splits > 1 ? (size_t)n * q_heads * splits * (dim + 1) * 4 : 0;
+    a.chunk = ceil_div(ceil_div(span, splits), least) * least;
+    if (a.chunk < least) a.chunk = least;
+    a.splits = ceil_div(span, a.chunk);
+    if (a.splits < 1) a.splits = 1;
+    a.ctas = units * a.splits;
+    return a;
+}
+
+cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, cudaStream_t stream)
+{
+    P.splits = (int)a.splits;
+    P.chunk = a.chunk;
+    P.row_tiles = (int)a.row_tiles;
+    P.part_out = static_cast<float*>(workspace);
+    P.part_lse = a.splits > 1 ? P.part_out + P.n * P.q_heads * a.splits * P.dim : nullptr;
+    AttnMaps M;
+    const int box = P.page < kTile ? P.page : kTile;
+    if (!make_map(&M.k, P.k_codes, P, box) || !make_map(&M.v, P.v_codes, P, box)) return cudaErrorInvalidValue;
+    cudaError_t e;
+    if (P.dim == 128)
+        e = a.row_warps == 1 ? launch_decode<128, 1, 2>(P, M, a.ctas, stream)
+          : a.row_warps == 2 ? launch_decode<128, 2, 3>(P, M, a.ctas, stream) : launch_decode<128, 4, 4>(P, M, a.ctas, stream);
+    else
+        e = a.row_warps == 1 ? launch_decode<64, 1, 2>(P, M, a.ctas, stream)
+          : a.row_warps == 2 ? launch_decode<64, 2, 3>(P, M, a.ctas, stream) : launch_decode<64, 4, 4>(P, M, a.ctas, stream);
+    if (e != cudaSuccess || a.splits == 1) return e;
+    const int64_t ctas = ceil_div(P.n * P.q_heads, 4);
+    return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, 128, 0, stream, P) : launch(attn_join_kernel<64>, ctas, 128, 0, stream, P);
+}
+
+cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad)
+{
+    const cudaError_t e = cudaMemcpyFromSymbol(timeouts, g_attn_timeouts, sizeof(unsigned int));
+    return e != cudaSuccess ? e : cudaMemcpyFromSymbol(bad, g_attn_bad, sizeof(unsigned int));
+}
+cudaError_t reset_attn_timeouts()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(g_attn_timeouts, &zero, sizeof(unsigned int));
+}
+cudaError_t reset_attn_bad()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(g_attn_bad, &zero, sizeof(unsigned int));
+}
+
+}  // namespace mxn

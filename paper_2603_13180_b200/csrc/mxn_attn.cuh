@@ -1,0 +1,35 @@
+// Declarations shared by the two attention kernels over the 8-bit cache.
+#pragma once
+
+#include <cuda.h>
+
+#include "mxn_async.cuh"
+#include "mxn_device.cuh"
+#include "mxn_internal.h"
+
+namespace mxn {
+
+struct AttnMaps {
+    CUtensorMap k, v;   // codes as [pages * heads, page, dim] bytes
+};
+
+// tiled copy of a box of codes (no multicast); x = 0, y = first token within its page, z = page * heads + head
+__device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(0), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 2^(byte - 127), the value of an E8M0 byte
+__device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 0 ? 0x00400000u : b << 23); }
+
+}  // namespace mxn

@@ -74,4 +74,71 @@ cudaError_t read_timeouts(unsigned int* out);
 cudaError_t reset_timeouts();
 cudaError_t selftest_bounded_wait(unsigned int polls, cudaStream_t stream);
 
+// per-head norm with the position rotation; index 0: queries, 1: keys
+struct HeadsParams {
+    const uint16_t* x[2];       // bf16, token stride x_stride, heads side by side (backward: may be null without a norm)
+    const uint16_t* grad[2];    // backward: gradient of the output
+    uint16_t* y[2];             // output (backward: gradient of x)
+    int64_t x_stride[2], grad_stride[2], y_stride[2];
+    int heads[2];
+    const uint16_t* gain[2];    // bf16 [dim] or nullptr
+    float* dgain[2];            // backward: fp32 [dim] or nullptr
+    float* partial;             // backward: workspace [ctas, dim] or nullptr
+    const float* cos_sin;       // fp32 [table_rows, rot] or nullptr (no rotation)
+    const int32_t* positions;   // [T] or nullptr (row index)
+    int64_t T, table_rows;
+    int dim, rot, pairs, norm;
+    float eps, inv_dim;
+    int parts, per_part, ctas_q;   // filled by the launchers
+};
+cudaError_t launch_rope_fwd(HeadsParams P, cudaStream_t stream);
+cudaError_t launch_rope_bwd(HeadsParams P, cudaStream_t stream);
+int rope_bwd_ctas(int64_t T, int q_heads, int k_heads, int dim);   // rows of the workspace
+cudaError_t read_heads_bad(unsigned int* out);
+cudaError_t reset_heads_bad();
+
+// append to the paged 8-bit cache; index 0: keys, 1: values
+struct KvAppendParams {
+    const uint16_t* x[2];       // bf16 [n, heads, dim], token stride x_stride
+    int64_t x_stride[2];
+    uint8_t* codes[2];          // [num_pages, heads, page, dim]
+    uint8_t* scales[2];         // [num_pages, heads, page / block]
+    const int32_t* cu;          // [seqs + 1]
+    const int32_t* lens;        // [seqs], with the new tokens
+    const int32_t* page_table;  // [seqs, max_pages]
+    const float* cos_sin;       // [table_rows, rot] or nullptr
+    int64_t n, num_pages, max_pages, table_rows;
+    int seqs, heads, dim, page, block, rot, pairs;
+    int run;                    // filled by the launcher
+};
+cudaError_t launch_kv_append(KvAppendParams P, cudaStream_t stream);
+cudaError_t read_kv_bad(unsigned int* out);
+cudaError_t reset_kv_bad();
+
+// attention over the paged 8-bit cache
+struct AttnParams {
+    const uint16_t* q;          // bf16 [n, q_heads, dim], token stride q_stride
+    uint16_t* out;              // bf16, token stride out_stride
+    float* lse;                 // [n, q_heads] or nullptr
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const int32_t *cu_q, *lens, *page_table;
+    int64_t n, q_stride, out_stride, max_pages;
+    int num_pages, seqs, q_heads, kv_heads, group, dim, page, page_shift, block_shift, max_q, max_len, causal, window;
+    float scale;
+    // filled by the launcher
+    float *part_out, *part_lse;
+    int64_t chunk;
+    int splits, row_tiles;
+};
+struct AttnPlan {
+    int64_t chunk, splits, row_tiles, ctas;
+    int row_warps;
+    size_t workspace;
+};
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim);
+cudaError_t launch_attention(AttnParams P, const AttnPlan& plan, void* workspace, cudaStream_t stream);
+cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad);
+cudaError_t reset_attn_timeouts();
+cudaError_t reset_attn_bad();
+
 }  // namespace mxn

@@ -1,0 +1,221 @@
+// Append of keys and values to a paged cache of E4M3 codes with one E8M0 scale for each block of tokens and head.
+//
+//   k' = R(position) k (when a rotation is given);  S = 2^(ceil(log2 absmax) - 8) over a block's tokens of one head;
+//   codes = E4M3(k' / S).
+// A block that already holds earlier tokens keeps at least its scale; where the new tokens raise it, the earlier codes are
+// rounded again on the new scale (exact but for codes that become subnormal).  Power-of-two scales are what makes appending
+// one token at a time cheap and repeatable: appending the same tokens to the same places again changes nothing.
+//
+// One warp owns one (block of tokens, head) of the keys or of the values, so that no two warps ever meet in a block and no
+// atomic is needed.  A warp is given a run of token rows and works on the blocks whose first new token lies in its run; a
+// block's tokens are read twice (maximum, then codes), the second time from L1.  Bound: HBM, 3 bytes an element
+// (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of loads.
+#include "mxn_internal.h"
+#include "mxn_rope.cuh"
+
+namespace mxn {
+
+namespace {
+
+constexpr int kWarps = 4;
+
+__device__ unsigned int g_kv_bad = 0;   // blocks whose page, position or length is out of range
+
+// index of the sequence that row j belongs to: the last s with cu[s] <= j, found 32 probes at a time
+__device__ __forceinline__ int find_sequence(const int32_t* cu, int seqs, int64_t j, int lane)
+{
+    int lo = 0, n = seqs;   // the answer is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const bool below = lane * step < n && (int64_t)__ldg(cu + at) <= j;
+        const unsigned b = __ballot_sync(0xFFFFFFFFu, below);
+        const int k = b ? 31 - __clz(b) : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+
+// four E4M3 bytes -> binary32
+__device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float* f)
+{
+    uint32_t a, b;
+    asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi; }" : "=r"(a), "=r"(b) : "r"(w));
+    asm("{ .reg .f16 lo, hi; mov.b32 {lo, hi}, %2; cvt.f32.f16 %0, lo; cvt.f32.f16 %1, hi; }" : "=f"(f[0]), "=f"(f[1]) : "r"(a));
+    asm("{ .reg .f16 lo, hi; mov.b32 {lo, hi}, %2; cvt.f32.f16 %0, lo; cvt.f32.f16 %1, hi; }" : "=f"(f[2]), "=f"(f[3]) : "r"(b));
+}
+
+template <int LP, bool PAIRS>
+__global__ void __launch_bounds__(kWarps * 32) kv_append_kernel(const KvAppendParams P)
+{
+    constexpr int G = 32 / LP;   // tokens a warp holds at a time
+    pdl_prologue();
+    const int lane = threadIdx.x & 31, sub = lane % LP, grp = lane / LP;
+    const int hv = (int)blockIdx.y * kWarps + (threadIdx.x >> 5);   // keys' heads, then values' heads
+    if (hv >= 2 * P.heads) return;
+    const int which = hv >= P.heads, h = hv - which * P.heads;
+    const bool rotate = which == 0 && P.cos_sin != nullptr;
+    const bool live = 16 * sub < P.dim;
+    const int rot = rotate ? P.rot : 0;
+    const LanePairs lp = lane_pairs(live ? sub : 0, rot, PAIRS);
+    const int64_t rows = min((int64_t)__ldg(P.cu + P.seqs), P.n);
+    int64_t j = (int64_t)blockIdx.x * P.run;
+    const int64_t j_end = min(j + P.run, rows);
+    const int64_t first_row = __ldg(P.cu);
+    if (j < first_row) j = first_row;
+    int s = -1;
+    int64_t c0 = 0, c1 = 0, len = 0;
+    while (j < j_end) {
+        if (s < 0 || j >= c1) {
+            s = find_sequence(P.cu, P.seqs, j, lane);
+            c0 = __ldg(P.cu + s);
+            c1 = min((int64_t)__ldg(P.cu + s + 1), rows);
+            len = __ldg(P.lens + s);
+            if (j < c0 || j >= c1) {   // no sequence holds this row (cu is not a rising list): leave it
+                ++j;
+                s = -1;
+                continue;
+            }
+        }
+        const int64_t pos = len - ((int64_t)__ldg(P.cu + s + 1) - j), start = pos - (j - c0);
+        if (start < 0) {   // more new tokens than the sequence is long
+            if (lane == 0 && j == c0) atomicAdd(&g_kv_bad, 1u);
+            j = c1;
+            continue;
+        }
+        const int in_block = (int)(pos % P.block);
+        const int count = (int)min((int64_t)(P.block - in_block), c1 - j);
+        if (in_block != 0 && j != c0) {   // the block belongs to the warp of its first new token
+            j += count;
+            continue;
+        }
+        const int64_t page_at = pos / P.page;
+        const int64_t page = page_at < P.max_pages ? (int64_t)__ldg(P.page_table + s * P.max_pages + page_at) : -1;
+        if (page < 0 || page >= P.num_pages || (rotate && pos + count > P.table_rows)) {
+            if (lane == 0) atomicAdd(&g_kv_bad, 1u);
+            j += count;
+            continue;
+        }
+        const int off = (int)(pos % P.page);   // of the first new token within its page
+        const int64_t tile = page * P.heads + h;
+        uint8_t* const codes = P.codes[which] + (tile * P.page + (off - in_block)) * P.dim;   // the block's first token
+        uint8_t* const scale = P.scales[which] + tile * (P.page / P.block) + off / P.block;
+        const uint16_t* const x0 = P.x[which] + j * P.x_stride[which] + (int64_t)h * P.dim;
+
+        auto load = [&](int i, float* x) {   // token i of the new ones, rotated
+            uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+            if (live && i < count) {
+                const uint16_t* p = x0 + i * P.x_stride[which];
+                a = __ldg(reinterpret_cast<const uint4*>(p + lp.o0));
+                b = __ldg(reinterpret_cast<const uint4*>(p + lp.o1));
+            }
+            unpack8(x, a);
+            unpack8(x + 8, b);
+            if (rot != 0 && lp.turns && i < count) {
+                Turn turn;
+                load_turn(turn, P.cos_sin + (pos + i) * rot, sub, rot);
+                apply_turn<PAIRS, false>(x, turn);
+            }
+        };
+        float top = 0.0f;
+        for (int i0 = 0; i0 < count; i0 += G) {
+            float x[16];
+            load(i0 + grp, x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+        }
+        uint32_t sb = e8m0_scale_rceil_pow2<8>(warp_max(top));
+        if (in_block != 0) {
+            const uint32_t old = *scale;
+            if (old >= sb) {
+                sb = old;
+            } else if (old != sb) {
+                // earlier tokens on the new scale; 2^(old - sb) below 2^-126 leaves nothing of any code
+                const int d = (int)sb - (int)old;
+                const float by = d > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - d) << 23);
+                for (int i = grp; i < in_block; i += G) {
+                    if (!live) continue;
+                    uint4* p = reinterpret_cast<uint4*>(codes + (int64_t)i * P.dim + 16 * sub);
+                    uint4 w = *p;
+                    uint32_t* v = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float f[4];
+                        e4m3x4_to_f32(v[e], f);
+                        v[e] = cvt_e4m3x4(__fmul_rn(f[0], by), __fmul_rn(f[1], by), __fmul_rn(f[2], by), __fmul_rn(f[3], by));
+                    }
+                    *p = w;
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) *scale = (uint8_t)sb;
+        const float inv = inv_scale(sb);
+        for (int i0 = 0; i0 < count; i0 += G) {
+            const int i = i0 + grp;
+            float x[16];
+            load(i, x);
+            if (!live || i >= count) continue;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = cvt_e4m3x4(__fmul_rn(x[4 * e], inv), __fmul_rn(x[4 * e + 1], inv), __fmul_rn(x[4 * e + 2], inv),
+                                  __fmul_rn(x[4 * e + 3], inv));
+            uint8_t* y = codes + (int64_t)(in_block + i) * P.dim;
+            if (lp.o1 == lp.o0 + 8) {
+                st_v4(y + lp.o0, w);
+            } else {
+                st_v2(y + lp.o0, w);
+                st_v2(y + lp.o1, w + 2);
+            }
+        }
+        j += count;
+    }
+}
+
+template <int LP>
+cudaError_t launch_lp(const KvAppendParams& P, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((P.n + P.run - 1) / P.run), (unsigned)((2 * P.heads + kWarps - 1) / kWarps));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return P.pairs ? cudaLaunchKernelEx(&cfg, kv_append_kernel<LP, true>, P) : cudaLaunchKernelEx(&cfg, kv_append_kernel<LP, false>, P);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append(KvAppendParams P, cudaStream_t stream)
+{
+    // rows a warp looks after: a block's worth for prompts; one where sequences bring about one token each, so that each
+    // block has a warp of its own
+    P.run = P.n >= (int64_t)P.seqs * P.block ? P.block : 1;
+    switch (lanes_per_head(P.dim)) {
+        case 1: return launch_lp<1>(P, stream);
+        case 2: return launch_lp<2>(P, stream);
+        case 4: return launch_lp<4>(P, stream);
+        case 8: return launch_lp<8>(P, stream);
+        default: return launch_lp<16>(P, stream);
+    }
+}
+
+cudaError_t read_kv_bad(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_kv_bad, sizeof(unsigned int)); }
+cudaError_t reset_kv_bad()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(g_kv_bad, &zero, sizeof(unsigned int));
+}
+
+}  // namespace mxn
