@@ -8,7 +8,7 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmxnorm.so")
-SOURCES = ["mxn_api.cu", "mxn_fwd.cu", "mxn_fwd_fp4.cu", "mxn_bwd.cu", "mxn_transposed.cu", "mxn_heads.cu", "mxn_kv.cu", "mxn_attn.cu"]
+SOURCES = ["mxn_api.cu", "mxn_fwd.cu", "mxn_fwd_fp4.cu", "mxn_bwd.cu", "mxn_transposed.cu", "mxn_heads.cu", "mxn_kv.cu", "mxn_attn.cu", "mxn_prompt.cu"]
 HEADERS = ["mxn_device.cuh", "mxn_internal.h", "mxn_row.cuh", "mxn_fwd_common.cuh", "mxn_col.cuh", "mxn_async.cuh", "mxn_rope.cuh", "mxn_attn.cuh",
            os.path.join("..", "..", "include", "mxnorm.h")]
 

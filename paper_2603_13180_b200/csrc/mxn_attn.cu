@@ -42,6 +42,7 @@ namespace {
 constexpr int kSMs = 148;
 constexpr int kWarps = 4;
 constexpr int kTile = 32;      // tokens of a tile
+constexpr int kPromptRows = 32;   // more query rows a sequence and key head than this: the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ unsigned int g_attn_timeouts = 0;
@@ -576,16 +577,18 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     AttnPlan a{};
     if (max_q > n) max_q = n;
     const int64_t rows = max_q * (q_heads / kv_heads);
+    a.prompt = rows > kPromptRows;
     a.row_warps = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-    a.row_tiles = ceil_div(rows, 8 * a.row_warps);
+    a.row_tiles = ceil_div(rows, a.prompt ? 256 : 8 * a.row_warps);
     // enough chunks for four rounds of the CTAs that are resident at a time (sequences differ in length), none
     // shorter than a tile for every group of warps
-    const int64_t units = seqs * kv_heads * a.row_tiles, least = kTile * (kWarps / a.row_warps);
-    int64_t splits = ceil_div((int64_t)kSMs * (dim == 128 ? 3 : 4) * 4, units);
+    const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile, least = a.prompt ? 128 : kTile * (kWarps / a.row_warps);
+    // (many rows: one CTA an SM, whose start costs as much as a few hundred keys; two rounds)
+    int64_t splits = a.prompt ? (units >= kSMs ? 1 : ceil_div(kSMs * 2, units)) : ceil_div((int64_t)kSMs * (dim == 128 ? 3 : 4) * 4, units);
     // keys that the rows of a tile can see between them
-    const int64_t tokens = ceil_div(8 * a.row_warps, q_heads / kv_heads) + 1;
-    const int64_t span = window > 0 && window + tokens + kTile < max_len ? window + tokens + kTile : max_len;
-    const int64_t most = ceil_div(max_len, least);   // of the workspace: for any window
+    const int64_t tokens = ceil_div(a.prompt ? 256 : 8 * a.row_warps, q_heads / kv_heads) + 1;
+    const int64_t span = window > 0 && window + tokens + tile < max_len ? window + tokens + tile : max_len;
+    const int64_t most = ceil_div(max_len, a.prompt ? 512 : least);   // of the workspace: for any window
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     a.workspace = splits > 1 ? (size_t)n * q_heads * splits * (dim + 1) * 4 : 0;
@@ -605,10 +608,12 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     P.part_out = static_cast<float*>(workspace);
     P.part_lse = a.splits > 1 ? P.part_out + P.n * P.q_heads * a.splits * P.dim : nullptr;
     AttnMaps M;
-    const int box = P.page < kTile ? P.page : kTile;
+    const int tile = a.prompt ? 128 : kTile, box = P.page < tile ? P.page : tile;
     if (!make_map(&M.k, P.k_codes, P, box) || !make_map(&M.v, P.v_codes, P, box)) return cudaErrorInvalidValue;
     cudaError_t e;
-    if (P.dim == 128)
+    if (a.prompt)
+        e = launch_prompt(P, M, a.ctas, stream);
+    else if (P.dim == 128)
         e = a.row_warps == 1 ? launch_decode<128, 1, 2>(P, M, a.ctas, stream)
           : a.row_warps == 2 ? launch_decode<128, 2, 3>(P, M, a.ctas, stream) : launch_decode<128, 4, 4>(P, M, a.ctas, stream);
     else
@@ -621,18 +626,25 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
 
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad)
 {
-    const cudaError_t e = cudaMemcpyFromSymbol(timeouts, g_attn_timeouts, sizeof(unsigned int));
-    return e != cudaSuccess ? e : cudaMemcpyFromSymbol(bad, g_attn_bad, sizeof(unsigned int));
+    unsigned int more_timeouts = 0, more_bad = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(timeouts, g_attn_timeouts, sizeof(unsigned int));
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(bad, g_attn_bad, sizeof(unsigned int));
+    if (e == cudaSuccess) e = read_prompt_counters(&more_timeouts, &more_bad);
+    *timeouts += more_timeouts;
+    *bad += more_bad;
+    return e;
 }
 cudaError_t reset_attn_timeouts()
 {
     const unsigned int zero = 0;
-    return cudaMemcpyToSymbol(g_attn_timeouts, &zero, sizeof(unsigned int));
+    const cudaError_t e = cudaMemcpyToSymbol(g_attn_timeouts, &zero, sizeof(unsigned int));
+    return e != cudaSuccess ? e : reset_prompt_counters(true);
 }
 cudaError_t reset_attn_bad()
 {
     const unsigned int zero = 0;
-    return cudaMemcpyToSymbol(g_attn_bad, &zero, sizeof(unsigned int));
+    const cudaError_t e = cudaMemcpyToSymbol(g_attn_bad, &zero, sizeof(unsigned int));
+    return e != cudaSuccess ? e : reset_prompt_counters(false);
 }
 
 }  // namespace mxn

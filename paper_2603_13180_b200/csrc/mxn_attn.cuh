@@ -13,6 +13,11 @@ struct AttnMaps {
     CUtensorMap k, v;   // codes as [pages * heads, page, dim] bytes
 };
 
+// the kernel for many query rows (mxn_prompt.cu)
+cudaError_t launch_prompt(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream);
+cudaError_t read_prompt_counters(unsigned int* timeouts, unsigned int* bad);
+cudaError_t reset_prompt_counters(bool timeouts);
+
 // tiled copy of a box of codes (no multicast); x = 0, y = first token within its page, z = page * heads + head
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar)
 {

@@ -133,6 +133,7 @@ struct AttnParams {
 struct AttnPlan {
     int64_t chunk, splits, row_tiles, ctas;
     int row_warps;
+    bool prompt;                // many query rows: the tcgen05 kernel
     size_t workspace;
 };
 AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim);

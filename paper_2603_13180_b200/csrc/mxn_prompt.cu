@@ -1,0 +1,615 @@
+// Attention over the paged 8-bit cache for many query rows (prompts): both products on the 5th-generation tensor cores.
+//
+//   o = sum_t softmax(scale q . k_t) v_t,   k_t = 2^(sk - 127) * code, v_t likewise
+//
+// Work of a CTA: 256 query rows of one sequence and key head (query heads that share a key head are rows like any other: row =
+// token * group + head), in two tiles of 128, over a chunk of the keys in tiles of 128 tokens.  Tensor memory holds the scores
+// and the output of both tiles (2 * (128 + dim) columns of binary32).  Roles, by warp:
+//   0      copies: codes of keys and values by the tensor copy engine, a box for each page; scales by plain loads
+//   1      issues the products (one thread)
+//   4-7    values: E4M3 codes -> f16 (exact), zeros for what no row may see
+//   8-15   softmax, one warpgroup for each row tile, a thread for each row
+// The two row tiles alternate: while one's scores are in the softmax, the other's products run.
+//
+// Scores: E4M3 x E4M3 products on the key codes as they are; q is scaled by a power of two to [128, 256) at its row's largest
+//   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-10 of the row's largest (to 2^-18
+//   of it).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
+// Weights: w_t = 2^(s_t + sv_t - R + 4) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
+//   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
+//   is moved only when a tile's largest is 8 above or 12 below it: f16 keeps 2^-25 of the weight 1, at least 2^-17 of the
+//   tile's largest, and the output in tensor memory rarely has to be corrected.
+// The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA.
+// The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
+// second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
+//
+// Bound: at head size 128 the two products of a 256 x 128 tile take 2048 cycles at the tensor cores' rate, its 32768 exponentials
+// 2048 cycles of the special function units: the kernel needs both busy at once.
+//
+// Every wait is bounded; see mxn_device_timeouts.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "mxn_attn.cuh"
+
+namespace mxn {
+
+namespace {
+
+constexpr int kTile = 128;        // tokens of a key tile, rows of a row tile
+constexpr int kThreads = 512;
+constexpr int kKeyStages = 3, kValStages = 2, kHalfStages = 2, kScaleSlots = 8;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kRun = 16;          // tokens that share a scale at the finest
+constexpr float kTop = 4.0f;      // log2 of the weight at the reference
+
+__device__ unsigned int g_prompt_timeouts = 0;
+__device__ unsigned int g_prompt_bad = 0;
+
+template <int DIM>
+struct PromptShape {
+    static constexpr int kCodes = kTile * DIM;                 // bytes of a tile of codes (keys, values, q hi, q lo)
+    static constexpr int kHalf = kTile * DIM * 2;              // bytes of a tile of f16 values
+    static constexpr int kQ = 0;                               // [row tile][hi, lo]
+    static constexpr int kK = kQ + 4 * kCodes;
+    static constexpr int kV = kK + kKeyStages * kCodes;
+    static constexpr int kH = kV + kValStages * kCodes;
+    static constexpr int kEnd = kH + kHalfStages * kHalf;
+    static constexpr int kSmem = kEnd + 1024;
+};
+
+// one slot of the scales' ring: what the softmax needs to know about a key tile.  The ring is deeper than the keys': a slot is
+// written again once the keys kKeyStages tiles before are free, i.e. when the softmax of both row tiles is past the tile before those.
+struct alignas(16) TileScales {
+    float k[kTile / kRun];        // 2^(sk - 127)
+    float v[kTile / kRun];        // sv - 127
+    uint32_t readable;            // bit i: the page of run i could be read
+    uint32_t wide;                // the value scales lie so far apart that l needs exponentials of its own
+};
+
+// ---- tensor core plumbing ------------------------------------------------------------------------------------
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// shared-memory operand descriptor: address, stride between groups of 8 rows (`group`), between repeats along the other
+// axis (`repeat`), and the swizzle (2: 128 bytes, 4: 64 bytes)
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t group, uint32_t repeat, uint32_t swizzle)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(repeat >> 4) << 16) | ((uint64_t)(group >> 4) << 32) | (1ull << 46) |
+           ((uint64_t)swizzle << 61);
+}
+// instruction descriptors: binary32 sums, M = 128
+__host__ __device__ constexpr uint32_t idesc_e4m3(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+__host__ __device__ constexpr uint32_t idesc_f16_bt(int n) { return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+
+__device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add)
+{
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p; }"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add)
+{
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+#define MXN_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define MXN_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of this warp's 32 lanes, a lane's row in its thread
+__device__ __forceinline__ void tm_load(uint32_t (&r)[32], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+                 "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : MXN_R8(r, 0), MXN_R8(r, 8), MXN_R8(r, 16), MXN_R8(r, 24) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+                 "%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 :: "r"(addr), MXN_I8(r, 0), MXN_I8(r, 8), MXN_I8(r, 16), MXN_I8(r, 24) : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(addr), MXN_I8(r, 0), MXN_I8(r, 8) : "memory");
+}
+__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// waits with a limit; a wait that runs out, or one that sees another's, ends the CTA's work
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* dead)
+{
+    for (uint32_t spin = 0; spin < (1u << 20); ++spin) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((spin & 255u) == 255u && *dead) return false;
+    }
+    *dead = 1;
+    return false;
+}
+
+__device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
+
+template <int DIM>
+__global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
+{
+    using Sh = PromptShape<DIM>;
+    constexpr uint32_t SW = DIM == 128 ? 2 : 4;         // swizzle of a tile of codes: its rows are DIM bytes
+    constexpr uint32_t GROUP = 8 * DIM;                 // bytes of 8 rows of codes
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[2 * kKeyStages + 2 * kValStages + 2 * kHalfStages + 5 + kScaleSlots];
+    __shared__ TileScales scales[kScaleSlots];
+    __shared__ uint32_t tmem_at;
+    __shared__ int dead_flag;
+
+    pdl_prologue();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t b = blockIdx.x;
+    const int split = (int)(b % P.splits);
+    b /= P.splits;
+    const int seq = (int)(b % P.seqs);
+    b /= P.seqs;
+    const int h = (int)(b % P.kv_heads);
+    const int block = P.row_tiles - 1 - (int)(b / P.kv_heads);   // the rows that see most keys first
+
+    const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
+    const int len = min(__ldg(P.lens + seq), P.max_len);
+    const int nq = max(0, min(q1 - q0, P.max_q));
+    const int G = P.group, row0 = block * 2 * kTile, rows = nq * G;
+    if (q0 < 0 || row0 >= rows) return;
+    const int shift = len - (q1 - q0);
+    const int last = min(rows, row0 + 2 * kTile) - 1;
+    const int hi = max(0, min(len, P.causal ? shift + last / G + 1 : len));
+    const int lo = P.window > 0 ? max(0, shift + row0 / G - P.window + 1) / kTile * kTile : 0;
+    const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
+    const int tiles = (k1 - k0 + kTile - 1) / kTile;
+
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t k_full = bar0, k_empty = k_full + 8 * kKeyStages, v_full = k_empty + 8 * kKeyStages, v_empty = v_full + 8 * kValStages,
+                   h_full = v_empty + 8 * kValStages, h_empty = h_full + 8 * kHalfStages, s_full = h_empty + 8 * kHalfStages,
+                   p_full = s_full + 16, o_done = p_full + 16, sc_full = o_done + 8;
+    volatile int* const dead = &dead_flag;
+    if (threadIdx.x == 0) {
+        dead_flag = 0;
+        for (int i = 0; i < kKeyStages; ++i) {
+            mbar_init(k_full + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kValStages; ++i) {
+            mbar_init(v_full + 8 * i, 1);
+            mbar_init(v_empty + 8 * i, 4);
+        }
+        for (int i = 0; i < kHalfStages; ++i) {
+            mbar_init(h_full + 8 * i, 4);
+            mbar_init(h_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 4);
+        }
+        mbar_init(o_done, 1);
+        for (int i = 0; i < kScaleSlots; ++i) mbar_init(sc_full + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // q: a thread of the softmax warps loads its row, splits it and leaves hi and lo for the tensor cores
+    const int rt = (warp >> 2) & 1;                       // row tile of warps 8-15
+    const int r_in = threadIdx.x & 127;                   // row within its tile
+    const int row = row0 + rt * kTile + r_in;
+    const bool row_live = warp >= 8 && row < rows;
+    const int64_t tok = q0 + (row_live ? row / G : 0);
+    const int head = h * G + (row_live ? row % G : 0);
+    float row_factor = 0.0f;
+    if (warp >= 8) {
+        uint4 w[DIM / 8];
+        const uint16_t* qp = P.q + tok * P.q_stride + (int64_t)head * DIM;
+#pragma unroll
+        for (int i = 0; i < DIM / 8; ++i) w[i] = row_live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < DIM / 2; ++i) m = absmax_bf16x2(m, u[i]);
+        const uint32_t E = __float_as_uint(hmax_abs_to_f32(m)) >> 23;
+        const uint32_t Ec = min(max(E, 8u), 254u);
+        float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);             // 2^(7 - (E - 127))
+        row_factor = fabsf(P.scale) * kLog2e * __uint_as_float((Ec - 7u) << 23);
+        if (P.scale < 0.0f) up = -up;
+        const uint32_t hi_at = base + Sh::kQ + rt * 2 * Sh::kCodes, lo_at = hi_at + Sh::kCodes;
+#pragma unroll
+        for (int i = 0; i < DIM / 16; ++i) {   // 16 elements: one 16-byte chunk of hi, one of lo
+            uint32_t a[4], c[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t u0 = u[8 * i + 2 * x], u1 = u[8 * i + 2 * x + 1];
+                uint32_t hh[2], ll[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const __half2 v = __floats2half2_rn(bf16_lo(y ? u1 : u0) * up, bf16_hi(y ? u1 : u0) * up);
+                    hh[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(v), __NV_SATFINITE, __NV_E4M3);
+                    const __half2 left = __hsub2(v, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hh[y], __NV_E4M3)));
+                    ll[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(left), __NV_SATFINITE, __NV_E4M3);
+                }
+                a[x] = hh[0] | (hh[1] << 16);
+                c[x] = ll[0] | (ll[1] << 16);
+            }
+            const uint32_t off = (uint32_t)r_in * DIM + (uint32_t)((DIM == 128 ? i ^ (r_in & 7) : i ^ ((r_in >> 1) & 3)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(hi_at + off), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(lo_at + off), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]) : "memory");
+        }
+        fence_async();
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_at;
+    const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + DIM};
+
+    if (warp == 0) {
+        // ---- copies ----
+        const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
+        const int box = min(P.page, kTile), boxes = kTile / box;     // tokens of a box, boxes of a tile
+        const int per_page_shift = P.page_shift - P.block_shift;
+        bool any_bad = false;
+        int page_next = -1;                                          // lane i: page of run i (lanes 0-7) of the next tile
+        auto look_up = [&](int j) {
+            const int t = k0 + j * kTile + kRun * (lane & 7);
+            int pg = -1;
+            if (j < tiles && lane < 8 && t < k1) {
+                pg = __ldg(table + (t >> P.page_shift));
+                if (pg < 0 || pg >= P.num_pages) {
+                    pg = -1;
+                    any_bad = true;
+                }
+            }
+            return pg;
+        };
+        page_next = look_up(0);
+        bool ok = true;
+        for (int j = 0; j < tiles; ++j) {
+            const int pg = page_next;
+            page_next = look_up(j + 1);
+            const int t0 = k0 + j * kTile, ks = j % kKeyStages, vs = j % kValStages;
+            // scales
+            uint32_t sk = 0, sv = 0;
+            if (pg >= 0) {
+                const int64_t at = (((int64_t)pg * P.kv_heads + h) << per_page_shift) + (((t0 + kRun * lane) & (P.page - 1)) >> P.block_shift);
+                sk = __ldg(P.k_scales + at);
+                sv = __ldg(P.v_scales + at);
+            }
+            const uint32_t readable = __ballot_sync(0xFFFFFFFFu, pg >= 0);
+            // this lane's box starts at run lane * (box / 16)
+            const int src = lane * (box / kRun);
+            const int box_page = __shfl_sync(0xFFFFFFFFu, pg, src & 7);
+            const bool mine = lane < boxes && box_page >= 0;
+            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(box * DIM);
+            const int y = (t0 + src * kRun) & (P.page - 1), z = box_page * P.kv_heads + h;
+
+            if (j >= kKeyStages) ok = ok && wait(k_empty + 8 * ks, (uint32_t)(j / kKeyStages - 1) & 1u, dead);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            TileScales& slot = scales[j % kScaleSlots];
+            if (lane < 8) {
+                slot.k[lane] = e8m0_to_f32(sk);
+                slot.v[lane] = (float)(int)sv - 127.0f;
+            }
+            if (lane == 0) slot.readable = readable;
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(sc_full + 8 * (j % kScaleSlots));
+                if (bytes) mbar_expect_tx(k_full + 8 * ks, bytes);
+                else mbar_arrive(k_full + 8 * ks);
+            }
+            __syncwarp();
+            if (mine) tma_load_codes(base + Sh::kK + ks * Sh::kCodes + lane * box * DIM, &M.k, y, z, k_full + 8 * ks);
+            if (j >= kValStages) ok = ok && wait(v_empty + 8 * vs, (uint32_t)(j / kValStages - 1) & 1u, dead);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (lane == 0) {
+                if (bytes) mbar_expect_tx(v_full + 8 * vs, bytes);
+                else mbar_arrive(v_full + 8 * vs);
+            }
+            __syncwarp();
+            if (mine) tma_load_codes(base + Sh::kV + vs * Sh::kCodes + lane * box * DIM, &M.v, y, z, v_full + 8 * vs);
+        }
+        if (__any_sync(0xFFFFFFFFu, any_bad) && lane == 0) atomicAdd(&g_prompt_bad, 1u);
+    } else if (warp == 1) {
+        // ---- products ----
+        if (lane == 0 && tiles > 0) {
+            bool ok = true;
+            auto scores = [&](int r, int j) {   // S_r = (hi + lo) K^T
+                const uint32_t q = base + Sh::kQ + r * 2 * Sh::kCodes, k = base + Sh::kK + (j % kKeyStages) * Sh::kCodes;
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int s = 0; s < DIM / 32; ++s)
+                        mma_scores(s_col[r], operand(q + part * Sh::kCodes + 32 * s, GROUP, 16, SW), operand(k + 32 * s, GROUP, 16, SW),
+                                   idesc_e4m3(kTile), (part | s) != 0);
+                mma_commit(s_full + 8 * r);
+            };
+            ok = wait(k_full, 0, dead);
+            if (ok) {
+                tc_after();
+                scores(0, 0);
+                scores(1, 0);
+                mma_commit(k_empty);
+            }
+            for (int j = 0; ok && j < tiles; ++j) {
+                const int hs = j % kHalfStages, ks = (j + 1) % kKeyStages;
+                ok = wait(h_full + 8 * hs, (uint32_t)(j / kHalfStages) & 1u, dead);
+                if (ok && j + 1 < tiles) ok = wait(k_full + 8 * ks, (uint32_t)((j + 1) / kKeyStages) & 1u, dead);
+                for (int r = 0; ok && r < 2; ++r) {
+                    ok = wait(p_full + 8 * r, (uint32_t)j & 1u, dead);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t v = base + Sh::kH + hs * Sh::kHalf;
+#pragma unroll
+                    for (int s = 0; s < kTile / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
+                        mma_values(o_col[r], s_col[r] + 8 * s, operand(v + s * 2048, 1024, kTile * 128, 2), idesc_f16_bt(DIM), j > 0 || s > 0);
+                    if (r == 1) mma_commit(h_empty + 8 * hs);
+                    if (j + 1 < tiles) scores(r, j + 1);
+                }
+                if (ok && j + 1 < tiles) mma_commit(k_empty + 8 * ks);
+            }
+            mma_commit(o_done);
+            if (!ok) (void)mbar_wait_bounded(o_done, 0, 1u << 16);
+        }
+    } else if (warp >= 4 && warp < 8) {
+        // ---- values to f16 ----
+        const int t = threadIdx.x - 128;   // token row of the tile
+        bool ok = true;
+        for (int j = 0; j < tiles; ++j) {
+            const int vs = j % kValStages, hs = j % kHalfStages;
+            ok = wait(v_full + 8 * vs, (uint32_t)(j / kValStages) & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            const int place = k0 + j * kTile + t;
+            const bool real = place < k1 && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
+            const uint32_t src = base + Sh::kV + vs * Sh::kCodes + (uint32_t)t * DIM;
+            uint4 w[DIM / 16];
+#pragma unroll
+            for (int i = 0; i < DIM / 16; ++i) {
+                w[i] = lds_v4(src + (uint32_t)((DIM == 128 ? i ^ (t & 7) : i ^ ((t >> 1) & 3)) << 4));
+                if (!real) w[i] = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(v_empty + 8 * vs);
+            if (j >= kHalfStages) ok = wait(h_empty + 8 * hs, (uint32_t)(j / kHalfStages - 1) & 1u, dead);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            // panels of 64 dimensions: [token][128 bytes], 128-byte swizzle
+            const uint32_t dst = base + Sh::kH + hs * Sh::kHalf + (uint32_t)t * 128;
+#pragma unroll
+            for (int i = 0; i < DIM / 16; ++i) {
+                const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                uint32_t o[8];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u[x] & 0xFFFFu), __NV_E4M3);
+                    const __half2_raw c = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u[x] >> 16), __NV_E4M3);
+                    o[2 * x] = (uint32_t)a.x | ((uint32_t)a.y << 16);
+                    o[2 * x + 1] = (uint32_t)c.x | ((uint32_t)c.y << 16);
+                }
+                const uint32_t panel = dst + (uint32_t)(i / 4) * (kTile * 128);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t at = panel + (uint32_t)(((2 * (i % 4) + x) ^ (t & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(o[4 * x]), "r"(o[4 * x + 1]), "r"(o[4 * x + 2]), "r"(o[4 * x + 3]) : "memory");
+                }
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(h_full + 8 * hs);
+        }
+    } else if (warp >= 8) {
+        // ---- softmax ----
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = s_col[rt] + lanes, o_at = o_col[rt] + lanes;
+        const int pos = shift + (row_live ? row / G : nq - 1);
+        const int see_hi = P.causal ? min(pos + 1, len) : len;
+        const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+        const float kNone = -INFINITY;
+        float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
+        bool ok = true;
+        for (int j = 0; j < tiles; ++j) {
+            const TileScales& slot = scales[j % kScaleSlots];
+            ok = wait(s_full + 8 * rt, (uint32_t)j & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            tc_after();
+            const int t0 = k0 + j * kTile;
+            const uint32_t readable = slot.readable;
+            const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kTile <= see_hi) && readable == 0xFFu && t0 + kTile <= k1;
+            // bit e: the row sees token 32 c + e of the tile
+            auto visible = [&](int c) -> uint32_t {
+                const int tc = t0 + 32 * c, up = min(max(min(see_hi, k1) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
+                const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u, above = down == 32 ? 0u : 0xFFFFFFFFu << down;
+                return below & above & (((readable >> (2 * c)) & 1u ? 0xFFFFu : 0u) | ((readable >> (2 * c + 1)) & 1u ? 0xFFFF0000u : 0u));
+            };
+            uint32_t x[32];
+            // largest s + sv of the row
+            float utop = kNone;
+            float far = 0.0f;
+            if (j == 0) {
+                c0 = fmaxf(fmaxf(fmaxf(slot.v[0], slot.v[1]), fmaxf(slot.v[2], slot.v[3])), fmaxf(fmaxf(slot.v[4], slot.v[5]), fmaxf(slot.v[6], slot.v[7])));
+                c0 = fminf(fmaxf(c0, -60.0f), 60.0f);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                tm_load(x, s_at + 32 * c);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    float m = kNone;
+                    if (all) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) m = fmaxf(m, __uint_as_float(x[16 * g + e]));
+                    } else {
+                        const uint32_t see = visible(c);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) m = fmaxf(m, (see >> (16 * g + e)) & 1u ? __uint_as_float(x[16 * g + e]) : kNone);
+                    }
+                    const float sv = slot.v[2 * c + g];
+                    far = fmaxf(far, fabsf(sv - c0));
+                    utop = fmaxf(utop, fmaf(m, row_factor * slot.k[2 * c + g], sv));
+                }
+            }
+            utop = ceilf(utop);
+            top_all = fmaxf(top_all, utop);
+            float next = ref;
+            if (utop > ref + 8.0f || (ref == kNone && utop > kNone)) next = utop;
+            else if (utop < ref - 12.0f && utop > kNone) next = fmaxf(utop, top_all - 40.0f);
+            if (__any_sync(0xFFFFFFFFu, next != ref)) {
+                const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
+                l *= alpha;
+                ref = next;
+                if (j > 0) {   // the products up to the last tile's are done: their end was signalled with these scores'
+#pragma unroll
+                    for (int c = 0; c < DIM / 32; ++c) {
+                        tm_load(x, o_at + 32 * c);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
+                        tm_store32(o_at + 32 * c, x);
+                    }
+                }
+            }
+            const float rs = ref == kNone ? 0.0f : ref;
+            const bool wide = far > 40.0f;   // the same for every row
+            // weights, over the scores already read
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                tm_load(x, s_at + 32 * c);
+                uint32_t w[16];
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const float sv = slot.v[2 * c + g], f = row_factor * slot.k[2 * c + g], add = sv + kTop - rs;
+                    float2 sum = f2(0.0f);
+                    const uint32_t see = all ? 0xFFFFu : visible(c) >> (16 * g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 s = make_float2(__uint_as_float(x[16 * g + 2 * e]), __uint_as_float(x[16 * g + 2 * e + 1]));
+                        float2 u = __ffma2_rn(s, f2(f), f2(add));
+                        if (!all) {
+                            if (!((see >> (2 * e)) & 1u)) u.x = kNone;
+                            if (!((see >> (2 * e + 1)) & 1u)) u.y = kNone;
+                        }
+                        const float2 p = make_float2(ex2(u.x), ex2(u.y));
+                        if (!wide) {
+                            sum = __fadd2_rn(sum, p);
+                        } else {
+                            sum.x += ex2(u.x + (c0 - sv));
+                            sum.y += ex2(u.y + (c0 - sv));
+                        }
+                        const __half2 q = __floats2half2_rn(p.x, p.y);
+                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                    }
+                    l = wide ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, ex2(c0 - sv), l);
+                }
+                tm_store16(s_at + 16 * c, w);
+            }
+            tm_store_wait();
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 8 * rt);
+        }
+        // ---- output ----
+        if (ok && tiles > 0) ok = wait(o_done, 0, dead);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        tc_after();
+        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 4 - c0
+        const bool some = l > 0.0f;
+        const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
+        const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
+        const int64_t out_row = tok * P.q_heads + head;
+#pragma unroll
+        for (int c = 0; c < DIM / 32; ++c) {
+            uint32_t x[32];
+            if (tiles > 0) {
+                tm_load(x, o_at + 32 * c);
+            }
+            __syncwarp();
+            float* const o = reinterpret_cast<float*>(x);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * inv : 0.0f;
+            if (!row_live) {
+            } else if (P.splits == 1) {
+                uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + 32 * c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t r[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(o[8 * e + 2 * i], o[8 * e + 2 * i + 1]);
+                        r[i] = *reinterpret_cast<const uint32_t*>(&v);
+                    }
+                    st_v4(y + 8 * e, r);
+                }
+            } else if (some) {
+                float* const y = P.part_out + (out_row * P.splits + split) * DIM + 32 * c;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            }
+            __syncwarp();
+        }
+        if (row_live) {
+            if (P.splits > 1) P.part_lse[out_row * P.splits + split] = lse2;
+            else if (P.lse != nullptr) P.lse[out_row] = lse2 * kLn2;
+        }
+        tc_before();
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && dead_flag) {
+        // a wait ran out: the copies in flight get a second, shorter wait before the shared memory is given up
+        atomicAdd(&g_prompt_timeouts, 1u);
+        for (int i = 0; i < kKeyStages + kValStages; ++i) {
+            const uint32_t bar = i < kKeyStages ? k_full + 8 * i : v_full + 8 * (i - kKeyStages);
+            (void)mbar_wait_bounded(bar, 0, 1u << 14);
+            (void)mbar_wait_bounded(bar, 1, 1u << 14);
+        }
+    }
+    __syncwarp();
+    if (warp == 1) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    }
+}
+
+template <int DIM>
+cudaError_t launch_dim(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
+{
+    const int smem = PromptShape<DIM>::kSmem;
+    const cudaError_t e = cudaFuncSetAttribute(attn_prompt_kernel<DIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attn_prompt_kernel<DIM>, P, M);
+}
+
+}  // namespace
+
+cudaError_t launch_prompt(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
+{
+    return P.dim == 128 ? launch_dim<128>(P, M, ctas, stream) : launch_dim<64>(P, M, ctas, stream);
+}
+
+cudaError_t read_prompt_counters(unsigned int* timeouts, unsigned int* bad)
+{
+    const cudaError_t e = cudaMemcpyFromSymbol(timeouts, g_prompt_timeouts, sizeof(unsigned int));
+    return e != cudaSuccess ? e : cudaMemcpyFromSymbol(bad, g_prompt_bad, sizeof(unsigned int));
+}
+cudaError_t reset_prompt_counters(bool timeouts)
+{
+    const unsigned int zero = 0;
+    return timeouts ? cudaMemcpyToSymbol(g_prompt_timeouts, &zero, sizeof(unsigned int)) : cudaMemcpyToSymbol(g_prompt_bad, &zero, sizeof(unsigned int));
+}
+
+}  // namespace mxn
