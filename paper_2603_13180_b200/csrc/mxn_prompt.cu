@@ -14,10 +14,10 @@
 // Scores: E4M3 x E4M3 products on the key codes as they are; q is scaled by a power of two to [128, 256) at its row's largest
 //   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-10 of the row's largest (to 2^-18
 //   of it).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
-// Weights: w_t = 2^(s_t + sv_t - R + 4) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
+// Weights: w_t = 2^(s_t + sv_t - R + 5) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
-//   is moved only when a tile's largest is 8 above or 12 below it: f16 keeps 2^-25 of the weight 1, at least 2^-17 of the
-//   tile's largest, and the output in tensor memory rarely has to be corrected.
+//   is moved only when a tile's largest is 10 above or 15 below it, so that the output in tensor memory rarely has to be corrected.
+//   f16 drops what is below 2^-25, i.e. 2^-30 of the weight at R and 2^-15 of the largest of a tile at the window's lower end.
 // The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA.
 // The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
@@ -30,6 +30,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "mxn_attn.cuh"
 
 namespace mxn {
@@ -41,7 +43,10 @@ constexpr int kThreads = 512;
 constexpr int kKeyStages = 3, kValStages = 2, kHalfStages = 2, kScaleSlots = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRun = 16;          // tokens that share a scale at the finest
-constexpr float kTop = 4.0f;      // log2 of the weight at the reference
+// Weights: 2^kTop at the reference; the reference is moved when a tile's largest is more than kUp above or kDown below it, but to
+// no more than kDepth below the largest so far (the output's sums must not overflow)
+constexpr float kTop = 5.0f, kUp = 10.0f, kDown = 15.0f, kDepth = 40.0f;
+constexpr float kBig = 32768.0f, kSmall = 0.0009765625f;   // 2^(kTop + kUp), 2^(kTop - kDown)
 
 __device__ unsigned int g_prompt_timeouts = 0;
 __device__ unsigned int g_prompt_bad = 0;
@@ -63,8 +68,10 @@ struct PromptShape {
 struct alignas(16) TileScales {
     float k[kTile / kRun];        // 2^(sk - 127)
     float v[kTile / kRun];        // sv - 127
+    float l[kTile / kRun];        // 2^(c0 - v): from weights to the softmax's sum
     uint32_t readable;            // bit i: the page of run i could be read
-    uint32_t wide;                // the value scales lie so far apart that l needs exponentials of its own
+    uint32_t wide;                // a value scale lies so far from c0 that l needs exponentials of its own
+    float c0;
 };
 
 // ---- tensor core plumbing ------------------------------------------------------------------------------------
@@ -98,6 +105,7 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
 #define MXN_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define MXN_U8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
 #define MXN_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
 // 32 columns of this warp's 32 lanes, a lane's row in its thread
 __device__ __forceinline__ void tm_load(uint32_t (&r)[32], uint32_t addr)
@@ -105,6 +113,17 @@ __device__ __forceinline__ void tm_load(uint32_t (&r)[32], uint32_t addr)
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
                  "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
                  : MXN_R8(r, 0), MXN_R8(r, 8), MXN_R8(r, 16), MXN_R8(r, 24) : "r"(addr) : "memory");
+}
+// the same in two steps: the values are there after tm_arrived of the same registers
+__device__ __forceinline__ void tm_request(uint32_t (&r)[32], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+                 "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : MXN_R8(r, 0), MXN_R8(r, 8), MXN_R8(r, 16), MXN_R8(r, 24) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_arrived(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : MXN_U8(r, 0), MXN_U8(r, 8), MXN_U8(r, 16), MXN_U8(r, 24) :: "memory");
 }
 __device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t (&r)[32])
 {
@@ -252,12 +271,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const uint32_t tmem = tmem_at;
     const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + DIM};
 
+    // 512 threads at 128 registers: the softmax warps take what the others give up (256 * 56 + 256 * 200 = 512 * 128)
+#define MXN_FEW_REGISTERS() asm volatile("setmaxnreg.dec.sync.aligned.u32 56;")
     if (warp == 0) {
         // ---- copies ----
+        MXN_FEW_REGISTERS();
         const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
         const int box = min(P.page, kTile), boxes = kTile / box;     // tokens of a box, boxes of a tile
         const int per_page_shift = P.page_shift - P.block_shift;
         bool any_bad = false;
+        float c0 = 0.0f;
         int page_next = -1;                                          // lane i: page of run i (lanes 0-7) of the next tile
         auto look_up = [&](int j) {
             const int t = k0 + j * kTile + kRun * (lane & 7);
@@ -295,11 +318,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             if (j >= kKeyStages) ok = ok && wait(k_empty + 8 * ks, (uint32_t)(j / kKeyStages - 1) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             TileScales& slot = scales[j % kScaleSlots];
+            const float v = (float)(int)sv - 127.0f;
+            if (j == 0) {   // near the value scales: the largest of the first tile
+                c0 = v;
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) c0 = fmaxf(c0, __shfl_xor_sync(0xFFFFFFFFu, c0, o));
+                c0 = fminf(fmaxf(__shfl_sync(0xFFFFFFFFu, c0, 0), -60.0f), 60.0f);
+            }
+            const bool wide = __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - c0) > 40.0f);
             if (lane < 8) {
                 slot.k[lane] = e8m0_to_f32(sk);
-                slot.v[lane] = (float)(int)sv - 127.0f;
+                slot.v[lane] = v;
+                slot.l[lane] = ex2(fminf(fmaxf(c0 - v, -40.0f), 40.0f));
             }
-            if (lane == 0) slot.readable = readable;
+            if (lane == 0) {
+                slot.readable = readable;
+                slot.wide = wide;
+                slot.c0 = c0;
+            }
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(sc_full + 8 * (j % kScaleSlots));
@@ -320,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         if (__any_sync(0xFFFFFFFFu, any_bad) && lane == 0) atomicAdd(&g_prompt_bad, 1u);
     } else if (warp == 1) {
         // ---- products ----
+        MXN_FEW_REGISTERS();
         if (lane == 0 && tiles > 0) {
             bool ok = true;
             auto scores = [&](int r, int j) {   // S_r = (hi + lo) K^T
@@ -361,6 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         }
     } else if (warp >= 4 && warp < 8) {
         // ---- values to f16 ----
+        MXN_FEW_REGISTERS();
         const int t = threadIdx.x - 128;   // token row of the tile
         bool ok = true;
         for (int j = 0; j < tiles; ++j) {
@@ -369,22 +407,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const int place = k0 + j * kTile + t;
             const bool real = place < k1 && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
-            const uint32_t src = base + Sh::kV + vs * Sh::kCodes + (uint32_t)t * DIM;
-            uint4 w[DIM / 16];
-#pragma unroll
-            for (int i = 0; i < DIM / 16; ++i) {
-                w[i] = lds_v4(src + (uint32_t)((DIM == 128 ? i ^ (t & 7) : i ^ ((t >> 1) & 3)) << 4));
-                if (!real) w[i] = make_uint4(0, 0, 0, 0);
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(v_empty + 8 * vs);
             if (j >= kHalfStages) ok = wait(h_empty + 8 * hs, (uint32_t)(j / kHalfStages - 1) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            const uint32_t src = base + Sh::kV + vs * Sh::kCodes + (uint32_t)t * DIM;
             // panels of 64 dimensions: [token][128 bytes], 128-byte swizzle
             const uint32_t dst = base + Sh::kH + hs * Sh::kHalf + (uint32_t)t * 128;
 #pragma unroll
             for (int i = 0; i < DIM / 16; ++i) {
-                const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                uint4 w = lds_v4(src + (uint32_t)((DIM == 128 ? i ^ (t & 7) : i ^ ((t >> 1) & 3)) << 4));
+                if (!real) w = make_uint4(0, 0, 0, 0);
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
                 uint32_t o[8];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -402,10 +434,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             }
             fence_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(h_full + 8 * hs);
+            if (lane == 0) {
+                mbar_arrive(v_empty + 8 * vs);
+                mbar_arrive(h_full + 8 * hs);
+            }
         }
     } else if (warp >= 8) {
         // ---- softmax ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = s_col[rt] + lanes, o_at = o_col[rt] + lanes;
         const int pos = shift + (row_live ? row / G : nq - 1);
@@ -421,92 +457,120 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             tc_after();
             const int t0 = k0 + j * kTile;
             const uint32_t readable = slot.readable;
-            const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kTile <= see_hi) && readable == 0xFFu && t0 + kTile <= k1;
+            const bool wide = slot.wide != 0;
+            c0 = slot.c0;
             // bit e: the row sees token 32 c + e of the tile
             auto visible = [&](int c) -> uint32_t {
                 const int tc = t0 + 32 * c, up = min(max(min(see_hi, k1) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
                 const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u, above = down == 32 ? 0u : 0xFFFFFFFFu << down;
                 return below & above & (((readable >> (2 * c)) & 1u ? 0xFFFFu : 0u) | ((readable >> (2 * c + 1)) & 1u ? 0xFFFF0000u : 0u));
             };
-            uint32_t x[32];
-            // largest s + sv of the row
-            float utop = kNone;
-            float far = 0.0f;
-            if (j == 0) {
-                c0 = fmaxf(fmaxf(fmaxf(slot.v[0], slot.v[1]), fmaxf(slot.v[2], slot.v[3])), fmaxf(fmaxf(slot.v[4], slot.v[5]), fmaxf(slot.v[6], slot.v[7])));
-                c0 = fminf(fmaxf(c0, -60.0f), 60.0f);
+            // One pass over the scores with the reference as it stands.  False, with nothing written, where a row's weights leave
+            // the window that f16 holds well.
+            auto one_pass = [&](auto masked) -> bool {
+                constexpr bool MASKED = decltype(masked)::value;
+                uint32_t x[2][32], w[64];
+                __half2 top = __float2half2_rn(0.0f);
+                float more = 0.0f;
+                tm_request(x[0], s_at);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t see = MASKED ? visible(c) : 0u;
+                    tm_arrived(x[c & 1]);
+                    if (c < 3) tm_request(x[(c + 1) & 1], s_at + 32 * (c + 1));
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const float2 f = f2(row_factor * slot.k[2 * c + g]), add = f2(slot.v[2 * c + g] + (kTop - ref));
+                        float2 sum[2] = {f2(0.0f), f2(0.0f)};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int at = 16 * g + 2 * e;
+                            float2 u = __ffma2_rn(make_float2(__uint_as_float(x[c & 1][at]), __uint_as_float(x[c & 1][at + 1])), f, add);
+                            if (MASKED) {
+                                if (!((see >> at) & 1u)) u.x = kNone;
+                                if (!((see >> (at + 1)) & 1u)) u.y = kNone;
+                            }
+                            const float2 p = make_float2(ex2(u.x), ex2(u.y));
+                            sum[e & 1] = __fadd2_rn(sum[e & 1], p);
+                            const __half2 q = __floats2half2_rn(p.x, p.y);
+                            top = __hmax2(top, q);
+                            w[16 * c + 8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                        }
+                        const float2 both = __fadd2_rn(sum[0], sum[1]);
+                        more = fmaf(both.x + both.y, slot.l[2 * c + g], more);
+                    }
+                }
+                const float big = fmaxf(__low2float(top), __high2float(top));
+                const bool stays = big <= kBig && (big >= kSmall || big == 0.0f || ref <= top_all - kDepth);
+                if (!__all_sync(0xFFFFFFFFu, stays)) return false;
+                l += more;
+                tm_store32(s_at, *reinterpret_cast<uint32_t(*)[32]>(w));
+                tm_store32(s_at + 32, *reinterpret_cast<uint32_t(*)[32]>(w + 32));
+                return true;
+            };
+            bool done = false;
+            if (!wide && __all_sync(0xFFFFFFFFu, ref > kNone)) {
+                const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kTile <= min(see_hi, k1)) && readable == 0xFFu;
+                done = all ? one_pass(std::false_type{}) : one_pass(std::true_type{});
             }
+            if (!done) {
+                uint32_t x[32];
+                float utop = kNone;   // largest s + sv of the row
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t see = visible(c);
+                    tm_load(x, s_at + 32 * c);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tm_load(x, s_at + 32 * c);
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    float m = kNone;
-                    if (all) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) m = fmaxf(m, __uint_as_float(x[16 * g + e]));
-                    } else {
-                        const uint32_t see = visible(c);
+                    for (int g = 0; g < 2; ++g) {
+                        float m = kNone;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) m = fmaxf(m, (see >> (16 * g + e)) & 1u ? __uint_as_float(x[16 * g + e]) : kNone);
-                    }
-                    const float sv = slot.v[2 * c + g];
-                    far = fmaxf(far, fabsf(sv - c0));
-                    utop = fmaxf(utop, fmaf(m, row_factor * slot.k[2 * c + g], sv));
-                }
-            }
-            utop = ceilf(utop);
-            top_all = fmaxf(top_all, utop);
-            float next = ref;
-            if (utop > ref + 8.0f || (ref == kNone && utop > kNone)) next = utop;
-            else if (utop < ref - 12.0f && utop > kNone) next = fmaxf(utop, top_all - 40.0f);
-            if (__any_sync(0xFFFFFFFFu, next != ref)) {
-                const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
-                l *= alpha;
-                ref = next;
-                if (j > 0) {   // the products up to the last tile's are done: their end was signalled with these scores'
-#pragma unroll
-                    for (int c = 0; c < DIM / 32; ++c) {
-                        tm_load(x, o_at + 32 * c);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
-                        tm_store32(o_at + 32 * c, x);
+                        utop = fmaxf(utop, fmaf(m, row_factor * slot.k[2 * c + g], slot.v[2 * c + g]));
                     }
                 }
-            }
-            const float rs = ref == kNone ? 0.0f : ref;
-            const bool wide = far > 40.0f;   // the same for every row
-            // weights, over the scores already read
+                const float whole = ceilf(utop);
+                top_all = fmaxf(top_all, whole);
+                float next = ref;
+                if (utop > ref + kUp || (ref == kNone && utop > kNone)) next = whole;
+                else if (utop < ref - kDown && utop > kNone) next = fmaxf(whole, top_all - kDepth);
+                if (__any_sync(0xFFFFFFFFu, next != ref)) {
+                    const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
+                    l *= alpha;
+                    ref = next;
+                    if (j > 0) {   // the products up to the last tile's are done: their end was signalled with these scores'
+#pragma unroll 1
+                        for (int c = 0; c < DIM / 32; ++c) {
+                            tm_load(x, o_at + 32 * c);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tm_load(x, s_at + 32 * c);
-                uint32_t w[16];
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const float sv = slot.v[2 * c + g], f = row_factor * slot.k[2 * c + g], add = sv + kTop - rs;
-                    float2 sum = f2(0.0f);
-                    const uint32_t see = all ? 0xFFFFu : visible(c) >> (16 * g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 s = make_float2(__uint_as_float(x[16 * g + 2 * e]), __uint_as_float(x[16 * g + 2 * e + 1]));
-                        float2 u = __ffma2_rn(s, f2(f), f2(add));
-                        if (!all) {
-                            if (!((see >> (2 * e)) & 1u)) u.x = kNone;
-                            if (!((see >> (2 * e + 1)) & 1u)) u.y = kNone;
+                            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
+                            tm_store32(o_at + 32 * c, x);
                         }
-                        const float2 p = make_float2(ex2(u.x), ex2(u.y));
-                        if (!wide) {
-                            sum = __fadd2_rn(sum, p);
-                        } else {
-                            sum.x += ex2(u.x + (c0 - sv));
-                            sum.y += ex2(u.y + (c0 - sv));
-                        }
-                        const __half2 q = __floats2half2_rn(p.x, p.y);
-                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
                     }
-                    l = wide ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, ex2(c0 - sv), l);
                 }
-                tm_store16(s_at + 16 * c, w);
+                const float rs = ref == kNone ? 0.0f : ref;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {   // weights, over the scores already read
+                    const uint32_t see = visible(c);
+                    tm_load(x, s_at + 32 * c);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const float sv = slot.v[2 * c + g], f = row_factor * slot.k[2 * c + g], add = sv + kTop - rs;
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float u0 = fmaf(__uint_as_float(x[16 * g + 2 * e]), f, add), u1 = fmaf(__uint_as_float(x[16 * g + 2 * e + 1]), f, add);
+                            if (!((see >> (16 * g + 2 * e)) & 1u)) u0 = kNone;
+                            if (!((see >> (16 * g + 2 * e + 1)) & 1u)) u1 = kNone;
+                            const float p0 = ex2(u0), p1 = ex2(u1);
+                            sum += wide ? ex2(u0 + (c0 - sv)) + ex2(u1 + (c0 - sv)) : p0 + p1;
+                            const __half2 q = __floats2half2_rn(p0, p1);
+                            w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                        }
+                        l = wide ? l + sum : fmaf(sum, slot.l[2 * c + g], l);
+                    }
+                    tm_store16(s_at + 16 * c, w);
+                }
             }
             tm_store_wait();
             tc_before();
@@ -517,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         if (ok && tiles > 0) ok = wait(o_done, 0, dead);
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
-        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 4 - c0
+        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 5 - c0
         const bool some = l > 0.0f;
         const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
         const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
@@ -557,6 +621,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             else if (P.lse != nullptr) P.lse[out_row] = lse2 * kLn2;
         }
         tc_before();
+    } else {
+        MXN_FEW_REGISTERS();
     }
     __syncthreads();
     if (threadIdx.x == 0 && dead_flag) {
