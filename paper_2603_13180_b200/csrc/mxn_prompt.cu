@@ -14,10 +14,10 @@
 // Scores: E4M3 x E4M3 products on the key codes as they are; q is scaled by a power of two to [128, 256) at its row's largest
 //   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-10 of the row's largest (to 2^-18
 //   of it).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
-// Weights: w_t = 2^(s_t + sv_t - R + 5) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
+// Weights: w_t = 2^(s_t + sv_t - R + 7) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
-//   is moved only when a tile's largest is 10 above or 15 below it, so that the output in tensor memory rarely has to be corrected.
-//   f16 drops what is below 2^-25, i.e. 2^-30 of the weight at R and 2^-15 of the largest of a tile at the window's lower end.
+//   is moved only when a step's largest is 8 above or 20 below it, so that the output in tensor memory rarely has to be corrected.
+//   f16 drops what is below 2^-25, i.e. 2^-32 of the weight at R and 2^-12 of the largest of a step at the window's lower end.
 // The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA.
 // The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
@@ -39,14 +39,14 @@ namespace mxn {
 namespace {
 
 constexpr int kTile = 128;        // tokens of a key tile, rows of a row tile
+constexpr int kStep = 64;         // tokens of a step of the softmax: half a tile
 constexpr int kThreads = 512;
 constexpr int kKeyStages = 3, kValStages = 2, kHalfStages = 2, kScaleSlots = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRun = 16;          // tokens that share a scale at the finest
 // Weights: 2^kTop at the reference; the reference is moved when a tile's largest is more than kUp above or kDown below it, but to
 // no more than kDepth below the largest so far (the output's sums must not overflow)
-constexpr float kTop = 5.0f, kUp = 10.0f, kDown = 15.0f, kDepth = 40.0f;
-constexpr float kBig = 32768.0f, kSmall = 0.0009765625f;   // 2^(kTop + kUp), 2^(kTop - kDown)
+constexpr float kTop = 7.0f, kUp = 8.0f, kDown = 20.0f, kDepth = 40.0f;
 
 __device__ unsigned int g_prompt_timeouts = 0;
 __device__ unsigned int g_prompt_bad = 0;
@@ -149,6 +149,12 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     return false;
 }
 
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return d;
+}
 __device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
 
 template <int DIM>
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     constexpr uint32_t SW = DIM == 128 ? 2 : 4;         // swizzle of a tile of codes: its rows are DIM bytes
     constexpr uint32_t GROUP = 8 * DIM;                 // bytes of 8 rows of codes
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * kKeyStages + 2 * kValStages + 2 * kHalfStages + 5 + kScaleSlots];
+    __shared__ uint64_t bars[2 * kKeyStages + 2 * kValStages + 2 * kHalfStages + 8 + kScaleSlots];
     __shared__ TileScales scales[kScaleSlots];
     __shared__ uint32_t tmem_at;
     __shared__ int dead_flag;
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t k_full = bar0, k_empty = k_full + 8 * kKeyStages, v_full = k_empty + 8 * kKeyStages, v_empty = v_full + 8 * kValStages,
                    h_full = v_empty + 8 * kValStages, h_empty = h_full + 8 * kHalfStages, s_full = h_empty + 8 * kHalfStages,
-                   p_full = s_full + 16, o_done = p_full + 16, sc_full = o_done + 8;
+                   p_full = s_full + 32, sc_full = p_full + 32;   // [row tile][buffer]
     volatile int* const dead = &dead_flag;
     if (threadIdx.x == 0) {
         dead_flag = 0;
@@ -205,11 +211,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             mbar_init(h_full + 8 * i, 4);
             mbar_init(h_empty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 4);
         }
-        mbar_init(o_done, 1);
         for (int i = 0; i < kScaleSlots; ++i) mbar_init(sc_full + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -358,43 +363,52 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         // ---- products ----
         MXN_FEW_REGISTERS();
         if (lane == 0 && tiles > 0) {
+            // Step i is half a key tile.  Scores are two steps ahead of the weights: while the softmax works on one buffer, the
+            // other's scores are made.  The weights of step i lie in their scores' columns, so the scores of step i + 2 are
+            // issued behind the product that reads those weights; products run in the order of issue.
             bool ok = true;
-            auto scores = [&](int r, int j) {   // S_r = (hi + lo) K^T
-                const uint32_t q = base + Sh::kQ + r * 2 * Sh::kCodes, k = base + Sh::kK + (j % kKeyStages) * Sh::kCodes;
+            const int steps = 2 * tiles;
+            auto scores = [&](int r, int i) {   // S = (hi + lo) K^T
+                const uint32_t q = base + Sh::kQ + r * 2 * Sh::kCodes, k = base + Sh::kK + ((i >> 1) % kKeyStages) * Sh::kCodes + (i & 1) * kStep * DIM;
 #pragma unroll
                 for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int s = 0; s < DIM / 32; ++s)
-                        mma_scores(s_col[r], operand(q + part * Sh::kCodes + 32 * s, GROUP, 16, SW), operand(k + 32 * s, GROUP, 16, SW),
-                                   idesc_e4m3(kTile), (part | s) != 0);
-                mma_commit(s_full + 8 * r);
+                        mma_scores(s_col[r] + (i & 1) * kStep, operand(q + part * Sh::kCodes + 32 * s, GROUP, 16, SW), operand(k + 32 * s, GROUP, 16, SW),
+                                   idesc_e4m3(kStep), (part | s) != 0);
+                if (r == 1 && (i & 1)) mma_commit(k_empty + 8 * ((i >> 1) % kKeyStages));
             };
             ok = wait(k_full, 0, dead);
             if (ok) {
                 tc_after();
-                scores(0, 0);
-                scores(1, 0);
-                mma_commit(k_empty);
+                for (int i = 0; i < 2; ++i)
+                    for (int r = 0; r < 2; ++r) {
+                        scores(r, i);
+                        mma_commit(s_full + 16 * r + 8 * i);
+                    }
             }
-            for (int j = 0; ok && j < tiles; ++j) {
-                const int hs = j % kHalfStages, ks = (j + 1) % kKeyStages;
-                ok = wait(h_full + 8 * hs, (uint32_t)(j / kHalfStages) & 1u, dead);
-                if (ok && j + 1 < tiles) ok = wait(k_full + 8 * ks, (uint32_t)((j + 1) / kKeyStages) & 1u, dead);
+            for (int i = 0; ok && i < steps; ++i) {
+                const int j = i >> 1, hs = j % kHalfStages;
+                if (!(i & 1)) ok = wait(h_full + 8 * hs, (uint32_t)(j / kHalfStages) & 1u, dead);
+                if (ok && !(i & 1) && j + 1 < tiles) ok = wait(k_full + 8 * ((j + 1) % kKeyStages), (uint32_t)((j + 1) / kKeyStages) & 1u, dead);
                 for (int r = 0; ok && r < 2; ++r) {
-                    ok = wait(p_full + 8 * r, (uint32_t)j & 1u, dead);
+                    ok = wait(p_full + 16 * r + 8 * (i & 1), (uint32_t)j & 1u, dead);
                     if (!ok) break;
                     tc_after();
-                    const uint32_t v = base + Sh::kH + hs * Sh::kHalf;
+                    const uint32_t v = base + Sh::kH + hs * Sh::kHalf + (i & 1) * kStep * 128;
 #pragma unroll
-                    for (int s = 0; s < kTile / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
-                        mma_values(o_col[r], s_col[r] + 8 * s, operand(v + s * 2048, 1024, kTile * 128, 2), idesc_f16_bt(DIM), j > 0 || s > 0);
-                    if (r == 1) mma_commit(h_empty + 8 * hs);
-                    if (j + 1 < tiles) scores(r, j + 1);
+                    for (int s = 0; s < kStep / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
+                        mma_values(o_col[r], s_col[r] + (i & 1) * kStep + 8 * s, operand(v + s * 2048, 1024, kTile * 128, 2), idesc_f16_bt(DIM), i > 0 || s > 0);
+                    if (r == 1 && (i & 1)) mma_commit(h_empty + 8 * hs);
+                    if (i + 2 < steps) scores(r, i + 2);
+                    mma_commit(s_full + 16 * r + 8 * (i & 1));   // step i + 2's scores, and the output up to step i
                 }
-                if (ok && j + 1 < tiles) mma_commit(k_empty + 8 * ks);
             }
-            mma_commit(o_done);
-            if (!ok) (void)mbar_wait_bounded(o_done, 0, 1u << 16);
+            if (!ok) {   // what has been issued ends before the tensor memory is given up
+                mma_commit(k_empty);
+                (void)mbar_wait_bounded(k_empty, 0, 1u << 14);
+                (void)mbar_wait_bounded(k_empty, 1, 1u << 14);
+            }
         }
     } else if (warp >= 4 && warp < 8) {
         // ---- values to f16 ----
@@ -443,145 +457,129 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         // ---- softmax ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = s_col[rt] + lanes, o_at = o_col[rt] + lanes;
+        const uint32_t o_at = o_col[rt] + lanes;
         const int pos = shift + (row_live ? row / G : nq - 1);
         const int see_hi = P.causal ? min(pos + 1, len) : len;
         const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
         const float kNone = -INFINITY;
         float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
         bool ok = true;
-        for (int j = 0; j < tiles; ++j) {
+        const int steps = 2 * tiles;
+        for (int i = 0; i < steps; ++i) {
+            const int j = i >> 1, buf = i & 1;
             const TileScales& slot = scales[j % kScaleSlots];
-            ok = wait(s_full + 8 * rt, (uint32_t)j & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
+            const float* const slot_k = slot.k + 4 * buf;
+            const float* const slot_v = slot.v + 4 * buf;
+            const float* const slot_l = slot.l + 4 * buf;
+            ok = wait(s_full + 16 * rt + 8 * buf, (uint32_t)j & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_after();
-            const int t0 = k0 + j * kTile;
-            const uint32_t readable = slot.readable;
+            const uint32_t s_at = s_col[rt] + lanes + buf * kStep;
+            const int t0 = k0 + i * kStep;
+            const uint32_t readable = (slot.readable >> (4 * buf)) & 0xFu;
             const bool wide = slot.wide != 0;
             c0 = slot.c0;
-            // bit e: the row sees token 32 c + e of the tile
+            // bit e: the row sees token 32 c + e of the step
             auto visible = [&](int c) -> uint32_t {
                 const int tc = t0 + 32 * c, up = min(max(min(see_hi, k1) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
                 const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u, above = down == 32 ? 0u : 0xFFFFFFFFu << down;
                 return below & above & (((readable >> (2 * c)) & 1u ? 0xFFFFu : 0u) | ((readable >> (2 * c + 1)) & 1u ? 0xFFFF0000u : 0u));
             };
-            // One pass over the scores with the reference as it stands.  False, with nothing written, where a row's weights leave
-            // the window that f16 holds well.
-            auto one_pass = [&](auto masked) -> bool {
-                constexpr bool MASKED = decltype(masked)::value;
-                uint32_t x[2][32], w[64];
-                __half2 top = __float2half2_rn(0.0f);
-                float more = 0.0f;
-                tm_request(x[0], s_at);
+            const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kStep <= min(see_hi, k1)) && readable == 0xFu;
+            uint32_t x[2][32];
+            tm_request(x[0], s_at);
+            tm_arrived(x[0]);
+            tm_request(x[1], s_at + 32);
+            tm_arrived(x[1]);
+            if (!all) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t see = MASKED ? visible(c) : 0u;
-                    tm_arrived(x[c & 1]);
-                    if (c < 3) tm_request(x[(c + 1) & 1], s_at + 32 * (c + 1));
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        const float2 f = f2(row_factor * slot.k[2 * c + g]), add = f2(slot.v[2 * c + g] + (kTop - ref));
-                        float2 sum[2] = {f2(0.0f), f2(0.0f)};
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int at = 16 * g + 2 * e;
-                            float2 u = __ffma2_rn(make_float2(__uint_as_float(x[c & 1][at]), __uint_as_float(x[c & 1][at + 1])), f, add);
-                            if (MASKED) {
-                                if (!((see >> at) & 1u)) u.x = kNone;
-                                if (!((see >> (at + 1)) & 1u)) u.y = kNone;
-                            }
-                            const float2 p = make_float2(ex2(u.x), ex2(u.y));
-                            sum[e & 1] = __fadd2_rn(sum[e & 1], p);
-                            const __half2 q = __floats2half2_rn(p.x, p.y);
-                            top = __hmax2(top, q);
-                            w[16 * c + 8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
-                        }
-                        const float2 both = __fadd2_rn(sum[0], sum[1]);
-                        more = fmaf(both.x + both.y, slot.l[2 * c + g], more);
-                    }
-                }
-                const float big = fmaxf(__low2float(top), __high2float(top));
-                const bool stays = big <= kBig && (big >= kSmall || big == 0.0f || ref <= top_all - kDepth);
-                if (!__all_sync(0xFFFFFFFFu, stays)) return false;
-                l += more;
-                tm_store32(s_at, *reinterpret_cast<uint32_t(*)[32]>(w));
-                tm_store32(s_at + 32, *reinterpret_cast<uint32_t(*)[32]>(w + 32));
-                return true;
-            };
-            bool done = false;
-            if (!wide && __all_sync(0xFFFFFFFFu, ref > kNone)) {
-                const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kTile <= min(see_hi, k1)) && readable == 0xFFu;
-                done = all ? one_pass(std::false_type{}) : one_pass(std::true_type{});
-            }
-            if (!done) {
-                uint32_t x[32];
-                float utop = kNone;   // largest s + sv of the row
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     const uint32_t see = visible(c);
-                    tm_load(x, s_at + 32 * c);
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        float m = kNone;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) m = fmaxf(m, (see >> (16 * g + e)) & 1u ? __uint_as_float(x[16 * g + e]) : kNone);
-                        utop = fmaxf(utop, fmaf(m, row_factor * slot.k[2 * c + g], slot.v[2 * c + g]));
-                    }
-                }
-                const float whole = ceilf(utop);
-                top_all = fmaxf(top_all, whole);
-                float next = ref;
-                if (utop > ref + kUp || (ref == kNone && utop > kNone)) next = whole;
-                else if (utop < ref - kDown && utop > kNone) next = fmaxf(whole, top_all - kDepth);
-                if (__any_sync(0xFFFFFFFFu, next != ref)) {
-                    const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
-                    l *= alpha;
-                    ref = next;
-                    if (j > 0) {   // the products up to the last tile's are done: their end was signalled with these scores'
-#pragma unroll 1
-                        for (int c = 0; c < DIM / 32; ++c) {
-                            tm_load(x, o_at + 32 * c);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
-                            tm_store32(o_at + 32 * c, x);
-                        }
-                    }
-                }
-                const float rs = ref == kNone ? 0.0f : ref;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {   // weights, over the scores already read
-                    const uint32_t see = visible(c);
-                    tm_load(x, s_at + 32 * c);
-                    uint32_t w[16];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        const float sv = slot.v[2 * c + g], f = row_factor * slot.k[2 * c + g], add = sv + kTop - rs;
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float u0 = fmaf(__uint_as_float(x[16 * g + 2 * e]), f, add), u1 = fmaf(__uint_as_float(x[16 * g + 2 * e + 1]), f, add);
-                            if (!((see >> (16 * g + 2 * e)) & 1u)) u0 = kNone;
-                            if (!((see >> (16 * g + 2 * e + 1)) & 1u)) u1 = kNone;
-                            const float p0 = ex2(u0), p1 = ex2(u1);
-                            sum += wide ? ex2(u0 + (c0 - sv)) + ex2(u1 + (c0 - sv)) : p0 + p1;
-                            const __half2 q = __floats2half2_rn(p0, p1);
-                            w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
-                        }
-                        l = wide ? l + sum : fmaf(sum, slot.l[2 * c + g], l);
-                    }
-                    tm_store16(s_at + 16 * c, w);
+                    for (int e = 0; e < 32; ++e)
+                        if (!((see >> e) & 1u)) x[c][e] = 0xFF800000u;   // -infinity; a factor is never 0, so it stays that
                 }
             }
+            // the step's largest s + sv, and the reference
+            float fac[4], utop = kNone;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
+                float m = max3(y[0], y[1], y[2]);
+#pragma unroll
+                for (int e = 3; e < 15; e += 2) m = max3(__float_as_uint(m), y[e], y[e + 1]);
+                m = fmaxf(m, __uint_as_float(y[15]));
+                fac[g] = fmaxf(row_factor * slot_k[g], 1.17549435e-38f);
+                utop = fmaxf(utop, fmaf(m, fac[g], slot_v[g]));
+            }
+            const float whole = ceilf(utop);
+            top_all = fmaxf(top_all, whole);
+            float next = ref;
+            if (utop > ref + kUp || (ref == kNone && utop > kNone)) next = whole;
+            else if (utop < ref - kDown && utop > kNone) next = fmaxf(whole, top_all - kDepth);
+            if (__any_sync(0xFFFFFFFFu, next != ref)) {
+                const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
+                l *= alpha;
+                ref = next;
+                if (i > 0) {   // the output up to the last step: its end is signalled with the next step's scores
+                    ok = wait(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u, dead);
+                    if (!__all_sync(0xFFFFFFFFu, ok)) break;
+                    tc_after();
+#pragma unroll 1
+                    for (int c = 0; c < DIM / 32; ++c) {
+                        uint32_t y[32];
+                        tm_load(y, o_at + 32 * c);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+                        tm_store32(o_at + 32 * c, y);
+                    }
+                }
+            }
+            // weights, over their scores
+            const float shift_by = ref == kNone ? 0.0f : kTop - ref;
+            uint32_t w[32];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
+                const float2 f = f2(fac[g]), add = f2(slot_v[g] + shift_by);
+                float2 sum[2] = {f2(0.0f), f2(0.0f)};
+                auto pair = [&](int e) {
+                    const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, add);
+                    return u;
+                };
+                if (!wide) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 u = pair(e);
+                        const float2 p = make_float2(ex2(u.x), ex2(u.y));
+                        sum[e & 1] = __fadd2_rn(sum[e & 1], p);
+                        const __half2 q = __floats2half2_rn(p.x, p.y);
+                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                    }
+                    const float2 both = __fadd2_rn(sum[0], sum[1]);
+                    l = fmaf(both.x + both.y, slot_l[g], l);
+                } else {
+                    const float apart = c0 - slot_v[g];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 u = pair(e);
+                        l += ex2(u.x + apart) + ex2(u.y + apart);
+                        const __half2 q = __floats2half2_rn(ex2(u.x), ex2(u.y));
+                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                    }
+                }
+            }
+            tm_store32(s_at, w);
             tm_store_wait();
             tc_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * rt);
+            if (lane == 0) mbar_arrive(p_full + 16 * rt + 8 * buf);
         }
         // ---- output ----
-        if (ok && tiles > 0) ok = wait(o_done, 0, dead);
+        if (ok && tiles > 0) ok = wait(s_full + 16 * rt + 8, (uint32_t)tiles & 1u, dead);   // behind the last step's product
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
-        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 5 - c0
+        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 7 - c0
         const bool some = l > 0.0f;
         const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
         const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
