@@ -14,10 +14,10 @@
 // Scores: E4M3 x E4M3 products on the key codes as they are; q is scaled by a power of two to [128, 256) at its row's largest
 //   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-10 of the row's largest (to 2^-18
 //   of it).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
-// Weights: w_t = 2^(s_t + sv_t - R + 7) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
+// Weights: w_t = 2^(s_t + sv_t - R + 1) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
-//   is moved only when a step's largest is 8 above or 20 below it, so that the output in tensor memory rarely has to be corrected.
-//   f16 drops what is below 2^-25, i.e. 2^-32 of the weight at R and 2^-12 of the largest of a step at the window's lower end.
+//   is moved only when a step's largest is 14 above or 16 below it, so that the output in tensor memory rarely has to be corrected.
+//   f16 drops what is below 2^-25, i.e. 2^-26 of the weight at R and 2^-10 of the largest of a step at the window's lower end.
 // The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA.
 // The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
@@ -46,7 +46,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRun = 16;          // tokens that share a scale at the finest
 // Weights: 2^kTop at the reference; the reference is moved when a tile's largest is more than kUp above or kDown below it, but to
 // no more than kDepth below the largest so far (the output's sums must not overflow)
-constexpr float kTop = 7.0f, kUp = 8.0f, kDown = 20.0f, kDepth = 40.0f;
+constexpr float kTop = 1.0f, kUp = 14.0f, kDown = 16.0f, kDepth = 40.0f;
 
 __device__ unsigned int g_prompt_timeouts = 0;
 __device__ unsigned int g_prompt_bad = 0;
@@ -138,6 +138,12 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(is));
+    return is != 0;
+}
 // waits with a limit; a wait that runs out, or one that sees another's, ends the CTA's work
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* dead)
 {
@@ -362,50 +368,83 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     } else if (warp == 1) {
         // ---- products ----
         MXN_FEW_REGISTERS();
-        if (lane == 0 && tiles > 0) {
+        if (tiles > 0) {
             // Step i is half a key tile.  Scores are two steps ahead of the weights: while the softmax works on one buffer, the
             // other's scores are made.  The weights of step i lie in their scores' columns, so the scores of step i + 2 are
             // issued behind the product that reads those weights; products run in the order of issue.
+            // One thread issues it all, a product every 50 cycles: the whole warp goes through the loop, so that descriptors (bases
+            // plus constants) are uniform values.
+            const bool one = elect_one();
             bool ok = true;
-            const int steps = 2 * tiles;
-            auto scores = [&](int r, int i) {   // S = (hi + lo) K^T
-                const uint32_t q = base + Sh::kQ + r * 2 * Sh::kCodes, k = base + Sh::kK + ((i >> 1) % kKeyStages) * Sh::kCodes + (i & 1) * kStep * DIM;
+            const uint64_t q_desc = operand(base + Sh::kQ, GROUP, 16, SW), k_base = operand(base + Sh::kK, GROUP, 16, SW),
+                           h_base = operand(base + Sh::kH, 1024, kTile * 128, 2);
+            auto scores = [&](int r, int half, uint64_t k_desc) {   // S = (hi + lo) K^T
 #pragma unroll
                 for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int s = 0; s < DIM / 32; ++s)
-                        mma_scores(s_col[r] + (i & 1) * kStep, operand(q + part * Sh::kCodes + 32 * s, GROUP, 16, SW), operand(k + 32 * s, GROUP, 16, SW),
-                                   idesc_e4m3(kStep), (part | s) != 0);
-                if (r == 1 && (i & 1)) mma_commit(k_empty + 8 * ((i >> 1) % kKeyStages));
+                        mma_scores(s_col[r] + half * kStep, q_desc + (uint64_t)(((2 * r + part) * Sh::kCodes + 32 * s) >> 4),
+                                   k_desc + (uint64_t)((half * kStep * DIM + 32 * s) >> 4), idesc_e4m3(kStep), (part | s) != 0);
+            };
+            uint32_t ks = 0, k_par = 0, hs = 0, h_par = 0, p_par = 0;
+            uint64_t k_desc = k_base;
+            auto next_keys = [&]() {   // the next key tile
+                if (++ks == kKeyStages) {
+                    ks = 0;
+                    k_par ^= 1u;
+                }
+                k_desc = k_base + (uint64_t)((ks * Sh::kCodes) >> 4);
             };
             ok = wait(k_full, 0, dead);
             if (ok) {
                 tc_after();
-                for (int i = 0; i < 2; ++i)
-                    for (int r = 0; r < 2; ++r) {
-                        scores(r, i);
-                        mma_commit(s_full + 16 * r + 8 * i);
-                    }
-            }
-            for (int i = 0; ok && i < steps; ++i) {
-                const int j = i >> 1, hs = j % kHalfStages;
-                if (!(i & 1)) ok = wait(h_full + 8 * hs, (uint32_t)(j / kHalfStages) & 1u, dead);
-                if (ok && !(i & 1) && j + 1 < tiles) ok = wait(k_full + 8 * ((j + 1) % kKeyStages), (uint32_t)((j + 1) / kKeyStages) & 1u, dead);
-                for (int r = 0; ok && r < 2; ++r) {
-                    ok = wait(p_full + 16 * r + 8 * (i & 1), (uint32_t)j & 1u, dead);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t v = base + Sh::kH + hs * Sh::kHalf + (i & 1) * kStep * 128;
 #pragma unroll
-                    for (int s = 0; s < kStep / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
-                        mma_values(o_col[r], s_col[r] + (i & 1) * kStep + 8 * s, operand(v + s * 2048, 1024, kTile * 128, 2), idesc_f16_bt(DIM), i > 0 || s > 0);
-                    if (r == 1 && (i & 1)) mma_commit(h_empty + 8 * hs);
-                    if (i + 2 < steps) scores(r, i + 2);
-                    mma_commit(s_full + 16 * r + 8 * (i & 1));   // step i + 2's scores, and the output up to step i
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if (one) {
+                            scores(r, half, k_desc);
+                            mma_commit(s_full + 16 * r + 8 * half);
+                        }
+                    }
+                if (one) mma_commit(k_empty);
+                next_keys();
+            }
+            for (int j = 0; ok && j < tiles; ++j) {
+                const bool more = j + 1 < tiles;
+                ok = wait(h_full + 8 * hs, h_par, dead) && (!more || wait(k_full + 8 * ks, k_par, dead));
+                if (!ok) break;
+                const uint64_t h_desc = h_base + (uint64_t)((hs * Sh::kHalf) >> 4);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        ok = ok && wait(p_full + 16 * r + 8 * half, p_par, dead);
+                        if (!ok) continue;
+                        tc_after();
+                        if (one) {
+#pragma unroll
+                            for (int s = 0; s < kStep / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
+                                mma_values(o_col[r], s_col[r] + half * kStep + 8 * s, h_desc + (uint64_t)((half * kStep * 128 + s * 2048) >> 4),
+                                           idesc_f16_bt(DIM), (half | s) != 0 || j > 0);
+                            if (more) scores(r, half, k_desc);
+                            mma_commit(s_full + 16 * r + 8 * half);   // the scores two steps on, and the output up to this step
+                        }
+                    }
                 }
+                if (one) {
+                    mma_commit(h_empty + 8 * hs);
+                    if (more) mma_commit(k_empty + 8 * ks);
+                }
+                if (more) next_keys();
+                if (++hs == kHalfStages) {
+                    hs = 0;
+                    h_par ^= 1u;
+                }
+                p_par ^= 1u;
             }
             if (!ok) {   // what has been issued ends before the tensor memory is given up
-                mma_commit(k_empty);
+                if (one) mma_commit(k_empty);
                 (void)mbar_wait_bounded(k_empty, 0, 1u << 14);
                 (void)mbar_wait_bounded(k_empty, 1, 1u << 14);
             }
@@ -579,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         if (ok && tiles > 0) ok = wait(s_full + 16 * rt + 8, (uint32_t)tiles & 1u, dead);   // behind the last step's product
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
-        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 7 - c0
+        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 1 - c0
         const bool some = l > 0.0f;
         const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
         const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
