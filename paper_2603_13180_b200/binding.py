@@ -342,29 +342,32 @@ def device_bad_indices_reset() -> None:
     _check(lib.mxn_device_bad_indices_reset(), "mxn_device_bad_indices_reset")
 
 
-def _on(device, **tensors):
-    """Every tensor lies on `device`, and that is the current one (calls enqueue on the current device)."""
-    if device.type != "cuda":
-        raise ValueError(f"expected CUDA tensors, not tensors on {device}")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name}: on {t.device}, expected {device}")
+def _on_current_device(stream, first, *tensors):
+    """Every tensor lies on the current device (calls enqueue there); returns the raw stream to enqueue on."""
+    if not first.is_cuda:
+        raise ValueError(f"expected CUDA tensors, not tensors on {first.device}")
+    device = torch._C._cuda_getDevice()
+    if first.get_device() != device:
+        raise ValueError(f"tensors are on {first.device}, the current device is cuda:{device}")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor is on {t.device}, expected cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _heads(t, name, like=None):
     """(pointer, token stride, heads) of a bf16 [T, heads, dim] tensor whose heads are contiguous; (None, 0, 0) for None."""
     if t is None:
         return None, 0, 0
-    if t.dtype is not torch.bfloat16 or t.dim() != 3:
+    shape = t.shape
+    if t.dtype is not torch.bfloat16 or len(shape) != 3:
         raise ValueError(f"{name}: expected a bf16 tensor [tokens, heads, dim]")
-    n, h, d = t.shape
+    if like is not None and shape != like:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected {tuple(like)}")
+    n, h, d = shape
     st, sh, sd = t.stride()
     if (sd != 1 and d > 1) or (sh != d and h > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    if like is not None and t.shape != like.shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(like.shape)}")
     return t.data_ptr(), (st if n > 1 else h * d), h
 
 
@@ -374,7 +377,7 @@ def _vec(t, dtype, name, shape=None):
         return None
     if t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous tensor of {dtype}")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
     return t.data_ptr()
 
@@ -392,19 +395,22 @@ def rmsnorm_rope_fwd(q, k, q_gain, k_gain, cos_sin, positions, q_out, k_out, eps
                      stream=None):
     """RMS norm of every head of q [T, Hq, D] and k [T, Hk, D] (k may be None) and rotation by cos_sin [P, rot] (may be None)
     at int32 positions [T] (None: row index).  q_out / k_out may be q / k themselves."""
-    _on(q.device, k=k, q_gain=q_gain, k_gain=k_gain, cos_sin=cos_sin, positions=positions, q_out=q_out, k_out=k_out)
-    T, _, D = q.shape
-    if k is not None and (k.shape[0] != T or k.shape[2] != D or k_out is None):
-        raise ValueError("k: expected [tokens, heads, dim] with q's tokens and dim, and a k_out")
+    raw = _on_current_device(stream, q, k, q_gain, k_gain, cos_sin, positions, q_out, k_out)
     qp, qs, qh = _heads(q, "q")
-    kp, ks, kh = _heads(k, "k")
-    qop, qos, _ = _heads(q_out, "q_out", q)
-    kop, kos, _ = _heads(k_out if k is not None else None, "k_out", k)
+    T, _, D = shape = q.shape
+    qop, qos, _ = _heads(q_out, "q_out", shape)
+    if k is None:
+        kp = kop = None
+        ks = kos = kh = 0
+    else:
+        kp, ks, kh = _heads(k, "k")
+        if k_out is None or k.shape != (T, kh, D):
+            raise ValueError("k: expected [tokens, heads, dim] with q's tokens and dim, and a k_out")
+        kop, kos, _ = _heads(k_out, "k_out", (T, kh, D))
     tp, rows, rot = _table(cos_sin)
     _check(lib.rmsnorm_rope_fwd(qp, qs, qh, kp, ks, kh, T, D, 1 if normalise else 0, _vec(q_gain, torch.bfloat16, "q_gain", (D,)),
                                 _vec(k_gain, torch.bfloat16, "k_gain", (D,)), eps, tp, rows, rot, 1 if interleaved else 0,
-                                _vec(positions, torch.int32, "positions", (T,)), qop, qos, kop, kos, _stream(stream)),
-           "rmsnorm_rope_fwd")
+                                _vec(positions, torch.int32, "positions", (T,)), qop, qos, kop, kos, raw), "rmsnorm_rope_fwd")
 
 
 def rmsnorm_rope_bwd_workspace_bytes(T: int, q_heads: int, k_heads: int, dim: int) -> int:
@@ -415,26 +421,26 @@ def rmsnorm_rope_bwd(q, k, grad_q, grad_k, q_gain, k_gain, cos_sin, positions, d
                      eps=1e-6, interleaved=False, normalise=True, stream=None):
     """Gradient of rmsnorm_rope_fwd: grad_q / grad_k -> dq / dk (and fp32 q_dgain / k_dgain [D]); q and k are the forward's inputs
     (None with normalise=False, which does not read them)."""
-    _on(grad_q.device, q=q, k=k, grad_k=grad_k, q_gain=q_gain, k_gain=k_gain, cos_sin=cos_sin, positions=positions, dq=dq, dk=dk,
-        q_dgain=q_dgain, k_dgain=k_dgain, workspace=workspace)
-    T, _, D = grad_q.shape
+    raw = _on_current_device(stream, grad_q, q, k, grad_k, q_gain, k_gain, cos_sin, positions, dq, dk, q_dgain, k_dgain, workspace)
+    gqp, gqs, qh = _heads(grad_q, "grad_q")
+    T, _, D = shape = grad_q.shape
     if grad_k is not None and (grad_k.shape[0] != T or grad_k.shape[2] != D or dk is None):
         raise ValueError("grad_k: expected [tokens, heads, dim] with grad_q's tokens and dim, and a dk")
     if normalise and (q is None or (k is None) != (grad_k is None)):
         raise ValueError("q / k: the forward's inputs are needed")
-    gqp, gqs, qh = _heads(grad_q, "grad_q")
     gkp, gks, kh = _heads(grad_k, "grad_k")
-    qp, qs, _ = _heads(q, "q", grad_q)
-    kp, ks, _ = _heads(k if grad_k is not None else None, "k", grad_k)
-    dqp, dqs, _ = _heads(dq, "dq", grad_q)
-    dkp, dks, _ = _heads(dk if grad_k is not None else None, "dk", grad_k)
+    k_shape = (T, kh, D)
+    qp, qs, _ = _heads(q, "q", shape)
+    kp, ks, _ = _heads(k if kh else None, "k", k_shape)
+    dqp, dqs, _ = _heads(dq, "dq", shape)
+    dkp, dks, _ = _heads(dk if kh else None, "dk", k_shape)
     tp, rows, rot = _table(cos_sin)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.rmsnorm_rope_bwd(qp, qs, qh, kp, ks, kh, gqp, gqs, gkp, gks, T, D, 1 if normalise else 0,
                                 _vec(q_gain, torch.bfloat16, "q_gain", (D,)), _vec(k_gain, torch.bfloat16, "k_gain", (D,)), eps, tp,
                                 rows, rot, 1 if interleaved else 0, _vec(positions, torch.int32, "positions", (T,)), dqp, dqs, dkp, dks,
                                 _vec(q_dgain, torch.float32, "q_dgain", (D,)), _vec(k_dgain, torch.float32, "k_dgain", (D,)),
-                                _ptr(workspace), ws_bytes, _stream(stream)), "rmsnorm_rope_bwd")
+                                _ptr(workspace), ws_bytes, raw), "rmsnorm_rope_bwd")
 
 
 def alloc_kv_cache(num_pages: int, kv_heads: int, page_size: int, dim: int, block: int = 16, device="cuda"):
@@ -448,20 +454,20 @@ def alloc_kv_cache(num_pages: int, kv_heads: int, page_size: int, dim: int, bloc
 
 def _cache(k_codes, k_scales, v_codes, v_scales):
     """(pages, heads, page size, dim, block) of a cache's four tensors and their pointers."""
-    if k_codes.dim() != 4 or k_scales.dim() != 3 or k_scales.shape[2] < 1:
+    cs, ss = k_codes.shape, k_scales.shape
+    if len(cs) != 4 or len(ss) != 3 or ss[2] < 1 or ss[:2] != cs[:2]:
         raise ValueError("cache: expected codes [pages, heads, page, dim] and scales [pages, heads, page / block]")
-    pages, heads, page, dim = k_codes.shape
-    cs, ss = (pages, heads, page, dim), (pages, heads, k_scales.shape[2])
-    return (pages, heads, page, dim, page // k_scales.shape[2] if page % k_scales.shape[2] == 0 else 0,
-            _vec(k_codes, torch.uint8, "k_codes"), _vec(k_scales, torch.uint8, "k_scales", ss),
-            _vec(v_codes, torch.uint8, "v_codes", cs), _vec(v_scales, torch.uint8, "v_scales", ss))
+    pages, heads, page, dim = cs
+    return (pages, heads, page, dim, page // ss[2] if page % ss[2] == 0 else 0, _vec(k_codes, torch.uint8, "k_codes"),
+            _vec(k_scales, torch.uint8, "k_scales"), _vec(v_codes, torch.uint8, "v_codes", cs), _vec(v_scales, torch.uint8, "v_scales", ss))
 
 
 def _sequences(cu, lens, page_table):
     """(sequences, pages a sequence) and the pointers of the three lists."""
-    if page_table.dim() != 2:
+    shape = page_table.shape
+    if len(shape) != 2:
         raise ValueError("page_table: expected int32 [sequences, pages]")
-    s, width = page_table.shape
+    s, width = shape
     return (s, width, _vec(cu, torch.int32, "cu", (s + 1,)), _vec(lens, torch.int32, "kv_lens", (s,)),
             _vec(page_table, torch.int32, "page_table"))
 
@@ -469,17 +475,18 @@ def _sequences(cu, lens, page_table):
 def mxkv_append(k, v, cu_tokens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, cos_sin=None, interleaved=False, stream=None):
     """Writes new tokens' keys (rotated by their place when cos_sin is given) and values [n, H, D] into the paged cache.
     kv_lens counts the new tokens; rows cu_tokens[s] .. cu_tokens[s+1]-1 are the last ones of sequence s."""
-    _on(k.device, v=v, cu_tokens=cu_tokens, kv_lens=kv_lens, page_table=page_table, k_codes=k_codes, k_scales=k_scales,
-        v_codes=v_codes, v_scales=v_scales, cos_sin=cos_sin)
+    raw = _on_current_device(stream, k, v, cu_tokens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, cos_sin)
     pages, heads, page, dim, block, kc, ks, vc, vs = _cache(k_codes, k_scales, v_codes, v_scales)
     s, width, cup, lp, pt = _sequences(cu_tokens, kv_lens, page_table)
     kp, kst, kh = _heads(k, "k")
-    vp, vst, _ = _heads(v, "v", k)
-    if kh != heads or k.shape[2] != dim:
+    shape = k.shape
+    vp, vst, _ = _heads(v, "v", shape)
+    n = shape[0]
+    if kh != heads or shape[2] != dim:
         raise ValueError("k, v: heads and dim differ from the cache's")
     tp, rows, rot = _table(cos_sin)
-    _check(lib.mxkv_append(kp, kst, vp, vst, k.shape[0], heads, dim, cup, s, lp, pt, width, pages, page, block, tp, rows, rot,
-                           1 if interleaved else 0, kc, ks, vc, vs, _stream(stream)), "mxkv_append")
+    _check(lib.mxkv_append(kp, kst, vp, vst, n, heads, dim, cup, s, lp, pt, width, pages, page, block, tp, rows, rot,
+                           1 if interleaved else 0, kc, ks, vc, vs, raw), "mxkv_append")
 
 
 def mxkv_attention_workspace_bytes(n_tokens: int, n_seqs: int, max_q_len: int, max_kv_len: int, q_heads: int, kv_heads: int, dim: int) -> int:
@@ -489,16 +496,15 @@ def mxkv_attention_workspace_bytes(n_tokens: int, n_seqs: int, max_q_len: int, m
 def mxkv_attention(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, causal=True,
                    window=0, lse=None, workspace=None, stream=None):
     """Attention of the queries [n, Hq, D] over the paged cache; see mxkv_attention in include/mxnorm.h."""
-    _on(q.device, cu_q=cu_q, kv_lens=kv_lens, page_table=page_table, k_codes=k_codes, k_scales=k_scales, v_codes=v_codes,
-        v_scales=v_scales, out=out, lse=lse, workspace=workspace)
+    raw = _on_current_device(stream, q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, lse, workspace)
     pages, heads, page, dim, block, kc, ks, vc, vs = _cache(k_codes, k_scales, v_codes, v_scales)
     s, width, cup, lp, pt = _sequences(cu_q, kv_lens, page_table)
     qp, qst, qh = _heads(q, "q")
-    op, ost, _ = _heads(out, "out", q)
-    if q.shape[2] != dim:
+    n, _, d = shape = q.shape
+    op, ost, _ = _heads(out, "out", shape)
+    if d != dim:
         raise ValueError("q: dim differs from the cache's")
-    n = q.shape[0]
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.mxkv_attention(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
                               scale, 1 if causal else 0, window, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), _ptr(workspace),
-                              ws_bytes, _stream(stream)), "mxkv_attention")
+                              ws_bytes, raw), "mxkv_attention")

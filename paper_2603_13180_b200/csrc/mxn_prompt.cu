@@ -136,6 +136,12 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  :: "r"(addr), MXN_I8(r, 0), MXN_I8(r, 8) : "memory");
 }
+__device__ __forceinline__ void tm_load16(uint32_t (&r)[16], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : MXN_R8(r, 0), MXN_R8(r, 8) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ bool elect_one()
@@ -504,13 +510,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
         bool ok = true;
         const int steps = 2 * tiles;
+        bool here = false;
         for (int i = 0; i < steps; ++i) {
             const int j = i >> 1, buf = i & 1;
             const TileScales& slot = scales[j % kScaleSlots];
             const float* const slot_k = slot.k + 4 * buf;
             const float* const slot_v = slot.v + 4 * buf;
             const float* const slot_l = slot.l + 4 * buf;
-            ok = wait(s_full + 16 * rt + 8 * buf, (uint32_t)j & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
+            ok = (here || wait(s_full + 16 * rt + 8 * buf, (uint32_t)j & 1u, dead)) && (buf || wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead));
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_after();
             const uint32_t s_at = s_col[rt] + lanes + buf * kStep;
@@ -527,8 +534,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kStep <= min(see_hi, k1)) && readable == 0xFu;
             uint32_t x[2][32];
             tm_request(x[0], s_at);
-            tm_arrived(x[0]);
             tm_request(x[1], s_at + 32);
+            tm_arrived(x[0]);
             tm_arrived(x[1]);
             if (!all) {
 #pragma unroll
@@ -565,49 +572,50 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                     if (!__all_sync(0xFFFFFFFFu, ok)) break;
                     tc_after();
 #pragma unroll 1
-                    for (int c = 0; c < DIM / 32; ++c) {
-                        uint32_t y[32];
-                        tm_load(y, o_at + 32 * c);
+                    for (int c = 0; c < DIM / 16; ++c) {
+                        uint32_t z[16];
+                        tm_load16(z, o_at + 16 * c);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
-                        tm_store32(o_at + 32 * c, y);
+                        for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * alpha);
+                        tm_store16(o_at + 16 * c, z);
                     }
                 }
             }
+            here = i + 1 < steps && mbar_try_wait(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             // weights, over their scores
             const float shift_by = ref == kNone ? 0.0f : kTop - ref;
             uint32_t w[32];
+            float more = 0.0f;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
                 const float2 f = f2(fac[g]), add = f2(slot_v[g] + shift_by);
                 float2 sum[2] = {f2(0.0f), f2(0.0f)};
-                auto pair = [&](int e) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
                     const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, add);
-                    return u;
-                };
-                if (!wide) {
+                    const float2 p = make_float2(ex2(u.x), ex2(u.y));
+                    sum[e & 1] = __fadd2_rn(sum[e & 1], p);
+                    const __half2 q = __floats2half2_rn(p.x, p.y);
+                    w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                }
+                const float2 both = __fadd2_rn(sum[0], sum[1]);
+                more = fmaf(both.x + both.y, slot_l[g], more);
+            }
+            if (wide && ref > kNone) {   // the sum by exponentials of its own, from the scores as they still stand
+                more = 0.0f;
+#pragma unroll 1
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t z[16];
+                    tm_load16(z, s_at + 16 * g);
+                    const uint32_t see = visible(g >> 1) >> (16 * (g & 1));
+                    const float f = fmaxf(row_factor * slot_k[g], 1.17549435e-38f), add = c0 + kTop - ref;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 u = pair(e);
-                        const float2 p = make_float2(ex2(u.x), ex2(u.y));
-                        sum[e & 1] = __fadd2_rn(sum[e & 1], p);
-                        const __half2 q = __floats2half2_rn(p.x, p.y);
-                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
-                    }
-                    const float2 both = __fadd2_rn(sum[0], sum[1]);
-                    l = fmaf(both.x + both.y, slot_l[g], l);
-                } else {
-                    const float apart = c0 - slot_v[g];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 u = pair(e);
-                        l += ex2(u.x + apart) + ex2(u.y + apart);
-                        const __half2 q = __floats2half2_rn(ex2(u.x), ex2(u.y));
-                        w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
-                    }
+                    for (int e = 0; e < 16; ++e)
+                        if ((see >> e) & 1u) more += ex2(fmaf(__uint_as_float(z[e]), f, add));
                 }
             }
+            l += more;
             tm_store32(s_at, w);
             tm_store_wait();
             tc_before();

@@ -119,7 +119,7 @@ def test_binding_refuses_other_tensors(binding):
         with pytest.raises(ValueError):
             binding._heads(bad, "q")
     with pytest.raises(ValueError):
-        binding._heads(q, "q_out", q[:1])
+        binding._heads(q, "q_out", q[:1].shape)
     with pytest.raises(ValueError):
         binding._vec(torch.zeros(4, dtype=torch.int64), torch.int32, "positions")
     with pytest.raises(ValueError):
