@@ -2,26 +2,23 @@
 //
 //   s_t = scale * q . k_t,   o = sum_t softmax(s)_t v_t,   k_t = 2^(sk - 127) * code, v_t likewise
 //
-// Every code is read once from HBM, which bounds the call (2 * dim bytes a token and head); the arithmetic runs on the codes
-// as they are.  The tensor cores multiply E4M3 by E4M3 with binary32 sums, so q and the softmax's weights are written as
-// sums of two E4M3 numbers, hi + lo/16.  The product tile has 16 rows and a group of query heads rarely more than eight, so
-// eight query rows fill a tile: row g is hi and row g + 8 lo of the same query row, and one multiplication does both.  The two
-// sums of a query row end in the same thread.  The splits:
-//   q  is scaled by a power of two that brings the row's largest magnitude to [128, 256).  hi is q to 4 significant bits, what
-//      is left of a bf16 value has at most 4 significant bits again: hi + lo/16 IS q, but for elements below 2^-14 of the
-//      row's largest, which keep an absolute error of 2^-22 of it.
-//   p  keeps 8 bits (relative error at most 2^-8, as a bf16 would), or 2^-23 of the largest weight of its tile in absolute terms.
-// The scales of the cache never touch the codes: a key block's scale multiplies the finished product, a value block's is
-// folded into the weight, w_t = 2^(s_t + sv_t - R), with the reference R following the tiles' largest s + sv (an integer,
-// so that the correction of the sums is exact).  The softmax's own sum l keeps a reference of its own and unrounded weights.
+// Every code is read once from HBM, which bounds the call (2 * dim bytes a token and head).  The codes are widened to f16, which
+// is exact, two at a time in registers, and multiplied there with binary32 sums (mma m16n8k16; fp8 operands of this instruction
+// would be widened one by one by the compiler, twice as many instructions):
+//   q  is scaled by a power of two that brings the row's largest magnitude to [2^14, 2^15), so that f16 holds a bf16 value exactly
+//      but for elements below 2^-28 of the row's largest (to 2^-39 of it).
+//   The scales of the cache never touch the codes: a key block's scale multiplies the finished product, a value block's is
+//      folded into the softmax's weight, w_t = 2^(s_t + sv_t - R + 1) in f16.  The reference R (an integer, so that corrections of
+//      the sums are exact) is moved when a tile's largest s + sv is 14 above or 16 below it: f16 keeps 11 bits of what is above
+//      2^-14 and drops what is below 2^-25.  The softmax's own sum l has a reference of its own and unrounded weights.
 //
-// A CTA of four warps takes `rows` = 8 * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
+// A CTA of four warps takes up to 16 * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
 // of warps walk over the chunk's tiles of 32 tokens in turn; each group feeds itself through a ring of tiles that the
-// tensor copy engine fills (128-byte swizzle: the two access patterns below are then free of bank conflicts).  Within a tile,
+// tensor copy engine fills (swizzled: the two access patterns below are then free of bank conflicts).  Within a tile,
 // a thread reads its operand words with 16-byte loads: the order of the dimensions within a product and of the tokens within a
-// sum is free, and is chosen so that a thread's share is contiguous.  The values' operand wants four tokens of one dimension
-// in a word: a 4 x 4 byte transposition by eight byte permutations.  The weights go from the first product's accumulators to
-// the second product's operand without leaving the thread.
+// sum is free, and is chosen so that a thread's share is contiguous: a word of four key codes is one step's operand.  The values'
+// operand wants two tokens of one dimension side by side: one byte permutation makes two such pairs of codes.  The weights go
+// from the first product's accumulators to the second product's operand without leaving the thread.
 //
 // Partial results of the chunks go to the workspace as (normalised row, logarithm of its sum) and are joined in a fixed
 // order by a second kernel; with one chunk the row is written at once.
@@ -29,7 +26,6 @@
 // Every wait is bounded (see mxn_device_timeouts).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 
 #include <cmath>
 
@@ -41,40 +37,36 @@ namespace {
 
 constexpr int kSMs = 148;
 constexpr int kWarps = 4;
+#ifndef MXN_DEC_CTAS
+#define MXN_DEC_CTAS 3
+#endif
 constexpr int kTile = 32;      // tokens of a tile
-constexpr int kPromptRows = 32;   // more query rows a sequence and key head than this: the tcgen05 kernel
+constexpr int kPromptRows = 64;   // more query rows a sequence and key head than this: the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ unsigned int g_attn_timeouts = 0;
 __device__ unsigned int g_attn_bad = 0;   // pages out of range within a sequence's length
 
-__device__ __forceinline__ void mma_e4m3(float* c, const uint32_t* a, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the four E4M3 codes of a word -> two f16 pairs
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ uint2 lds_v2(uint32_t addr)
 {
     uint2 r;
     asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr));
     return r;
-}
-// four binary32 -> hi and lo words: hi = E4M3(x), lo = E4M3(16 (x - hi)); |x| <= 256
-__device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_t& lo)
-{
-    // in f16 pairs: 11 bits hold what hi + lo can express, and x - hi is exact
-    const __half2 a = __floats2half2_rn(x0, x1);
-    hi = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(a), __NV_SATFINITE, __NV_E4M3);
-    const __half2 left = __hsub2(a, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3)));
-    lo = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(__hmul2(left, __float2half2_rn(16.0f))), __NV_SATFINITE, __NV_E4M3);
-}
-__device__ __forceinline__ void split4(float x0, float x1, float x2, float x3, uint32_t& hi, uint32_t& lo)
-{
-    uint32_t h0, h1, l0, l1;
-    split2(x0, x1, h0, l0);
-    split2(x2, x3, h1, l1);
-    hi = h0 | (h1 << 16);
-    lo = l0 | (l1 << 16);
 }
 __device__ __forceinline__ float quad_max(float v)
 {
@@ -92,22 +84,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<uint32_t*>(&v);
 }
 
-template <int DIM, int RW, int STAGES>
+// weights: 2^kTop at the reference, which is moved when a tile's largest is kUp above or kDown below it, but to no more than kDepth
+// below the largest so far (the output's sums must not overflow)
+constexpr float kTop = 1.0f, kUp = 14.0f, kDown = 16.0f, kDepth = 40.0f;
+
+template <int DIM, int RW, int HALVES, int STAGES>
 struct DecodeShape {
     static constexpr int kGroups = kWarps / RW;                  // warp groups that share out the tiles
     static constexpr int kTileBytes = kTile * DIM;               // codes of a tile, keys or values
     static constexpr int kRingBytes = kGroups * STAGES * 2 * kTileBytes;
-    static constexpr int kRows = 8 * RW;
+    static constexpr int kRows = 8 * HALVES * RW;
     static constexpr int kJoinBytes = kGroups * kRows * (DIM * 4 + 8);
     static constexpr int kSmem = (kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes) + 1024;
 };
 
-template <int DIM, int RW, int STAGES>
-__global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
+// HALVES: 1 where a warp has at most 8 rows (the lower half of the product's 16 stays empty), else 2
+template <int DIM, int RW, int HALVES, int STAGES>
+__global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
-    using Sh = DecodeShape<DIM, RW, STAGES>;
+    using Sh = DecodeShape<DIM, RW, HALVES, STAGES>;
     constexpr int NT = DIM / 8;      // column tiles of the second product
-    constexpr int KS = DIM / 32;     // steps of the first
+    constexpr int KS = DIM / 16;     // steps of the first
     constexpr int GROUPS = Sh::kGroups;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * GROUPS * STAGES];   // full, then empty
@@ -136,14 +133,20 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
-    // this thread's row: its query token, head and place among the outputs
-    const int row = row0 + rw * 8 + g;
-    const bool row_live = row < rows;
-    const int64_t tok = q0 + (row_live ? row / G : 0);
-    const int head = h * G + (row_live ? row % G : 0);
-    const int pos = shift + (row_live ? row / G : nq - 1);
-    const int see_hi = P.causal ? min(pos + 1, len) : len;                     // keys [see_lo, see_hi)
-    const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+    // this thread's rows (g, and g + 8): query token, head, and the keys they see
+    bool row_live[HALVES];
+    int64_t tok[HALVES];
+    int head[HALVES], see_hi[HALVES], see_lo[HALVES];
+#pragma unroll
+    for (int x = 0; x < HALVES; ++x) {
+        const int row = row0 + rw * 8 * HALVES + 8 * x + g;
+        row_live[x] = row < rows;
+        tok[x] = q0 + (row_live[x] ? row / G : 0);
+        head[x] = h * G + (row_live[x] ? row % G : 0);
+        const int pos = shift + (row_live[x] ? row / G : nq - 1);
+        see_hi[x] = P.causal ? min(pos + 1, len) : len;                     // keys [see_lo, see_hi)
+        see_lo[x] = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+    }
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t ring = base + (uint32_t)group * STAGES * 2 * Sh::kTileBytes;
@@ -216,29 +219,28 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
     };
     uint32_t sc_next = scale_at(0, pages[0]);
 
-    // q: the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on, split; the power of two goes to the row's factor
-    uint32_t qa[KS][4];
-    float row_factor;
-    {
-        uint4 w[DIM / 32];
-        const uint16_t* qp = P.q + tok * P.q_stride + (int64_t)head * DIM + c * (DIM / 4);
+    // q: the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on; the power of two goes to the row's factor
+    uint32_t qa[KS][2][HALVES];
+    float row_factor[HALVES];
 #pragma unroll
-        for (int i = 0; i < DIM / 32; ++i) w[i] = row_live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+    for (int x = 0; x < HALVES; ++x) {
+        uint4 w[DIM / 32];
+        const uint16_t* qp = P.q + tok[x] * P.q_stride + (int64_t)head[x] * DIM + c * (DIM / 4);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; ++i) w[i] = row_live[x] ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
         const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
         const uint32_t E = __float_as_uint(quad_max(hmax_abs_to_f32(m))) >> 23;
-        const uint32_t Ec = min(max(E, 8u), 254u);
-        const float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);   // 2^(7 - (E - 127))
-        row_factor = P.scale * kLog2e * __uint_as_float((Ec - 7u) << 23);                // ... and its inverse
+        const uint32_t Ec = min(max(E, 15u), 254u);
+        const float up = __uint_as_float((268u - Ec) << 23);                                // 2^(14 - (E - 127))
+        row_factor[x] = P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23);               // ... and its inverse
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint32_t a = u[4 * k + 2 * x], d = u[4 * k + 2 * x + 1];
-                split4(bf16_lo(a) * up, bf16_hi(a) * up, bf16_lo(d) * up, bf16_hi(d) * up, qa[k][2 * x], qa[k][2 * x + 1]);
-            }
+        for (int k = 0; k < KS; ++k) {
+            qa[k][0][x] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
+            qa[k][1][x] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
+        }
     }
 
     float acc[NT][4];
@@ -247,8 +249,13 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
     const float kNone = -INFINITY;
-    float m_ref = kNone, l = 0.0f;             // softmax: reference (an integer) and this thread's part of the sum
-    float r_ref = kNone, r_top = kNone;        // second product: reference (an integer) and the largest so far
+    float m_ref[HALVES], l[HALVES];            // softmax: reference (an integer) and this thread's part of the sum
+    float r_ref[HALVES], r_top[HALVES];        // second product: reference (an integer) and the largest so far
+#pragma unroll
+    for (int x = 0; x < HALVES; ++x) {
+        m_ref[x] = r_ref[x] = r_top[x] = kNone;
+        l[x] = 0.0f;
+    }
     bool ok = true;
 
     for (int i = 0; i < mine; ++i) {
@@ -257,7 +264,7 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
         const int t0 = tile_at(i);
         const uint32_t sc = sc_next;
         sc_next = scale_at(i + 1, pages[1]);
-        const float kf0 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)) * row_factor, kf1 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16)) * row_factor;
+        const float kf0 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)), kf1 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16));
         const float sv0 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, sv1 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f;
         // tokens of the tile that exist and whose page could be read
         const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && pages[0] >= 0);
@@ -269,107 +276,129 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
         const uint32_t kt = ring + (uint32_t)st * 2 * Sh::kTileBytes, vt = kt + Sh::kTileBytes;
 
         // ---- s = q . k: token 8j + g is column g of column tile j ----
-        float s[8];
+        float s[HALVES][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int r = 8 * j + g;
-            uint32_t w[2 * KS];
+            uint32_t w[KS];
             if constexpr (DIM == 128) {
                 const uint4 a = lds_v4(kt + r * 128 + (((2 * c) ^ g) << 4)), d = lds_v4(kt + r * 128 + (((2 * c + 1) ^ g) << 4));
                 w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-                w[KS * 2 - 4] = d.x; w[KS * 2 - 3] = d.y; w[KS * 2 - 2] = d.z; w[KS * 2 - 1] = d.w;
+                w[4] = d.x; w[5] = d.y; w[6] = d.z; w[7] = d.w;
             } else {
                 const uint4 a = lds_v4(kt + r * 64 + ((c ^ ((g >> 1) & 3)) << 4));
                 w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
             }
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < KS; ++k) mma_e4m3(d, qa[k], w[2 * k], w[2 * k + 1]);
-            const float f = j < 2 ? kf0 : kf1;
-            s[2 * j] = fmaf(d[2], 0.0625f, d[0]) * f;
-            s[2 * j + 1] = fmaf(d[3], 0.0625f, d[1]) * f;
+            for (int k = 0; k < KS; ++k) {
+                uint32_t b0, b1;
+                widen(w[k], b0, b1);
+                mma_f16(d, qa[k][0][0], HALVES == 2 ? qa[k][0][HALVES - 1] : 0u, qa[k][1][0], HALVES == 2 ? qa[k][1][HALVES - 1] : 0u, b0, b1);
+            }
+#pragma unroll
+            for (int x = 0; x < HALVES; ++x) {
+                const float f = (j < 2 ? kf0 : kf1) * row_factor[x];
+                s[x][2 * j] = d[2 * x] * f;
+                s[x][2 * j + 1] = d[2 * x + 1] * f;
+            }
         }
-        // ---- what this row may not see ----
-        const bool all = there == 0xFFFFFFFFu && t0 >= see_lo && t0 + kTile <= see_hi;
+        // ---- what the rows may not see ----
+        bool all = there == 0xFFFFFFFFu;
+#pragma unroll
+        for (int x = 0; x < HALVES; ++x) all = all && t0 >= see_lo[x] && t0 + kTile <= see_hi[x];
         if (!__all_sync(0xFFFFFFFFu, all)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = 8 * (e >> 1) + 2 * c + (e & 1);
-                if (!((there >> t) & 1u) || t0 + t < see_lo || t0 + t >= see_hi) s[e] = kNone;
-            }
+            for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = 8 * (e >> 1) + 2 * c + (e & 1);
+                    if (!((there >> t) & 1u) || t0 + t < see_lo[x] || t0 + t >= see_hi[x]) s[x][e] = kNone;
+                }
         }
         // ---- references ----
-        const float top0 = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top1 = fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]));
-        const float top = quad_max(fmaxf(top0, top1));
-        const float utop = ceilf(quad_max(fmaxf(top0 + sv0, top1 + sv1)));
-        if (top > m_ref) {
-            const float n = ceilf(top);
-            l *= ex2(m_ref - n);
-            m_ref = n;
+        float r_new[HALVES];
+        bool moved = false;
+#pragma unroll
+        for (int x = 0; x < HALVES; ++x) {
+            const float top0 = fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3])), top1 = fmaxf(fmaxf(s[x][4], s[x][5]), fmaxf(s[x][6], s[x][7]));
+            const float top = quad_max(fmaxf(top0, top1)), utop = quad_max(fmaxf(top0 + sv0, top1 + sv1));
+            if (top > m_ref[x]) {
+                const float n = ceilf(top);
+                l[x] *= ex2(m_ref[x] - n);
+                m_ref[x] = n;
+            }
+            r_new[x] = r_ref[x];
+            if (utop > r_ref[x] + kUp || (r_ref[x] == kNone && utop > kNone)) r_new[x] = ceilf(utop);
+            else if (utop < r_ref[x] - kDown && utop > kNone) r_new[x] = fmaxf(ceilf(utop), r_top[x] - kDepth);
+            r_top[x] = fmaxf(r_top[x], r_new[x]);
+            moved = moved || r_new[x] != r_ref[x];
         }
-        r_top = fmaxf(r_top, utop);
-        // follow the tile's largest: up at once, down when six binades are lost (never 40 below the largest so far, so
-        // that the sums cannot overflow)
-        float r_new = r_ref;
-        if (utop > r_ref) r_new = utop;
-        else if (utop < r_ref - 6.0f && utop > kNone) r_new = fmaxf(utop, r_top - 40.0f);
-        if (__any_sync(0xFFFFFFFFu, r_new != r_ref)) {
-            const float alpha = r_ref == kNone ? 0.0f : ex2(r_ref - r_new);
-            r_ref = r_new;
+        if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+            for (int x = 0; x < HALVES; ++x) {
+                const float alpha = r_ref[x] == kNone ? 0.0f : ex2(r_ref[x] - r_new[x]);
+                r_ref[x] = r_new[x];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[j][e] *= alpha;
+                for (int j = 0; j < NT; ++j) {
+                    acc[j][2 * x] *= alpha;
+                    acc[j][2 * x + 1] *= alpha;
+                }
+            }
         }
         // ---- weights ----
-        const float ms = m_ref == kNone ? 0.0f : m_ref, rs = r_ref == kNone ? 0.0f : r_ref;
-        const float b0 = sv0 + 8.0f - rs, b1 = sv1 + 8.0f - rs;   // largest weight 2^8
-        float w[8];
+        uint32_t pa[2][2][HALVES];   // [16 tokens][first, second 8 of them][row]
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            l += ex2(s[e] - ms);
-            w[e] = ex2(s[e] + (e < 4 ? b0 : b1));
+        for (int x = 0; x < HALVES; ++x) {
+            const float ms = m_ref[x] == kNone ? 0.0f : m_ref[x], rs = r_ref[x] == kNone ? 0.0f : r_ref[x];
+            const float b0 = sv0 + kTop - rs, b1 = sv1 + kTop - rs;
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                l[x] += ex2(s[x][e] - ms);
+                w[e] = ex2(s[x][e] + (e < 4 ? b0 : b1));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pa[e >> 1][e & 1][x] = pack_f16(w[2 * e], w[2 * e + 1]);
         }
-        uint32_t pa[4];
-        split4(w[0], w[1], w[2], w[3], pa[0], pa[1]);
-        split4(w[4], w[5], w[6], w[7], pa[2], pa[3]);
         // ---- o += w v: tokens 2c, 2c+1, 8+2c, 9+2c (then 16 more) of DIM/8 dimensions from g * DIM/8 on ----
         constexpr int VW = DIM / 32;   // words a thread reads of each token
-        uint32_t v[8][VW];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const int r = 8 * (x >> 1) + 2 * c + (x & 1);
-            if constexpr (DIM == 128) {
-                const uint4 a = lds_v4(vt + r * 128 + ((g ^ (r & 7)) << 4));
-                v[x][0] = a.x; v[x][1] = a.y; v[x][VW - 2] = a.z; v[x][VW - 1] = a.w;
-            } else {
-                const uint2 a = lds_v2(vt + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
-                v[x][0] = a.x; v[x][1] = a.y;
+        for (int half = 0; half < 2; ++half) {
+            uint32_t v[4][VW];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int r = 16 * half + 8 * (x >> 1) + 2 * c + (x & 1);
+                if constexpr (DIM == 128) {
+                    const uint4 a = lds_v4(vt + r * 128 + ((g ^ (r & 7)) << 4));
+                    v[x][0] = a.x; v[x][1] = a.y; v[x][2] = a.z; v[x][3] = a.w;
+                } else {
+                    const uint2 a = lds_v2(vt + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
+                    v[x][0] = a.x; v[x][1] = a.y;
+                }
             }
-        }
-        if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token, a NaN among it, must not meet the zero weights
+            if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token, a NaN among it, must not meet the zero weights
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const int t = 8 * (x >> 1) + 2 * c + (x & 1);
-                if (!((there >> t) & 1u))
+                for (int x = 0; x < 4; ++x) {
+                    const int t = 16 * half + 8 * (x >> 1) + 2 * c + (x & 1);
+                    if (!((there >> t) & 1u))
 #pragma unroll
-                    for (int y = 0; y < VW; ++y) v[x][y] = 0u;
-            }
-        }
-#pragma unroll
-        for (int y = 0; y < VW; ++y) {
-            uint32_t o[2][4];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint32_t a0 = __byte_perm(v[4 * x][y], v[4 * x + 1][y], 0x5140), a1 = __byte_perm(v[4 * x][y], v[4 * x + 1][y], 0x7362);
-                const uint32_t a2 = __byte_perm(v[4 * x + 2][y], v[4 * x + 3][y], 0x5140), a3 = __byte_perm(v[4 * x + 2][y], v[4 * x + 3][y], 0x7362);
-                o[x][0] = __byte_perm(a0, a2, 0x5410);
-                o[x][1] = __byte_perm(a0, a2, 0x7632);
-                o[x][2] = __byte_perm(a1, a3, 0x5410);
-                o[x][3] = __byte_perm(a1, a3, 0x7632);
+                        for (int y = 0; y < VW; ++y) v[x][y] = 0u;
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mma_e4m3(acc[4 * y + e], pa, o[0][e], o[1][e]);
+            for (int y = 0; y < VW; ++y) {
+                uint32_t b[2][4];   // [8 tokens][dimension]: f16 pairs of two tokens
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x5140), b[x][0], b[x][1]);
+                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x7362), b[x][2], b[x][3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    mma_f16(acc[4 * y + e], pa[half][0][0], HALVES == 2 ? pa[half][0][HALVES - 1] : 0u, pa[half][1][0],
+                            HALVES == 2 ? pa[half][1][HALVES - 1] : 0u, b[0][e], b[1][e]);
+            }
         }
         // ---- hand the stage back ----
         __syncwarp();
@@ -402,77 +431,93 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? 3 : 4) attn_decode_k
     if (__any_sync(0xFFFFFFFFu, bad_page) && lane == 0) atomicAdd(&g_attn_bad, 1u);
 
     // ---- join the groups of warps ----
-    l = quad_sum(l);
-    const float ms = m_ref == kNone ? 0.0f : m_ref, rs = r_ref == kNone ? 0.0f : r_ref;
-    const float back = ex2(fminf(fmaxf(rs - 8.0f - ms, -126.0f), 127.0f));
-    constexpr int OUT = DIM / 4;   // dimensions a thread ends with: those from c * OUT on
-    float o[OUT];
+    constexpr int OUT = DIM / 4;   // dimensions a thread ends with: those from c * OUT on, of each of its rows
+    float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+    float* const stat = sm + GROUPS * Sh::kRows * DIM;
+    float o[HALVES][OUT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        o[j] = fmaf(acc[j][2], 0.0625f, acc[j][0]) * back;
-        o[NT + j] = fmaf(acc[j][3], 0.0625f, acc[j][1]) * back;
+    for (int x = 0; x < HALVES; ++x) {
+        l[x] = quad_sum(l[x]);
+        const float ms = m_ref[x] == kNone ? 0.0f : m_ref[x], rs = r_ref[x] == kNone ? 0.0f : r_ref[x];
+        const float back = ex2(fminf(fmaxf(rs - kTop - ms, -126.0f), 127.0f));
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            o[x][j] = acc[j][2 * x] * back;
+            o[x][NT + j] = acc[j][2 * x + 1] * back;
+        }
     }
     if (GROUPS > 1) {
-        float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
-        float* const stat = sm + GROUPS * Sh::kRows * DIM;
         __syncthreads();   // every copy has landed and been read
         if (group != 0) {
-            float* const p = sm + ((int64_t)group * Sh::kRows + rw * 8 + g) * DIM + c * OUT;
 #pragma unroll
-            for (int x = 0; x < OUT / 4; ++x) *reinterpret_cast<float4*>(p + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-            if (c == 0) {
-                stat[2 * (group * Sh::kRows + rw * 8 + g)] = m_ref;
-                stat[2 * (group * Sh::kRows + rw * 8 + g) + 1] = l;
+            for (int x = 0; x < HALVES; ++x) {
+                const int at = group * Sh::kRows + (rw * HALVES + x) * 8 + g;
+                float* const p = sm + (int64_t)at * DIM + c * OUT;
+#pragma unroll
+                for (int y = 0; y < OUT / 4; ++y) *reinterpret_cast<float4*>(p + 4 * y) = make_float4(o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]);
+                if (c == 0) {
+                    stat[2 * at] = m_ref[x];
+                    stat[2 * at + 1] = l[x];
+                }
             }
         }
         __syncthreads();
         if (group != 0) return;
-        float m_all = m_ref;
 #pragma unroll
-        for (int k = 1; k < GROUPS; ++k) m_all = fmaxf(m_all, stat[2 * (k * Sh::kRows + rw * 8 + g)]);
-        const float own = m_ref == kNone ? 0.0f : ex2(m_ref - m_all);
-        l *= own;
+        for (int x = 0; x < HALVES; ++x) {
+            const int mine_at = (rw * HALVES + x) * 8 + g;
+            float m_all = m_ref[x];
 #pragma unroll
-        for (int x = 0; x < OUT; ++x) o[x] *= own;
+            for (int k = 1; k < GROUPS; ++k) m_all = fmaxf(m_all, stat[2 * (k * Sh::kRows + mine_at)]);
+            const float own = m_ref[x] == kNone ? 0.0f : ex2(m_ref[x] - m_all);
+            l[x] *= own;
 #pragma unroll
-        for (int k = 1; k < GROUPS; ++k) {
-            const int at = k * Sh::kRows + rw * 8 + g;
-            const float mk = stat[2 * at];
-            if (mk == kNone) continue;
-            const float f = ex2(mk - m_all);
-            l = fmaf(stat[2 * at + 1], f, l);
-            const float* const p = sm + (int64_t)at * DIM + c * OUT;
+            for (int y = 0; y < OUT; ++y) o[x][y] *= own;
 #pragma unroll
-            for (int x = 0; x < OUT / 4; ++x) {
-                const float4 a = *reinterpret_cast<const float4*>(p + 4 * x);
-                o[4 * x] = fmaf(a.x, f, o[4 * x]);
-                o[4 * x + 1] = fmaf(a.y, f, o[4 * x + 1]);
-                o[4 * x + 2] = fmaf(a.z, f, o[4 * x + 2]);
-                o[4 * x + 3] = fmaf(a.w, f, o[4 * x + 3]);
+            for (int k = 1; k < GROUPS; ++k) {
+                const int at = k * Sh::kRows + mine_at;
+                const float mk = stat[2 * at];
+                if (mk == kNone) continue;
+                const float f = ex2(mk - m_all);
+                l[x] = fmaf(stat[2 * at + 1], f, l[x]);
+                const float* const p = sm + (int64_t)at * DIM + c * OUT;
+#pragma unroll
+                for (int y = 0; y < OUT / 4; ++y) {
+                    const float4 a = *reinterpret_cast<const float4*>(p + 4 * y);
+                    o[x][4 * y] = fmaf(a.x, f, o[x][4 * y]);
+                    o[x][4 * y + 1] = fmaf(a.y, f, o[x][4 * y + 1]);
+                    o[x][4 * y + 2] = fmaf(a.z, f, o[x][4 * y + 2]);
+                    o[x][4 * y + 3] = fmaf(a.w, f, o[x][4 * y + 3]);
+                }
             }
+            m_ref[x] = m_all;
         }
-        m_ref = m_all;
     }
-    if (!row_live) return;
-    const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;       // a row that sees nothing: zeros
-    const float lse2 = l > 0.0f ? m_ref + log2f(l) : kNone;
-    if (P.splits == 1) {
-        uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + c * OUT;
 #pragma unroll
-        for (int x = 0; x < OUT / 8; ++x) {
-            const uint32_t r[4] = {pack_bf16(o[8 * x] * inv, o[8 * x + 1] * inv), pack_bf16(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
-                                   pack_bf16(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack_bf16(o[8 * x + 6] * inv, o[8 * x + 7] * inv)};
-            st_v4(y + 8 * x, r);
-        }
-        if (P.lse != nullptr && c == 0) P.lse[tok * P.q_heads + head] = lse2 * kLn2;
-    } else {
-        const int64_t at = (tok * P.q_heads + head) * P.splits + split;
-        if (c == 0) P.part_lse[at] = lse2;
-        if (l > 0.0f) {
-            float* const y = P.part_out + at * DIM + c * OUT;
+    for (int x = 0; x < HALVES; ++x) {
+        if (!row_live[x]) continue;
+        const float inv = l[x] > 0.0f ? __fdiv_rn(1.0f, l[x]) : 0.0f;       // a row that sees nothing: zeros
+        const float lse2 = l[x] > 0.0f ? m_ref[x] + log2f(l[x]) : kNone;
+        const int64_t out_row = tok[x] * P.q_heads + head[x];
+        if (P.splits == 1) {
+            uint16_t* const y = P.out + tok[x] * P.out_stride + (int64_t)head[x] * DIM + c * OUT;
 #pragma unroll
-            for (int x = 0; x < OUT / 4; ++x)
-                *reinterpret_cast<float4*>(y + 4 * x) = make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
+            for (int e = 0; e < OUT / 8; ++e) {
+                uint32_t r[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = pack_bf16(o[x][8 * e + 2 * k] * inv, o[x][8 * e + 2 * k + 1] * inv);
+                st_v4(y + 8 * e, r);
+            }
+            if (P.lse != nullptr && c == 0) P.lse[out_row] = lse2 * kLn2;
+        } else {
+            const int64_t at = out_row * P.splits + split;
+            if (c == 0) P.part_lse[at] = lse2;
+            if (l[x] > 0.0f) {
+                float* const y = P.part_out + at * DIM + c * OUT;
+#pragma unroll
+                for (int e = 0; e < OUT / 4; ++e)
+                    *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[x][4 * e] * inv, o[x][4 * e + 1] * inv, o[x][4 * e + 2] * inv, o[x][4 * e + 3] * inv);
+            }
         }
     }
 }
@@ -561,10 +606,17 @@ bool make_map(CUtensorMap* map, const uint8_t* codes, const AttnParams& P, int b
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DIM, int RW, int STAGES>
+template <int DIM, int RW, int HALVES, int STAGES>
 cudaError_t launch_decode(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
 {
-    return launch(attn_decode_kernel<DIM, RW, STAGES>, ctas, kWarps * 32, DecodeShape<DIM, RW, STAGES>::kSmem, stream, P, M);
+    return launch(attn_decode_kernel<DIM, RW, HALVES, STAGES>, ctas, kWarps * 32, DecodeShape<DIM, RW, HALVES, STAGES>::kSmem, stream, P, M);
+}
+template <int DIM>
+cudaError_t launch_rows(const AttnParams& P, const AttnMaps& M, const AttnPlan& a, cudaStream_t stream)
+{
+    if (a.row_warps == 1)
+        return a.halves == 1 ? launch_decode<DIM, 1, 1, 2>(P, M, a.ctas, stream) : launch_decode<DIM, 1, 2, 2>(P, M, a.ctas, stream);
+    return a.row_warps == 2 ? launch_decode<DIM, 2, 2, 3>(P, M, a.ctas, stream) : launch_decode<DIM, 4, 2, 4>(P, M, a.ctas, stream);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -578,15 +630,17 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     if (max_q > n) max_q = n;
     const int64_t rows = max_q * (q_heads / kv_heads);
     a.prompt = rows > kPromptRows;
-    a.row_warps = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-    a.row_tiles = ceil_div(rows, a.prompt ? 256 : 8 * a.row_warps);
+    a.halves = rows <= 8 ? 1 : 2;
+    a.row_warps = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int64_t tile_rows = a.prompt ? 256 : 8 * a.halves * a.row_warps;
+    a.row_tiles = ceil_div(rows, tile_rows);
     // enough chunks for four rounds of the CTAs that are resident at a time (sequences differ in length), none
     // shorter than a tile for every group of warps
     const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile, least = a.prompt ? 128 : kTile * (kWarps / a.row_warps);
     // (many rows: one CTA an SM, whose start costs as much as a few hundred keys; two rounds)
     int64_t splits = a.prompt ? (units >= kSMs ? 1 : ceil_div(kSMs * 2, units)) : ceil_div((int64_t)kSMs * (dim == 128 ? 3 : 4) * 4, units);
     // keys that the rows of a tile can see between them
-    const int64_t tokens = ceil_div(a.prompt ? 256 : 8 * a.row_warps, q_heads / kv_heads) + 1;
+    const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
     const int64_t span = window > 0 && window + tokens + tile < max_len ? window + tokens + tile : max_len;
     const int64_t most = ceil_div(max_len, a.prompt ? 512 : least);   // of the workspace: for any window
     if (splits > most) splits = most;
@@ -613,12 +667,8 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     cudaError_t e;
     if (a.prompt)
         e = launch_prompt(P, M, a.ctas, stream);
-    else if (P.dim == 128)
-        e = a.row_warps == 1 ? launch_decode<128, 1, 2>(P, M, a.ctas, stream)
-          : a.row_warps == 2 ? launch_decode<128, 2, 3>(P, M, a.ctas, stream) : launch_decode<128, 4, 4>(P, M, a.ctas, stream);
     else
-        e = a.row_warps == 1 ? launch_decode<64, 1, 2>(P, M, a.ctas, stream)
-          : a.row_warps == 2 ? launch_decode<64, 2, 3>(P, M, a.ctas, stream) : launch_decode<64, 4, 4>(P, M, a.ctas, stream);
+        e = P.dim == 128 ? launch_rows<128>(P, M, a, stream) : launch_rows<64>(P, M, a, stream);
     if (e != cudaSuccess || a.splits == 1) return e;
     const int64_t ctas = ceil_div(P.n * P.q_heads, 4);
     return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, 128, 0, stream, P) : launch(attn_join_kernel<64>, ctas, 128, 0, stream, P);
