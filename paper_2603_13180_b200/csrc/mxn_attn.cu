@@ -522,14 +522,17 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
     }
 }
 
-// joins the chunks of each row: one warp a row, chunks in order
+// joins the chunks of each row.  A CTA takes a row: each of its eight warps adds every eighth chunk, four at a time in flight, and
+// the warps' sums are added in order.
+constexpr int kJoinWarps = 8;
 template <int DIM>
-__global__ void __launch_bounds__(128) attn_join_kernel(const AttnParams P)
+__global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnParams P)
 {
+    constexpr int E = DIM / 32;   // dimensions of a thread
+    __shared__ float sums[kJoinWarps][DIM + 1];
     pdl_prologue();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int64_t tok = row / P.q_heads;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = blockIdx.x, tok = row / P.q_heads;
     // rows of no sequence are left as they were
     if (tok >= min((int64_t)__ldg(P.cu_q + P.seqs), P.n) || tok < __ldg(P.cu_q)) return;
     const float* const part = P.part_lse + row * P.splits;
@@ -538,24 +541,38 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnParams P)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const bool none = top == -INFINITY;
-    constexpr int E = DIM / 32;
     float sum = 0.0f, acc[E] = {};
     if (!none) {
-        for (int i = 0; i < P.splits; ++i) {
-            const float li = part[i];
-            if (li == -INFINITY) continue;
-            const float f = ex2(li - top);
+#pragma unroll 4
+        for (int i = warp; i < P.splits; i += kJoinWarps) {
+            const float li = part[i], f = ex2(li - top);
             sum += f;
             const float* const p = P.part_out + (row * P.splits + i) * DIM + lane * E;
+            float v[E];
+            if constexpr (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(p);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(p[e], f, acc[e]);
+            for (int e = 0; e < E; ++e) acc[e] = li == -INFINITY ? acc[e] : fmaf(v[e], f, acc[e]);   // (an empty chunk wrote no row)
         }
     }
-    const float inv = none ? 0.0f : __fdiv_rn(1.0f, sum);
-    uint32_t* const y = reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM + lane * E);
 #pragma unroll
-    for (int e = 0; e < E / 2; ++e) y[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    if (P.lse != nullptr && lane == 0) P.lse[row] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+    for (int e = 0; e < E; ++e) sums[warp][lane * E + e] = acc[e];
+    if (lane == 0) sums[warp][DIM] = sum;
+    __syncthreads();
+    float all = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kJoinWarps; ++k) all += sums[k][DIM];
+    const float inv = none ? 0.0f : __fdiv_rn(1.0f, all);
+    if (threadIdx.x < DIM / 2) {
+        float a = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kJoinWarps; ++k) {
+            a += sums[k][2 * threadIdx.x];
+            b += sums[k][2 * threadIdx.x + 1];
+        }
+        reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM)[threadIdx.x] = pack_bf16(a * inv, b * inv);
+    }
+    if (P.lse != nullptr && threadIdx.x == 0) P.lse[row] = none ? -INFINITY : (top + log2f(all)) * kLn2;
 }
 
 template <class K, class... Args>
@@ -634,20 +651,26 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     a.row_warps = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t tile_rows = a.prompt ? 256 : 8 * a.halves * a.row_warps;
     a.row_tiles = ceil_div(rows, tile_rows);
-    // enough chunks for four rounds of the CTAs that are resident at a time (sequences differ in length), none
-    // shorter than a tile for every group of warps
-    const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile, least = a.prompt ? 128 : kTile * (kWarps / a.row_warps);
-    // (many rows: one CTA an SM, whose start costs as much as a few hundred keys; two rounds)
-    int64_t splits = a.prompt ? (units >= kSMs ? 1 : ceil_div(kSMs * 2, units)) : ceil_div((int64_t)kSMs * (dim == 128 ? 3 : 4) * 4, units);
+    const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile;
+    const int64_t step = a.prompt ? 128 : kTile * (kWarps / a.row_warps);   // keys that a CTA works on at a time
+    // Chunks: as many as the CTAs that are resident at a time leave room for; four rounds of them where sequences may differ in
+    // length (64 sequences of 2048 ... 8192 keys: one round 152 us, four 135 us).  A chunk is at least eight steps long, so that a
+    // CTA's start and the join are worth it, unless most SMs would be idle.
+    const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : dim == 128 ? 3 : 4);
+    int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
     const int64_t span = window > 0 && window + tokens + tile < max_len ? window + tokens + tile : max_len;
-    const int64_t most = ceil_div(max_len, a.prompt ? 512 : least);   // of the workspace: for any window
-    if (splits > most) splits = most;
+    auto most = [&](int64_t keys) {
+        const int64_t by_eight = ceil_div(keys, 8 * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
+        return by_eight >= idle ? by_eight : by_one < idle ? by_one : idle;
+    };
+    const int64_t bound = splits < most(max_len) ? splits : most(max_len);   // for the workspace: whatever the window
+    a.workspace = bound > 1 ? (size_t)n * q_heads * bound * (dim + 1) * 4 : 0;
+    if (splits > most(span)) splits = most(span);
     if (splits < 1) splits = 1;
-    a.workspace = splits > 1 ? (size_t)n * q_heads * splits * (dim + 1) * 4 : 0;
-    a.chunk = ceil_div(ceil_div(span, splits), least) * least;
-    if (a.chunk < least) a.chunk = least;
+    a.chunk = ceil_div(ceil_div(span, splits), step) * step;
+    if (a.chunk < step) a.chunk = step;
     a.splits = ceil_div(span, a.chunk);
     if (a.splits < 1) a.splits = 1;
     a.ctas = units * a.splits;
@@ -670,8 +693,9 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     else
         e = P.dim == 128 ? launch_rows<128>(P, M, a, stream) : launch_rows<64>(P, M, a, stream);
     if (e != cudaSuccess || a.splits == 1) return e;
-    const int64_t ctas = ceil_div(P.n * P.q_heads, 4);
-    return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, 128, 0, stream, P) : launch(attn_join_kernel<64>, ctas, 128, 0, stream, P);
+    const int64_t ctas = P.n * P.q_heads;
+    return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, kJoinWarps * 32, 0, stream, P)
+                        : launch(attn_join_kernel<64>, ctas, kJoinWarps * 32, 0, stream, P);
 }
 
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad)
