@@ -3,22 +3,23 @@
 //   s_t = scale * q . k_t,   o = sum_t softmax(s)_t v_t,   k_t = 2^(sk - 127) * code, v_t likewise
 //
 // Every code is read once from HBM, which bounds the call (2 * dim bytes a token and head).  The codes are widened to f16, which
-// is exact, two at a time in registers, and multiplied there with binary32 sums (mma m16n8k16; fp8 operands of this instruction
-// would be widened one by one by the compiler, twice as many instructions):
+// is exact, two at a time in registers, and multiplied there with binary32 sums (mma m16n8k16), keys and values as the 16-row
+// operand, so that the query rows are the 8 columns: eight query heads that share a key head fill a product.
 //   q  is scaled by a power of two that brings the row's largest magnitude to [2^14, 2^15), so that f16 holds a bf16 value exactly
 //      but for elements below 2^-28 of the row's largest (to 2^-39 of it).
 //   The scales of the cache never touch the codes: a key block's scale multiplies the finished product, a value block's is
 //      folded into the softmax's weight, w_t = 2^(s_t + sv_t - R + 1) in f16.  The reference R (an integer, so that corrections of
 //      the sums are exact) is moved when a tile's largest s + sv is 14 above or 16 below it: f16 keeps 11 bits of what is above
-//      2^-14 and drops what is below 2^-25.  The softmax's own sum l has a reference of its own and unrounded weights.
+//      2^-14 and drops what is below 2^-25.  The softmax's own sum is l = sum of the unrounded w_t 2^(c0 - sv_t), a factor for each
+//      run of 16 tokens, c0 a constant of the warp; where a scale is more than 40 binades from c0 it takes exponentials of its own.
 //
-// A CTA of four warps takes up to 16 * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
+// A CTA of four warps takes up to 8 * NQ * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
 // of warps walk over the chunk's tiles of 32 tokens in turn; each group feeds itself through a ring of tiles that the
 // tensor copy engine fills (swizzled: the two access patterns below are then free of bank conflicts).  Within a tile,
 // a thread reads its operand words with 16-byte loads: the order of the dimensions within a product and of the tokens within a
-// sum is free, and is chosen so that a thread's share is contiguous: a word of four key codes is one step's operand.  The values'
-// operand wants two tokens of one dimension side by side: one byte permutation makes two such pairs of codes.  The weights go
-// from the first product's accumulators to the second product's operand without leaving the thread.
+// sum is free, and is chosen so that a thread's share is contiguous: a word of four key codes is half of one step's operand.  The
+// values' operand wants two tokens of one dimension side by side: one byte permutation makes two such pairs of codes.  The
+// weights turn from the first product's result layout to the second's operand with one 8 x 8 transposition for eight tokens.
 //
 // Partial results of the chunks go to the workspace as (normalised row, logarithm of its sum) and are joined in a fixed
 // order by a second kernel; with one chunk the row is written at once.
@@ -37,9 +38,8 @@ namespace {
 
 constexpr int kSMs = 148;
 constexpr int kWarps = 4;
-#ifndef MXN_DEC_CTAS
-#define MXN_DEC_CTAS 3
-#endif
+// CTAs an SM that the register allocation makes room for
+__host__ __device__ constexpr int decode_ctas(int dim, int nq) { return nq == 1 ? (dim == 128 ? 3 : 4) : dim == 128 || nq == 4 ? 2 : 3; }
 constexpr int kTile = 32;      // tokens of a tile
 constexpr int kPromptRows = 64;   // more query rows a sequence and key head than this: the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -61,6 +61,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+// transposes an 8 x 8 matrix of f16: row g, columns 2c, 2c + 1 in a thread's register
+__device__ __forceinline__ uint32_t turn8x8(uint32_t v)
+{
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
 }
 __device__ __forceinline__ uint2 lds_v2(uint32_t addr)
 {
@@ -88,23 +95,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 // below the largest so far (the output's sums must not overflow)
 constexpr float kTop = 1.0f, kUp = 14.0f, kDown = 16.0f, kDepth = 40.0f;
 
-template <int DIM, int RW, int HALVES, int STAGES>
+template <int DIM, int RW, int NQ, int STAGES>
 struct DecodeShape {
     static constexpr int kGroups = kWarps / RW;                  // warp groups that share out the tiles
     static constexpr int kTileBytes = kTile * DIM;               // codes of a tile, keys or values
     static constexpr int kRingBytes = kGroups * STAGES * 2 * kTileBytes;
-    static constexpr int kRows = 8 * HALVES * RW;
+    static constexpr int kRows = 8 * NQ * RW;
     static constexpr int kJoinBytes = kGroups * kRows * (DIM * 4 + 8);
     static constexpr int kSmem = (kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes) + 1024;
 };
 
-// HALVES: 1 where a warp has at most 8 rows (the lower half of the product's 16 stays empty), else 2
-template <int DIM, int RW, int HALVES, int STAGES>
-__global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
+// NQ: groups of eight query rows that a warp works on (they share the widened codes); RW: warps that share out the rows
+template <int DIM, int RW, int NQ, int STAGES>
+__global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
-    using Sh = DecodeShape<DIM, RW, HALVES, STAGES>;
-    constexpr int NT = DIM / 8;      // column tiles of the second product
+    using Sh = DecodeShape<DIM, RW, NQ, STAGES>;
+    constexpr int MT = DIM / 16;     // row tiles of the second product: 16 dimensions each
     constexpr int KS = DIM / 16;     // steps of the first
+    constexpr int QN = 2 * NQ;       // query rows whose softmax this thread looks after: 8 (x/2) + 2c + x%2
     constexpr int GROUPS = Sh::kGroups;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * GROUPS * STAGES];   // full, then empty
@@ -133,19 +141,27 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
-    // this thread's rows (g, and g + 8): query token, head, and the keys they see
-    bool row_live[HALVES];
-    int64_t tok[HALVES];
-    int head[HALVES], see_hi[HALVES], see_lo[HALVES];
+    // keys [see_lo, see_hi) of this thread's rows; the tile's rows that every row sees in full
+    const int row_base = row0 + rw * 8 * NQ;
+    int see_hi[QN], see_lo[QN];
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x) {
-        const int row = row0 + rw * 8 * HALVES + 8 * x + g;
-        row_live[x] = row < rows;
-        tok[x] = q0 + (row_live[x] ? row / G : 0);
-        head[x] = h * G + (row_live[x] ? row % G : 0);
-        const int pos = shift + (row_live[x] ? row / G : nq - 1);
-        see_hi[x] = P.causal ? min(pos + 1, len) : len;                     // keys [see_lo, see_hi)
+    for (int x = 0; x < QN; ++x) {
+        const int row = min(row_base + 8 * (x >> 1) + 2 * c + (x & 1), rows - 1);
+        const int pos = shift + row / G;
+        see_hi[x] = P.causal ? min(pos + 1, len) : len;
         see_lo[x] = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+    }
+    int all_hi = see_hi[0], all_lo = see_lo[0];
+#pragma unroll
+    for (int x = 1; x < QN; ++x) {
+        all_hi = min(all_hi, see_hi[x]);
+        all_lo = max(all_lo, see_lo[x]);
+    }
+    all_hi = min(all_hi, k1);
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        all_hi = min(all_hi, __shfl_xor_sync(0xFFFFFFFFu, all_hi, o));
+        all_lo = max(all_lo, __shfl_xor_sync(0xFFFFFFFFu, all_lo, o));
     }
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -219,15 +235,18 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
     };
     uint32_t sc_next = scale_at(0, pages[0]);
 
-    // q: the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on; the power of two goes to the row's factor
-    uint32_t qa[KS][2][HALVES];
-    float row_factor[HALVES];
+    // q: row g of each eight, the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on; the power of two goes to the
+    // row's factor, which the softmax needs in the threads of its columns
+    uint32_t qb[KS][NQ][2];
+    float row_factor[QN];
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x) {
+    for (int x = 0; x < NQ; ++x) {
+        const int row = row_base + 8 * x + g;
+        const bool live = row < rows;
         uint4 w[DIM / 32];
-        const uint16_t* qp = P.q + tok[x] * P.q_stride + (int64_t)head[x] * DIM + c * (DIM / 4);
+        const uint16_t* qp = P.q + (int64_t)(q0 + (live ? row / G : 0)) * P.q_stride + (int64_t)(h * G + (live ? row % G : 0)) * DIM + c * (DIM / 4);
 #pragma unroll
-        for (int i = 0; i < DIM / 32; ++i) w[i] = row_live[x] ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < DIM / 32; ++i) w[i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
         const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
         uint32_t m = 0;
 #pragma unroll
@@ -235,27 +254,31 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
         const uint32_t E = __float_as_uint(quad_max(hmax_abs_to_f32(m))) >> 23;
         const uint32_t Ec = min(max(E, 15u), 254u);
         const float up = __uint_as_float((268u - Ec) << 23);                                // 2^(14 - (E - 127))
-        row_factor[x] = P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23);               // ... and its inverse
+        const float factor = P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23);          // ... and its inverse
+        row_factor[2 * x] = __shfl_sync(0xFFFFFFFFu, factor, 8 * c);
+        row_factor[2 * x + 1] = __shfl_sync(0xFFFFFFFFu, factor, 8 * c + 4);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            qa[k][0][x] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
-            qa[k][1][x] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
+            qb[k][x][0] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
+            qb[k][x][1] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
         }
     }
 
-    float acc[NT][4];
+    float acc[MT][NQ][4];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < MT; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][x][e] = 0.0f;
     const float kNone = -INFINITY;
-    float m_ref[HALVES], l[HALVES];            // softmax: reference (an integer) and this thread's part of the sum
-    float r_ref[HALVES], r_top[HALVES];        // second product: reference (an integer) and the largest so far
+    float ref[QN], top_all[QN], l[QN];   // reference (an integer), the largest so far, this thread's part of the sum
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x) {
-        m_ref[x] = r_ref[x] = r_top[x] = kNone;
+    for (int x = 0; x < QN; ++x) {
+        ref[x] = top_all[x] = kNone;
         l[x] = 0.0f;
     }
+    float c0 = 0.0f;
     bool ok = true;
 
     for (int i = 0; i < mine; ++i) {
@@ -264,8 +287,9 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
         const int t0 = tile_at(i);
         const uint32_t sc = sc_next;
         sc_next = scale_at(i + 1, pages[1]);
-        const float kf0 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)), kf1 = e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16));
-        const float sv0 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, sv1 = (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f;
+        const float kf[2] = {e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)), e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16))};
+        const float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
+        if (i == 0) c0 = fminf(fmaxf(fmaxf(sv[0], sv[1]), -60.0f), 60.0f);
         // tokens of the tile that exist and whose page could be read
         const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && pages[0] >= 0);
 
@@ -275,100 +299,118 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
         }
         const uint32_t kt = ring + (uint32_t)st * 2 * Sh::kTileBytes, vt = kt + Sh::kTileBytes;
 
-        // ---- s = q . k: token 8j + g is column g of column tile j ----
-        float s[HALVES][8];
+        // ---- s = k . q: this thread gets tokens 16t + g and 16t + 8 + g for its query rows ----
+        float s[2][NQ][4];   // [16 tokens][eight rows]: (g, 2c), (g, 2c + 1), (g + 8, 2c), (g + 8, 2c + 1)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = 8 * j + g;
-            uint32_t w[KS];
-            if constexpr (DIM == 128) {
-                const uint4 a = lds_v4(kt + r * 128 + (((2 * c) ^ g) << 4)), d = lds_v4(kt + r * 128 + (((2 * c + 1) ^ g) << 4));
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-                w[4] = d.x; w[5] = d.y; w[6] = d.z; w[7] = d.w;
-            } else {
-                const uint4 a = lds_v4(kt + r * 64 + ((c ^ ((g >> 1) & 3)) << 4));
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        for (int t = 0; t < 2; ++t) {
+            uint32_t w[2][KS];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int r = 16 * t + 8 * x + g;
+                if constexpr (DIM == 128) {
+                    const uint4 a = lds_v4(kt + r * 128 + (((2 * c) ^ g) << 4)), d = lds_v4(kt + r * 128 + (((2 * c + 1) ^ g) << 4));
+                    w[x][0] = a.x; w[x][1] = a.y; w[x][2] = a.z; w[x][3] = a.w;
+                    w[x][4] = d.x; w[x][5] = d.y; w[x][6] = d.z; w[x][7] = d.w;
+                } else {
+                    const uint4 a = lds_v4(kt + r * 64 + ((c ^ ((g >> 1) & 3)) << 4));
+                    w[x][0] = a.x; w[x][1] = a.y; w[x][2] = a.z; w[x][3] = a.w;
+                }
             }
-            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][x][e] = 0.0f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                uint32_t b0, b1;
-                widen(w[k], b0, b1);
-                mma_f16(d, qa[k][0][0], HALVES == 2 ? qa[k][0][HALVES - 1] : 0u, qa[k][1][0], HALVES == 2 ? qa[k][1][HALVES - 1] : 0u, b0, b1);
-            }
+                uint32_t a0, a1, a2, a3;
+                widen(w[0][k], a0, a2);
+                widen(w[1][k], a1, a3);
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x) {
-                const float f = (j < 2 ? kf0 : kf1) * row_factor[x];
-                s[x][2 * j] = d[2 * x] * f;
-                s[x][2 * j + 1] = d[2 * x + 1] * f;
+                for (int x = 0; x < NQ; ++x) mma_f16(s[t][x], a0, a1, a2, a3, qb[k][x][0], qb[k][x][1]);
             }
         }
-        // ---- what the rows may not see ----
-        bool all = there == 0xFFFFFFFFu;
+        // ---- s + sv, and what the rows may not see ----
+        float f[2][QN];
 #pragma unroll
-        for (int x = 0; x < HALVES; ++x) all = all && t0 >= see_lo[x] && t0 + kTile <= see_hi[x];
-        if (!__all_sync(0xFFFFFFFFu, all)) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x)
+            for (int x = 0; x < QN; ++x) {
+                f[t][x] = kf[t] * row_factor[x];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int t = 8 * (e >> 1) + 2 * c + (e & 1);
-                    if (!((there >> t) & 1u) || t0 + t < see_lo[x] || t0 + t >= see_hi[x]) s[x][e] = kNone;
+                for (int e = 0; e < 2; ++e) s[t][x >> 1][2 * e + (x & 1)] = fmaf(s[t][x >> 1][2 * e + (x & 1)], f[t][x], sv[t]);
+            }
+        if (there != 0xFFFFFFFFu || t0 < all_lo || t0 + kTile > all_hi) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int at = 16 * t + 8 * e + g, place = t0 + at;
+#pragma unroll
+                    for (int x = 0; x < QN; ++x)
+                        if (!((there >> at) & 1u) || place < see_lo[x] || place >= see_hi[x]) s[t][x >> 1][2 * e + (x & 1)] = kNone;
                 }
         }
-        // ---- references ----
-        float r_new[HALVES];
-        bool moved = false;
+        // ---- reference: moved where a weight would leave the window ----
+        bool out = false;
 #pragma unroll
-        for (int x = 0; x < HALVES; ++x) {
-            const float top0 = fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3])), top1 = fmaxf(fmaxf(s[x][4], s[x][5]), fmaxf(s[x][6], s[x][7]));
-            const float top = quad_max(fmaxf(top0, top1)), utop = quad_max(fmaxf(top0 + sv0, top1 + sv1));
-            if (top > m_ref[x]) {
-                const float n = ceilf(top);
-                l[x] *= ex2(m_ref[x] - n);
-                m_ref[x] = n;
-            }
-            r_new[x] = r_ref[x];
-            if (utop > r_ref[x] + kUp || (r_ref[x] == kNone && utop > kNone)) r_new[x] = ceilf(utop);
-            else if (utop < r_ref[x] - kDown && utop > kNone) r_new[x] = fmaxf(ceilf(utop), r_top[x] - kDepth);
-            r_top[x] = fmaxf(r_top[x], r_new[x]);
-            moved = moved || r_new[x] != r_ref[x];
+        for (int x = 0; x < QN; ++x) {
+            const float m = fmaxf(fmaxf(s[0][x >> 1][x & 1], s[0][x >> 1][2 + (x & 1)]), fmaxf(s[1][x >> 1][x & 1], s[1][x >> 1][2 + (x & 1)]));
+            // of the eight threads that share the row: one above, or none but some token in reach of it
+            const uint32_t mates = 0x11111111u << c;
+            const bool none = (__ballot_sync(0xFFFFFFFFu, m >= ref[x] - kDown) & mates) == 0u;
+            out = out || (m > ref[x] + kUp) || (ref[x] == kNone && m > kNone) || (none && m > kNone && ref[x] > top_all[x] - kDepth);
         }
-        if (__any_sync(0xFFFFFFFFu, moved)) {
+        if (__any_sync(0xFFFFFFFFu, out)) {
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x) {
-                const float alpha = r_ref[x] == kNone ? 0.0f : ex2(r_ref[x] - r_new[x]);
-                r_ref[x] = r_new[x];
+            for (int x = 0; x < QN; ++x) {
+                float m = fmaxf(fmaxf(s[0][x >> 1][x & 1], s[0][x >> 1][2 + (x & 1)]), fmaxf(s[1][x >> 1][x & 1], s[1][x >> 1][2 + (x & 1)]));
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    acc[j][2 * x] *= alpha;
-                    acc[j][2 * x + 1] *= alpha;
+                for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                float next = ref[x];
+                if (m > ref[x] + kUp || (ref[x] == kNone && m > kNone)) next = ceilf(m);
+                else if (m < ref[x] - kDown && m > kNone) next = fmaxf(ceilf(m), top_all[x] - kDepth);
+                top_all[x] = fmaxf(top_all[x], next);
+                const float alpha = ref[x] == kNone ? 0.0f : ex2(ref[x] - next);
+                ref[x] = next;
+                l[x] *= alpha;
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    acc[j][x >> 1][x & 1] *= alpha;
+                    acc[j][x >> 1][2 + (x & 1)] *= alpha;
                 }
             }
         }
-        // ---- weights ----
-        uint32_t pa[2][2][HALVES];   // [16 tokens][first, second 8 of them][row]
+        // ---- weights, turned to the second product's operand; the softmax's sum ----
+        const bool wide = fabsf(sv[0] - c0) > 40.0f || fabsf(sv[1] - c0) > 40.0f;
+        uint32_t pb[2][NQ][2];
 #pragma unroll
-        for (int x = 0; x < HALVES; ++x) {
-            const float ms = m_ref[x] == kNone ? 0.0f : m_ref[x], rs = r_ref[x] == kNone ? 0.0f : r_ref[x];
-            const float b0 = sv0 + kTop - rs, b1 = sv1 + kTop - rs;
-            float w[8];
+        for (int t = 0; t < 2; ++t) {
+            const float back = ex2(c0 - sv[t]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                l[x] += ex2(s[x][e] - ms);
-                w[e] = ex2(s[x][e] + (e < 4 ? b0 : b1));
+            for (int x = 0; x < NQ; ++x) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float r = ref[2 * x + (e & 1)], by = r == kNone ? 0.0f : kTop - r;
+                    w[e] = ex2(s[t][x][e] + by);
+                    if (wide && r > kNone) l[2 * x + (e & 1)] += ex2(s[t][x][e] + (by + (c0 - sv[t])));
+                }
+                if (!wide) {
+                    l[2 * x] = fmaf(w[0] + w[2], back, l[2 * x]);
+                    l[2 * x + 1] = fmaf(w[1] + w[3], back, l[2 * x + 1]);
+                }
+                pb[t][x][0] = turn8x8(pack_f16(w[0], w[1]));
+                pb[t][x][1] = turn8x8(pack_f16(w[2], w[3]));
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) pa[e >> 1][e & 1][x] = pack_f16(w[2 * e], w[2 * e + 1]);
         }
-        // ---- o += w v: tokens 2c, 2c+1, 8+2c, 9+2c (then 16 more) of DIM/8 dimensions from g * DIM/8 on ----
+        // ---- o += v w: tokens 2c, 2c+1, 8+2c, 9+2c (then 16 more) of DIM/8 dimensions from g * DIM/8 on ----
         constexpr int VW = DIM / 32;   // words a thread reads of each token
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int t = 0; t < 2; ++t) {
             uint32_t v[4][VW];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int r = 16 * half + 8 * (x >> 1) + 2 * c + (x & 1);
+                const int r = 16 * t + 8 * (x >> 1) + 2 * c + (x & 1);
                 if constexpr (DIM == 128) {
                     const uint4 a = lds_v4(vt + r * 128 + ((g ^ (r & 7)) << 4));
                     v[x][0] = a.x; v[x][1] = a.y; v[x][2] = a.z; v[x][3] = a.w;
@@ -380,24 +422,25 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
             if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token, a NaN among it, must not meet the zero weights
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int t = 16 * half + 8 * (x >> 1) + 2 * c + (x & 1);
-                    if (!((there >> t) & 1u))
+                    const int at = 16 * t + 8 * (x >> 1) + 2 * c + (x & 1);
+                    if (!((there >> at) & 1u))
 #pragma unroll
                         for (int y = 0; y < VW; ++y) v[x][y] = 0u;
                 }
             }
 #pragma unroll
             for (int y = 0; y < VW; ++y) {
-                uint32_t b[2][4];   // [8 tokens][dimension]: f16 pairs of two tokens
+                uint32_t a[2][4];   // [8 tokens][dimension]: f16 pairs of two tokens
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x5140), b[x][0], b[x][1]);
-                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x7362), b[x][2], b[x][3]);
+                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x5140), a[x][0], a[x][1]);
+                    widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x7362), a[x][2], a[x][3]);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    mma_f16(acc[4 * y + e], pa[half][0][0], HALVES == 2 ? pa[half][0][HALVES - 1] : 0u, pa[half][1][0],
-                            HALVES == 2 ? pa[half][1][HALVES - 1] : 0u, b[0][e], b[1][e]);
+                for (int e = 0; e < 2; ++e)   // row g of the product: dimension 4y + 2e of this thread's, row g + 8: the next
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x)
+                        mma_f16(acc[2 * y + e][x], a[0][2 * e], a[0][2 * e + 1], a[1][2 * e], a[1][2 * e + 1], pb[t][x][0], pb[t][x][1]);
             }
         }
         // ---- hand the stage back ----
@@ -431,92 +474,107 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 128 ? MXN_DEC_CTAS : 4) at
     if (__any_sync(0xFFFFFFFFu, bad_page) && lane == 0) atomicAdd(&g_attn_bad, 1u);
 
     // ---- join the groups of warps ----
-    constexpr int OUT = DIM / 4;   // dimensions a thread ends with: those from c * OUT on, of each of its rows
+    // row x of this thread: sum l 2^at, output acc 2^c0 2^at with at = ref - kTop - c0; dimensions g * DIM/8 ... + DIM/8 - 1
+    constexpr int OUT = DIM / 8;
     float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
     float* const stat = sm + GROUPS * Sh::kRows * DIM;
-    float o[HALVES][OUT];
+    float at[QN];
+    const float unit = ex2(c0);
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x) {
-        l[x] = quad_sum(l[x]);
-        const float ms = m_ref[x] == kNone ? 0.0f : m_ref[x], rs = r_ref[x] == kNone ? 0.0f : r_ref[x];
-        const float back = ex2(fminf(fmaxf(rs - kTop - ms, -126.0f), 127.0f));
+    for (int x = 0; x < QN; ++x) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            o[x][j] = acc[j][2 * x] * back;
-            o[x][NT + j] = acc[j][2 * x + 1] * back;
+        for (int o = 4; o < 32; o <<= 1) l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], o);
+        at[x] = ref[x] - kTop - c0;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            acc[j][x >> 1][x & 1] *= unit;
+            acc[j][x >> 1][2 + (x & 1)] *= unit;
         }
     }
     if (GROUPS > 1) {
         __syncthreads();   // every copy has landed and been read
         if (group != 0) {
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x) {
-                const int at = group * Sh::kRows + (rw * HALVES + x) * 8 + g;
-                float* const p = sm + (int64_t)at * DIM + c * OUT;
+            for (int x = 0; x < QN; ++x) {
+                const int place = group * Sh::kRows + rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
+                float* const p = sm + (int64_t)place * DIM + g * OUT;
 #pragma unroll
-                for (int y = 0; y < OUT / 4; ++y) *reinterpret_cast<float4*>(p + 4 * y) = make_float4(o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]);
-                if (c == 0) {
-                    stat[2 * at] = m_ref[x];
-                    stat[2 * at + 1] = l[x];
+                for (int y = 0; y < MT / 2; ++y)
+                    *reinterpret_cast<float4*>(p + 4 * y) = make_float4(acc[2 * y][x >> 1][x & 1], acc[2 * y][x >> 1][2 + (x & 1)],
+                                                                        acc[2 * y + 1][x >> 1][x & 1], acc[2 * y + 1][x >> 1][2 + (x & 1)]);
+                if (g == 0) {
+                    stat[2 * place] = at[x];
+                    stat[2 * place + 1] = l[x];
                 }
             }
         }
         __syncthreads();
         if (group != 0) return;
 #pragma unroll
-        for (int x = 0; x < HALVES; ++x) {
-            const int mine_at = (rw * HALVES + x) * 8 + g;
-            float m_all = m_ref[x];
+        for (int x = 0; x < QN; ++x) {
+            const int own_place = rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
+            float top = at[x];
 #pragma unroll
-            for (int k = 1; k < GROUPS; ++k) m_all = fmaxf(m_all, stat[2 * (k * Sh::kRows + mine_at)]);
-            const float own = m_ref[x] == kNone ? 0.0f : ex2(m_ref[x] - m_all);
+            for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, stat[2 * (k * Sh::kRows + own_place)]);
+            const float own = at[x] == kNone ? 0.0f : ex2(at[x] - top);
             l[x] *= own;
 #pragma unroll
-            for (int y = 0; y < OUT; ++y) o[x][y] *= own;
+            for (int j = 0; j < MT; ++j) {
+                acc[j][x >> 1][x & 1] *= own;
+                acc[j][x >> 1][2 + (x & 1)] *= own;
+            }
 #pragma unroll
             for (int k = 1; k < GROUPS; ++k) {
-                const int at = k * Sh::kRows + mine_at;
-                const float mk = stat[2 * at];
-                if (mk == kNone) continue;
-                const float f = ex2(mk - m_all);
-                l[x] = fmaf(stat[2 * at + 1], f, l[x]);
-                const float* const p = sm + (int64_t)at * DIM + c * OUT;
+                const int place = k * Sh::kRows + own_place;
+                const float there = stat[2 * place];
+                if (there == kNone) continue;
+                const float by = ex2(there - top);
+                l[x] = fmaf(stat[2 * place + 1], by, l[x]);
+                const float* const p = sm + (int64_t)place * DIM + g * OUT;
 #pragma unroll
-                for (int y = 0; y < OUT / 4; ++y) {
-                    const float4 a = *reinterpret_cast<const float4*>(p + 4 * y);
-                    o[x][4 * y] = fmaf(a.x, f, o[x][4 * y]);
-                    o[x][4 * y + 1] = fmaf(a.y, f, o[x][4 * y + 1]);
-                    o[x][4 * y + 2] = fmaf(a.z, f, o[x][4 * y + 2]);
-                    o[x][4 * y + 3] = fmaf(a.w, f, o[x][4 * y + 3]);
+                for (int y = 0; y < MT / 2; ++y) {
+                    const float4 v = *reinterpret_cast<const float4*>(p + 4 * y);
+                    acc[2 * y][x >> 1][x & 1] = fmaf(v.x, by, acc[2 * y][x >> 1][x & 1]);
+                    acc[2 * y][x >> 1][2 + (x & 1)] = fmaf(v.y, by, acc[2 * y][x >> 1][2 + (x & 1)]);
+                    acc[2 * y + 1][x >> 1][x & 1] = fmaf(v.z, by, acc[2 * y + 1][x >> 1][x & 1]);
+                    acc[2 * y + 1][x >> 1][2 + (x & 1)] = fmaf(v.w, by, acc[2 * y + 1][x >> 1][2 + (x & 1)]);
                 }
             }
-            m_ref[x] = m_all;
+            at[x] = top;
         }
     }
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x) {
-        if (!row_live[x]) continue;
+    for (int x = 0; x < QN; ++x) {
+        const int row = row_base + 8 * (x >> 1) + 2 * c + (x & 1);
+        if (row >= rows) continue;
+        const int64_t tok = q0 + row / G;
+        const int head = h * G + row % G;
         const float inv = l[x] > 0.0f ? __fdiv_rn(1.0f, l[x]) : 0.0f;       // a row that sees nothing: zeros
-        const float lse2 = l[x] > 0.0f ? m_ref[x] + log2f(l[x]) : kNone;
-        const int64_t out_row = tok[x] * P.q_heads + head[x];
+        const float lse2 = l[x] > 0.0f ? at[x] + log2f(l[x]) : kNone;
+        const int64_t out_row = tok * P.q_heads + head;
+        float o[OUT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            o[2 * j] = acc[j][x >> 1][x & 1] * inv;
+            o[2 * j + 1] = acc[j][x >> 1][2 + (x & 1)] * inv;
+        }
         if (P.splits == 1) {
-            uint16_t* const y = P.out + tok[x] * P.out_stride + (int64_t)head[x] * DIM + c * OUT;
+            uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + g * OUT;
 #pragma unroll
             for (int e = 0; e < OUT / 8; ++e) {
                 uint32_t r[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = pack_bf16(o[x][8 * e + 2 * k] * inv, o[x][8 * e + 2 * k + 1] * inv);
+                for (int k = 0; k < 4; ++k) r[k] = pack_bf16(o[8 * e + 2 * k], o[8 * e + 2 * k + 1]);
                 st_v4(y + 8 * e, r);
             }
-            if (P.lse != nullptr && c == 0) P.lse[out_row] = lse2 * kLn2;
+            if (P.lse != nullptr && g == 0) P.lse[out_row] = lse2 * kLn2;
         } else {
-            const int64_t at = out_row * P.splits + split;
-            if (c == 0) P.part_lse[at] = lse2;
+            const int64_t to = out_row * P.splits + split;
+            if (g == 0) P.part_lse[to] = lse2;
             if (l[x] > 0.0f) {
-                float* const y = P.part_out + at * DIM + c * OUT;
+                float* const y = P.part_out + to * DIM + g * OUT;
 #pragma unroll
-                for (int e = 0; e < OUT / 4; ++e)
-                    *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[x][4 * e] * inv, o[x][4 * e + 1] * inv, o[x][4 * e + 2] * inv, o[x][4 * e + 3] * inv);
+                for (int e = 0; e < OUT / 4; ++e) *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             }
         }
     }
@@ -623,17 +681,20 @@ bool make_map(CUtensorMap* map, const uint8_t* codes, const AttnParams& P, int b
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DIM, int RW, int HALVES, int STAGES>
+template <int DIM, int RW, int NQ, int STAGES>
 cudaError_t launch_decode(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
 {
-    return launch(attn_decode_kernel<DIM, RW, HALVES, STAGES>, ctas, kWarps * 32, DecodeShape<DIM, RW, HALVES, STAGES>::kSmem, stream, P, M);
+    return launch(attn_decode_kernel<DIM, RW, NQ, STAGES>, ctas, kWarps * 32, DecodeShape<DIM, RW, NQ, STAGES>::kSmem, stream, P, M);
 }
-template <int DIM>
 cudaError_t launch_rows(const AttnParams& P, const AttnMaps& M, const AttnPlan& a, cudaStream_t stream)
 {
-    if (a.row_warps == 1)
-        return a.halves == 1 ? launch_decode<DIM, 1, 1, 2>(P, M, a.ctas, stream) : launch_decode<DIM, 1, 2, 2>(P, M, a.ctas, stream);
-    return a.row_warps == 2 ? launch_decode<DIM, 2, 2, 3>(P, M, a.ctas, stream) : launch_decode<DIM, 4, 2, 4>(P, M, a.ctas, stream);
+    if (P.dim == 128)
+        return a.row_eights == 1 ? launch_decode<128, 1, 1, 2>(P, M, a.ctas, stream)
+             : a.row_warps == 1  ? launch_decode<128, 1, 2, 2>(P, M, a.ctas, stream)
+             : a.row_warps == 2  ? launch_decode<128, 2, 2, 3>(P, M, a.ctas, stream) : launch_decode<128, 4, 2, 4>(P, M, a.ctas, stream);
+    return a.row_eights == 1 ? launch_decode<64, 1, 1, 3>(P, M, a.ctas, stream)
+         : a.row_eights == 2 ? launch_decode<64, 1, 2, 3>(P, M, a.ctas, stream)
+         : a.row_warps == 1  ? launch_decode<64, 1, 4, 3>(P, M, a.ctas, stream) : launch_decode<64, 2, 4, 3>(P, M, a.ctas, stream);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -647,16 +708,17 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     if (max_q > n) max_q = n;
     const int64_t rows = max_q * (q_heads / kv_heads);
     a.prompt = rows > kPromptRows;
-    a.halves = rows <= 8 ? 1 : 2;
-    a.row_warps = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t tile_rows = a.prompt ? 256 : 8 * a.halves * a.row_warps;
+    // a warp holds the output of up to 16 rows of 128 or 32 of 64; more rows are shared out among the CTA's warps
+    a.row_eights = rows <= 8 ? 1 : rows <= 16 || dim == 128 ? 2 : 4;
+    a.row_warps = (int)(rows <= 8 * a.row_eights ? 1 : rows <= 16 * a.row_eights ? 2 : 4);
+    const int64_t tile_rows = a.prompt ? 256 : 8 * a.row_eights * a.row_warps;
     a.row_tiles = ceil_div(rows, tile_rows);
     const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile;
     const int64_t step = a.prompt ? 128 : kTile * (kWarps / a.row_warps);   // keys that a CTA works on at a time
     // Chunks: as many as the CTAs that are resident at a time leave room for; four rounds of them where sequences may differ in
     // length (64 sequences of 2048 ... 8192 keys: one round 152 us, four 135 us).  A chunk is at least eight steps long, so that a
     // CTA's start and the join are worth it, unless most SMs would be idle.
-    const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : dim == 128 ? 3 : 4);
+    const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : decode_ctas(dim, a.row_eights));
     int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
@@ -691,7 +753,7 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     if (a.prompt)
         e = launch_prompt(P, M, a.ctas, stream);
     else
-        e = P.dim == 128 ? launch_rows<128>(P, M, a, stream) : launch_rows<64>(P, M, a, stream);
+        e = launch_rows(P, M, a, stream);
     if (e != cudaSuccess || a.splits == 1) return e;
     const int64_t ctas = P.n * P.q_heads;
     return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, kJoinWarps * 32, 0, stream, P)

@@ -132,7 +132,7 @@ struct AttnParams {
 };
 struct AttnPlan {
     int64_t chunk, splits, row_tiles, ctas;
-    int row_warps, halves;      // warps that share out the query rows of a CTA; halves of the product's 16 rows in use
+    int row_warps, row_eights;  // warps that share out the query rows of a CTA; groups of eight rows that a warp holds
     bool prompt;                // many query rows: the tcgen05 kernel
     size_t workspace;
 };
