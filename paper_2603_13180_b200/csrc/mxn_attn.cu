@@ -181,38 +181,35 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // the group's tiles are group, group + GROUPS, ...; tile i of them goes to stage i % STAGES
     const int mine = tiles > group ? (tiles - group + GROUPS - 1) / GROUPS : 0;
     const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
-    // a tile has two runs of 16 tokens, each within one page; lanes 0-15 look after the first, 16-31 after the second.
-    // page_at(i): the page of this lane's run of tile i; -1 behind the last token or where the table is out of range
+    // A tile has two runs of 16 tokens, each within one page; lanes 0-15 look after the first, 16-31 after the second.
+    // page_at(i): the table's entry for this lane's run of tile i, -1 behind the last token.  It is looked at a tile later at the
+    // earliest, so that nothing waits for it.
     const int run = lane >> 4;
     bool bad_page = false;
     auto tile_at = [&](int i) { return k0 + (group + i * GROUPS) * kTile; };
     auto page_at = [&](int i) -> int {
         const int t = tile_at(i) + 16 * run;
-        if (i >= mine || t >= k1) return -1;
-        const int pg = __ldg(table + (t >> P.page_shift));
-        const bool good = pg >= 0 && pg < P.num_pages;
-        bad_page |= !good;
-        return good ? pg : -1;
+        return i < mine && t < k1 ? __ldg(table + (t >> P.page_shift)) : -1;
     };
+    auto in_pool = [&](int pg) { return (uint32_t)pg < (uint32_t)P.num_pages; };
     const bool two_boxes = P.page < kTile;   // a page of 16 tokens takes two boxes to a tile
-    auto request = [&](int i, int pg) {      // by a whole warp, with page_at(i) in hand
-        const int pg1 = __shfl_sync(0xFFFFFFFFu, pg, 16);
+    const uint32_t box_bytes = two_boxes ? Sh::kTileBytes / 2 : Sh::kTileBytes;
+    auto request = [&](int i, int st, int pg) {   // by a whole warp, with page_at(i) in hand
+        const int pg1 = two_boxes ? __shfl_sync(0xFFFFFFFFu, pg, 16) : -1;
         if (!leader) return;
-        const int t0 = tile_at(i);
-        const uint32_t dst = ring + (uint32_t)(i % STAGES) * 2 * Sh::kTileBytes, bar = full + 8 * (i % STAGES);
-        const uint32_t box_bytes = two_boxes ? Sh::kTileBytes / 2 : Sh::kTileBytes;
-        const uint32_t bytes = (uint32_t)((pg >= 0) + (two_boxes && pg1 >= 0)) * 2 * box_bytes;
+        const uint32_t dst = ring + (uint32_t)st * 2 * Sh::kTileBytes, bar = full + 8 * st;
+        const uint32_t bytes = (uint32_t)(in_pool(pg) + in_pool(pg1)) * 2 * box_bytes;
         if (bytes == 0) {
             mbar_arrive(bar);
             return;
         }
         mbar_expect_tx(bar, bytes);
-        const int y = t0 & (P.page - 1);
-        if (pg >= 0) {
+        const int y = tile_at(i) & (P.page - 1);
+        if (in_pool(pg)) {
             tma_load_codes(dst, &M.k, y, pg * P.kv_heads + h, bar);
             tma_load_codes(dst + Sh::kTileBytes, &M.v, y, pg * P.kv_heads + h, bar);
         }
-        if (two_boxes && pg1 >= 0) {
+        if (in_pool(pg1)) {
             tma_load_codes(dst + box_bytes, &M.k, 0, pg1 * P.kv_heads + h, bar);
             tma_load_codes(dst + Sh::kTileBytes + box_bytes, &M.v, 0, pg1 * P.kv_heads + h, bar);
         }
@@ -224,14 +221,15 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     if (rw == 0) {
 #pragma unroll
         for (int d = 0; d < STAGES; ++d)
-            if (d < mine) request(d, pages[d]);
+            if (d < mine) request(d, d, pages[d]);
     }
     // scales, one tile ahead: lanes 0 and 16 hold the key scales of the two runs, lanes 1 and 17 the value scales
+    const uint8_t* const scale_base = lane & 1 ? P.v_scales : P.k_scales;
+    const int per_page = P.page_shift - P.block_shift;
     auto scale_at = [&](int i, int pg) -> uint32_t {
-        if ((lane & 15) >= 2 || pg < 0) return 0;
-        const uint8_t* s = lane & 1 ? P.v_scales : P.k_scales;
-        return __ldg(s + ((((int64_t)pg * P.kv_heads + h) << (P.page_shift - P.block_shift)) +
-                          (((tile_at(i) + 16 * run) & (P.page - 1)) >> P.block_shift)));
+        if ((lane & 15) >= 2 || !in_pool(pg)) return 0;
+        const int64_t tile = (int64_t)pg * P.kv_heads + h;
+        return __ldg(scale_base + (tile << per_page) + (((tile_at(i) + 16 * run) & (P.page - 1)) >> P.block_shift));
     };
     uint32_t sc_next = scale_at(0, pages[0]);
 
@@ -281,9 +279,9 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     float c0 = 0.0f;
     bool ok = true;
 
+    int st = 0;
+    uint32_t ph = 0;
     for (int i = 0; i < mine; ++i) {
-        const int st = i % STAGES;
-        const uint32_t ph = (uint32_t)(i / STAGES) & 1u;
         const int t0 = tile_at(i);
         const uint32_t sc = sc_next;
         sc_next = scale_at(i + 1, pages[1]);
@@ -291,7 +289,9 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
         if (i == 0) c0 = fminf(fmaxf(fmaxf(sv[0], sv[1]), -60.0f), 60.0f);
         // tokens of the tile that exist and whose page could be read
-        const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && pages[0] >= 0);
+        const bool readable = in_pool(pages[0]);
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && readable);
+        bad_page |= t0 + lane < k1 && !readable;
 
         if (!mbar_wait_bounded(full + 8 * st, ph)) {
             ok = false;
@@ -382,23 +382,27 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         }
         // ---- weights, turned to the second product's operand; the softmax's sum ----
         const bool wide = fabsf(sv[0] - c0) > 40.0f || fabsf(sv[1] - c0) > 40.0f;
+        float by[QN];
+#pragma unroll
+        for (int x = 0; x < QN; ++x) by[x] = ref[x] == kNone ? 0.0f : kTop - ref[x];
+        if (wide) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int x = 0; x < QN; ++x)
+                    if (ref[x] > kNone) l[x] += ex2(s[t][x >> 1][x & 1] + (by[x] + (c0 - sv[t]))) + ex2(s[t][x >> 1][2 + (x & 1)] + (by[x] + (c0 - sv[t])));
+        }
         uint32_t pb[2][NQ][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float back = ex2(c0 - sv[t]);
+            const float back = wide ? 0.0f : ex2(c0 - sv[t]);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
                 float w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float r = ref[2 * x + (e & 1)], by = r == kNone ? 0.0f : kTop - r;
-                    w[e] = ex2(s[t][x][e] + by);
-                    if (wide && r > kNone) l[2 * x + (e & 1)] += ex2(s[t][x][e] + (by + (c0 - sv[t])));
-                }
-                if (!wide) {
-                    l[2 * x] = fmaf(w[0] + w[2], back, l[2 * x]);
-                    l[2 * x + 1] = fmaf(w[1] + w[3], back, l[2 * x + 1]);
-                }
+                for (int e = 0; e < 4; ++e) w[e] = ex2(s[t][x][e] + by[2 * x + (e & 1)]);
+                l[2 * x] = fmaf(w[0] + w[2], back, l[2 * x]);
+                l[2 * x + 1] = fmaf(w[1] + w[3], back, l[2 * x + 1]);
                 pb[t][x][0] = turn8x8(pack_f16(w[0], w[1]));
                 pb[t][x][1] = turn8x8(pack_f16(w[2], w[3]));
             }
@@ -452,10 +456,14 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                     ok = false;
                     break;
                 }
-                request(i + STAGES, pages[STAGES]);
+                request(i + STAGES, st, pages[STAGES]);
             }
         } else if (i + STAGES < mine) {
-            request(i + STAGES, pages[STAGES]);
+            request(i + STAGES, st, pages[STAGES]);
+        }
+        if (++st == STAGES) {
+            st = 0;
+            ph ^= 1u;
         }
 #pragma unroll
         for (int d = 0; d < STAGES + 1; ++d) pages[d] = pages[d + 1];
