@@ -763,6 +763,9 @@ mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens
     P.q_heads = q_heads;
     P.kv_heads = kv_heads;
     P.group = q_heads / kv_heads;
+    // with s = ceil(log2 group) and mul = ceil(2^(31 + s) / group) the product's error stays below 2^(31 + s) / group for rows < 2^31
+    P.group_shift = P.group > 1 ? (uint32_t)log2_of(P.group) - 1 : 0;
+    P.group_mul = P.group > 1 ? (uint32_t)(((1ull << (32 + P.group_shift)) + P.group - 1) / P.group) : 0;
     P.dim = head_dim;
     P.page = page_size;
     P.page_shift = log2_of(page_size);

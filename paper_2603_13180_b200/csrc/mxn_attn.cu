@@ -101,7 +101,7 @@ struct DecodeShape {
     static constexpr int kTileBytes = kTile * DIM;               // codes of a tile, keys or values
     static constexpr int kRingBytes = kGroups * STAGES * 2 * kTileBytes;
     static constexpr int kRows = 8 * NQ * RW;
-    static constexpr int kJoinBytes = kGroups * kRows * (DIM * 4 + 8);
+    static constexpr int kJoinBytes = kGroups * kRows * ((DIM + 4) * 4 + 8);
     static constexpr int kSmem = (kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes) + 1024;
 };
 
@@ -120,13 +120,13 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int group = warp / RW, rw = warp % RW;
-    int64_t b = blockIdx.x;
-    const int split = (int)(b % P.splits);
-    b /= P.splits;
-    const int rt = (int)(b % P.row_tiles);
-    b /= P.row_tiles;
-    const int h = (int)(b % P.kv_heads);
-    const int seq = (int)(b / P.kv_heads);
+    uint32_t b = blockIdx.x;
+    const int split = (int)(b % (uint32_t)P.splits);
+    b /= (uint32_t)P.splits;
+    const int rt = (int)(b % (uint32_t)P.row_tiles);
+    b /= (uint32_t)P.row_tiles;
+    const int h = (int)(b % (uint32_t)P.kv_heads);
+    const int seq = (int)(b / (uint32_t)P.kv_heads);
 
     const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
     const int len = min(__ldg(P.lens + seq), P.max_len);
@@ -136,8 +136,8 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // keys that any row of this tile sees: [lo, hi)
     const int shift = len - (q1 - q0);              // position of the sequence's first query
     const int last = min(rows, row0 + Sh::kRows) - 1;
-    const int hi = max(0, min(len, P.causal ? shift + last / G + 1 : len));
-    const int lo = P.window > 0 ? max(0, shift + row0 / G - P.window + 1) / kTile * kTile : 0;
+    const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
+    const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
 #pragma unroll
     for (int x = 0; x < QN; ++x) {
         const int row = min(row_base + 8 * (x >> 1) + 2 * c + (x & 1), rows - 1);
-        const int pos = shift + row / G;
+        const int pos = shift + P.by_group(row);
         see_hi[x] = P.causal ? min(pos + 1, len) : len;
         see_lo[x] = P.window > 0 ? max(0, pos - P.window + 1) : 0;
     }
@@ -162,6 +162,18 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     for (int o = 1; o < 4; o <<= 1) {
         all_hi = min(all_hi, __shfl_xor_sync(0xFFFFFFFFu, all_hi, o));
         all_lo = max(all_lo, __shfl_xor_sync(0xFFFFFFFFu, all_lo, o));
+    }
+
+    // row g of each eight query rows, the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on: on their way while the
+    // first tiles are asked for
+    uint4 q_raw[NQ][DIM / 32];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int row = row_base + 8 * x + g, qt = P.by_group(row);
+        const bool live = row < rows;
+        const uint16_t* qp = P.q + (int64_t)(q0 + qt) * P.q_stride + (h * G + row - qt * G) * DIM + c * (DIM / 4);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; ++i) q_raw[x][i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
     }
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -233,19 +245,12 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     };
     uint32_t sc_next = scale_at(0, pages[0]);
 
-    // q: row g of each eight, the 32 (DIM = 128) or 16 (DIM = 64) dimensions from c * DIM/4 on; the power of two goes to the
-    // row's factor, which the softmax needs in the threads of its columns
+    // q: the power of two goes to the row's factor, which the softmax needs in the threads of its columns
     uint32_t qb[KS][NQ][2];
     float row_factor[QN];
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-        const int row = row_base + 8 * x + g;
-        const bool live = row < rows;
-        uint4 w[DIM / 32];
-        const uint16_t* qp = P.q + (int64_t)(q0 + (live ? row / G : 0)) * P.q_stride + (int64_t)(h * G + (live ? row % G : 0)) * DIM + c * (DIM / 4);
-#pragma unroll
-        for (int i = 0; i < DIM / 32; ++i) w[i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
-        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(q_raw[x]);
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
@@ -483,106 +488,62 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
 
     // ---- join the groups of warps ----
     // row x of this thread: sum l 2^at, output acc 2^c0 2^at with at = ref - kTop - c0; dimensions g * DIM/8 ... + DIM/8 - 1
-    constexpr int OUT = DIM / 8;
+    constexpr int OUT = DIM / 8, PITCH = DIM + 4;
     float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
-    float* const stat = sm + GROUPS * Sh::kRows * DIM;
-    float at[QN];
+    float2* const stat = reinterpret_cast<float2*>(sm + GROUPS * Sh::kRows * PITCH);   // (at, l)
     const float unit = ex2(c0);
+    __syncthreads();   // every copy has landed and been read
 #pragma unroll
     for (int x = 0; x < QN; ++x) {
+        const int place = group * Sh::kRows + rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], o);
-        at[x] = ref[x] - kTop - c0;
+        float* const p = sm + place * PITCH + g * OUT;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            acc[j][x >> 1][x & 1] *= unit;
-            acc[j][x >> 1][2 + (x & 1)] *= unit;
-        }
+        for (int y = 0; y < MT / 2; ++y)
+            *reinterpret_cast<float4*>(p + 4 * y) = make_float4(acc[2 * y][x >> 1][x & 1] * unit, acc[2 * y][x >> 1][2 + (x & 1)] * unit,
+                                                                acc[2 * y + 1][x >> 1][x & 1] * unit, acc[2 * y + 1][x >> 1][2 + (x & 1)] * unit);
+        if (g == 0) stat[place] = make_float2(ref[x] - kTop - c0, l[x]);
     }
-    if (GROUPS > 1) {
-        __syncthreads();   // every copy has landed and been read
-        if (group != 0) {
+    __syncthreads();
+    // all threads: eight dimensions of a row at a time
+    for (int item = threadIdx.x; item < Sh::kRows * OUT; item += kWarps * 32) {
+        const int in_tile = item / OUT, part = item % OUT, row = row0 + in_tile;
+        if (row >= rows) break;
+        float2 st[GROUPS];
+        float top = kNone, sum = 0.0f, o[8];
 #pragma unroll
-            for (int x = 0; x < QN; ++x) {
-                const int place = group * Sh::kRows + rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
-                float* const p = sm + (int64_t)place * DIM + g * OUT;
-#pragma unroll
-                for (int y = 0; y < MT / 2; ++y)
-                    *reinterpret_cast<float4*>(p + 4 * y) = make_float4(acc[2 * y][x >> 1][x & 1], acc[2 * y][x >> 1][2 + (x & 1)],
-                                                                        acc[2 * y + 1][x >> 1][x & 1], acc[2 * y + 1][x >> 1][2 + (x & 1)]);
-                if (g == 0) {
-                    stat[2 * place] = at[x];
-                    stat[2 * place + 1] = l[x];
-                }
-            }
+        for (int k = 0; k < GROUPS; ++k) {
+            st[k] = stat[k * Sh::kRows + in_tile];
+            top = fmaxf(top, st[k].x);
         }
-        __syncthreads();
-        if (group != 0) return;
 #pragma unroll
-        for (int x = 0; x < QN; ++x) {
-            const int own_place = rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
-            float top = at[x];
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
 #pragma unroll
-            for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, stat[2 * (k * Sh::kRows + own_place)]);
-            const float own = at[x] == kNone ? 0.0f : ex2(at[x] - top);
-            l[x] *= own;
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                acc[j][x >> 1][x & 1] *= own;
-                acc[j][x >> 1][2 + (x & 1)] *= own;
-            }
-#pragma unroll
-            for (int k = 1; k < GROUPS; ++k) {
-                const int place = k * Sh::kRows + own_place;
-                const float there = stat[2 * place];
-                if (there == kNone) continue;
-                const float by = ex2(there - top);
-                l[x] = fmaf(stat[2 * place + 1], by, l[x]);
-                const float* const p = sm + (int64_t)place * DIM + g * OUT;
-#pragma unroll
-                for (int y = 0; y < MT / 2; ++y) {
-                    const float4 v = *reinterpret_cast<const float4*>(p + 4 * y);
-                    acc[2 * y][x >> 1][x & 1] = fmaf(v.x, by, acc[2 * y][x >> 1][x & 1]);
-                    acc[2 * y][x >> 1][2 + (x & 1)] = fmaf(v.y, by, acc[2 * y][x >> 1][2 + (x & 1)]);
-                    acc[2 * y + 1][x >> 1][x & 1] = fmaf(v.z, by, acc[2 * y + 1][x >> 1][x & 1]);
-                    acc[2 * y + 1][x >> 1][2 + (x & 1)] = fmaf(v.w, by, acc[2 * y + 1][x >> 1][2 + (x & 1)]);
-                }
-            }
-            at[x] = top;
+        for (int k = 0; k < GROUPS; ++k) {
+            const float by = st[k].x == kNone ? 0.0f : ex2(st[k].x - top);
+            sum = fmaf(st[k].y, by, sum);
+            const float* const p = sm + (k * Sh::kRows + in_tile) * PITCH + 8 * part;
+            const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
+            o[0] = fmaf(u.x, by, o[0]); o[1] = fmaf(u.y, by, o[1]); o[2] = fmaf(u.z, by, o[2]); o[3] = fmaf(u.w, by, o[3]);
+            o[4] = fmaf(v.x, by, o[4]); o[5] = fmaf(v.y, by, o[5]); o[6] = fmaf(v.z, by, o[6]); o[7] = fmaf(v.w, by, o[7]);
         }
-    }
-#pragma unroll
-    for (int x = 0; x < QN; ++x) {
-        const int row = row_base + 8 * (x >> 1) + 2 * c + (x & 1);
-        if (row >= rows) continue;
-        const int64_t tok = q0 + row / G;
-        const int head = h * G + row % G;
-        const float inv = l[x] > 0.0f ? __fdiv_rn(1.0f, l[x]) : 0.0f;       // a row that sees nothing: zeros
-        const float lse2 = l[x] > 0.0f ? at[x] + log2f(l[x]) : kNone;
-        const int64_t out_row = tok * P.q_heads + head;
-        float o[OUT];
-#pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            o[2 * j] = acc[j][x >> 1][x & 1] * inv;
-            o[2 * j + 1] = acc[j][x >> 1][2 + (x & 1)] * inv;
-        }
+        const bool some = sum > 0.0f;                                     // a row that sees nothing: zeros
+        const float inv = some ? __fdiv_rn(1.0f, sum) : 0.0f;
+        const int qt = P.by_group(row), head = h * G + row - qt * G;
+        const int64_t tok = q0 + qt, out_row = tok * P.q_heads + head;
         if (P.splits == 1) {
-            uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + g * OUT;
-#pragma unroll
-            for (int e = 0; e < OUT / 8; ++e) {
-                uint32_t r[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = pack_bf16(o[8 * e + 2 * k], o[8 * e + 2 * k + 1]);
-                st_v4(y + 8 * e, r);
-            }
-            if (P.lse != nullptr && g == 0) P.lse[out_row] = lse2 * kLn2;
+            const uint32_t r[4] = {pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv), pack_bf16(o[4] * inv, o[5] * inv),
+                                   pack_bf16(o[6] * inv, o[7] * inv)};
+            st_v4(P.out + tok * P.out_stride + head * DIM + 8 * part, r);
+            if (P.lse != nullptr && part == 0) P.lse[out_row] = some ? (top + log2f(sum)) * kLn2 : kNone;
         } else {
             const int64_t to = out_row * P.splits + split;
-            if (g == 0) P.part_lse[to] = lse2;
-            if (l[x] > 0.0f) {
-                float* const y = P.part_out + to * DIM + g * OUT;
-#pragma unroll
-                for (int e = 0; e < OUT / 4; ++e) *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            if (part == 0) P.part_lse[to] = some ? top + log2f(sum) : kNone;
+            if (some) {
+                float* const y = P.part_out + to * DIM + 8 * part;
+                *reinterpret_cast<float4*>(y) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+                *reinterpret_cast<float4*>(y + 4) = make_float4(o[4] * inv, o[5] * inv, o[6] * inv, o[7] * inv);
             }
         }
     }
@@ -598,7 +559,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnPa
     __shared__ float sums[kJoinWarps][DIM + 1];
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row = blockIdx.x, tok = row / P.q_heads;
+    const int64_t row = blockIdx.x, tok = blockIdx.x / (uint32_t)P.q_heads;
     // rows of no sequence are left as they were
     if (tok >= min((int64_t)__ldg(P.cu_q + P.seqs), P.n) || tok < __ldg(P.cu_q)) return;
     const float* const part = P.part_lse + row * P.splits;

@@ -125,6 +125,11 @@ struct AttnParams {
     int64_t n, q_stride, out_stride, max_pages;
     int num_pages, seqs, q_heads, kv_heads, group, dim, page, page_shift, block_shift, max_q, max_len, causal, window;
     float scale;
+    uint32_t group_mul, group_shift;   // row / group = (row * group_mul) >> (32 + group_shift) for rows below 2^31
+    __host__ __device__ int by_group(int row) const
+    {
+        return group == 1 ? row : (int)((((uint64_t)(uint32_t)row * group_mul) >> 32) >> group_shift);
+    }
     // filled by the launcher
     float *part_out, *part_lse;
     int64_t chunk;

@@ -183,13 +183,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
 
     pdl_prologue();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t b = blockIdx.x;
-    const int split = (int)(b % P.splits);
-    b /= P.splits;
-    const int seq = (int)(b % P.seqs);
-    b /= P.seqs;
-    const int h = (int)(b % P.kv_heads);
-    const int block = P.row_tiles - 1 - (int)(b / P.kv_heads);   // the rows that see most keys first
+    uint32_t b = blockIdx.x;
+    const int split = (int)(b % (uint32_t)P.splits);
+    b /= (uint32_t)P.splits;
+    const int seq = (int)(b % (uint32_t)P.seqs);
+    b /= (uint32_t)P.seqs;
+    const int h = (int)(b % (uint32_t)P.kv_heads);
+    const int block = P.row_tiles - 1 - (int)(b / (uint32_t)P.kv_heads);   // the rows that see most keys first
 
     const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
     const int len = min(__ldg(P.lens + seq), P.max_len);
@@ -198,8 +198,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     if (q0 < 0 || row0 >= rows) return;
     const int shift = len - (q1 - q0);
     const int last = min(rows, row0 + 2 * kTile) - 1;
-    const int hi = max(0, min(len, P.causal ? shift + last / G + 1 : len));
-    const int lo = P.window > 0 ? max(0, shift + row0 / G - P.window + 1) / kTile * kTile : 0;
+    const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
+    const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -241,8 +241,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const int r_in = threadIdx.x & 127;                   // row within its tile
     const int row = row0 + rt * kTile + r_in;
     const bool row_live = warp >= 8 && row < rows;
-    const int64_t tok = q0 + (row_live ? row / G : 0);
-    const int head = h * G + (row_live ? row % G : 0);
+    const int q_tok = row_live ? P.by_group(row) : 0;
+    const int64_t tok = q0 + q_tok;
+    const int head = h * G + (row_live ? row - q_tok * G : 0);
     float row_factor = 0.0f;
     if (warp >= 8) {
         uint4 w[DIM / 8];
@@ -503,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = o_col[rt] + lanes;
-        const int pos = shift + (row_live ? row / G : nq - 1);
+        const int pos = shift + (row_live ? P.by_group(row) : nq - 1);
         const int see_hi = P.causal ? min(pos + 1, len) : len;
         const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
         const float kNone = -INFINITY;
