@@ -32,10 +32,66 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&v);
 }
-__device__ __forceinline__ void st16(uint16_t* p, const float* x)
+template <bool PAIRS>
+__device__ __forceinline__ void store(uint16_t* p, int second, const Lane16& x)   // second: bytes to the second run
 {
-    const uint32_t r[4] = {pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (PAIRS) {
+            r[2 * i] = pack2(x.a[i].x, x.b[i].x);
+            r[2 * i + 1] = pack2(x.a[i].y, x.b[i].y);
+        } else {
+            r[i] = pack2(x.a[i].x, x.a[i].y);
+            r[4 + i] = pack2(x.b[i].x, x.b[i].y);
+        }
+    }
     st_v4(p, r);
+    st_v4(reinterpret_cast<char*>(p) + second, r + 4);
+}
+__device__ __forceinline__ void scale(Lane16& x, float r)
+{
+    const float2 f = make_float2(r, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x.a[i] = __fmul2_rn(x.a[i], f);
+        x.b[i] = __fmul2_rn(x.b[i], f);
+    }
+}
+__device__ __forceinline__ void scale(Lane16& x, const Lane16& g)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x.a[i] = __fmul2_rn(x.a[i], g.a[i]);
+        x.b[i] = __fmul2_rn(x.b[i], g.b[i]);
+    }
+}
+// sum of x y over the lane's elements
+__device__ __forceinline__ float dot(const Lane16& x, const Lane16& y)
+{
+    float2 s = __fmul2_rn(x.a[0], y.a[0]), t = __fmul2_rn(x.b[0], y.b[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        s = __ffma2_rn(x.a[i], y.a[i], s);
+        t = __ffma2_rn(x.b[i], y.b[i], t);
+    }
+    s = __fadd2_rn(s, t);
+    return s.x + s.y;
+}
+__device__ __forceinline__ void fill(Lane16& x, float v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.a[i] = x.b[i] = make_float2(v, v);
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const char* src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr)
+{
+    uint4 r;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr) : "memory");
+    return r;
 }
 template <int LP>
 __device__ __forceinline__ float head_sum(float v)
@@ -61,191 +117,209 @@ __device__ __forceinline__ bool token_turn(const HeadsParams& P, int64_t t, int 
     return true;
 }
 
-template <int LP, bool PAIRS, bool NORM>
+// A warp takes U * G heads of one token, all of its loads at once.
+template <int LP, int U, bool PAIRS, bool NORM>
 __global__ void __launch_bounds__(kWarps * 32) rope_fwd_kernel(const HeadsParams P)
 {
     constexpr int G = 32 / LP;   // heads a warp holds at a time
-    constexpr int U = 2;         // ... twice, to have more loads in flight
     pdl_prologue();
     const int lane = threadIdx.x & 31, sub = lane % LP, grp = lane / LP;
     const int64_t w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t t = w / P.parts;
+    const int64_t t = P.parts == 1 ? w : (int64_t)((uint64_t)w / (uint32_t)P.parts);
     if (t >= P.T) return;
     const int part = (int)(w - t * P.parts);
     const int heads = P.heads[0] + P.heads[1];
-    const int begin = part * P.per_part, end = min(heads, begin + P.per_part);
+    const int h0 = part * U * G + grp;
     const bool live = 16 * sub < P.dim;
     const LanePairs lp = lane_pairs(live ? sub : 0, P.rot, PAIRS);
+
+    // head h of the two operands as one list
+    const uint16_t* const xq = P.x[0] + t * P.x_stride[0];
+    const uint16_t* const xk = P.x[1] + t * P.x_stride[1] - P.heads[0] * P.dim;
+    uint16_t* const yq = P.y[0] + t * P.y_stride[0];
+    uint16_t* const yk = P.y[1] + t * P.y_stride[1] - P.heads[0] * P.dim;
+    uint4 raw[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int h = h0 + u * G;
+        raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && h < heads) {
+            const uint16_t* x = (h < P.heads[0] ? xq : xk) + h * P.dim;
+            raw[u][0] = ld16(x + lp.o0);
+            raw[u][1] = ld16(x + lp.o1);
+        }
+    }
     Turn turn;
     const bool good = token_turn(P, t, sub, lp, turn);
     if (!good && lane == 0 && part == 0) atomicAdd(&g_heads_bad, 1u);
-
-    for (int h0 = begin + grp; h0 - grp < end; h0 += G * U) {
-        uint4 raw[U][2];
+    Lane16 g;
+    int g_of = -1;   // whose gain g holds
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * G;
-            raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
-            if (live && h < end) {
-                const int which = h >= P.heads[0];
-                const uint16_t* x = P.x[which] + t * P.x_stride[which] + (int64_t)(h - (which ? P.heads[0] : 0)) * P.dim;
-                raw[u][0] = ld16(x + lp.o0);
-                raw[u][1] = ld16(x + lp.o1);
+    for (int u = 0; u < U; ++u) {
+        const int h = h0 + u * G;
+        const int which = h >= P.heads[0];
+        Lane16 x;
+        unpack<PAIRS>(x, raw[u]);
+        float r = 1.0f;
+        if (NORM) {
+            r = head_rcp(head_sum<LP>(dot(x, x)), P.inv_dim, P.eps);
+            const uint16_t* gain = which ? P.gain[1] : P.gain[0];
+            if (gain != nullptr && live) {
+                if (g_of != which) {
+                    const uint4 w[2] = {__ldg(reinterpret_cast<const uint4*>(gain + lp.o0)), __ldg(reinterpret_cast<const uint4*>(gain + lp.o1))};
+                    unpack<PAIRS>(g, w);
+                    g_of = which;
+                }
+                scale(x, g);
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * G;
-            const int which = h >= P.heads[0];
-            float x[16];
-            unpack8(x, raw[u][0]);
-            unpack8(x + 8, raw[u][1]);
-            if (NORM) {
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
-                const float r = head_rcp(head_sum<LP>(s), P.inv_dim, P.eps);
-                const uint16_t* gain = P.gain[which];
-                if (gain != nullptr && live) {
-                    float g[16];
-                    unpack8(g, __ldg(reinterpret_cast<const uint4*>(gain + lp.o0)));
-                    unpack8(g + 8, __ldg(reinterpret_cast<const uint4*>(gain + lp.o1)));
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = x[i] * r * g[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] *= r;
-                }
-            }
-            if (P.cos_sin != nullptr) {
-                if (!good) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(0x7FC00000u);   // loud: no angle for this token
-                } else if (lp.turns) {
-                    apply_turn<PAIRS, false>(x, turn);
-                }
-            }
-            if (live && h < end) {
-                uint16_t* y = P.y[which] + t * P.y_stride[which] + (int64_t)(h - (which ? P.heads[0] : 0)) * P.dim;
-                st16(y + lp.o0, x);
-                st16(y + lp.o1, x + 8);
-            }
+        if (P.cos_sin != nullptr) {
+            if (!good) fill(x, __uint_as_float(0x7FC00000u));   // loud: no angle for this token
+            else if (lp.turns) apply_turn<false, NORM>(x, turn);
         }
+        if (NORM) scale(x, r);   // the rotation leaves a common factor alone
+        if (live && h < heads) store<PAIRS>((which ? yk : yq) + h * P.dim + lp.o0, 2 * (lp.o1 - lp.o0), x);
     }
 }
 
 // One CTA works for the queries or for the keys only (the CTAs are shared out by their head counts), so that a lane carries
-// 16 sums of one gain's gradient.  A warp walks over a contiguous run of (token, group of heads) items and asks for the next
-// item's x and dy before it works on the present one.
+// 16 sums of one gain's gradient.  A warp walks over a contiguous run of (token, group of heads) items, kRing - 1 of which are on
+// their way to shared memory at a time (16-byte asynchronous copies; a thread reads back only what it asked for, so that nothing
+// has to be synchronised): 4 KB in flight a warp against 2 KB that registers would hold.
+constexpr int kRing = 4;
 template <int LP, bool PAIRS, bool NORM>
 __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsParams P)
 {
-    constexpr int G = 32 / LP;
+    constexpr int G = 32 / LP, N = NORM ? 4 : 2;        // 16-byte pieces of a thread's item
+    constexpr uint32_t PIECE = kWarps * 32 * 16, SLOT = N * PIECE;
     __shared__ float sums[kWarps][256];
+    __shared__ __align__(16) uint8_t ring[kRing * SLOT];
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LP, grp = lane / LP;
     const int which = (int)blockIdx.x >= P.ctas_q;
     const int64_t cta = which ? (int)blockIdx.x - P.ctas_q : (int)blockIdx.x, ctas = which ? (int)gridDim.x - P.ctas_q : P.ctas_q;
-    const int heads = P.heads[which], groups = (heads + G - 1) / G;
+    const int heads = which ? P.heads[1] : P.heads[0], groups = (heads + G - 1) / G;
     const int64_t items = P.T * groups, warps = ctas * kWarps, w = cta * kWarps + warp;
     const int64_t begin = items * w / warps, end = items * (w + 1) / warps;
     const bool live = 16 * sub < P.dim;
+    const int in_last = heads - (groups - 1) * G;       // heads of a token's last group
     const LanePairs lp = lane_pairs(live ? sub : 0, P.rot, PAIRS);
-    const uint16_t* const x_base = P.x[which];
-    const uint16_t* const g_base = P.grad[which];
-    float acc[16];
+    const int64_t first = groups > 0 ? begin / groups : 0;
+
+    // byte addresses that run along with the walk: what is asked for (d: gradient, x: input) and what is written
+    const int64_t d_stride = 2 * (which ? P.grad_stride[1] : P.grad_stride[0]), x_stride = 2 * (which ? P.x_stride[1] : P.x_stride[0]),
+                  y_stride = 2 * (which ? P.y_stride[1] : P.y_stride[0]);
+    const int step = 2 * G * P.dim, second = 2 * (lp.o1 - lp.o0);
+    const int begin_group = (int)(begin - first * groups);
+    const int64_t lane_at = 2 * ((int64_t)(begin_group * G + grp) * P.dim + lp.o0);
+    const char* fd = reinterpret_cast<const char*>(which ? P.grad[1] : P.grad[0]) + first * d_stride + lane_at;
+    const char* fx = reinterpret_cast<const char*>(which ? P.x[1] : P.x[0]) + first * x_stride + lane_at;
+    char* y = reinterpret_cast<char*>(which ? P.y[1] : P.y[0]) + first * y_stride + lane_at;
+    const int64_t token_bytes = (int64_t)groups * step;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    uint32_t f_at = ring_at, at = ring_at;
+    int fg = begin_group, g = begin_group;
+    int64_t f_left = end - begin;
+    auto fetch = [&]() {
+        if (f_left > 0) {
+            --f_left;
+            const bool last = fg == groups - 1;
+            const int bytes = live && (!last || grp < in_last) ? 16 : 0;   // 0: the piece is filled with zeros, nothing is read
+            copy16(f_at, fd, bytes);
+            copy16(f_at + PIECE, fd + second, bytes);
+            if (NORM) {
+                copy16(f_at + 2 * PIECE, fx, bytes);
+                copy16(f_at + 3 * PIECE, fx + second, bytes);
+            }
+            f_at = f_at + SLOT == ring_at + kRing * SLOT ? ring_at : f_at + SLOT;
+            fd += step;
+            fx += step;
+            ++fg;
+            if (last) {
+                fg = 0;
+                fd += d_stride - token_bytes;
+                fx += x_stride - token_bytes;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
-    uint4 gain[2];   // bf16 pairs
-    gain[0] = gain[1] = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);   // ones
-    if (NORM && P.gain[which] != nullptr && live) {
-        gain[0] = __ldg(reinterpret_cast<const uint4*>(P.gain[which] + lp.o0));
-        gain[1] = __ldg(reinterpret_cast<const uint4*>(P.gain[which] + lp.o1));
+    for (int i = 0; i < kRing - 1; ++i) fetch();
+
+    Lane16 acc, gamma;
+    fill(acc, 0.0f);
+    fill(gamma, 1.0f);
+    const uint16_t* const gain = which ? P.gain[1] : P.gain[0];
+    if (NORM && gain != nullptr && live) {
+        const uint4 u[2] = {__ldg(reinterpret_cast<const uint4*>(gain + lp.o0)), __ldg(reinterpret_cast<const uint4*>(gain + lp.o1))};
+        unpack<PAIRS>(gamma, u);
     }
     Turn turn;
-    bool good = true;
-    int64_t t = begin / groups;
-    int g = (int)(begin - t * groups);
-    int64_t turn_of = -1;
-
-    uint4 nx[2], ng[2];
-    auto fetch = [&](int64_t tt, int gg) {
-        const int h = gg * G + grp;
-        nx[0] = nx[1] = ng[0] = ng[1] = make_uint4(0u, 0u, 0u, 0u);
-        if (live && h < heads) {
-            if (NORM) {
-                const uint16_t* x = x_base + tt * P.x_stride[which] + (int64_t)h * P.dim;
-                nx[0] = ld16(x + lp.o0);
-                nx[1] = ld16(x + lp.o1);
-            }
-            const uint16_t* d = g_base + tt * P.grad_stride[which] + (int64_t)h * P.dim;
-            ng[0] = ld16(d + lp.o0);
-            ng[1] = ld16(d + lp.o1);
-        }
-    };
-    if (begin < end) fetch(t, g);
-    for (int64_t i = begin; i < end; ++i) {
-        uint4 cx[2] = {nx[0], nx[1]}, cg[2] = {ng[0], ng[1]};
-        const int64_t ct = t;
-        const int h = g * G + grp;
-        if (++g == groups) {
-            g = 0;
-            ++t;
-        }
-        if (i + 1 < end) fetch(t, g);
-        if (ct != turn_of) {
-            good = token_turn(P, ct, sub, lp, turn);
-            turn_of = ct;
+    bool good = true, fresh = true;
+    int64_t t = first;
+    for (int64_t left = end - begin; left > 0; --left) {
+        fetch();
+        if (fresh && P.cos_sin != nullptr) {
+            good = token_turn(P, t, sub, lp, turn);
             if (!good && lane == 0) atomicAdd(&g_heads_bad, 1u);
         }
-        float d[16];
-        unpack8(d, cg[0]);
-        unpack8(d + 8, cg[1]);
-        if (P.cos_sin != nullptr && good && lp.turns) apply_turn<PAIRS, true>(d, turn);
+        asm volatile("cp.async.wait_group %0;" :: "n"(kRing - 1) : "memory");
+        const uint4 cg[2] = {lds16(at), lds16(at + PIECE)};
+        Lane16 d;
+        unpack<PAIRS>(d, cg);
+        if (P.cos_sin != nullptr && good && lp.turns) apply_turn<true, NORM>(d, turn);
         if (NORM) {
-            float x[16], gamma[16], ss = 0.0f, sd = 0.0f;
-            unpack8(gamma, gain[0]);
-            unpack8(gamma + 8, gain[1]);
-            unpack8(x, cx[0]);
-            unpack8(x + 8, cx[1]);
+            const uint4 cx[2] = {lds16(at + 2 * PIECE), lds16(at + 3 * PIECE)};
+            Lane16 x;
+            unpack<PAIRS>(x, cx);
+            float2 sd = make_float2(0.0f, 0.0f), se = sd;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                ss = fmaf(x[j], x[j], ss);
-                sd = fmaf(d[j] * gamma[j], x[j], sd);
+            for (int j = 0; j < 4; ++j) {
+                sd = __ffma2_rn(__fmul2_rn(d.a[j], x.a[j]), gamma.a[j], sd);
+                se = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), gamma.b[j], se);
             }
-            ss = head_sum<LP>(ss);
-            sd = head_sum<LP>(sd);
+            sd = __fadd2_rn(sd, se);
+            const float ss = head_sum<LP>(dot(x, x)), hx = head_sum<LP>(sd.x + sd.y);
             const float r = head_rcp(ss, P.inv_dim, P.eps);
-            const float m = sd * r * P.inv_dim * r;   // mean(h n) * r: dx = r * (h - x * m)
+            const float m = -hx * r * P.inv_dim * r;  // -mean(h n) * r: dx = r * (h + x * m)
             const float rg = good ? r : 0.0f;         // a token without an angle adds nothing to the gain's gradient
+            const float2 r2 = make_float2(r, r), m2 = make_float2(m, m), rg2 = make_float2(rg, rg);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                acc[j] = fmaf(d[j], x[j] * rg, acc[j]);
-                d[j] = r * (d[j] * gamma[j] - x[j] * m);
+            for (int j = 0; j < 4; ++j) {
+                acc.a[j] = __ffma2_rn(__fmul2_rn(d.a[j], x.a[j]), rg2, acc.a[j]);
+                acc.b[j] = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), rg2, acc.b[j]);
+                d.a[j] = __fmul2_rn(__ffma2_rn(x.a[j], m2, __fmul2_rn(d.a[j], gamma.a[j])), r2);
+                d.b[j] = __fmul2_rn(__ffma2_rn(x.b[j], m2, __fmul2_rn(d.b[j], gamma.b[j])), r2);
             }
         }
-        if (live && h < heads) {
-            if (!good) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) d[j] = __uint_as_float(0x7FC00000u);
-            }
-            uint16_t* y = P.y[which] + ct * P.y_stride[which] + (int64_t)h * P.dim;
-            st16(y + lp.o0, d);
-            st16(y + lp.o1, d + 8);
+        const bool last = g == groups - 1;
+        if (live && (!last || grp < in_last)) {
+            if (!good) fill(d, __uint_as_float(0x7FC00000u));
+            store<PAIRS>(reinterpret_cast<uint16_t*>(y), second, d);
+        }
+        at = at + SLOT == ring_at + kRing * SLOT ? ring_at : at + SLOT;
+        y += step;
+        ++g;
+        fresh = last;
+        if (last) {
+            g = 0;
+            ++t;
+            y += y_stride - token_bytes;
         }
     }
     if constexpr (NORM) {
         if (P.partial == nullptr) return;
         // the CTA's row of partial sums: groups of the warp by shuffles, then the warps in order
 #pragma unroll
-        for (int o = LP; o < 32; o <<= 1)
+        for (int j = 0; j < 4; ++j) {
+            float v[4] = {acc.a[j].x, acc.a[j].y, acc.b[j].x, acc.b[j].y};
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[j] += __shfl_xor_sync(0xFFFFFFFFu, acc[j], o);
-        if (grp == 0 && live) {
+            for (int k = 0; k < 4; ++k) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sums[warp][lp.o0 + j] = acc[j];
-                sums[warp][lp.o1 + j] = acc[8 + j];
+                for (int o = LP; o < 32; o <<= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+                // member k / 2 of pair 2j + k % 2
+                const int pair = 2 * j + (k & 1), at = PAIRS ? 2 * pair + (k >> 1) : pair + 8 * (k >> 1);
+                if (grp == 0 && live) sums[warp][at < 8 ? lp.o0 + at : lp.o1 + at - 8] = v[k];
             }
         }
         __syncthreads();
@@ -295,16 +369,13 @@ cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// calls f.template operator()<LP, PAIRS, NORM>() for the case at hand
+// calls f(lanes per head, pairs, norm) for the case at hand, as compile-time constants
 template <class F>
 cudaError_t by_case(const HeadsParams& P, F f)
 {
     auto by_flags = [&](auto lp) {
-        constexpr int LP = decltype(lp)::value;
-        if (P.pairs) return P.norm ? f(std::integral_constant<int, LP>{}, std::true_type{}, std::true_type{})
-                                   : f(std::integral_constant<int, LP>{}, std::true_type{}, std::false_type{});
-        return P.norm ? f(std::integral_constant<int, LP>{}, std::false_type{}, std::true_type{})
-                      : f(std::integral_constant<int, LP>{}, std::false_type{}, std::false_type{});
+        if (P.pairs) return P.norm ? f(lp, std::true_type{}, std::true_type{}) : f(lp, std::true_type{}, std::false_type{});
+        return P.norm ? f(lp, std::false_type{}, std::true_type{}) : f(lp, std::false_type{}, std::false_type{});
     };
     switch (lanes_per_head(P.dim)) {
         case 1: return by_flags(std::integral_constant<int, 1>{});
@@ -315,22 +386,41 @@ cudaError_t by_case(const HeadsParams& P, F f)
     }
 }
 
+template <int U, int LP, bool PAIRS, bool NORM>
+cudaError_t launch_fwd_kernel(const HeadsParams& P, cudaStream_t stream)
+{
+    return launch(rope_fwd_kernel<LP, U, PAIRS, NORM>, dim3((unsigned)((P.T * P.parts + kWarps - 1) / kWarps)), kWarps * 32, stream, (const HeadsParams)P);
+}
+
 }  // namespace
 
 cudaError_t launch_rope_fwd(HeadsParams P, cudaStream_t stream)
 {
-    const int heads = P.heads[0] + P.heads[1], at_once = 32 / lanes_per_head(P.dim);
-    // a warp takes all heads of a token, unless that would leave SMs without work (few tokens): then the heads are
-    // shared out among as many warps as it takes to reach about four a scheduler
-    const int most = (heads + at_once - 1) / at_once;
-    const int64_t want = ((int64_t)kSMs * 16 + P.T - 1) / P.T;
-    P.parts = (int)(want < 1 ? 1 : want > most ? most : want);
-    P.per_part = ((most + P.parts - 1) / P.parts) * at_once;
-    P.parts = (heads + P.per_part - 1) / P.per_part;
-    const int64_t ctas = (P.T * P.parts + kWarps - 1) / kWarps;
+    // groups of heads that a warp takes at once: five where that divides the heads with least left over (40 heads of 128:
+    // 2 warps a token), one where there are too few tokens to keep the SMs busy otherwise
+    const int groups = (P.heads[0] + P.heads[1] + 32 / lanes_per_head(P.dim) - 1) / (32 / lanes_per_head(P.dim));
+    int u = 1;
+    if (P.T * groups >= (int64_t)kSMs * 32) {
+        static constexpr int kChoices[] = {5, 3, 2, 1};
+        int best = 1 << 30;
+        for (int c : kChoices) {
+            const int slots = (groups + c - 1) / c * c;
+            if (slots < best) {
+                best = slots;
+                u = c;
+            }
+        }
+    }
+    P.parts = (groups + u - 1) / u;
     return by_case(P, [&](auto lp, auto pairs, auto norm) {
-        return launch(rope_fwd_kernel<decltype(lp)::value, decltype(pairs)::value, decltype(norm)::value>, dim3((unsigned)ctas), kWarps * 32,
-                      stream, (const HeadsParams)P);
+        constexpr int LP = decltype(lp)::value;
+        constexpr bool PAIRS = decltype(pairs)::value, NORM = decltype(norm)::value;
+        switch (u) {
+            case 5: return launch_fwd_kernel<5, LP, PAIRS, NORM>(P, stream);
+            case 3: return launch_fwd_kernel<3, LP, PAIRS, NORM>(P, stream);
+            case 2: return launch_fwd_kernel<2, LP, PAIRS, NORM>(P, stream);
+            default: return launch_fwd_kernel<1, LP, PAIRS, NORM>(P, stream);
+        }
     });
 }
 
@@ -346,8 +436,11 @@ int rope_bwd_ctas(int64_t T, int q_heads, int k_heads, int dim)
 
 cudaError_t launch_rope_bwd(HeadsParams P, cudaStream_t stream)
 {
-    const int ctas = rope_bwd_ctas(P.T, P.heads[0], P.heads[1], P.dim), heads = P.heads[0] + P.heads[1];
-    int q = (int)(((int64_t)ctas * P.heads[0] + heads / 2) / heads);
+    const int ctas = rope_bwd_ctas(P.T, P.heads[0], P.heads[1], P.dim);
+    // CTAs for the queries: by the groups of heads a token has, plus what a token costs by itself (its angles)
+    const int at_once = 32 / lanes_per_head(P.dim), token = 2;
+    const int64_t wq = 2 * ((P.heads[0] + at_once - 1) / at_once) + token, wk = 2 * ((P.heads[1] + at_once - 1) / at_once) + token;
+    int q = P.heads[1] == 0 ? ctas : P.heads[0] == 0 ? 0 : (int)((ctas * wq + (wq + wk) / 2) / (wq + wk));
     if (P.heads[0] > 0 && q < 1) q = 1;
     if (P.heads[1] > 0 && q > ctas - 1) q = ctas - 1;
     P.ctas_q = q;

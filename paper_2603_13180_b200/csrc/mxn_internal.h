@@ -89,7 +89,7 @@ struct HeadsParams {
     int64_t T, table_rows;
     int dim, rot, pairs, norm;
     float eps, inv_dim;
-    int parts, per_part, ctas_q;   // filled by the launchers
+    int parts, ctas_q;          // filled by the launchers
 };
 cudaError_t launch_rope_fwd(HeadsParams P, cudaStream_t stream);
 cudaError_t launch_rope_bwd(HeadsParams P, cudaStream_t stream);

@@ -7,8 +7,8 @@
 // one token at a time cheap and repeatable: appending the same tokens to the same places again changes nothing.
 //
 // One warp owns one (block of tokens, head) of the keys or of the values, so that no two warps ever meet in a block and no
-// atomic is needed.  A warp is given a run of token rows and works on the blocks whose first new token lies in its run; a
-// block's tokens are read twice (maximum, then codes), the second time from L1.  Bound: HBM, 3 bytes an element
+// atomic is needed.  A warp is given a run of token rows and works on the blocks whose first new token lies in its run; the
+// first 2 * 512 / dim of a block's tokens stay in registers between the maximum and the codes, the others are read again from L1.  Bound: HBM, 3 bytes an element
 // (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of loads.
 #include "mxn_internal.h"
 #include "mxn_rope.cuh"
@@ -18,6 +18,7 @@ namespace mxn {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kHeld = 2;
 
 __device__ unsigned int g_kv_bad = 0;   // blocks whose page, position or length is out of range
 
@@ -43,6 +44,14 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
+__device__ __forceinline__ float largest(float top, const Lane16& x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        top = fmaxf(fmaxf(fmaxf(top, fabsf(x.a[i].x)), fmaxf(fabsf(x.a[i].y), fabsf(x.b[i].x))), fabsf(x.b[i].y));
+    return top;
+}
+
 // four E4M3 bytes -> binary32
 __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float* f)
 {
@@ -53,7 +62,7 @@ __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float* f)
 }
 
 template <int LP, bool PAIRS>
-__global__ void __launch_bounds__(kWarps * 32) kv_append_kernel(const KvAppendParams P)
+__global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppendParams P)
 {
     constexpr int G = 32 / LP;   // tokens a warp holds at a time
     pdl_prologue();
@@ -109,27 +118,39 @@ __global__ void __launch_bounds__(kWarps * 32) kv_append_kernel(const KvAppendPa
         uint8_t* const scale = P.scales[which] + tile * (P.page / P.block) + off / P.block;
         const uint16_t* const x0 = P.x[which] + j * P.x_stride[which] + (int64_t)h * P.dim;
 
-        auto load = [&](int i, float* x) {   // token i of the new ones, rotated
-            uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+        auto fetch = [&](int i, uint4* w) {   // token i of the new ones
+            w[0] = w[1] = make_uint4(0u, 0u, 0u, 0u);
             if (live && i < count) {
                 const uint16_t* p = x0 + i * P.x_stride[which];
-                a = __ldg(reinterpret_cast<const uint4*>(p + lp.o0));
-                b = __ldg(reinterpret_cast<const uint4*>(p + lp.o1));
+                w[0] = __ldg(reinterpret_cast<const uint4*>(p + lp.o0));
+                w[1] = __ldg(reinterpret_cast<const uint4*>(p + lp.o1));
             }
-            unpack8(x, a);
-            unpack8(x + 8, b);
+        };
+        auto turned = [&](int i, const uint4* w, Lane16& x) {
+            unpack<PAIRS>(x, w);
             if (rot != 0 && lp.turns && i < count) {
                 Turn turn;
                 load_turn(turn, P.cos_sin + (pos + i) * rot, sub, rot);
-                apply_turn<PAIRS, false>(x, turn);
+                apply_turn<false, false>(x, turn);
             }
         };
-        float top = 0.0f;
-        for (int i0 = 0; i0 < count; i0 += G) {
-            float x[16];
-            load(i0 + grp, x);
+        // kHeld turns of G tokens are loaded at once and stay in registers between the maximum and the codes
+        uint4 held[kHeld][2];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+        for (int k = 0; k < kHeld; ++k) fetch(k * G + grp, held[k]);
+        float top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            Lane16 x;
+            turned(k * G + grp, held[k], x);
+            top = largest(top, x);
+        }
+        for (int i0 = kHeld * G; i0 < count; i0 += G) {
+            uint4 w[2];
+            Lane16 x;
+            fetch(i0 + grp, w);
+            turned(i0 + grp, w, x);
+            top = largest(top, x);
         }
         uint32_t sb = e8m0_scale_rceil_pow2<8>(warp_max(top));
         if (in_block != 0) {
@@ -158,16 +179,25 @@ __global__ void __launch_bounds__(kWarps * 32) kv_append_kernel(const KvAppendPa
         __syncwarp();
         if (lane == 0) *scale = (uint8_t)sb;
         const float inv = inv_scale(sb);
-        for (int i0 = 0; i0 < count; i0 += G) {
-            const int i = i0 + grp;
-            float x[16];
-            load(i, x);
-            if (!live || i >= count) continue;
-            uint32_t w[4];
+        auto store = [&](int i, Lane16& x) {
+            if (!live || i >= count) return;
+            const float2 f = make_float2(inv, inv);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = cvt_e4m3x4(__fmul_rn(x[4 * e], inv), __fmul_rn(x[4 * e + 1], inv), __fmul_rn(x[4 * e + 2], inv),
-                                  __fmul_rn(x[4 * e + 3], inv));
+            for (int e = 0; e < 4; ++e) {
+                x.a[e] = __fmul2_rn(x.a[e], f);
+                x.b[e] = __fmul2_rn(x.b[e], f);
+            }
+            uint32_t w[4];
+            if (PAIRS) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = cvt_e4m3x4(x.a[e].x, x.b[e].x, x.a[e].y, x.b[e].y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    w[e] = cvt_e4m3x4(x.a[2 * e].x, x.a[2 * e].y, x.a[2 * e + 1].x, x.a[2 * e + 1].y);
+                    w[2 + e] = cvt_e4m3x4(x.b[2 * e].x, x.b[2 * e].y, x.b[2 * e + 1].x, x.b[2 * e + 1].y);
+                }
+            }
             uint8_t* y = codes + (int64_t)(in_block + i) * P.dim;
             if (lp.o1 == lp.o0 + 8) {
                 st_v4(y + lp.o0, w);
@@ -175,6 +205,19 @@ __global__ void __launch_bounds__(kWarps * 32) kv_append_kernel(const KvAppendPa
                 st_v2(y + lp.o0, w);
                 st_v2(y + lp.o1, w + 2);
             }
+        };
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            Lane16 x;
+            turned(k * G + grp, held[k], x);
+            store(k * G + grp, x);
+        }
+        for (int i0 = kHeld * G; i0 < count; i0 += G) {
+            uint4 w[2];
+            Lane16 x;
+            fetch(i0 + grp, w);
+            turned(i0 + grp, w, x);
+            store(i0 + grp, x);
         }
         j += count;
     }

@@ -28,7 +28,7 @@ __device__ __forceinline__ LanePairs lane_pairs(int sub, int rot, bool pairs)
 }
 
 struct Turn {
-    float c[8], s[8];
+    float2 c[4], s[4];
 };
 
 __device__ __forceinline__ void load_turn(Turn& t, const float* row, int sub, int rot)
@@ -36,29 +36,52 @@ __device__ __forceinline__ void load_turn(Turn& t, const float* row, int sub, in
     const float4* c = reinterpret_cast<const float4*>(row + 8 * sub);
     const float4* s = reinterpret_cast<const float4*>(row + rot / 2 + 8 * sub);
     *reinterpret_cast<float4*>(t.c) = __ldg(c);
-    *reinterpret_cast<float4*>(t.c + 4) = __ldg(c + 1);
+    *reinterpret_cast<float4*>(t.c + 2) = __ldg(c + 1);
     *reinterpret_cast<float4*>(t.s) = __ldg(s);
-    *reinterpret_cast<float4*>(t.s + 4) = __ldg(s + 1);
+    *reinterpret_cast<float4*>(t.s + 2) = __ldg(s + 1);
 }
 
-// x[0..7], x[8..15]: the lane's two runs.  Every product and sum is one IEEE binary32 operation.  BACK turns by the
-// opposite angle (the transposed rotation, for the gradient).
-template <bool PAIRS, bool BACK>
-__device__ __forceinline__ void apply_turn(float* x, const Turn& t)
+// The lane's 16 elements as binary32 pairs for packed arithmetic: a[i] = first members 2i, 2i + 1 of the pairs that turn
+// together, b[i] = their second members, for either order of the elements in memory (halves: the lane's two runs; pairs: the even
+// and the odd elements of both).  Lanes that do not turn use the same arrangement.
+struct Lane16 {
+    float2 a[4], b[4];
+};
+
+template <bool PAIRS>
+__device__ __forceinline__ void unpack(Lane16& x, const uint4* w)
 {
+    const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int ia = PAIRS ? 2 * i : i, ib = PAIRS ? 2 * i + 1 : i + 8;
-        const float a = x[ia], b = x[ib], c = t.c[i], s = BACK ? -t.s[i] : t.s[i];
-        x[ia] = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
-        x[ib] = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+    for (int i = 0; i < 4; ++i) {
+        if (PAIRS) {
+            x.a[i] = make_float2(bf16_lo(u[2 * i]), bf16_lo(u[2 * i + 1]));
+            x.b[i] = make_float2(bf16_hi(u[2 * i]), bf16_hi(u[2 * i + 1]));
+        } else {
+            x.a[i] = make_float2(bf16_lo(u[i]), bf16_hi(u[i]));
+            x.b[i] = make_float2(bf16_lo(u[4 + i]), bf16_hi(u[4 + i]));
+        }
     }
 }
 
-__device__ __forceinline__ void unpack8(float* x, uint4 w)
+// (a, b) -> (a cos - b sin, b cos + a sin), or the opposite angle (BACK: the transposed rotation, for the gradient).  FUSED: a
+// product and a sum in one rounding; else every product and sum is one IEEE binary32 operation.
+template <bool BACK, bool FUSED>
+__device__ __forceinline__ void apply_turn(Lane16& x, const Turn& t)
 {
-    x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
-    x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = x.a[i], b = x.b[i], s = BACK ? make_float2(-t.s[i].x, -t.s[i].y) : t.s[i], m = make_float2(-s.x, -s.y);
+        if (FUSED) {
+            x.a[i] = __ffma2_rn(b, m, __fmul2_rn(a, t.c[i]));
+            x.b[i] = __ffma2_rn(a, s, __fmul2_rn(b, t.c[i]));
+        } else {
+            // one by one: the compiler joins a packed product and a packed sum to one rounding
+            const float2 c = t.c[i];
+            x.a[i] = make_float2(__fadd_rn(__fmul_rn(a.x, c.x), __fmul_rn(b.x, m.x)), __fadd_rn(__fmul_rn(a.y, c.y), __fmul_rn(b.y, m.y)));
+            x.b[i] = make_float2(__fadd_rn(__fmul_rn(b.x, c.x), __fmul_rn(a.x, s.x)), __fadd_rn(__fmul_rn(b.y, c.y), __fmul_rn(a.y, s.y)));
+        }
+    }
 }
 
 // lanes that hold one head: dim / 16, rounded up to a power of two
