@@ -707,6 +707,8 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
     P.dim = head_dim;
     P.page = page_size;
     P.block = block;
+    P.page_shift = log2_of(page_size);
+    P.block_shift = log2_of(block);
     P.rot = rot_dim;
     P.pairs = pairing == MXN_ROPE_PAIRS;
     return mxn::launch_kv_append(P, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;

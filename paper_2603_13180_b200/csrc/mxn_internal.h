@@ -108,7 +108,7 @@ struct KvAppendParams {
     const int32_t* page_table;  // [seqs, max_pages]
     const float* cos_sin;       // [table_rows, rot] or nullptr
     int64_t n, num_pages, max_pages, table_rows;
-    int seqs, heads, dim, page, block, rot, pairs;
+    int seqs, heads, dim, page, block, page_shift, block_shift, rot, pairs;
     int run;                    // filled by the launcher
 };
 cudaError_t launch_kv_append(KvAppendParams P, cudaStream_t stream);

@@ -8,8 +8,10 @@
 //
 // One warp owns one (block of tokens, head) of the keys or of the values, so that no two warps ever meet in a block and no
 // atomic is needed.  A warp is given a run of token rows and works on the blocks whose first new token lies in its run; the
-// first 2 * 512 / dim of a block's tokens stay in registers between the maximum and the codes, the others are read again from L1.  Bound: HBM, 3 bytes an element
+// first 16 tokens (8 of heads beyond 128) of a block are copied to shared memory all at once and read there for the maximum and for the codes, the others
+// are read again from L1.  The run's rows are asked into L2 while the warp looks up its sequence.  Bound: HBM, 3 bytes an element
 // (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of loads.
+#include "mxn_async.cuh"
 #include "mxn_internal.h"
 #include "mxn_rope.cuh"
 
@@ -18,17 +20,16 @@ namespace mxn {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kHeld = 2;
 
 __device__ unsigned int g_kv_bad = 0;   // blocks whose page, position or length is out of range
 
 // index of the sequence that row j belongs to: the last s with cu[s] <= j, found 32 probes at a time
-__device__ __forceinline__ int find_sequence(const int32_t* cu, int seqs, int64_t j, int lane)
+__device__ __forceinline__ int find_sequence(const int32_t* cu, int seqs, int j, int lane)
 {
     int lo = 0, n = seqs;   // the answer is in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 31) / 32, at = lo + lane * step;
-        const bool below = lane * step < n && (int64_t)__ldg(cu + at) <= j;
+        const bool below = lane * step < n && __ldg(cu + at) <= j;
         const unsigned b = __ballot_sync(0xFFFFFFFFu, below);
         const int k = b ? 31 - __clz(b) : 0;
         lo += k * step;
@@ -52,6 +53,17 @@ __device__ __forceinline__ float largest(float top, const Lane16& x)
     return top;
 }
 
+// 16 bytes to shared memory, or zeros (bytes = 0)
+__device__ __forceinline__ void copy16(uint32_t dst, const uint16_t* src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void sts_v4(uint32_t at, float2 a, float2 b)
+{
+    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" :: "r"(at), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y) : "memory");
+}
+
 // four E4M3 bytes -> binary32
 __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float* f)
 {
@@ -65,8 +77,12 @@ template <int LP, bool PAIRS>
 __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppendParams P)
 {
     constexpr int G = 32 / LP;   // tokens a warp holds at a time
+    constexpr int kStaged = LP == 16 ? 8 : 16;        // tokens of a block that go through shared memory
+    constexpr int kTurns = G < kStaged ? kStaged / G : 1, kTurnBytes = 2048;
+    __shared__ __align__(16) uint8_t staged[kWarps][kTurns * kTurnBytes];
     pdl_prologue();
     const int lane = threadIdx.x & 31, sub = lane % LP, grp = lane / LP;
+    const uint32_t stage = smem_u32(staged[threadIdx.x >> 5]) + lane * 16;
     const int hv = (int)blockIdx.y * kWarps + (threadIdx.x >> 5);   // keys' heads, then values' heads
     if (hv >= 2 * P.heads) return;
     const int which = hv >= P.heads, h = hv - which * P.heads;
@@ -74,83 +90,103 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
     const bool live = 16 * sub < P.dim;
     const int rot = rotate ? P.rot : 0;
     const LanePairs lp = lane_pairs(live ? sub : 0, rot, PAIRS);
-    const int64_t rows = min((int64_t)__ldg(P.cu + P.seqs), P.n);
-    int64_t j = (int64_t)blockIdx.x * P.run;
-    const int64_t j_end = min(j + P.run, rows);
-    const int64_t first_row = __ldg(P.cu);
+    const int n = (int)P.n, rows = min(__ldg(P.cu + P.seqs), n), first_row = __ldg(P.cu);
+    int j = (int)blockIdx.x * P.run;
+    const int j_end = min(j + P.run, rows);
+    {
+        const int per_row = (2 * P.dim + 127) / 128;   // lines of a head
+        for (int i = lane; i < P.run * per_row; i += 32) {
+            const int row = j + i / per_row;
+            if (row < n) {
+                const char* at = reinterpret_cast<const char*>(P.x[which] + row * P.x_stride[which] + h * P.dim) + 128 * (i % per_row);
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(at));
+            }
+        }
+    }
     if (j < first_row) j = first_row;
-    int s = -1;
-    int64_t c0 = 0, c1 = 0, len = 0;
+    int s = -1, c0 = 0, c1 = 0, start = 0;
     while (j < j_end) {
         if (s < 0 || j >= c1) {
             s = find_sequence(P.cu, P.seqs, j, lane);
             c0 = __ldg(P.cu + s);
-            c1 = min((int64_t)__ldg(P.cu + s + 1), rows);
-            len = __ldg(P.lens + s);
-            if (j < c0 || j >= c1) {   // no sequence holds this row (cu is not a rising list): leave it
+            const int c_end = __ldg(P.cu + s + 1);
+            c1 = min(c_end, rows);
+            start = (int)max((int64_t)-1, (int64_t)__ldg(P.lens + s) - ((int64_t)c_end - c0));   // place of the sequence's first new token
+            if (c0 < 0 || j < c0 || j >= c1) {   // no sequence holds this row (cu is not a rising list): leave it
                 ++j;
                 s = -1;
                 continue;
             }
         }
-        const int64_t pos = len - ((int64_t)__ldg(P.cu + s + 1) - j), start = pos - (j - c0);
         if (start < 0) {   // more new tokens than the sequence is long
             if (lane == 0 && j == c0) atomicAdd(&g_kv_bad, 1u);
             j = c1;
             continue;
         }
-        const int in_block = (int)(pos % P.block);
-        const int count = (int)min((int64_t)(P.block - in_block), c1 - j);
+        const int pos = start + (j - c0), in_block = pos & (P.block - 1), count = min(P.block - in_block, c1 - j);
         if (in_block != 0 && j != c0) {   // the block belongs to the warp of its first new token
             j += count;
             continue;
         }
-        const int64_t page_at = pos / P.page;
-        const int64_t page = page_at < P.max_pages ? (int64_t)__ldg(P.page_table + s * P.max_pages + page_at) : -1;
-        if (page < 0 || page >= P.num_pages || (rotate && pos + count > P.table_rows)) {
+        const int page_at = pos >> P.page_shift;
+        const int page = page_at < P.max_pages ? __ldg(P.page_table + s * P.max_pages + page_at) : -1;
+        if (page < 0 || page >= P.num_pages || (rotate && (int64_t)pos + count > P.table_rows)) {
             if (lane == 0) atomicAdd(&g_kv_bad, 1u);
             j += count;
             continue;
         }
-        const int off = (int)(pos % P.page);   // of the first new token within its page
-        const int64_t tile = page * P.heads + h;
+        const int off = pos & (P.page - 1);   // of the first new token within its page
+        const int64_t tile = (int64_t)page * P.heads + h;
         uint8_t* const codes = P.codes[which] + (tile * P.page + (off - in_block)) * P.dim;   // the block's first token
-        uint8_t* const scale = P.scales[which] + tile * (P.page / P.block) + off / P.block;
-        const uint16_t* const x0 = P.x[which] + j * P.x_stride[which] + (int64_t)h * P.dim;
+        uint8_t* const scale = P.scales[which] + (tile << (P.page_shift - P.block_shift)) + (off >> P.block_shift);
+        const uint16_t* const x0 = P.x[which] + j * P.x_stride[which] + h * P.dim;
 
-        auto fetch = [&](int i, uint4* w) {   // token i of the new ones
-            w[0] = w[1] = make_uint4(0u, 0u, 0u, 0u);
-            if (live && i < count) {
-                const uint16_t* p = x0 + i * P.x_stride[which];
-                w[0] = __ldg(reinterpret_cast<const uint4*>(p + lp.o0));
-                w[1] = __ldg(reinterpret_cast<const uint4*>(p + lp.o1));
+        // The block's first kStaged tokens on their way to shared memory all at once; a thread reads back only its own pieces.
+        // Rotated elements are left there in binary32 for the second reading.
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            const int i = k * G + grp, bytes = live && i < count ? 16 : 0;
+            const uint16_t* p = x0 + (bytes ? i : 0) * P.x_stride[which];
+            copy16(stage + k * kTurnBytes, p + lp.o0, bytes);
+            copy16(stage + k * kTurnBytes + 512, p + lp.o1, bytes);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        const bool turns = rot != 0 && lp.turns;
+        const float* const angles = P.cos_sin + (int64_t)pos * rot;
+        auto load = [&](int i, uint32_t at, Lane16& x) {   // token i of the new ones, rotated
+            uint4 w[2];
+            if (i < kStaged) {
+                w[0] = lds_v4(at);
+                w[1] = lds_v4(at + 512);
+            } else {
+                w[0] = w[1] = make_uint4(0u, 0u, 0u, 0u);
+                if (live && i < count) {
+                    const uint16_t* p = x0 + i * P.x_stride[which];
+                    w[0] = __ldg(reinterpret_cast<const uint4*>(p + lp.o0));
+                    w[1] = __ldg(reinterpret_cast<const uint4*>(p + lp.o1));
+                }
             }
-        };
-        auto turned = [&](int i, const uint4* w, Lane16& x) {
             unpack<PAIRS>(x, w);
-            if (rot != 0 && lp.turns && i < count) {
+            if (turns && i < count) {
                 Turn turn;
-                load_turn(turn, P.cos_sin + (pos + i) * rot, sub, rot);
+                load_turn(turn, angles + i * rot, sub, rot);
                 apply_turn<false, false>(x, turn);
             }
         };
-        // kHeld turns of G tokens are loaded at once and stay in registers between the maximum and the codes
-        uint4 held[kHeld][2];
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) fetch(k * G + grp, held[k]);
         float top = 0.0f;
+        uint32_t at = stage;
+#pragma unroll 2
+        for (int i = grp; i - grp < count; i += G, at += kTurnBytes) {
+            Lane16 x;
+            load(i, at, x);
+            top = largest(top, x);
+            if (turns && i < kStaged) {
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            Lane16 x;
-            turned(k * G + grp, held[k], x);
-            top = largest(top, x);
-        }
-        for (int i0 = kHeld * G; i0 < count; i0 += G) {
-            uint4 w[2];
-            Lane16 x;
-            fetch(i0 + grp, w);
-            turned(i0 + grp, w, x);
-            top = largest(top, x);
+                for (int e = 0; e < 2; ++e) {
+                    sts_v4(at + 512 * e, x.a[2 * e], x.a[2 * e + 1]);
+                    sts_v4(at + 1024 + 512 * e, x.b[2 * e], x.b[2 * e + 1]);
+                }
+            }
         }
         uint32_t sb = e8m0_scale_rceil_pow2<8>(warp_max(top));
         if (in_block != 0) {
@@ -163,7 +199,7 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
                 const float by = d > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - d) << 23);
                 for (int i = grp; i < in_block; i += G) {
                     if (!live) continue;
-                    uint4* p = reinterpret_cast<uint4*>(codes + (int64_t)i * P.dim + 16 * sub);
+                    uint4* p = reinterpret_cast<uint4*>(codes + i * P.dim + 16 * sub);
                     uint4 w = *p;
                     uint32_t* v = reinterpret_cast<uint32_t*>(&w);
 #pragma unroll
@@ -198,7 +234,7 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
                     w[2 + e] = cvt_e4m3x4(x.b[2 * e].x, x.b[2 * e].y, x.b[2 * e + 1].x, x.b[2 * e + 1].y);
                 }
             }
-            uint8_t* y = codes + (int64_t)(in_block + i) * P.dim;
+            uint8_t* y = codes + (in_block + i) * P.dim;
             if (lp.o1 == lp.o0 + 8) {
                 st_v4(y + lp.o0, w);
             } else {
@@ -206,18 +242,20 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
                 st_v2(y + lp.o1, w + 2);
             }
         };
+        at = stage;
+#pragma unroll 2
+        for (int i = grp; i - grp < count; i += G, at += kTurnBytes) {
+            Lane16 x;
+            if (turns && i < kStaged) {
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            Lane16 x;
-            turned(k * G + grp, held[k], x);
-            store(k * G + grp, x);
-        }
-        for (int i0 = kHeld * G; i0 < count; i0 += G) {
-            uint4 w[2];
-            Lane16 x;
-            fetch(i0 + grp, w);
-            turned(i0 + grp, w, x);
-            store(i0 + grp, x);
+                for (int e = 0; e < 2; ++e) {
+                    *reinterpret_cast<uint4*>(&x.a[2 * e]) = lds_v4(at + 512 * e);
+                    *reinterpret_cast<uint4*>(&x.b[2 * e]) = lds_v4(at + 1024 + 512 * e);
+                }
+            } else {
+                load(i, at, x);
+            }
+            store(i, x);
         }
         j += count;
     }
