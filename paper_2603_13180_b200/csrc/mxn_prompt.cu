@@ -6,7 +6,7 @@
 // token * group + head), in two tiles of 128, over a chunk of the keys in tiles of 128 tokens.  Tensor memory holds the scores
 // and the output of both tiles (2 * (128 + dim) columns of binary32).  Roles, by warp:
 //   0      copies: codes of keys and values by the tensor copy engine, a box for each page; scales by plain loads
-//   1      issues the products (one thread)
+//   1, 2   issue the products, one warp for each row tile
 //   4-7    values: E4M3 codes -> f16 (exact), zeros for what no row may see
 //   8-15   softmax, one warpgroup for each row tile, a thread for each row
 // The two row tiles alternate: while one's scores are in the softmax, the other's products run.
@@ -150,9 +150,17 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(is));
     return is != 0;
 }
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 // waits with a limit; a wait that runs out, or one that sees another's, ends the CTA's work
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* dead)
 {
+    if (mbar_test(bar, parity)) return true;
     for (uint32_t spin = 0; spin < (1u << 20); ++spin) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((spin & 255u) == 255u && *dead) return false;
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         dead_flag = 0;
         for (int i = 0; i < kKeyStages; ++i) {
             mbar_init(k_full + 8 * i, 1);
-            mbar_init(k_empty + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, 2);
         }
         for (int i = 0; i < kValStages; ++i) {
             mbar_init(v_full + 8 * i, 1);
@@ -221,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         }
         for (int i = 0; i < kHalfStages; ++i) {
             mbar_init(h_full + 8 * i, 4);
-            mbar_init(h_empty + 8 * i, 1);
+            mbar_init(h_empty + 8 * i, 2);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(s_full + 8 * i, 1);
@@ -372,29 +380,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             if (mine) tma_load_codes(base + Sh::kV + vs * Sh::kCodes + lane * box * DIM, &M.v, y, z, v_full + 8 * vs);
         }
         if (__any_sync(0xFFFFFFFFu, any_bad) && lane == 0) atomicAdd(&g_prompt_bad, 1u);
-    } else if (warp == 1) {
-        // ---- products ----
+    } else if (warp == 1 || warp == 2) {
+        // ---- products: a warp for each row tile, so that neither waits for the other's softmax ----
         MXN_FEW_REGISTERS();
         if (tiles > 0) {
             // Step i is half a key tile.  Scores are two steps ahead of the weights: while the softmax works on one buffer, the
             // other's scores are made.  The weights of step i lie in their scores' columns, so the scores of step i + 2 are
             // issued behind the product that reads those weights; products run in the order of issue.
-            // One thread issues it all, a product every 50 cycles: the whole warp goes through the loop, so that descriptors (bases
+            // One thread issues a row tile's products, one every 50 cycles: the whole warp goes through the loop, so that descriptors (bases
             // plus constants) are uniform values.
             const bool one = elect_one();
+            const int r = warp - 1;
+            const uint32_t s_mine = s_col[0] + r * 128, o_mine = o_col[0] + r * DIM, s_bar = s_full + 16 * r, p_bar = p_full + 16 * r;
             bool ok = true;
-            const uint64_t q_desc = operand(base + Sh::kQ, GROUP, 16, SW), k_base = operand(base + Sh::kK, GROUP, 16, SW),
+            const uint64_t q_desc = operand(base + Sh::kQ + r * 2 * Sh::kCodes, GROUP, 16, SW), k_base = operand(base + Sh::kK, GROUP, 16, SW),
                            h_base = operand(base + Sh::kH, 1024, kTile * 128, 2);
-            auto scores = [&](int r, int half, uint64_t k_desc) {   // S = (hi + lo) K^T
+            uint32_t ks = 0, k_par = 0, hs = 0, h_par = 0, p_par = 0;
+            uint64_t k_desc = k_base;
+            auto scores = [&](int half) {   // S = (hi + lo) K^T
 #pragma unroll
                 for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int s = 0; s < DIM / 32; ++s)
-                        mma_scores(s_col[r] + half * kStep, q_desc + (uint64_t)(((2 * r + part) * Sh::kCodes + 32 * s) >> 4),
+                        mma_scores(s_mine + half * kStep, q_desc + (uint64_t)((part * Sh::kCodes + 32 * s) >> 4),
                                    k_desc + (uint64_t)((half * kStep * DIM + 32 * s) >> 4), idesc_e4m3(kStep), (part | s) != 0);
             };
-            uint32_t ks = 0, k_par = 0, hs = 0, h_par = 0, p_par = 0;
-            uint64_t k_desc = k_base;
             auto next_keys = [&]() {   // the next key tile
                 if (++ks == kKeyStages) {
                     ks = 0;
@@ -407,12 +417,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 tc_after();
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        if (one) {
-                            scores(r, half, k_desc);
-                            mma_commit(s_full + 16 * r + 8 * half);
-                        }
+                    if (one) {
+                        scores(half);
+                        mma_commit(s_bar + 8 * half);
                     }
                 if (one) mma_commit(k_empty);
                 next_keys();
@@ -424,19 +431,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 const uint64_t h_desc = h_base + (uint64_t)((hs * Sh::kHalf) >> 4);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
+                    ok = ok && wait(p_bar + 8 * half, p_par, dead);
+                    if (!ok) continue;
+                    tc_after();
+                    if (one) {
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        ok = ok && wait(p_full + 16 * r + 8 * half, p_par, dead);
-                        if (!ok) continue;
-                        tc_after();
-                        if (one) {
-#pragma unroll
-                            for (int s = 0; s < kStep / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
-                                mma_values(o_col[r], s_col[r] + half * kStep + 8 * s, h_desc + (uint64_t)((half * kStep * 128 + s * 2048) >> 4),
-                                           idesc_f16_bt(DIM), (half | s) != 0 || j > 0);
-                            if (more) scores(r, half, k_desc);
-                            mma_commit(s_full + 16 * r + 8 * half);   // the scores two steps on, and the output up to this step
-                        }
+                        for (int s = 0; s < kStep / 16; ++s)   // 16 tokens a step: 8 columns of weights, two groups of 8 token rows
+                            mma_values(o_mine, s_mine + half * kStep + 8 * s, h_desc + (uint64_t)((half * kStep * 128 + s * 2048) >> 4),
+                                       idesc_f16_bt(DIM), (half | s) != 0 || j > 0);
+                        if (more) scores(half);
+                        mma_commit(s_bar + 8 * half);   // the scores two steps on, and the output up to this step
                     }
                 }
                 if (one) {
@@ -582,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                     }
                 }
             }
-            here = i + 1 < steps && mbar_try_wait(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
+            here = i + 1 < steps && mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             // weights, over their scores
             const float shift_by = ref == kNone ? 0.0f : kTop - ref;
             uint32_t w[32];
