@@ -177,6 +177,18 @@ __device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
 }
 __device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
 
+__device__ __forceinline__ float2 ex2_fma(float2 u)
+{
+    const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));
+    const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
+    float2 p = f2(0.00958285287f);
+    p = __ffma2_rn(p, f, f2(0.0559064249f));
+    p = __ffma2_rn(p, f, f2(0.240240986f));
+    p = __ffma2_rn(p, f, f2(0.693124193f));
+    p = __ffma2_rn(p, f, f2(1.0f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
 template <int DIM>
 __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
@@ -186,6 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * kKeyStages + 2 * kValStages + 2 * kHalfStages + 8 + kScaleSlots];
     __shared__ TileScales scales[kScaleSlots];
+    __shared__ float row_factors[2 * kTile];
     __shared__ uint32_t tmem_at;
     __shared__ int dead_flag;
 
@@ -244,57 +257,61 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
 
-    // q: a thread of the softmax warps loads its row, splits it and leaves hi and lo for the tensor cores
     const int rt = (warp >> 2) & 1;                       // row tile of warps 8-15
     const int r_in = threadIdx.x & 127;                   // row within its tile
-    const int row = row0 + rt * kTile + r_in;
-    const bool row_live = warp >= 8 && row < rows;
-    const int q_tok = row_live ? P.by_group(row) : 0;
-    const int64_t tok = q0 + q_tok;
-    const int head = h * G + (row_live ? row - q_tok * G : 0);
-    float row_factor = 0.0f;
-    if (warp >= 8) {
-        uint4 w[DIM / 8];
-        const uint16_t* qp = P.q + tok * P.q_stride + (int64_t)head * DIM;
+    // q, by warps 4-15: DIM / 8 threads for a row, so that a row is read in one piece.  It is split into hi and lo for the tensor cores.
+    if (warp >= 4) {
+        constexpr int kLanes = DIM / 8, kAtOnce = 32 / kLanes, kPass = 12 * kAtOnce, kPasses = (2 * kTile + kPass - 1) / kPass;
+        const int c = lane % kLanes, first = (warp - 4) * kAtOnce + lane / kLanes;
+        uint4 w[kPasses];
 #pragma unroll
-        for (int i = 0; i < DIM / 8; ++i) w[i] = row_live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
-        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < DIM / 2; ++i) m = absmax_bf16x2(m, u[i]);
-        const uint32_t E = __float_as_uint(hmax_abs_to_f32(m)) >> 23;
-        const uint32_t Ec = min(max(E, 8u), 254u);
-        float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);             // 2^(7 - (E - 127))
-        row_factor = fabsf(P.scale) * kLog2e * __uint_as_float((Ec - 7u) << 23);
-        if (P.scale < 0.0f) up = -up;
-        const uint32_t hi_at = base + Sh::kQ + rt * 2 * Sh::kCodes, lo_at = hi_at + Sh::kCodes;
-#pragma unroll
-        for (int i = 0; i < DIM / 16; ++i) {   // 16 elements: one 16-byte chunk of hi, one of lo
-            uint32_t a[4], c[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t u0 = u[8 * i + 2 * x], u1 = u[8 * i + 2 * x + 1];
-                uint32_t hh[2], ll[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const __half2 v = __floats2half2_rn(bf16_lo(y ? u1 : u0) * up, bf16_hi(y ? u1 : u0) * up);
-                    hh[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(v), __NV_SATFINITE, __NV_E4M3);
-                    const __half2 left = __hsub2(v, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hh[y], __NV_E4M3)));
-                    ll[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(left), __NV_SATFINITE, __NV_E4M3);
-                }
-                a[x] = hh[0] | (hh[1] << 16);
-                c[x] = ll[0] | (ll[1] << 16);
+        for (int i = 0; i < kPasses; ++i) {
+            const int r = first + i * kPass, rr = row0 + r;
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (r < 2 * kTile && rr < rows) {
+                const int t = P.by_group(rr);
+                w[i] = __ldg(reinterpret_cast<const uint4*>(P.q + (q0 + t) * P.q_stride + (int64_t)(h * G + rr - t * G) * DIM) + c);
             }
-            const uint32_t off = (uint32_t)r_in * DIM + (uint32_t)((DIM == 128 ? i ^ (r_in & 7) : i ^ ((r_in >> 1) & 3)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(hi_at + off), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(lo_at + off), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]) : "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int r = first + i * kPass;
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            float m = hmax_abs_to_f32(absmax_bf16x2(absmax_bf16x2(absmax_bf16x2(absmax_bf16x2(0u, u[0]), u[1]), u[2]), u[3]));
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            const uint32_t E = __float_as_uint(m) >> 23, Ec = min(max(E, 8u), 254u);
+            float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);             // 2^(7 - (E - 127))
+            if (P.scale < 0.0f) up = -up;
+            uint32_t hh[4], ll[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const __half2 v = __floats2half2_rn(bf16_lo(u[y]) * up, bf16_hi(u[y]) * up);
+                hh[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(v), __NV_SATFINITE, __NV_E4M3);
+                const __half2 left = __hsub2(v, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hh[y], __NV_E4M3)));
+                ll[y] = __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(left), __NV_SATFINITE, __NV_E4M3);
+            }
+            if (r < 2 * kTile) {
+                const int rl = r & (kTile - 1);
+                const uint32_t at = base + Sh::kQ + (uint32_t)(r / kTile) * 2 * Sh::kCodes + (uint32_t)rl * DIM
+                                  + (uint32_t)(((c >> 1) ^ (DIM == 128 ? rl & 7 : (rl >> 1) & 3)) << 4) + (uint32_t)(c & 1) * 8;
+                asm volatile("st.shared.v2.b32 [%0], {%1,%2};" :: "r"(at), "r"(hh[0] | (hh[1] << 16)), "r"(hh[2] | (hh[3] << 16)) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1,%2};" :: "r"(at + Sh::kCodes), "r"(ll[0] | (ll[1] << 16)), "r"(ll[2] | (ll[3] << 16)) : "memory");
+                if (c == 0) row_factors[r] = fabsf(P.scale) * kLog2e * __uint_as_float((Ec - 7u) << 23);
+            }
         }
         fence_async();
     }
-    tc_before();
-    __syncthreads();
-    tc_after();
-    const uint32_t tmem = tmem_at;
+    // warp 0 made the barriers and waits for nobody: its copies start while q is read
+    if (warp == 0) {
+        __syncwarp();
+        asm volatile("barrier.arrive 1, %0;" :: "n"(kThreads) : "memory");
+    } else {
+        tc_before();
+        asm volatile("barrier.sync 1, %0;" :: "n"(kThreads) : "memory");
+        tc_after();
+    }
+    const uint32_t tmem = warp == 0 ? 0u : tmem_at;
     const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + DIM};
 
     // 512 threads at 128 registers: the softmax warps take what the others give up (256 * 56 + 256 * 200 = 512 * 128)
@@ -508,25 +525,37 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t o_at = o_col[rt] + lanes;
-        const int pos = shift + (row_live ? P.by_group(row) : nq - 1);
+        const int row = row0 + rt * kTile + r_in;
+        const bool row_live = row < rows;
+        const int q_tok = row_live ? P.by_group(row) : 0;
+        const int64_t tok = q0 + q_tok;
+        const int head = h * G + (row_live ? row - q_tok * G : 0);
+        const float row_factor = row_factors[rt * kTile + r_in];
+        const int pos = shift + (row_live ? q_tok : nq - 1);
         const int see_hi = P.causal ? min(pos + 1, len) : len;
         const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
         const float kNone = -INFINITY;
         float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
         bool ok = true;
         const int steps = 2 * tiles;
-        bool here = false;
+        // a row that nothing hides in a step needs no mask: the range that holds for the warp's rows
+        const int all_lo = __reduce_max_sync(0xFFFFFFFFu, see_lo), all_hi = __reduce_min_sync(0xFFFFFFFFu, min(see_hi, k1));
+        bool here = false, scales_here = false;
         for (int i = 0; i < steps; ++i) {
             const int j = i >> 1, buf = i & 1;
             const TileScales& slot = scales[j % kScaleSlots];
-            const float* const slot_k = slot.k + 4 * buf;
-            const float* const slot_v = slot.v + 4 * buf;
-            const float* const slot_l = slot.l + 4 * buf;
-            ok = (here || wait(s_full + 16 * rt + 8 * buf, (uint32_t)j & 1u, dead)) && (buf || wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead));
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (!here && !__all_sync(0xFFFFFFFFu, wait(s_full + 16 * rt + 8 * buf, (uint32_t)j & 1u, dead))) ok = false;
+            if (!buf && !scales_here && !__all_sync(0xFFFFFFFFu, wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead))) ok = false;
+            if (!ok) break;
             tc_after();
             const uint32_t s_at = s_col[rt] + lanes + buf * kStep;
             const int t0 = k0 + i * kStep;
+            uint32_t x[2][32];
+            tm_request(x[0], s_at);
+            tm_request(x[1], s_at + 32);
+            const float4 k4 = *reinterpret_cast<const float4*>(slot.k + 4 * buf), v4 = *reinterpret_cast<const float4*>(slot.v + 4 * buf),
+                         l4 = *reinterpret_cast<const float4*>(slot.l + 4 * buf);
+            const float slot_k[4] = {k4.x, k4.y, k4.z, k4.w}, slot_v[4] = {v4.x, v4.y, v4.z, v4.w}, slot_l[4] = {l4.x, l4.y, l4.z, l4.w};
             const uint32_t readable = (slot.readable >> (4 * buf)) & 0xFu;
             const bool wide = slot.wide != 0;
             c0 = slot.c0;
@@ -536,10 +565,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u, above = down == 32 ? 0u : 0xFFFFFFFFu << down;
                 return below & above & (((readable >> (2 * c)) & 1u ? 0xFFFFu : 0u) | ((readable >> (2 * c + 1)) & 1u ? 0xFFFF0000u : 0u));
             };
-            const bool all = __all_sync(0xFFFFFFFFu, t0 >= see_lo && t0 + kStep <= min(see_hi, k1)) && readable == 0xFu;
-            uint32_t x[2][32];
-            tm_request(x[0], s_at);
-            tm_request(x[1], s_at + 32);
+            const bool all = t0 >= all_lo && t0 + kStep <= all_hi && readable == 0xFu;
+            float fac[4], utop = kNone;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) fac[g] = fmaxf(row_factor * slot_k[g], 1.17549435e-38f);
             tm_arrived(x[0]);
             tm_arrived(x[1]);
             if (!all) {
@@ -552,7 +581,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 }
             }
             // the step's largest s + sv, and the reference
-            float fac[4], utop = kNone;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
@@ -560,15 +588,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
 #pragma unroll
                 for (int e = 3; e < 15; e += 2) m = max3(__float_as_uint(m), y[e], y[e + 1]);
                 m = fmaxf(m, __uint_as_float(y[15]));
-                fac[g] = fmaxf(row_factor * slot_k[g], 1.17549435e-38f);
                 utop = fmaxf(utop, fmaf(m, fac[g], slot_v[g]));
             }
-            const float whole = ceilf(utop);
-            top_all = fmaxf(top_all, whole);
-            float next = ref;
-            if (utop > ref + kUp || (ref == kNone && utop > kNone)) next = whole;
-            else if (utop < ref - kDown && utop > kNone) next = fmaxf(whole, top_all - kDepth);
-            if (__any_sync(0xFFFFFFFFu, next != ref)) {
+            top_all = fmaxf(top_all, utop);
+            if (__any_sync(0xFFFFFFFFu, utop > ref + kUp || (utop < ref - kDown && utop > kNone))) {
+                float next = ref;   // (ref + kUp is -infinity without a reference)
+                if (utop > ref + kUp) next = ceilf(utop);
+                else if (utop < ref - kDown && utop > kNone) next = ceilf(fmaxf(utop, top_all - kDepth));
                 const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
                 l *= alpha;
                 ref = next;
@@ -586,29 +612,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                     }
                 }
             }
-            here = i + 1 < steps && mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             // weights, over their scores
             const float shift_by = ref == kNone ? 0.0f : kTop - ref;
-            uint32_t w[32];
-            float more = 0.0f;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
-                const float2 f = f2(fac[g]), add = f2(slot_v[g] + shift_by);
-                float2 sum[2] = {f2(0.0f), f2(0.0f)};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, add);
-                    const float2 p = make_float2(ex2(u.x), ex2(u.y));
-                    sum[e & 1] = __fadd2_rn(sum[e & 1], p);
-                    const __half2 q = __floats2half2_rn(p.x, p.y);
-                    w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
-                }
-                const float2 both = __fadd2_rn(sum[0], sum[1]);
-                more = fmaf(both.x + both.y, slot_l[g], more);
-            }
+            float extra = 0.0f;
             if (wide && ref > kNone) {   // the sum by exponentials of its own, from the scores as they still stand
-                more = 0.0f;
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     uint32_t z[16];
@@ -617,11 +624,34 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                     const float f = fmaxf(row_factor * slot_k[g], 1.17549435e-38f), add = c0 + kTop - ref;
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if ((see >> e) & 1u) more += ex2(fmaf(__uint_as_float(z[e]), f, add));
+                        if ((see >> e) & 1u) extra += ex2(fmaf(__uint_as_float(z[e]), f, add));
                 }
             }
-            l += more;
+            uint32_t w[32];
+            float more = 0.0f;
+            bool probe[3];
+            probe[2] = mbar_test(sc_full + 8 * ((i + 1) / 2 % kScaleSlots), (uint32_t)((i + 1) / 2 / kScaleSlots) & 1u);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t* const y = &x[g >> 1][16 * (g & 1)];
+                const float2 f = f2(fac[g]), add = f2(slot_v[g] + shift_by);
+                float2 sum[2] = {f2(0.0f), f2(0.0f)};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, add);
+                    const float2 p = (128 >> e) & 1 ? ex2_fma(u) : make_float2(ex2(u.x), ex2(u.y));
+                    sum[e & 1] = __fadd2_rn(sum[e & 1], p);
+                    const __half2 q = __floats2half2_rn(p.x, p.y);
+                    w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);
+                }
+                const float2 both = __fadd2_rn(sum[0], sum[1]);
+                more = fmaf(both.x + both.y, slot_l[g], more);
+                if (g & 1) probe[g >> 1] = mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
+            }
+            l += wide ? extra : more;
             tm_store32(s_at, w);
+            here = __all_sync(0xFFFFFFFFu, i + 1 < steps && (probe[0] || probe[1]));
+            scales_here = __all_sync(0xFFFFFFFFu, probe[2]);
             tm_store_wait();
             tc_before();
             __syncwarp();
@@ -632,10 +662,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
         // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 1 - c0
-        const bool some = l > 0.0f;
+        const bool some = ref > kNone;
         const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
         const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
         const int64_t out_row = tok * P.q_heads + head;
+        const uint32_t out_at = base + Sh::kQ + (uint32_t)(warp - 8) * 32 * 2 * DIM;
 #pragma unroll
         for (int c = 0; c < DIM / 32; ++c) {
             uint32_t x[32];
@@ -646,9 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             float* const o = reinterpret_cast<float*>(x);
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * inv : 0.0f;
-            if (!row_live) {
-            } else if (P.splits == 1) {
-                uint16_t* const y = P.out + tok * P.out_stride + (int64_t)head * DIM + 32 * c;
+            if (P.splits == 1) {   // to shared memory (q's, which no product reads any more): 16-byte pieces, as swizzled as its rows are long
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t r[4];
@@ -657,14 +686,29 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                         const __nv_bfloat162 v = __floats2bfloat162_rn(o[8 * e + 2 * i], o[8 * e + 2 * i + 1]);
                         r[i] = *reinterpret_cast<const uint32_t*>(&v);
                     }
-                    st_v4(y + 8 * e, r);
+                    const uint32_t at = out_at + (uint32_t)lane * 2 * DIM + (uint32_t)(((4 * c + e) ^ (lane & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
                 }
-            } else if (some) {
+            } else if (row_live && some) {
                 float* const y = P.part_out + (out_row * P.splits + split) * DIM + 32 * c;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) *reinterpret_cast<float4*>(y + 4 * e) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             }
             __syncwarp();
+        }
+        if (P.splits == 1) {   // and from there a row in one piece
+            constexpr int kLanes = DIM / 8, kAtOnce = 32 / kLanes;
+            const int c = lane % kLanes;
+#pragma unroll 4
+            for (int i = 0; i < 32; i += kAtOnce) {
+                const int r = i + lane / kLanes, rr = row0 + (warp - 8) * 32 + r;
+                const uint4 v = lds_v4(out_at + (uint32_t)r * 2 * DIM + (uint32_t)((c ^ (r & 7)) << 4));
+                if (rr < rows) {
+                    const int t = P.by_group(rr);
+                    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+                    st_v4(P.out + (q0 + t) * P.out_stride + (int64_t)(h * G + rr - t * G) * DIM + 8 * c, u);
+                }
+            }
         }
         if (row_live) {
             if (P.splits > 1) P.part_lse[out_row * P.splits + split] = lse2;
