@@ -740,7 +740,7 @@ mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens
     if (lse_out_or_null != nullptr && misaligned(lse_out_or_null, 4)) return MXN_ERR_ALIGN;
     const mxn::AttnPlan plan = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, causal ? window : 0, q_heads, kv_heads,
                                                     head_dim);
-    if (plan.ctas > 0x7FFFFFFF || (n_tokens * q_heads + 3) / 4 > 0x7FFFFFFF) return MXN_ERR_SHAPE;
+    if (plan.ctas > 0x7FFFFFFF || n_tokens * q_heads > 0x7FFFFFFF) return MXN_ERR_SHAPE;
     if (plan.splits > 1) {
         if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
         if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;

@@ -134,9 +134,10 @@ struct AttnParams {
     float *part_out, *part_lse;
     int64_t chunk;
     int splits, row_tiles;
+    uint32_t whole_units;       // prompts: CTAs of two row tiles; behind them a unit is two CTAs of one
 };
 struct AttnPlan {
-    int64_t chunk, splits, row_tiles, ctas;
+    int64_t chunk, splits, row_tiles, whole_units, ctas;
     int row_warps, row_eights;  // warps that share out the query rows of a CTA; groups of eight rows that a warp holds
     bool prompt;                // many query rows: the tcgen05 kernel
     size_t workspace;

@@ -205,6 +205,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     pdl_prologue();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t b = blockIdx.x;
+    int half = -1;   // the last units may be in two halves of a row tile each
+    if (b >= P.whole_units) {
+        half = (int)((b - P.whole_units) & 1u);
+        b = P.whole_units + (b - P.whole_units) / 2;
+    }
     const int split = (int)(b % (uint32_t)P.splits);
     b /= (uint32_t)P.splits;
     const int seq = (int)(b % (uint32_t)P.seqs);
@@ -215,11 +220,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
     const int len = min(__ldg(P.lens + seq), P.max_len);
     const int nq = max(0, min(q1 - q0, P.max_q));
-    const int G = P.group, row0 = block * 2 * kTile, rows = nq * G;
+    const int G = P.group, row0 = (2 * block + (half == 1)) * kTile, rows = min(nq * G, row0 + (half < 0 ? 2 : 1) * kTile);
     if (q0 < 0 || row0 >= rows) return;
+    const bool two = rows - row0 > kTile;   // else nothing is done for the second row tile
     const int shift = len - (q1 - q0);
-    const int last = min(rows, row0 + 2 * kTile) - 1;
-    const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
+    const int hi = max(0, min(len, P.causal ? shift + P.by_group(rows - 1) + 1 : len));
     const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
@@ -234,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         dead_flag = 0;
         for (int i = 0; i < kKeyStages; ++i) {
             mbar_init(k_full + 8 * i, 1);
-            mbar_init(k_empty + 8 * i, 2);
+            mbar_init(k_empty + 8 * i, two ? 2 : 1);
         }
         for (int i = 0; i < kValStages; ++i) {
             mbar_init(v_full + 8 * i, 1);
@@ -242,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         }
         for (int i = 0; i < kHalfStages; ++i) {
             mbar_init(h_full + 8 * i, 4);
-            mbar_init(h_empty + 8 * i, 2);
+            mbar_init(h_empty + 8 * i, two ? 2 : 1);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(s_full + 8 * i, 1);
@@ -400,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     } else if (warp == 1 || warp == 2) {
         // ---- products: a warp for each row tile, so that neither waits for the other's softmax ----
         MXN_FEW_REGISTERS();
-        if (tiles > 0) {
+        if (tiles > 0 && (warp == 1 || two)) {
             // Step i is half a key tile.  Scores are two steps ahead of the weights: while the softmax works on one buffer, the
             // other's scores are made.  The weights of step i lie in their scores' columns, so the scores of step i + 2 are
             // issued behind the product that reads those weights; products run in the order of issue.
@@ -520,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 mbar_arrive(h_full + 8 * hs);
             }
         }
-    } else if (warp >= 8) {
+    } else if (warp >= 8 && (rt == 0 || two)) {
         // ---- softmax ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
