@@ -686,15 +686,17 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     const int64_t step = a.prompt ? 128 : kTile * (kWarps / a.row_warps);   // keys that a CTA works on at a time
     // Chunks: as many as the CTAs that are resident at a time leave room for; four rounds of them where sequences may differ in
     // length (64 sequences of 2048 ... 8192 keys: one round 152 us, four 135 us).  A chunk is at least eight steps long, so that a
-    // CTA's start and the join are worth it, unless most SMs would be idle.
+    // CTA's start and the join are worth it (64 sequences of up to 2000 keys: 41 us, five steps 43), or five where half of the places
+    // would stay empty (16 sequences: eight 20 us, five 16), less only where most SMs would be idle.
     const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : decode_ctas(dim, a.row_eights));
     int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
     const int64_t span = window > 0 && window + tokens + tile < max_len ? window + tokens + tile : max_len;
+    const int64_t least = !a.prompt && 2 * units < resident ? 5 : 8;
     auto most = [&](int64_t keys) {
-        const int64_t by_eight = ceil_div(keys, 8 * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
-        return by_eight >= idle ? by_eight : by_one < idle ? by_one : idle;
+        const int64_t by_least = ceil_div(keys, least * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
+        return by_least >= idle ? by_least : by_one < idle ? by_one : idle;
     };
     const int64_t bound = splits < most(max_len) ? splits : most(max_len);   // for the workspace: whatever the window
     a.workspace = bound > 1 ? (size_t)n * q_heads * bound * (dim + 1) * 4 : 0;
