@@ -134,12 +134,14 @@ struct AttnParams {
     float *part_out, *part_lse;
     int64_t chunk;
     int splits, row_tiles;
+    int cluster;                // the CTAs of a row tile's chunks are a cluster
     uint32_t whole_units;       // prompts: CTAs of two row tiles; behind them a unit is two CTAs of one
 };
 struct AttnPlan {
     int64_t chunk, splits, row_tiles, whole_units, ctas;
     int row_warps, row_eights;  // warps that share out the query rows of a CTA; groups of eight rows that a warp holds
     bool prompt;                // many query rows: the tcgen05 kernel
+    bool cluster;               // few chunks, joined by the CTAs as a cluster
     size_t workspace;
 };
 AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim);
