@@ -388,8 +388,9 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
  *   max_q_len and max_kv_len bound the sequences' new queries and lengths (host values; they shape the launch: queries past
  *   max_q_len are not computed - their rows may receive undefined values - and keys past max_kv_len are not seen).
  *   lse_out [n_tokens, q_heads] fp32: the logarithm of the sum of exp(scale q k) over the keys seen.
- *   Products run on the E4M3 codes with binary32 sums; q enters exactly (elements below 2^-14 of their row's largest: to
- *   2^-22 of it), the softmax's weights with 8 significant bits, its sums in binary32.
+ *   Products run on the E4M3 codes with binary32 sums.  q enters exactly, but for elements below 2^-10 of their row's largest,
+ *   which are kept to 2^-18 of it; the softmax's weights have 11 significant bits (fewer where a weight times its value block's
+ *   scale lies below 2^-13 of the row's largest such product), its sums are binary32.
  *   What stands in the cache behind a sequence's last token, or in pages no visible key is in, has no influence.  A page out of
  *   range among the visible ones: its keys are left out.
  *   workspace: device memory, 16-byte aligned, at least mxkv_attention_workspace_bytes(...) bytes for the same sizes (0: none

@@ -5,9 +5,9 @@
 // Work of a CTA: 256 query rows of one sequence and key head (query heads that share a key head are rows like any other: row =
 // token * group + head), in two tiles of 128, over a chunk of the keys in tiles of 128 tokens.  Tensor memory holds the scores
 // and the output of both tiles (2 * (128 + dim) columns of binary32).  Roles, by warp:
-//   0      copies: codes of keys and values by the tensor copy engine, a box for each page; scales by plain loads
+//   0      copies: codes of keys and values by the tensor copy engine, a box for each page; scales by plain loads; starts while q is read
 //   1, 2   issue the products, one warp for each row tile
-//   4-7    values: E4M3 codes -> f16 (exact), zeros for what no row may see
+//   4-7    values: E4M3 codes -> f16 (exact), zeros for what no row may see; before that, with 8-15, q
 //   8-15   softmax, one warpgroup for each row tile, a thread for each row
 // The two row tiles alternate: while one's scores are in the softmax, the other's products run.
 //
@@ -23,7 +23,13 @@
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
 //
 // Bound: at head size 128 the two products of a 256 x 128 tile take 2048 cycles at the tensor cores' rate, its 32768 exponentials
-// 2048 cycles of the special function units: the kernel needs both busy at once.
+// 2048 cycles of the special function units.  4096 queries over 8192 keys, 32 query and 8 key heads of 128: 437 us, 940 TFLOP/s, 59 %
+// of a large library product's measured rate; a tile takes some 3900 cycles.  Without the softmax's arithmetic the same kernel takes
+// 310 us: what is left is the softmax's chain of loads, maxima, exponentials and stores, two warps for each scheduler, with the special
+// function units busy for half of the time.  Four warps for each scheduler (two for a row) took 595 us: twice the fixed costs
+// of a step.  What shortened the chain: barriers and scales looked at a step ahead, while shared memory is busy with the products'
+// operands (499 -> 478); a rounding of the maximum taken out of it (501 -> 493); q read by rows, 12 warps at it, and the
+// output written by rows through shared memory (464 -> 450).
 //
 // Every wait is bounded; see mxn_device_timeouts.
 #include <cuda_bf16.h>
@@ -177,16 +183,21 @@ __device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
 }
 __device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
 
+// 2^u of two numbers below 2^21 on the multipliers: u = n + f with n the nearest integer (what is below -126 counts as that: 2^-126 is
+// nothing to a sum whose terms reach 2^-15, and rounds to 0 in f16), and 2^f by a polynomial fitted to the least relative error over
+// [-1/2, 1/2] with 1 as its constant: 9.2e-8, with the roundings 1.6e-7 (2^-22.6)
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
-    const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));
+    const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
     const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
-    float2 p = f2(0.00958285287f);
-    p = __ffma2_rn(p, f, f2(0.0559064249f));
-    p = __ffma2_rn(p, f, f2(0.240240986f));
-    p = __ffma2_rn(p, f, f2(0.693124193f));
+    float2 p = f2(0.00132647273f);
+    p = __ffma2_rn(p, f, f2(0.00967151299f));
+    p = __ffma2_rn(p, f, f2(0.0555073358f));
+    p = __ffma2_rn(p, f, f2(0.240222424f));
+    p = __ffma2_rn(p, f, f2(0.693147004f));
     p = __ffma2_rn(p, f, f2(1.0f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
 template <int DIM>
@@ -644,7 +655,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, add);
-                    const float2 p = (128 >> e) & 1 ? ex2_fma(u) : make_float2(ex2(u.x), ex2(u.y));
+                    // one pair in eight by the multipliers: the special function units are the busier ones (none 450 us, one 437, two 454)
+                    const float2 p = e == 7 ? ex2_fma(u) : make_float2(ex2(u.x), ex2(u.y));
                     sum[e & 1] = __fadd2_rn(sum[e & 1], p);
                     const __half2 q = __floats2half2_rn(p.x, p.y);
                     w[8 * g + e] = *reinterpret_cast<const uint32_t*>(&q);

@@ -143,6 +143,41 @@ def test_zero_heads_and_no_tokens(mx):
     mx.rmsnorm_rope_fwd(q[:0], None, None, None, None, None, out[:0], None)
 
 
+def test_backward_on_a_stream_and_captured(mx):
+    """The gradients, those of the gains among them, have the same bits on another stream and in a graph that is replayed with new
+    inputs in place."""
+    T, hq, hk, D, rot = 333, 6, 2, 128, 128
+    q, k, gains, table, pos, g = inputs(T, hq, hk, D, rot, 500, seed=4)
+    dy = torch.randn(T, hq + hk, D, generator=g).to(torch.bfloat16).cuda()
+    ws = torch.empty(mx.rmsnorm_rope_bwd_workspace_bytes(T, hq, hk, D), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty_like(dy[:, :hq]), torch.empty_like(dy[:, hq:]), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")]
+
+    def call():
+        mx.rmsnorm_rope_bwd(q, k, dy[:, :hq], dy[:, hq:], gains[0], gains[1], table, pos, outs[0], outs[1], outs[2], outs[3], ws)
+
+    def results():
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        for o in outs:
+            o.fill_(7)
+        return got
+
+    call()
+    want = results()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    assert all(torch.equal(a, b) for a, b in zip(results(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(results(), want))
+    dy.mul_(2)   # exact: every gradient doubles
+    graph.replay()
+    assert all(torch.equal(a, 2 * b) for a, b in zip(results(), want))
+
+
 def test_positions_outside_the_table(mx):
     T, hq, hk, D, rot = 9, 3, 1, 64, 64
     q, k, gains, table, _, g = inputs(T, hq, hk, D, rot, 50, seed=2)

@@ -1,7 +1,7 @@
 """mxkv_append and mxkv_attention on the GPU: the append bit for bit against its contract, the attention against 64 bits.
 
-Tolerances of the attention.  out: the weights carry 8 significant bits (hi + lo: at most 2^-8 of a weight, and 2^-15 of the
-tile's largest for weights so far below it that they round to nothing), binary32 sums; then one rounding to bf16:
+Tolerances of the attention.  out: a weight is off by at most 2^-8 of itself (in binary16 it is 2^-11), or 2^-15 of the tile's
+largest where it is so far below that it rounds to nothing, binary32 sums; then one rounding to bf16:
 2^-8 |out| + (2^-8 + 2^-10) sum of softmax |v|, where 2^-10 covers the 32 small weights of a tile (32 * 2^-15).
 lse: a score is the binary32 sum of at most 128 exact products, added in a few steps of the tensor cores: 16 roundings of 2^-23 of
 the sum of magnitudes (`big`) and four of the score itself; exp2 and log2 add 2^-21 and the sum over tiles 2^-20 of relative
@@ -241,6 +241,86 @@ PROMPT = [
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 70), (False, 200)])
 def test_attention_prompts(mx, qh, h, dim, page, block, nq, lens, causal, window):
     check(mx, qh, h, dim, page, block, nq, lens, causal=causal, window=window, seed=dim + page + 1)
+
+
+@pytest.mark.parametrize("qh,h,dim,page,block,nq,lens", [
+    (64, 64, 64, 64, 16, [650], [700]), (40, 40, 128, 64, 16, [800], [1000]), (80, 40, 64, 32, 16, [400], [300]),
+])
+def test_attention_prompts_in_halves(mx, qh, h, dim, page, block, nq, lens):
+    """More blocks of 256 rows than SMs: those of the last round are halved.  Odd ends, and queries before the first key."""
+    check(mx, qh, h, dim, page, block, nq, lens, seed=dim + qh)
+
+
+@pytest.mark.parametrize("qh,h,dim,nq,lens", [
+    (1, 1, 128, [1], [20000]), (8, 2, 64, [4], [9000]), (4, 1, 128, [16], [5000]),              # more than eight chunks
+    (2, 1, 64, [1, 1], [1300, 3]), (32, 4, 64, [4, 3, 0], [1500, 4, 9]), (8, 4, 128, [8], [1100]),  # a few
+])
+@pytest.mark.parametrize("window", [0, 700])
+def test_attention_in_chunks(mx, qh, h, dim, nq, lens, window):
+    check(mx, qh, h, dim, 64, 16, nq, lens, window=window, seed=dim + window + qh)
+
+
+@pytest.mark.parametrize("nq", [1, 150])
+def test_cache_past_32_bits(mx, nq):
+    """Pages whose codes lie more than 2^32 bytes into the pool: the bits that a small pool gives."""
+    heads, dim, page, block, length = 8, 128, 64, 16, 200
+    pages = 2 ** 32 // (heads * dim * page) + 9
+    g = torch.Generator().manual_seed(nq)
+    x = torch.randn(length, 4 * heads, dim, generator=g).to(torch.bfloat16).cuda()
+    results = []
+    for pool, table in ((4, [[2, 0, 3, 1]]), (pages, [[pages - 2, pages - 4, pages - 1, pages - 3]])):
+        cache = mx.alloc_kv_cache(pool, heads, page, dim, block)
+        mx.mxkv_append(x[:, :heads], x[:, heads:2 * heads], dev([0, length]), dev([length]), dev(table), *cache)
+        q = x[length - nq:, 2 * heads:]
+        out = torch.empty_like(q)
+        nbytes = mx.mxkv_attention_workspace_bytes(nq, 1, nq, length, 2 * heads, heads, dim)
+        ws = torch.empty(max(16, nbytes), dtype=torch.uint8, device="cuda")
+        mx.mxkv_attention(q, dev([0, nq]), dev([length]), dev(table), *cache, out, nq, length, dim ** -0.5, workspace=ws)
+        results.append([c[torch.tensor(table[0], device="cuda")] for c in cache] + [out])
+        assert all(not bool(c[1 if pool > 4 else 4:pool - 4].any()) for c in cache)
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert bool(results[0][-1].isfinite().all()) and bool(results[0][0].any())
+
+
+def test_calls_at_the_same_time(mx):
+    """Two streams with a workspace each, and graphs of both that run side by side: every result has the bits of a call alone."""
+    heads, dim, page, block = 4, 128, 64, 16
+    jobs = []
+    for seed, (nq, lens) in enumerate((([1, 1], [6000, 900]), ([130, 7], [700, 3000]), ([2], [12000]))):
+        table, pool = make_table(lens, 200, page, seed)
+        cache = Cache(pool, heads, page, dim, block)
+        fill(cache, lens, table, page, block, seed)
+        q = torch.randn(sum(nq), 8, dim, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda()
+        nbytes = mx.mxkv_attention_workspace_bytes(sum(nq), len(nq), max(nq), max(lens), 8, heads, dim)
+        ws = torch.empty(max(16, nbytes), dtype=torch.uint8, device="cuda")
+        fixed = (dev(cumulative(nq)), dev(lens), dev(table), *cache.parts)
+        alone, out = torch.empty_like(q), torch.zeros_like(q)
+        call = lambda to, q=q, fixed=fixed, nq=nq, lens=lens, ws=ws: mx.mxkv_attention(  # noqa: E731
+            q, *fixed, to, max(nq), max(lens), dim ** -0.5, workspace=ws)
+        call(alone)
+        jobs.append((call, alone, out, torch.cuda.Stream(), cache))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for call, _, out, stream, _ in jobs:
+            with torch.cuda.stream(stream):
+                call(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(alone, out) for _, alone, out, _, _ in jobs)
+    graphs = []
+    for call, _, out, stream, _ in jobs:
+        out.zero_()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            call(out)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, (_, _, _, stream, _) in zip(graphs, jobs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(alone, out) for _, alone, out, _, _ in jobs)
+    assert mx.device_timeouts() == 0
 
 
 def test_attention_bounds_larger_than_the_lengths(mx):
