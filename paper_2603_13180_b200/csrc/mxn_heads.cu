@@ -107,13 +107,14 @@ __device__ __forceinline__ float head_rcp(float sum_sq, float inv_dim, float eps
     return ms > 0.0f ? rsqrtf(ms) : 0.0f;
 }
 
-// false: the token's position lies outside the table
-__device__ __forceinline__ bool token_turn(const HeadsParams& P, int64_t t, int sub, const LanePairs& lp, Turn& turn)
+// a token's row of the rotation's table; rows and tokens are below 2^31
+__device__ __forceinline__ int position(const HeadsParams& P, int64_t t) { return P.positions != nullptr ? __ldg(P.positions + t) : (int)t; }
+// false: the position lies outside the table
+template <bool PAIRS>
+__device__ __forceinline__ bool turn_at(const HeadsParams& P, int pos, const LanePairs& lp, Turn& turn)
 {
-    if (P.cos_sin == nullptr) return true;
-    const int64_t pos = P.positions != nullptr ? (int64_t)__ldg(P.positions + t) : t;
     if (pos < 0 || pos >= P.table_rows) return false;
-    if (lp.turns) load_turn(turn, P.cos_sin + pos * P.rot, sub, P.rot);
+    if (lp.turns) load_turn<PAIRS>(turn, P.cos_sin + (int64_t)pos * P.rot, lp, P.rot);
     return true;
 }
 
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(kWarps * 32) rope_fwd_kernel(const HeadsParams
     const int heads = P.heads[0] + P.heads[1];
     const int h0 = part * U * G + grp;
     const bool live = 16 * sub < P.dim;
-    const LanePairs lp = lane_pairs(live ? sub : 0, P.rot, PAIRS);
+    const LanePairs lp = lane_pairs(live ? sub : 0, P.dim, P.rot, PAIRS);
 
     // head h of the two operands as one list
     const uint16_t* const xq = P.x[0] + t * P.x_stride[0];
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kWarps * 32) rope_fwd_kernel(const HeadsParams
         }
     }
     Turn turn;
-    const bool good = token_turn(P, t, sub, lp, turn);
+    const bool good = P.cos_sin == nullptr || turn_at<PAIRS>(P, position(P, t), lp, turn);
     if (!good && lane == 0 && part == 0) atomicAdd(&g_heads_bad, 1u);
     Lane16 g;
     int g_of = -1;   // whose gain g holds
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(kWarps * 32) rope_fwd_kernel(const HeadsParams
         }
         if (P.cos_sin != nullptr) {
             if (!good) fill(x, __uint_as_float(0x7FC00000u));   // loud: no angle for this token
-            else if (lp.turns) apply_turn<false, NORM>(x, turn);
+            else if (lp.turns) apply_turn<false, NORM, PAIRS>(x, turn, lp);
         }
         if (NORM) scale(x, r);   // the rotation leaves a common factor alone
         if (live && h < heads) store<PAIRS>((which ? yk : yq) + h * P.dim + lp.o0, 2 * (lp.o1 - lp.o0), x);
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
     const int64_t begin = items * w / warps, end = items * (w + 1) / warps;
     const bool live = 16 * sub < P.dim;
     const int in_last = heads - (groups - 1) * G;       // heads of a token's last group
-    const LanePairs lp = lane_pairs(live ? sub : 0, P.rot, PAIRS);
+    const LanePairs lp = lane_pairs(live ? sub : 0, P.dim, P.rot, PAIRS);
     const int64_t first = groups > 0 ? begin / groups : 0;
 
     // byte addresses that run along with the walk: what is asked for (d: gradient, x: input) and what is written
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
     uint32_t f_at = ring_at, at = ring_at;
     int fg = begin_group, g = begin_group;
-    int64_t f_left = end - begin;
+    int f_left = (int)(end - begin);   // a CTA for each kWarps items, or kSMs * 4 of them: far below 2^31
     auto fetch = [&]() {
         if (f_left > 0) {
             --f_left;
@@ -256,18 +257,28 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
     }
     Turn turn;
     bool good = true, fresh = true;
-    int64_t t = first;
-    for (int64_t left = end - begin; left > 0; --left) {
+    int t = (int)first;
+    // the token's row of the table, and the next one's: that is on its way to L2 a token ahead of its use
+    auto row_of = [&](int i) { return P.cos_sin != nullptr && i < P.T ? position(P, i) : -1; };
+    auto prefetch = [&](int pos) {
+        if (pos >= 0 && pos < P.table_rows && 8 * lane < P.rot)
+            asm volatile("prefetch.global.L2 [%0];" :: "l"(P.cos_sin + (int64_t)pos * P.rot + 8 * lane));
+    };
+    int pos[2] = {row_of(t), row_of(t + 1)};
+    for (int left = (int)(end - begin); left > 0; --left) {
         fetch();
         if (fresh && P.cos_sin != nullptr) {
-            good = token_turn(P, t, sub, lp, turn);
+            good = turn_at<PAIRS>(P, pos[0], lp, turn);
             if (!good && lane == 0) atomicAdd(&g_heads_bad, 1u);
+            pos[0] = pos[1];
+            prefetch(pos[0]);
+            pos[1] = row_of(t + 2);
         }
         asm volatile("cp.async.wait_group %0;" :: "n"(kRing - 1) : "memory");
         const uint4 cg[2] = {lds16(at), lds16(at + PIECE)};
         Lane16 d;
         unpack<PAIRS>(d, cg);
-        if (P.cos_sin != nullptr && good && lp.turns) apply_turn<true, NORM>(d, turn);
+        if (P.cos_sin != nullptr && good && lp.turns) apply_turn<true, NORM, PAIRS>(d, turn, lp);
         if (NORM) {
             const uint4 cx[2] = {lds16(at + 2 * PIECE), lds16(at + 3 * PIECE)};
             Lane16 x;

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
     const bool rotate = which == 0 && P.cos_sin != nullptr;
     const bool live = 16 * sub < P.dim;
     const int rot = rotate ? P.rot : 0;
-    const LanePairs lp = lane_pairs(live ? sub : 0, rot, PAIRS);
+    const LanePairs lp = lane_pairs(live ? sub : 0, P.dim, rot, PAIRS);
     const int n = (int)P.n, rows = min(__ldg(P.cu + P.seqs), n), first_row = __ldg(P.cu);
     int j = (int)blockIdx.x * P.run;
     const int j_end = min(j + P.run, rows);
@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(kWarps * 32, 6) kv_append_kernel(const KvAppen
             unpack<PAIRS>(x, w);
             if (turns && i < count) {
                 Turn turn;
-                load_turn(turn, angles + i * rot, sub, rot);
-                apply_turn<false, false>(x, turn);
+                load_turn<PAIRS>(turn, angles + i * rot, lp, rot);
+                apply_turn<false, false, PAIRS>(x, turn, lp);
             }
         };
         float top = 0.0f;
