@@ -310,7 +310,8 @@ size_t mxnorm_fwd_host_workspace_bytes(int64_t T, int64_t D, int block, mxn_scal
  * The entry points below take activations as `heads` heads of `head_dim` bf16 elements a token: the heads of a token are
  * contiguous, tokens are `stride` elements apart (so that queries, keys and values can be slices of one fused projection).
  * Pointers are 16-byte aligned, strides multiples of 8 elements and at least heads * head_dim; head_dim is a multiple of 16
- * up to 256 (mxkv_attention: 64 or 128); at most 4096 heads and 2^31 - 1 tokens.  A head count of 0 leaves its pointers unused.
+ * up to 256 (mxkv_attention: 64 or 128); at most 4096 heads and 2^31 - 1 tokens
+ * (max_kv_len: 2^31 - 512).  A head count of 0 leaves its pointers unused.
  *
  * Rotation: with rot_dim rotated elements (a multiple of 16, at most head_dim; the others are passed on) element pairs
  *   MXN_ROPE_HALVES: (i, i + rot_dim/2)      MXN_ROPE_PAIRS: (2i, 2i + 1)      i = 0 .. rot_dim/2 - 1

@@ -581,7 +581,7 @@ int log2_of(int v)
 bool attention_shape_ok(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads, int kv_heads, int dim)
 {
     return n_tokens >= 0 && n_tokens <= kMaxTokens && n_seqs >= 0 && n_seqs <= kMaxTokens && max_q_len >= 1 && max_q_len <= kMaxTokens &&
-           max_kv_len >= 0 && max_kv_len <= kMaxTokens - 64 && kv_heads >= 1 && q_heads >= kv_heads && q_heads <= kMaxHeads &&
+           max_kv_len >= 0 && max_kv_len <= kMaxTokens - 511 && kv_heads >= 1 && q_heads >= kv_heads && q_heads <= kMaxHeads &&
            q_heads % kv_heads == 0 && (dim == 64 || dim == 128);
 }
 

@@ -7,6 +7,10 @@
 // held by dim/16 lanes (see mxn_rope.cuh), so the head's sums take log2(dim/16) shuffles and the rotation none; a warp
 // works on 32*16/dim heads at a time and keeps the token's cosines and sines in registers over all of its heads.
 // The gradient recomputes r from x, which it reads anyway, instead of loading a saved one.
+//
+// Measured, 32 query and 8 key heads of 128: 16384 tokens forward 62 us, 5.4 TB/s; backward with both gains' gradients 89 us, 5.7 TB/s;
+// 64 tokens 2.1 us and 5.1 us, the latency of a start and one (two) trips to memory.  4099 tokens of 32 and 4 heads of 64 in pairs,
+// half of each rotated, backward: 18 us, 3.2 TB/s, of which 2.6 are the second launch that joins the gains' sums and some 3 the start.
 #include <cuda_bf16.h>
 
 #include "mxn_internal.h"
@@ -186,7 +190,8 @@ __global__ void __launch_bounds__(kWarps * 32) rope_fwd_kernel(const HeadsParams
 // One CTA works for the queries or for the keys only (the CTAs are shared out by their head counts), so that a lane carries
 // 16 sums of one gain's gradient.  A warp walks over a contiguous run of (token, group of heads) items, kRing - 1 of which are on
 // their way to shared memory at a time (16-byte asynchronous copies; a thread reads back only what it asked for, so that nothing
-// has to be synchronised): 4 KB in flight a warp against 2 KB that registers would hold.
+// has to be synchronised): 4 KB in flight a warp against 2 KB that registers would hold (16384 tokens: registers 119 us, the ring 94).
+// The row of the rotation's table that the next token needs is asked into L2 a token ahead (94 -> 89 us).
 constexpr int kRing = 4;
 template <int LP, bool PAIRS, bool NORM>
 __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsParams P)

@@ -323,6 +323,13 @@ def test_calls_at_the_same_time(mx):
     assert mx.device_timeouts() == 0
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("qh,nq", [(8, 8), (13, 5), (1, 64), (1, 65)])
+def test_attention_around_64_rows(mx, qh, nq, dim):
+    """64 and 65 query rows for a key head: the last of the one kernel, the first of the other."""
+    check(mx, qh, 1, dim, 64, 16, [nq, nq - 1, 1], [300, nq, 77], seed=qh + nq)
+
+
 def test_attention_bounds_larger_than_the_lengths(mx):
     check(mx, 8, 2, 128, 64, 16, [1, 1], [5, 90], max_q=4, max_len=20000, seed=4)
     check(mx, 8, 2, 64, 64, 16, [3, 40], [500, 90], max_q=64, max_len=5000, seed=5, with_lse=False)
