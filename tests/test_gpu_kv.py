@@ -325,9 +325,26 @@ def test_calls_at_the_same_time(mx):
 
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("qh,nq", [(8, 8), (13, 5), (1, 64), (1, 65)])
-def test_attention_around_64_rows(mx, qh, nq, dim):
-    """64 and 65 query rows for a key head: the last of the one kernel, the first of the other."""
-    check(mx, qh, 1, dim, 64, 16, [nq, nq - 1, 1], [300, nq, 77], seed=qh + nq)
+@pytest.mark.parametrize("longest", [150, 300])
+def test_attention_around_64_rows(mx, qh, nq, dim, longest):
+    """64 and 65 query rows for a key head: the last of the one kernel, the first of the other; a few chunks and more."""
+    check(mx, qh, 1, dim, 64, 16, [nq, nq - 1, 1], [longest, nq, 77], seed=qh + nq)
+
+
+def test_attention_over_its_queries(mx):
+    """out may be q itself: every row is read before it is written, whatever the chunks."""
+    for nq, length, window in (([1], 2000, 0), ([4], 20000, 0), ([70], 500, 0), ([300], 900, 100)):
+        table, pool = make_table([length], -(-length // 64), 64, 5)
+        cache = Cache(pool, 2, 64, 128, 16)
+        fill(cache, [length], table, 64, 16, 5)
+        q = torch.randn(nq[0], 8, 128, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+        nbytes = mx.mxkv_attention_workspace_bytes(nq[0], 1, nq[0], length, 8, 2, 128)
+        ws = torch.empty(max(16, nbytes), dtype=torch.uint8, device="cuda")
+        fixed = (dev([0] + nq), dev([length]), dev(table), *cache.parts)
+        out = torch.empty_like(q)
+        mx.mxkv_attention(q, *fixed, out, nq[0], length, 0.1, window=window, workspace=ws)
+        mx.mxkv_attention(q, *fixed, q, nq[0], length, 0.1, window=window, workspace=ws)
+        assert torch.equal(q, out)
 
 
 def test_attention_bounds_larger_than_the_lengths(mx):
