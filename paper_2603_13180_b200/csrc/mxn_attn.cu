@@ -743,15 +743,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 }  // namespace
 
 // How the keys are shared out: from sizes alone, so that the workspace can be asked for ahead of the call.
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim)
+namespace {
+
+// wide: heads of 64, 17 to 64 rows: 32 rows a warp (two warps where there are more), else 16 and more CTAs
+AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim, bool wide)
 {
     AttnPlan a{};
-    if (max_q > n) max_q = n;
     const int64_t rows = max_q * (q_heads / kv_heads);
     a.prompt = rows > kPromptRows;
     // a warp holds the output of up to 16 rows of 128 or 32 of 64; more rows are shared out among the CTA's warps
-    a.row_eights = rows <= 8 ? 1 : rows <= 16 || dim == 128 ? 2 : 4;
-    a.row_warps = (int)(rows <= 8 * a.row_eights ? 1 : rows <= 16 * a.row_eights ? 2 : 4);
+    a.row_eights = rows <= 8 ? 1 : rows <= 16 || dim == 128 || !wide ? 2 : 4;
+    a.row_warps = dim == 64 && a.row_eights == 2 ? 1 : (int)(rows <= 8 * a.row_eights ? 1 : rows <= 16 * a.row_eights ? 2 : 4);
     const int64_t tile_rows = a.prompt ? 256 : 8 * a.row_eights * a.row_warps;
     a.row_tiles = ceil_div(rows, tile_rows);
     const int64_t units = seqs * kv_heads * a.row_tiles, tile = a.prompt ? 128 : kTile;
@@ -791,6 +793,21 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
         a.ctas = 2 * units - a.whole_units;
     }
     return a;
+}
+
+}  // namespace
+
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim)
+{
+    if (max_q > n) max_q = n;
+    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, q_heads, kv_heads, dim, true);
+    if (a.prompt || a.row_eights != 4) return a;
+    // 32 rows a warp save conversions, 16 hide latency better: taken unless a few chunks of all sequences fit side by side
+    // (32 sequences of four drafted tokens, window 1024: 32 rows 19 us, 16 rows 29; 64 sequences of 4100 keys: 83 and 79; 16 of
+    // 8000, eight tokens: 75 and 66).  The workspace is that of either, whatever the window.
+    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, q_heads, kv_heads, dim, false);
+    a.workspace = b.workspace = a.workspace > b.workspace ? a.workspace : b.workspace;
+    return a.cluster ? a : b;
 }
 
 cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, cudaStream_t stream)
