@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     cluster_sync();   // nobody leaves while its shared memory is read
 }
 
-// joins the chunks of each row.  A CTA takes a row: each of its eight warps adds every eighth chunk, four at a time in flight, and
+// joins the chunks of each row.  A CTA takes a row: each of its eight warps adds every eighth chunk, eight at a time in flight, and
 // the warps' sums are added in order.
 constexpr int kJoinWarps = 8;
 template <int DIM>
@@ -630,26 +630,40 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnPa
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = blockIdx.x, tok = blockIdx.x / (uint32_t)P.q_heads;
-    // rows of no sequence are left as they were
-    if (tok >= min((int64_t)__ldg(P.cu_q + P.seqs), P.n) || tok < __ldg(P.cu_q)) return;
+    const int first = __ldg(P.cu_q), end = __ldg(P.cu_q + P.seqs);
     const float* const part = P.part_lse + row * P.splits;
+    // a warp's chunks, eight at a time, asked for before anything is known about them
+    float li[8], v[8][E];
+    auto ask = [&](int from) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = from + kJoinWarps * k + warp;
+            li[k] = -INFINITY;
+            if (i < P.splits) {
+                li[k] = part[i];
+                const float* const p = P.part_out + (row * P.splits + i) * DIM + lane * E;
+                if constexpr (E == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(p);
+                else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(p);
+            }
+        }
+    };
+    ask(0);
     float top = -INFINITY;
     for (int i = lane; i < P.splits; i += 32) top = fmaxf(top, part[i]);
+    if (tok >= end || tok < first) return;   // rows of no sequence are left as they were
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const bool none = top == -INFINITY;
     float sum = 0.0f, acc[E] = {};
-    if (!none) {
-#pragma unroll 4
-        for (int i = warp; i < P.splits; i += kJoinWarps) {
-            const float li = part[i], f = ex2(li - top);
-            sum += f;
-            const float* const p = P.part_out + (row * P.splits + i) * DIM + lane * E;
-            float v[E];
-            if constexpr (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-            else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(p);
+    for (int from = 0; from < P.splits; from += 8 * kJoinWarps) {
+        if (from > 0) ask(from);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = li == -INFINITY ? acc[e] : fmaf(v[e], f, acc[e]);   // (an empty chunk wrote no row)
+        for (int k = 0; k < 8; ++k) {
+            if (li[k] == -INFINITY) continue;   // an empty chunk wrote no row
+            const float f = ex2(li[k] - top);
+            sum += f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
         }
     }
 #pragma unroll
@@ -670,6 +684,48 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnPa
         reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM)[threadIdx.x] = pack_bf16(a * inv, b * inv);
     }
     if (P.lse != nullptr && threadIdx.x == 0) P.lse[row] = none ? -INFINITY : (top + log2f(all)) * kLn2;
+}
+
+// the same for up to eight chunks: a warp takes a row, with all of its loads at once
+template <int DIM>
+__global__ void __launch_bounds__(kJoinWarps * 32) attn_join_few_kernel(const AttnParams P)
+{
+    constexpr int E = DIM / 32;
+    pdl_prologue();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+    if (row >= P.n * P.q_heads) return;
+    const int64_t tok = (uint32_t)row / (uint32_t)P.q_heads;
+    const int first = __ldg(P.cu_q), end = __ldg(P.cu_q + P.seqs);
+    float lse[8], v[8][E];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        lse[k] = -INFINITY;
+        if (k < P.splits) {
+            lse[k] = P.part_lse[row * P.splits + k];
+            const float* const p = P.part_out + (row * P.splits + k) * DIM + lane * E;
+            if constexpr (E == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(p);
+            else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(p);
+        }
+    }
+    if (tok >= end || tok < first) return;   // rows of no sequence are left as they were
+    float top = lse[0], sum = 0.0f, acc[E] = {};
+#pragma unroll
+    for (int k = 1; k < 8; ++k) top = fmaxf(top, lse[k]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (lse[k] == -INFINITY) continue;   // an empty chunk wrote no row
+        const float f = ex2(lse[k] - top);
+        sum += f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+    }
+    const bool none = top == -INFINITY;
+    const float inv = none ? 0.0f : __fdiv_rn(1.0f, sum);
+    uint32_t* const y = reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM + lane * E);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) y[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+    if (P.lse != nullptr && lane == 0) P.lse[row] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 template <class K, class... Args>
@@ -828,9 +884,12 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     else
         e = launch_rows(P, M, a, stream);
     if (e != cudaSuccess || a.splits == 1 || a.cluster) return e;
-    const int64_t ctas = P.n * P.q_heads;
-    return P.dim == 128 ? launch(attn_join_kernel<128>, ctas, 1, kJoinWarps * 32, 0, stream, P)
-                        : launch(attn_join_kernel<64>, ctas, 1, kJoinWarps * 32, 0, stream, P);
+    const int64_t rows = P.n * P.q_heads;
+    if (a.splits <= 8)
+        return P.dim == 128 ? launch(attn_join_few_kernel<128>, ceil_div(rows, kJoinWarps), 1, kJoinWarps * 32, 0, stream, P)
+                            : launch(attn_join_few_kernel<64>, ceil_div(rows, kJoinWarps), 1, kJoinWarps * 32, 0, stream, P);
+    return P.dim == 128 ? launch(attn_join_kernel<128>, rows, 1, kJoinWarps * 32, 0, stream, P)
+                        : launch(attn_join_kernel<64>, rows, 1, kJoinWarps * 32, 0, stream, P);
 }
 
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad)
