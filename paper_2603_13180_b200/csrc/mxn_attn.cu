@@ -24,7 +24,7 @@
 // With several chunks a CTA's result is (normalised row, logarithm of its sum).  Up to eight chunks are joined by their CTAs as a
 // cluster, through each other's shared memory; more go to the workspace and are joined in a fixed order by a second kernel.
 //
-// Measured (32 query and 8 key heads of 128): 64 sequences of up to 8192 keys 119 us, 5.7 TB/s; one of 131072 keys 52 us, 5.2 TB/s with
+// Measured (32 query and 8 key heads of 128): 64 sequences of up to 8192 keys 115 us, 5.9 TB/s; one of 131072 keys 50 us, 5.4 TB/s with
 // the join; one of 1000 keys 5.8 us, which is a start, two trips to memory and the join.  32 sequences of four drafted tokens, 32
 // and 4 heads of 64, window 1024: 19 us, bound by the chain of a warp's tiles (nine of 32 query rows, then the join).
 //
@@ -816,8 +816,8 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
     const int64_t step = a.prompt ? 128 : kTile * (kWarps / a.row_warps);   // keys that a CTA works on at a time
     // Chunks: as many as the CTAs that are resident at a time leave room for; four rounds of them where sequences may differ in
     // length (64 sequences of 2048 ... 8192 keys: one round 152 us, four 135 us).  A chunk is at least eight steps long, so that a
-    // CTA's start and the join are worth it (64 sequences of up to 2000 keys: 41 us, five steps 43), or five where half of the places
-    // would stay empty (16 sequences: eight 20 us, five 16), less only where most SMs would be idle.
+    // CTA's start and the join are worth it (64 sequences of up to 2000 keys: 37 us, five steps 40), or five where half of the places
+    // would stay empty (16 sequences: eight 20 us, five 16, 14 with the join as it is now), less only where most SMs would be idle.
     const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : decode_ctas(dim, a.row_eights));
     int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
