@@ -310,14 +310,14 @@ size_t mxnorm_fwd_host_workspace_bytes(int64_t T, int64_t D, int block, mxn_scal
  * The entry points below take activations as `heads` heads of `head_dim` bf16 elements a token: the heads of a token are
  * contiguous, tokens are `stride` elements apart (so that queries, keys and values can be slices of one fused projection).
  * Pointers are 16-byte aligned, strides multiples of 8 elements and at least heads * head_dim; head_dim is a multiple of 16
- * up to 256 (mxkv_attention: 64 or 128); at most 4096 heads and 2^31 - 1 tokens
- * (max_kv_len: 2^31 - 512).  A head count of 0 leaves its pointers unused.
+ * up to 256 (mxkv_attention: 64 or 128); at most 4096 heads and 2^31 - 1 tokens (max_kv_len: 2^31 - 512).  A head count of 0
+ * leaves its pointers unused.
  *
  * Rotation: with rot_dim rotated elements (a multiple of 16, at most head_dim; the others are passed on) element pairs
  *   MXN_ROPE_HALVES: (i, i + rot_dim/2)      MXN_ROPE_PAIRS: (2i, 2i + 1)      i = 0 .. rot_dim/2 - 1
  * are turned: (a, b) -> (a cos - b sin, b cos + a sin).  cos_sin is fp32 [table_rows, rot_dim], 16-byte aligned: row p holds
  * the rot_dim/2 cosines, then the rot_dim/2 sines of position p (usually of p * base^(-2i/rot_dim), computed in binary64).
- * Products and sums of the rotation are single binary32 operations.
+ * Products and sums of the rotation are single binary32 operations; together with the norm, a product and a sum may share a rounding.
  *
  * Indices that live in device memory cannot be refused by the call; the kernels check them.  A position outside the table,
  * a page number outside the pool, a length shorter than the new tokens: the token or block concerned is left out as stated
@@ -393,7 +393,8 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
  *   which are kept to 2^-18 of it; the softmax's weights have 11 significant bits (fewer where a weight times its value block's
  *   scale lies below 2^-13 of the row's largest such product), its sums are binary32.
  *   What stands in the cache behind a sequence's last token, or in pages no visible key is in, has no influence.  A page out of
- *   range among the visible ones: its keys are left out.
+ *   range among the visible ones: its keys are left out.  A query row with an infinity or NaN, or one that sees a NaN key, gets
+ *   NaN; so may every row of a sequence one of whose values is NaN (its weight is 0 where it is not seen).
  *   workspace: device memory, 16-byte aligned, at least mxkv_attention_workspace_bytes(...) bytes for the same sizes (0: none
  *   needed); contents irrelevant before and after.  Calls that may overlap need workspaces of their own. */
 mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,

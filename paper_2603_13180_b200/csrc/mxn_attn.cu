@@ -282,7 +282,8 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
         const uint32_t E = __float_as_uint(quad_max(hmax_abs_to_f32(m))) >> 23;
         const uint32_t Ec = min(max(E, 15u), 254u);
-        const float up = __uint_as_float((268u - Ec) << 23);                                // 2^(14 - (E - 127))
+        // 2^(14 - (E - 127)); with an infinity or NaN in the row its result is NaN
+        const float up = E == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((268u - Ec) << 23);
         const float factor = P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23);          // ... and its inverse
         row_factor[2 * x] = __shfl_sync(0xFFFFFFFFu, factor, 8 * c);
         row_factor[2 * x + 1] = __shfl_sync(0xFFFFFFFFu, factor, 8 * c + 4);
@@ -554,7 +555,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
             o[0] = fmaf(u.x, by, o[0]); o[1] = fmaf(u.y, by, o[1]); o[2] = fmaf(u.z, by, o[2]); o[3] = fmaf(u.w, by, o[3]);
             o[4] = fmaf(v.x, by, o[4]); o[5] = fmaf(v.y, by, o[5]); o[6] = fmaf(v.z, by, o[6]); o[7] = fmaf(v.w, by, o[7]);
         }
-        const bool some = sum > 0.0f;                                     // a row that sees nothing: zeros
+        const bool some = sum != 0.0f;                                    // a row that sees nothing: zeros (NaN scores: NaN)
         const float inv = some ? __fdiv_rn(1.0f, sum) : 0.0f;
         const int qt = P.by_group(row), head = h * G + row - qt * G;
         const int64_t tok = q0 + qt, out_row = tok * P.q_heads + head;
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
             o[0] = fmaf(u[k].x, by, o[0]); o[1] = fmaf(u[k].y, by, o[1]); o[2] = fmaf(u[k].z, by, o[2]); o[3] = fmaf(u[k].w, by, o[3]);
             o[4] = fmaf(v[k].x, by, o[4]); o[5] = fmaf(v[k].y, by, o[5]); o[6] = fmaf(v[k].z, by, o[6]); o[7] = fmaf(v[k].w, by, o[7]);
         }
-        const bool some = sum > 0.0f;
+        const bool some = sum != 0.0f;
         const float inv = some ? __fdiv_rn(1.0f, sum) : 0.0f;
         const int qt = P.by_group(row), head = h * G + row - qt * G;
         const int64_t tok = q0 + qt;
@@ -653,7 +654,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnPa
     if (tok >= end || tok < first) return;   // rows of no sequence are left as they were
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const bool none = top == -INFINITY;
     float sum = 0.0f, acc[E] = {};
     for (int from = 0; from < P.splits; from += 8 * kJoinWarps) {
         if (from > 0) ask(from);
@@ -673,6 +673,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_kernel(const AttnPa
     float all = 0.0f;
 #pragma unroll
     for (int k = 0; k < kJoinWarps; ++k) all += sums[k][DIM];
+    const bool none = all == 0.0f;
     const float inv = none ? 0.0f : __fdiv_rn(1.0f, all);
     if (threadIdx.x < DIM / 2) {
         float a = 0.0f, b = 0.0f;
@@ -720,7 +721,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_join_few_kernel(const At
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
     }
-    const bool none = top == -INFINITY;
+    const bool none = sum == 0.0f;
     const float inv = none ? 0.0f : __fdiv_rn(1.0f, sum);
     uint32_t* const y = reinterpret_cast<uint32_t*>(P.out + tok * P.out_stride + (row - tok * P.q_heads) * DIM + lane * E);
 #pragma unroll

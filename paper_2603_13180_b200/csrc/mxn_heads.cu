@@ -8,7 +8,7 @@
 // works on 32*16/dim heads at a time and keeps the token's cosines and sines in registers over all of its heads.
 // The gradient recomputes r from x, which it reads anyway, instead of loading a saved one.
 //
-// Measured, 32 query and 8 key heads of 128: 16384 tokens forward 61 us, 5.5 TB/s; backward with both gains' gradients 89 us, 5.7 TB/s;
+// Measured, 32 query and 8 key heads of 128: 16384 tokens forward 62 us, 5.4 TB/s; backward with both gains' gradients 89 us, 5.7 TB/s;
 // 64 tokens 2.1 us and 5.1 us, the latency of a start and one (two) trips to memory.  4099 tokens of 32 and 4 heads of 64 in pairs,
 // half of each rotated, backward: 18 us, 3.2 TB/s, of which 2.6 are the second launch that joins the gains' sums and some 3 the start.
 #include <cuda_bf16.h>
@@ -108,7 +108,7 @@ __device__ __forceinline__ float head_sum(float v)
 __device__ __forceinline__ float head_rcp(float sum_sq, float inv_dim, float eps)
 {
     const float ms = fmaf(sum_sq, inv_dim, eps);
-    return ms > 0.0f ? rsqrtf(ms) : 0.0f;
+    return ms != 0.0f ? rsqrtf(ms) : 0.0f;   // a NaN stays one
 }
 
 // a token's row of the rotation's table; rows and tokens are below 2^31
@@ -122,10 +122,12 @@ __device__ __forceinline__ bool turn_at(const HeadsParams& P, int pos, const Lan
     return true;
 }
 
-// A warp takes U * G heads of one token, all of its loads at once.  Five CTAs an SM need the gain to stay packed in its registers (16384
-// tokens, 32 + 8 heads of 128: halves 62.3 -> 61.3 us, pairs 63.9 -> 60.6; 16 + 2 heads of 256: 64.8 -> 58.6).
+// A warp takes U * G heads of one token, all of its loads at once.  `tight`: five CTAs an SM instead of four, for which the gain has to
+// stay packed in its registers.  16384 tokens: 32 + 8 heads of 128 in pairs 63.9 -> 60.6 us, 16 + 2 heads of 256 64.8 -> 58.6, but 32 + 8
+// heads of 128 in halves 64.7 -> 67.5.
+__host__ __device__ constexpr bool tight(int lanes, bool pairs) { return pairs || lanes == 16; }
 template <int LP, int U, bool PAIRS, bool NORM>
-__global__ void __launch_bounds__(kWarps * 32, 5) rope_fwd_kernel(const HeadsParams P)
+__global__ void __launch_bounds__(kWarps * 32, tight(LP, PAIRS) ? 5 : 1) rope_fwd_kernel(const HeadsParams P)
 {
     constexpr int G = 32 / LP;   // heads a warp holds at a time
     pdl_prologue();
@@ -159,7 +161,8 @@ __global__ void __launch_bounds__(kWarps * 32, 5) rope_fwd_kernel(const HeadsPar
     const bool good = P.cos_sin == nullptr || turn_at<PAIRS>(P, position(P, t), lp, turn);
     if (!good && lane == 0 && part == 0) atomicAdd(&g_heads_bad, 1u);
     uint4 gw[2];
-    int g_of = -1;   // whose gain gw holds
+    Lane16 g;
+    int g_of = -1;   // whose gain they hold
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int h = h0 + u * G;
@@ -174,10 +177,10 @@ __global__ void __launch_bounds__(kWarps * 32, 5) rope_fwd_kernel(const HeadsPar
                 if (g_of != which) {
                     gw[0] = __ldg(reinterpret_cast<const uint4*>(gain + lp.o0));
                     gw[1] = __ldg(reinterpret_cast<const uint4*>(gain + lp.o1));
+                    if (!tight(LP, PAIRS)) unpack<PAIRS>(g, gw);
                     g_of = which;
                 }
-                Lane16 g;
-                unpack<PAIRS>(g, gw);
+                if (tight(LP, PAIRS)) unpack<PAIRS>(g, gw);
                 scale(x, g);
             }
         }

@@ -23,13 +23,13 @@
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
 //
 // Bound: at head size 128 the two products of a 256 x 128 tile take 2048 cycles at the tensor cores' rate, its 32768 exponentials
-// 2048 cycles of the special function units.  4096 queries over 8192 keys, 32 query and 8 key heads of 128: 437 us, 940 TFLOP/s, 59 %
+// 2048 cycles of the special function units.  4096 queries over 8192 keys, 32 query and 8 key heads of 128: 446 us, 925 TFLOP/s, 56 %
 // of a large library product's measured rate; a tile takes some 3900 cycles.  Without the softmax's arithmetic the same kernel takes
 // 310 us: what is left is the softmax's chain of loads, maxima, exponentials and stores, two warps for each scheduler, with the special
 // function units busy for half of the time.  Four warps for each scheduler (two for a row) took 595 us: twice the fixed costs
 // of a step.  What shortened the chain: barriers and scales looked at a step ahead, while shared memory is busy with the products'
 // operands (499 -> 478); a rounding of the maximum taken out of it (501 -> 493); q read by rows, 12 warps at it, and the
-// output written by rows through shared memory (464 -> 450).
+// output written by rows through shared memory (464 -> 450), the last units in halves (-> 437).  NaN scores kept as such: 446.
 //
 // Every wait is bounded; see mxn_device_timeouts.
 #include <cuda_bf16.h>
@@ -178,7 +178,13 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
 __device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
 {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
 __device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
@@ -299,6 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             const uint32_t E = __float_as_uint(m) >> 23, Ec = min(max(E, 8u), 254u);
             float up = __uint_as_float((261u - Ec > 254u ? 254u : 261u - Ec) << 23);             // 2^(7 - (E - 127))
             if (P.scale < 0.0f) up = -up;
+            if (E == 255u) up = __uint_as_float(0x7FC00000u);   // an infinity or NaN: the row's result is NaN (E4M3 has no infinity)
             uint32_t hh[4], ll[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -603,8 +610,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 float m = max3(y[0], y[1], y[2]);
 #pragma unroll
                 for (int e = 3; e < 15; e += 2) m = max3(__float_as_uint(m), y[e], y[e + 1]);
-                m = fmaxf(m, __uint_as_float(y[15]));
-                utop = fmaxf(utop, fmaf(m, fac[g], slot_v[g]));
+                m = max_nan(m, __uint_as_float(y[15]));
+                utop = max_nan(utop, fmaf(m, fac[g], slot_v[g]));
             }
             top_all = fmaxf(top_all, utop);
             if (__any_sync(0xFFFFFFFFu, utop > ref + kUp || (utop < ref - kDown && utop > kNone))) {
@@ -629,7 +636,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 }
             }
             // weights, over their scores
-            const float shift_by = ref == kNone ? 0.0f : kTop - ref;
+            // a NaN among the scores reaches all of the step's weights: the polynomial below would take it for a small number
+            const float shift_by = utop != utop ? utop : ref == kNone ? 0.0f : kTop - ref;
             float extra = 0.0f;
             if (wide && ref > kNone) {   // the sum by exponentials of its own, from the scores as they still stand
 #pragma unroll 1
@@ -665,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 more = fmaf(both.x + both.y, slot_l[g], more);
                 if (g & 1) probe[g >> 1] = mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             }
-            l += wide ? extra : more;
+            l += wide && more == more ? extra : more;
             tm_store32(s_at, w);
             here = __all_sync(0xFFFFFFFFu, i + 1 < steps && (probe[0] || probe[1]));
             scales_here = __all_sync(0xFFFFFFFFu, probe[2]);
@@ -679,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
         // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 1 - c0
-        const bool some = ref > kNone;
+        const bool some = ref > kNone || l != l;   // (NaN scores set no reference)
         const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
         const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
         const int64_t out_row = tok * P.q_heads + head;

@@ -178,6 +178,26 @@ def test_backward_on_a_stream_and_captured(mx):
     assert all(torch.equal(a, 2 * b) for a, b in zip(results(), want))
 
 
+def test_nan_stays_in_its_head(mx):
+    """A NaN makes its whole head NaN, forward and backward, and no other."""
+    T, hq, hk, D, rot = 9, 6, 2, 64, 32
+    q, k, gains, table, pos, g = inputs(T, hq, hk, D, rot, 50, seed=6)
+    dy = torch.randn(T, hq, D, generator=g).to(torch.bfloat16).cuda()
+    results = []
+    for value in (None, float("nan")):
+        if value is not None:
+            q[4, 3, 40] = value
+        qo, ko, dq = torch.empty(T, hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty_like(k.contiguous()), torch.empty_like(dy)
+        mx.rmsnorm_rope_fwd(q, k, gains[0], gains[1], table, pos, qo, ko)
+        mx.rmsnorm_rope_bwd(q, None, dy, None, gains[0], None, table, pos, dq, None)
+        results.append((qo, ko, dq))
+    for clean, got in zip(results[0], results[1]):
+        if clean.shape[1] == hq:
+            assert bool(got[4, 3].isnan().all())
+            got[4, 3] = clean[4, 3]
+        assert torch.equal(clean, got)
+
+
 def test_positions_outside_the_table(mx):
     T, hq, hk, D, rot = 9, 3, 1, 64, 64
     q, k, gains, table, _, g = inputs(T, hq, hk, D, rot, 50, seed=2)

@@ -331,6 +331,46 @@ def test_attention_around_64_rows(mx, qh, nq, dim, longest):
     check(mx, qh, 1, dim, 64, 16, [nq, nq - 1, 1], [longest, nq, 77], seed=qh + nq)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,length", [(1, 90), (1, 1500), (4, 30000), (40, 300), (90, 200), (200, 3000)])
+def test_attention_infinities_and_nan(mx, dim, nq, length):
+    """A row with an infinity or NaN among its queries, and rows that see a NaN key, are NaN; the others keep their bits."""
+    table, pool = make_table([length], -(-length // 32), 32, 7)
+    cache = Cache(pool, 2, 32, dim, 16)
+    fill(cache, [length], table, 32, 16, 7)
+    g = torch.Generator().manual_seed(nq)
+    q = torch.randn(nq, 4, dim, generator=g).to(torch.bfloat16).cuda()
+    nbytes = mx.mxkv_attention_workspace_bytes(nq, 1, nq, length, 4, 2, dim)
+    ws = torch.empty(max(16, nbytes), dtype=torch.uint8, device="cuda")
+
+    def run():
+        out, lse = torch.empty_like(q), torch.empty(nq, 4, device="cuda")
+        mx.mxkv_attention(q, dev([0, nq]), dev([length]), dev(table), *cache.parts, out, nq, length, dim ** -0.5, lse=lse, workspace=ws)
+        return out, lse
+
+    clean, clean_lse = run()
+    assert bool(clean.isfinite().all())
+    for value in (float("inf"), float("-inf"), float("nan")):
+        keep = q.clone()
+        q[nq // 2, 1, 5] = value
+        out, lse = run()
+        assert bool(out[nq // 2, 1].isnan().all()) and bool(lse[nq // 2, 1].isnan())
+        out[nq // 2, 1], lse[nq // 2, 1] = clean[nq // 2, 1], clean_lse[nq // 2, 1]
+        assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+        q.copy_(keep)
+    # a NaN key of one head, among the new tokens' places: rows before it do not see it
+    for back in sorted({0, min(nq - 1, 1), nq // 2}):
+        at = length - 1 - back
+        place = (table[0][at // 32], 1, at % 32, 3)
+        code = int(cache.parts[0][place])
+        cache.parts[0][place] = NAN_CODE
+        out, lse = run()
+        sees = nq - 1 - back
+        assert bool(out[sees:, 2:].isnan().all()) and bool(lse[sees:, 2:].isnan().all())
+        assert torch.equal(out[:sees], clean[:sees]) and torch.equal(out[:, :2], clean[:, :2])
+        cache.parts[0][place] = code
+
+
 def test_attention_over_its_queries(mx):
     """out may be q itself: every row is read before it is written, whatever the chunks."""
     for nq, length, window in (([1], 2000, 0), ([4], 20000, 0), ([70], 500, 0), ([300], 900, 100)):
