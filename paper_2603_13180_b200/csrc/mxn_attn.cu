@@ -84,11 +84,6 @@ __device__ __forceinline__ float quad_max(float v)
     v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
     return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
 }
-__device__ __forceinline__ float quad_sum(float v)
-{
-    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
-    return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);

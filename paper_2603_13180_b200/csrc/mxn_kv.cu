@@ -9,10 +9,11 @@
 // One warp owns one (block of tokens, head) of the keys or of the values, so that no two warps ever meet in a block and no
 // atomic is needed.  A warp is given a run of token rows and works on the blocks whose first new token lies in its run; the
 // first 16 tokens (8 of heads beyond 128) of a block are copied to shared memory all at once and read there for the maximum and
-// for the codes, the others are read again from L1.  The run's rows are asked into L2 while the warp looks up its sequence.  Bound: HBM, 3 bytes an element
-// (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of loads.  Measured, 8 heads of 128 in
-// blocks of 16: six prompts of up to 4096 tokens 31 us, 3.5 TB/s (the shared-memory round trip and the conversions keep half of the
-// issue slots busy); one token for each of 64 sequences 3.7 us.
+// for the codes, the others are read again from L1.  The run's rows are asked into L2 while the warp looks up its sequence.
+//
+// Bound: HBM, 3 bytes an element (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of
+// loads.  Measured, 8 heads of 128 in blocks of 16: six prompts of up to 4096 tokens 31 us, 3.5 TB/s (the shared-memory round trip and
+// the conversions keep half of the issue slots busy); one token for each of 64 sequences 3.7 us.
 #include "mxn_async.cuh"
 #include "mxn_internal.h"
 #include "mxn_rope.cuh"
