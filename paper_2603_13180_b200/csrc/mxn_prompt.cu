@@ -639,7 +639,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             // a NaN among the scores reaches all of the step's weights: the polynomial below would take it for a small number
             const float shift_by = utop != utop ? utop : ref == kNone ? 0.0f : kTop - ref;
             float extra = 0.0f;
-            if (wide && ref > kNone) {   // the sum by exponentials of its own, from the scores as they still stand
+            // the sum by exponentials of its own, from the scores as they still stand; the whole warp or none of it (the loads are the
+            // warp's), whether or not each of its rows has seen a key
+            if (wide && __any_sync(0xFFFFFFFFu, ref > kNone)) {
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     uint32_t z[16];
@@ -648,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                     const float f = fmaxf(row_factor * slot_k[g], 1.17549435e-38f), add = c0 + kTop - ref;
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if ((see >> e) & 1u) extra += ex2(fmaf(__uint_as_float(z[e]), f, add));
+                        if (((see >> e) & 1u) && ref > kNone) extra += ex2(fmaf(__uint_as_float(z[e]), f, add));
                 }
             }
             uint32_t w[32];
