@@ -149,13 +149,11 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     const int h = (int)(b % (uint32_t)P.kv_heads);
     const int seq = (int)(b / (uint32_t)P.kv_heads);
 
-    const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
-    const int len = min(__ldg(P.lens + seq), P.max_len);
-    const int nq = max(0, min(q1 - q0, P.max_q));
+    const AttnSequence S = attn_sequence(P, seq);
+    const int q0 = S.q0, len = S.len, shift = S.shift, nq = S.nq;
     const int G = P.group, row0 = rt * Sh::kRows, rows = nq * G;
-    if (q0 < 0 || row0 >= rows) return;
+    if (row0 >= rows) return;
     // keys that any row of this tile sees: [lo, hi)
-    const int shift = len - (q1 - q0);              // position of the sequence's first query
     const int last = min(rows, row0 + Sh::kRows) - 1;
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
     const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;

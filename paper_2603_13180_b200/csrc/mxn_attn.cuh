@@ -18,6 +18,24 @@ cudaError_t launch_prompt(const AttnParams& P, const AttnMaps& M, int64_t ctas, 
 cudaError_t read_prompt_counters(unsigned int* timeouts, unsigned int* bad);
 cudaError_t reset_prompt_counters(bool timeouts);
 
+// A sequence's rows and places.  The last query stands at the sequence's last token, however many of the rows or of the keys the
+// call's bounds let through: places go by the lists as they stand, the bounds only cut what is computed and read.
+struct AttnSequence {
+    int q0, nq;    // first row, rows computed (0 where the list of rows is no rising one)
+    int shift;     // place of the first query
+    int len;       // keys that may be read
+};
+__device__ __forceinline__ AttnSequence attn_sequence(const AttnParams& P, int seq)
+{
+    AttnSequence s;
+    s.q0 = __ldg(P.cu_q + seq);
+    const int end = __ldg(P.cu_q + seq + 1), all = max(0, __ldg(P.lens + seq));
+    s.nq = s.q0 < 0 || end <= s.q0 ? 0 : max(0, min(min(end, (int)P.n) - s.q0, P.max_q));
+    s.shift = s.nq > 0 ? all - (end - s.q0) : 0;
+    s.len = min(all, P.max_len);
+    return s;
+}
+
 // tiled copy of a box of codes (no multicast); x = 0, y = first token within its page, z = page * heads + head
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar)
 {

@@ -234,13 +234,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const int h = (int)(b % (uint32_t)P.kv_heads);
     const int block = P.row_tiles - 1 - (int)(b / (uint32_t)P.kv_heads);   // the rows that see most keys first
 
-    const int q0 = __ldg(P.cu_q + seq), q1 = min(__ldg(P.cu_q + seq + 1), (int)P.n);
-    const int len = min(__ldg(P.lens + seq), P.max_len);
-    const int nq = max(0, min(q1 - q0, P.max_q));
+    const AttnSequence S = attn_sequence(P, seq);
+    const int q0 = S.q0, len = S.len, shift = S.shift, nq = S.nq;
     const int G = P.group, row0 = (2 * block + (half == 1)) * kTile, rows = min(nq * G, row0 + (half < 0 ? 2 : 1) * kTile);
-    if (q0 < 0 || row0 >= rows) return;
+    if (row0 >= rows) return;
     const bool two = rows - row0 > kTile;   // else nothing is done for the second row tile
-    const int shift = len - (q1 - q0);
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(rows - 1) + 1 : len));
     const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);

@@ -1,12 +1,71 @@
 """mxkv_attention and mxkv_append where scales, windows, bounds and places go to their ends.
 
 Tolerances are those of test_gpu_kv.py, whose helpers are used, unless a test says otherwise."""
+import math
+
 import pytest
 import torch
 
-from tests.test_gpu_kv import check, mx  # noqa: F401  (mx is the fixture)
+from tests import qkv_ref as ref
+from tests.test_gpu_kv import Cache, check, cumulative, dev, fill, make_table, mx  # noqa: F401  (mx is the fixture)
 
 pytestmark = pytest.mark.gpu
+
+
+def dense(q, place, k, v, scale, causal, window, limit):
+    """(out, lse, sum of softmax |v|, largest sum of |scale q k|) of one head in 64 bits: queries q [n, D] at `place` [n] over keys and
+    values [length, D], of which those from `limit` on are not seen."""
+    key = torch.arange(k.shape[0], device=k.device)[None]
+    seen = (key < limit) & ((key <= place[:, None]) if causal else (key >= 0))
+    if window:
+        seen = seen & (key > place[:, None] - window)
+    z = (q.double() @ k.T * scale).masked_fill(~seen, -math.inf)
+    p = torch.nan_to_num(torch.softmax(z, -1), 0.0)
+    big = ((q.double().abs() @ k.abs().T) * abs(scale)).masked_fill(~seen, 0).amax(-1)
+    return p @ v, torch.logsumexp(z, -1), p @ v.abs(), big
+
+
+def near(out, lse, want, want_lse, mag, big):
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * mag + 1e-30
+    assert bool(((out.double() - want).abs() <= tol).all()), f"out: {float(((out.double() - want).abs() / tol).max()):.3g} tolerances"
+    live = want_lse > -math.inf
+    assert bool((lse[~live] == -math.inf).all()) and not bool(out[~live].any())
+    t = (16 * 2.0 ** -23 * big + 2.0 ** -19 + 5 * 2.0 ** -23 * want_lse.abs())[live]
+    e = (lse.double() - want_lse).abs()[live]
+    assert bool((e <= t).all()), f"lse: {float((e / t).max()):.3g} tolerances"
+
+
+def attend(mx, q, cu, lens, table, cache, max_q, max_len, scale, **options):  # noqa: F811
+    """(out, lse) with rows that the call leaves alone at 7."""
+    n, q_heads, dim = q.shape
+    out, lse = torch.full_like(q, 7.0, memory_format=torch.contiguous_format), torch.full((n, q_heads), 7.0, device="cuda")
+    nbytes = mx.mxkv_attention_workspace_bytes(n, len(lens), max_q, max_len, q_heads, cache.parts[0].shape[1], dim)
+    ws = torch.full((max(16, nbytes),), 0xFF, dtype=torch.uint8, device="cuda")
+    mx.mxkv_attention(q, dev(cu), dev(lens), dev(table), *cache.parts, out, max_q, max_len, scale, lse=lse, workspace=ws, **options)
+    torch.cuda.synchronize()
+    assert mx.device_timeouts() == 0
+    return out, lse
+
+
+def agrees(mx, nq, lens, heads, group, dim, page, max_len, rows=None, seed=3, **options):  # noqa: F811
+    """The call against `dense`, sequence by sequence; `rows`: rows of q that there are (the last sequence may go on behind them)."""
+    block, cu = 16, cumulative(nq)
+    rows = cu[-1] if rows is None else rows
+    table, pool = make_table(lens, -(-max(lens) // page), page, seed)
+    cache = Cache(pool, heads, page, dim, block)
+    fill(cache, lens, table, page, block, seed)
+    q = torch.randn(rows, heads * group, dim, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda()
+    scale = dim ** -0.5
+    out, lse = attend(mx, q, cu, lens, table, cache, max(nq), max_len, scale, **options)
+    for s, length in enumerate(lens):
+        a, b = cu[s], min(cu[s + 1], rows)
+        place = length - nq[s] + torch.arange(b - a, device="cuda")
+        pages = torch.tensor(table[s][:-(-length // page)], device="cuda")
+        for h in range(heads * group):
+            k, v = (ref.dequantise(c, sc, pages, block, h // group, length) for c, sc in (cache.parts[:2], cache.parts[2:]))
+            near(out[a:b, h], lse[a:b, h],
+                 *dense(q[a:b, h], place, k, v, scale, options.get("causal", True), options.get("window", 0), max_len))
+    assert cache.guards_intact()
 
 
 def value_scales(low, high, seed=9):
@@ -32,3 +91,20 @@ def value_scales(low, high, seed=9):
 def test_value_scales_far_apart_with_rows_that_have_seen_nothing(mx, dim, qh, h, nq, lens, window):  # noqa: F811
     """Value scales fifty binades apart while some rows of a warp see a tile's keys and others none yet."""
     check(mx, qh, h, dim, 16, 16, nq, lens, window=window, seed=dim + qh, setup=value_scales(-56, -6))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,lens,max_len", [
+    ([10], [100], 90), ([1, 4, 3], [500, 90, 333], 320), ([70], [300], 250), ([200, 90], [400, 130], 256), ([40, 1], [1300, 2000], 1290),
+])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 25), (False, 0), (False, 100), (True, 400)])
+def test_lengths_above_the_bound(mx, dim, nq, lens, max_len, causal, window):  # noqa: F811
+    """Keys past max_kv_len are not seen; the queries stand where kv_lens puts them all the same."""
+    agrees(mx, nq, lens, 2, 2, dim, 32, max_len, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("nq,lens,rows", [([3, 8], [40, 100], 7), ([5, 300], [64, 500], 180), ([2, 4], [9, 3000], 4)])
+@pytest.mark.parametrize("window", [0, 30])
+def test_rows_end_before_the_last_sequence(mx, nq, lens, rows, window):  # noqa: F811
+    """cu_q goes on behind the rows that there are: those that are there keep their places."""
+    agrees(mx, nq, lens, 2, 4, 64, 16, max(lens), rows=rows, window=window)
