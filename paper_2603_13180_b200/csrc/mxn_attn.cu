@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // keys that any row of this tile sees: [lo, hi)
     const int last = min(rows, row0 + Sh::kRows) - 1;
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
-    const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
+    const int lo = first_seen(shift + P.by_group(row0), P.window) / kTile * kTile;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const int row = min(row_base + 8 * (x >> 1) + 2 * c + (x & 1), rows - 1);
         const int pos = shift + P.by_group(row);
         see_hi[x] = P.causal ? min(pos + 1, len) : len;
-        see_lo[x] = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+        see_lo[x] = first_seen(pos, P.window);
     }
     int all_hi = see_hi[0], all_lo = see_lo[0];
 #pragma unroll

@@ -35,6 +35,12 @@ __device__ __forceinline__ AttnSequence attn_sequence(const AttnParams& P, int s
     s.len = min(all, P.max_len);
     return s;
 }
+// first key that a query at `pos` sees.  The place may lie before the first token and the window be any up to 2^31 - 1, so the
+// difference takes more than 32 bits.
+__device__ __forceinline__ int first_seen(int pos, int window)
+{
+    return window > 0 ? (int)max((int64_t)0, (int64_t)pos - window + 1) : 0;
+}
 
 // tiled copy of a box of codes (no multicast); x = 0, y = first token within its page, z = page * heads + head
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar)

@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     if (row0 >= rows) return;
     const bool two = rows - row0 > kTile;   // else nothing is done for the second row tile
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(rows - 1) + 1 : len));
-    const int lo = P.window > 0 ? max(0, shift + P.by_group(row0) - P.window + 1) / kTile * kTile : 0;
+    const int lo = first_seen(shift + P.by_group(row0), P.window) / kTile * kTile;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const float row_factor = row_factors[rt * kTile + r_in];
         const int pos = shift + (row_live ? q_tok : nq - 1);
         const int see_hi = P.causal ? min(pos + 1, len) : len;
-        const int see_lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+        const int see_lo = first_seen(pos, P.window);
         const float kNone = -INFINITY;
         float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
         bool ok = true;

@@ -108,3 +108,12 @@ def test_lengths_above_the_bound(mx, dim, nq, lens, max_len, causal, window):  #
 def test_rows_end_before_the_last_sequence(mx, nq, lens, rows, window):  # noqa: F811
     """cu_q goes on behind the rows that there are: those that are there keep their places."""
     agrees(mx, nq, lens, 2, 4, 64, 16, max(lens), rows=rows, window=window)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,lens", [([8], [3]), ([6, 5, 40], [2, 5, 30]), ([100], [60]), ([300, 200], [100, 190])])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 5, 2 ** 30])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_without_end(mx, dim, nq, lens, window, causal):  # noqa: F811
+    """A window as large as it may be hides nothing, with queries that stand before the first key among the rows."""
+    agrees(mx, nq, lens, 2, 3, dim, 32, max(lens), window=window, causal=causal)
