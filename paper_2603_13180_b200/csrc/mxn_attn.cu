@@ -11,7 +11,8 @@
 //      folded into the softmax's weight, w_t = 2^(s_t + sv_t - R + 1) in f16.  The reference R (an integer, so that corrections of
 //      the sums are exact) is moved when a tile's largest s + sv is 14 above or 16 below it: f16 keeps 11 bits of what is above
 //      2^-14 and drops what is below 2^-25.  The softmax's own sum is l = sum of the unrounded w_t 2^(c0 - sv_t), a factor for each
-//      run of 16 tokens, c0 a constant of the warp; where a scale is more than 40 binades from c0 it takes exponentials of its own.
+//      run of 16 tokens, c0 a constant of the warp; from the first scale on that lies far from c0 it has exponentials and a
+//      reference of its own (see kApart).
 //
 // A CTA of four warps takes up to 8 * NQ * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
 // of warps walk over the chunk's tiles of 32 tokens in turn; each group feeds itself through a ring of tiles that the
@@ -137,6 +138,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * GROUPS * STAGES];   // full, then empty
     __shared__ float chunk_lse[Sh::kRows];           // for the other CTAs of a cluster
+    __shared__ float sum_refs[kWarps][8 * NQ];       // references of the rows' sums, once these are apart
 
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
@@ -257,8 +259,9 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // scales, one tile ahead: lanes 0 and 16 hold the key scales of the two runs, lanes 1 and 17 the value scales
     const uint8_t* const scale_base = lane & 1 ? P.v_scales : P.k_scales;
     const int per_page = P.page_shift - P.block_shift;
+    uint32_t no_scale = 0;   // for a run without tokens
     auto scale_at = [&](int i, int pg) -> uint32_t {
-        if ((lane & 15) >= 2 || !in_pool(pg)) return 0;
+        if ((lane & 15) >= 2 || !in_pool(pg)) return no_scale;
         const int64_t tile = (int64_t)pg * P.kv_heads + h;
         return __ldg(scale_base + (tile << per_page) + (((tile_at(i) + 16 * run) & (P.page - 1)) >> P.block_shift));
     };
@@ -301,8 +304,12 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         ref[x] = top_all[x] = kNone;
         l[x] = 0.0f;
     }
-    float c0 = 0.0f;
-    bool ok = true;
+    // near the value scales: the largest of the first tile; runs without tokens count as one of them
+    const uint32_t first_scale = max(__shfl_sync(0xFFFFFFFFu, sc_next, 1), __shfl_sync(0xFFFFFFFFu, sc_next, 17));
+    no_scale = min(max(first_scale, 67u), 187u);
+    const float c0 = (float)(int)no_scale - 127.0f;
+    if (!in_pool(pages[0])) sc_next = no_scale;
+    bool ok = true, apart = false;   // apart: the sums have references of their own
 
     int st = 0;
     uint32_t ph = 0;
@@ -312,11 +319,12 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         sc_next = scale_at(i + 1, pages[1]);
         const float kf[2] = {e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)), e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16))};
         const float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
-        if (i == 0) c0 = fminf(fmaxf(fmaxf(sv[0], sv[1]), -60.0f), 60.0f);
         // tokens of the tile that exist and whose page could be read
         const bool readable = in_pool(pages[0]);
         const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && readable);
         bad_page |= t0 + lane < k1 && !readable;
+        const bool was_apart = apart;
+        apart = apart || fabsf(sv[0] - c0) > kApart || fabsf(sv[1] - c0) > kApart;
 
         if (!mbar_wait_bounded(full + 8 * st, ph)) {
             ok = false;
@@ -354,7 +362,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                 for (int x = 0; x < NQ; ++x) mma_f16(s[t][x], a0, a1, a2, a3, qb[k][x][0], qb[k][x][1]);
             }
         }
-        // ---- s + sv, and what the rows may not see ----
+        // ---- s + sv (s alone for sums that are apart), and what the rows may not see ----
         float f[2][QN];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -362,7 +370,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
             for (int x = 0; x < QN; ++x) {
                 f[t][x] = kf[t] * row_factor[x];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) s[t][x >> 1][2 * e + (x & 1)] = fmaf(s[t][x >> 1][2 * e + (x & 1)], f[t][x], sv[t]);
+                for (int e = 0; e < 2; ++e) s[t][x >> 1][2 * e + (x & 1)] = fmaf(s[t][x >> 1][2 * e + (x & 1)], f[t][x], apart ? 0.0f : sv[t]);
             }
         if (there != 0xFFFFFFFFu || t0 < all_lo || t0 + kTile > all_hi) {
 #pragma unroll
@@ -374,6 +382,34 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                     for (int x = 0; x < QN; ++x)
                         if (!((there >> at) & 1u) || place < see_lo[x] || place >= see_hi[x]) s[t][x >> 1][2 * e + (x & 1)] = kNone;
                 }
+        }
+        if (__builtin_expect(apart, 0)) {
+            // the row's reference: shared by the eight threads that look after the row
+            float* const refs = sum_refs[warp] + 2 * c;
+#pragma unroll
+            for (int x = 0; x < QN; ++x) {
+                float* const at = refs + 8 * (x >> 1) + (x & 1);
+                const float z[4] = {s[0][x >> 1][x & 1], s[0][x >> 1][2 + (x & 1)], s[1][x >> 1][x & 1], s[1][x >> 1][2 + (x & 1)]};
+                float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                float r = was_apart ? *at : ref[x] == kNone ? kNone : ref[x] - kTop - c0;
+                if (m > r + kLift) {
+                    const float next = ceilf(m);
+                    l[x] = r == kNone ? l[x] : times_pow2(l[x], r - next);
+                    r = next;
+                }
+                if (r > kNone) l[x] += (ex2(z[0] - r) + ex2(z[1] - r)) + (ex2(z[2] - r) + ex2(z[3] - r));
+                __syncwarp();
+                if (g == 0) *at = r;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][x][e] += sv[t];
         }
         // ---- reference: moved where a weight would leave the window ----
         bool out = false;
@@ -397,7 +433,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                 top_all[x] = fmaxf(top_all[x], next);
                 const float alpha = ref[x] == kNone ? 0.0f : ex2(ref[x] - next);
                 ref[x] = next;
-                l[x] *= alpha;
+                l[x] *= apart ? 1.0f : alpha;
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
                     acc[j][x >> 1][x & 1] *= alpha;
@@ -406,21 +442,13 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
             }
         }
         // ---- weights, turned to the second product's operand; the softmax's sum ----
-        const bool wide = fabsf(sv[0] - c0) > 40.0f || fabsf(sv[1] - c0) > 40.0f;
         float by[QN];
 #pragma unroll
         for (int x = 0; x < QN; ++x) by[x] = ref[x] == kNone ? 0.0f : kTop - ref[x];
-        if (wide) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int x = 0; x < QN; ++x)
-                    if (ref[x] > kNone) l[x] += ex2(s[t][x >> 1][x & 1] + (by[x] + (c0 - sv[t]))) + ex2(s[t][x >> 1][2 + (x & 1)] + (by[x] + (c0 - sv[t])));
-        }
         uint32_t pb[2][NQ][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float back = wide ? 0.0f : ex2(c0 - sv[t]);
+            const float back = apart ? 0.0f : ex2(c0 - sv[t]);   // (a NaN among the weights reaches the sum all the same)
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
                 float w[4];
@@ -507,23 +535,46 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     if (__any_sync(0xFFFFFFFFu, bad_page) && lane == 0) atomicAdd(&g_attn_bad, 1u);
 
     // ---- join the groups of warps ----
-    // row x of this thread: sum l 2^at, output acc 2^c0 2^at with at = ref - kTop - c0; dimensions g * DIM/8 ... + DIM/8 - 1
+    // row x of this thread: sum l 2^at, output acc unit 2^at; dimensions g * DIM/8 ... + DIM/8 - 1.  at = ref - kTop - c0 and unit = 2^c0;
+    // with a reference of its own the sum is brought to [1, 2), and acc to the same unit in two steps, since the power may lie outside
+    // binary32's range where the product does not.
     constexpr int OUT = DIM / 8, PITCH = DIM + 4;
     float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
     float2* const stat = reinterpret_cast<float2*>(sm + GROUPS * Sh::kRows * PITCH);   // (at, l)
-    const float unit = ex2(c0);
+    const float unit = apart ? 1.0f : ex2(c0);
+    float at[QN];
+#pragma unroll
+    for (int x = 0; x < QN; ++x) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], o);
+        at[x] = ref[x] - kTop - c0;
+    }
+    if (__builtin_expect(apart, 0)) {
+#pragma unroll
+        for (int x = 0; x < QN; ++x) {
+            at[x] = sum_refs[warp][8 * (x >> 1) + 2 * c + (x & 1)];
+            if (at[x] == kNone) continue;
+            const int e = min(max((int)(__float_as_uint(l[x]) >> 23) - 127, -126), 127);
+            l[x] = times_pow2(l[x], (float)-e);
+            at[x] += (float)e;
+            const float d = ref[x] - kTop - at[x], half = floorf(0.5f * d), by1 = ex2(half), by2 = ex2(d - half);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                acc[j][x >> 1][x & 1] = acc[j][x >> 1][x & 1] * by1 * by2;
+                acc[j][x >> 1][2 + (x & 1)] = acc[j][x >> 1][2 + (x & 1)] * by1 * by2;
+            }
+        }
+    }
     __syncthreads();   // every copy has landed and been read
 #pragma unroll
     for (int x = 0; x < QN; ++x) {
         const int place = group * Sh::kRows + rw * 8 * NQ + 8 * (x >> 1) + 2 * c + (x & 1);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) l[x] += __shfl_xor_sync(0xFFFFFFFFu, l[x], o);
         float* const p = sm + place * PITCH + g * OUT;
 #pragma unroll
         for (int y = 0; y < MT / 2; ++y)
             *reinterpret_cast<float4*>(p + 4 * y) = make_float4(acc[2 * y][x >> 1][x & 1] * unit, acc[2 * y][x >> 1][2 + (x & 1)] * unit,
                                                                 acc[2 * y + 1][x >> 1][x & 1] * unit, acc[2 * y + 1][x >> 1][2 + (x & 1)] * unit);
-        if (g == 0) stat[place] = make_float2(ref[x] - kTop - c0, l[x]);
+        if (g == 0) stat[place] = make_float2(at[x], l[x]);
     }
     __syncthreads();
     // all threads: eight dimensions of a row at a time

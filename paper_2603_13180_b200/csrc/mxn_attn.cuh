@@ -58,6 +58,18 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The softmax's sum and its range.  While the value scales lie within kApart binades of c0, the sum is in units of 2^(R - 1 - c0): its
+// terms are the weights times 2^(c0 - sv).  R follows the largest s + sv to within 54, so the largest score's term lies between 2^-16
+// and 2^71, and a step of R that is too large for binary32 (the sum so far becomes 0) only drops terms below 2^-39 of it.  From the
+// first tile on whose scales lie farther away (a run of zero values has scale 2^-127) the sum has a reference of its own that follows the
+// scores alone: terms 2^(s - reference), the reference raised where a score lies kLift above it.
+constexpr float kApart = 16.0f, kLift = 60.0f;
+// v 2^d for a whole d whose power may lie outside binary32's range where the product does not
+__device__ __forceinline__ float times_pow2(float v, float d)
+{
+    const float h = floorf(0.5f * d);
+    return v * ex2(h) * ex2(d - h);
+}
 // 2^(byte - 127), the value of an E8M0 byte
 __device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 0 ? 0x00400000u : b << 23); }
 

@@ -18,7 +18,8 @@
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
 //   is moved only when a step's largest is 14 above or 16 below it, so that the output in tensor memory rarely has to be corrected.
 //   f16 drops what is below 2^-25, i.e. 2^-26 of the weight at R and 2^-10 of the largest of a step at the window's lower end.
-// The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA.
+// The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA;
+// from the first scale on that lies far from c0 it has exponentials and a reference of its own (see kApart).
 // The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
 //
@@ -76,7 +77,7 @@ struct alignas(16) TileScales {
     float v[kTile / kRun];        // sv - 127
     float l[kTile / kRun];        // 2^(c0 - v): from weights to the softmax's sum
     uint32_t readable;            // bit i: the page of run i could be read
-    uint32_t wide;                // a value scale lies so far from c0 that l needs exponentials of its own
+    uint32_t apart;               // a value scale of this or an earlier tile lies so far from c0 that l is summed apart
     float c0;
 };
 
@@ -343,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
         const int box = min(P.page, kTile), boxes = kTile / box;     // tokens of a box, boxes of a tile
         const int per_page_shift = P.page_shift - P.block_shift;
-        bool any_bad = false;
+        bool any_bad = false, apart = false;
         float c0 = 0.0f;
         int page_next = -1;                                          // lane i: page of run i (lanes 0-7) of the next tile
         auto look_up = [&](int j) {
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 for (int o = 4; o > 0; o >>= 1) c0 = fmaxf(c0, __shfl_xor_sync(0xFFFFFFFFu, c0, o));
                 c0 = fminf(fmaxf(__shfl_sync(0xFFFFFFFFu, c0, 0), -60.0f), 60.0f);
             }
-            const bool wide = __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - c0) > 40.0f);
+            apart = apart || __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - c0) > kApart);
             if (lane < 8) {
                 slot.k[lane] = e8m0_to_f32(sk);
                 slot.v[lane] = v;
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             }
             if (lane == 0) {
                 slot.readable = readable;
-                slot.wide = wide;
+                slot.apart = apart;
                 slot.c0 = c0;
             }
             __syncwarp();
@@ -556,8 +557,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const int see_hi = P.causal ? min(pos + 1, len) : len;
         const int see_lo = first_seen(pos, P.window);
         const float kNone = -INFINITY;
-        float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
-        bool ok = true;
+        float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f, sum_ref = kNone;   // sum_ref: of l, once that is summed apart
+        bool ok = true, apart = false;
         const int steps = 2 * tiles;
         // a row that nothing hides in a step needs no mask: the range that holds for the warp's rows
         const int all_lo = __reduce_max_sync(0xFFFFFFFFu, see_lo), all_hi = __reduce_min_sync(0xFFFFFFFFu, min(see_hi, k1));
@@ -578,7 +579,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                          l4 = *reinterpret_cast<const float4*>(slot.l + 4 * buf);
             const float slot_k[4] = {k4.x, k4.y, k4.z, k4.w}, slot_v[4] = {v4.x, v4.y, v4.z, v4.w}, slot_l[4] = {l4.x, l4.y, l4.z, l4.w};
             const uint32_t readable = (slot.readable >> (4 * buf)) & 0xFu;
-            const bool wide = slot.wide != 0;
+            const bool was_apart = apart;
+            apart = slot.apart != 0;
             c0 = slot.c0;
             // bit e: the row sees token 32 c + e of the step
             auto visible = [&](int c) -> uint32_t {
@@ -612,12 +614,30 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 utop = max_nan(utop, fmaf(m, fac[g], slot_v[g]));
             }
             top_all = fmaxf(top_all, utop);
+            if (__builtin_expect(apart, 0)) {
+                if (!was_apart && ref > kNone) sum_ref = ref - kTop - c0;
+                float ztop = kNone;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ztop = fmaxf(ztop, __uint_as_float(x[g >> 1][16 * (g & 1) + e]) * fac[g]);
+                if (ztop > sum_ref + kLift) {
+                    const float next = ceilf(ztop);
+                    if (sum_ref > kNone) l = times_pow2(l, sum_ref - next);
+                    sum_ref = next;
+                }
+                if (sum_ref > kNone)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) l += ex2(fmaf(__uint_as_float(x[g >> 1][16 * (g & 1) + e]), fac[g], -sum_ref));
+            }
             if (__any_sync(0xFFFFFFFFu, utop > ref + kUp || (utop < ref - kDown && utop > kNone))) {
                 float next = ref;   // (ref + kUp is -infinity without a reference)
                 if (utop > ref + kUp) next = ceilf(utop);
                 else if (utop < ref - kDown && utop > kNone) next = ceilf(fmaxf(utop, top_all - kDepth));
                 const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
-                l *= alpha;
+                l *= apart ? 1.0f : alpha;
                 ref = next;
                 if (i > 0) {   // the output up to the last step: its end is signalled with the next step's scores
                     ok = wait(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u, dead);
@@ -636,21 +656,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             // weights, over their scores
             // a NaN among the scores reaches all of the step's weights: the polynomial below would take it for a small number
             const float shift_by = utop != utop ? utop : ref == kNone ? 0.0f : kTop - ref;
-            float extra = 0.0f;
-            // the sum by exponentials of its own, from the scores as they still stand; the whole warp or none of it (the loads are the
-            // warp's), whether or not each of its rows has seen a key
-            if (wide && __any_sync(0xFFFFFFFFu, ref > kNone)) {
-#pragma unroll 1
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t z[16];
-                    tm_load16(z, s_at + 16 * g);
-                    const uint32_t see = visible(g >> 1) >> (16 * (g & 1));
-                    const float f = fmaxf(row_factor * slot_k[g], 1.17549435e-38f), add = c0 + kTop - ref;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (((see >> e) & 1u) && ref > kNone) extra += ex2(fmaf(__uint_as_float(z[e]), f, add));
-                }
-            }
             uint32_t w[32];
             float more = 0.0f;
             bool probe[3];
@@ -673,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 more = fmaf(both.x + both.y, slot_l[g], more);
                 if (g & 1) probe[g >> 1] = mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             }
-            l += wide && more == more ? extra : more;
+            l += apart && more == more ? 0.0f : more;   // (a NaN among the weights reaches the sum all the same)
             tm_store32(s_at, w);
             here = __all_sync(0xFFFFFFFFu, i + 1 < steps && (probe[0] || probe[1]));
             scales_here = __all_sync(0xFFFFFFFFu, probe[2]);
@@ -686,10 +691,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         if (ok && tiles > 0) ok = wait(s_full + 16 * rt + 8, (uint32_t)tiles & 1u, dead);   // behind the last step's product
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_after();
-        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 1 - c0
+        // out = acc 2^c0 / l;  log2 of the softmax's sum = log2 l + R - 1 - c0.  Summed apart, with a reference r of l: out = acc 2^(R - 1 - r) / l,
+        // the power in two factors, since it may lie outside binary32's range where the product does not
         const bool some = ref > kNone || l != l;   // (NaN scores set no reference)
-        const float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f;
-        const float lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
+        float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f, inv2 = 1.0f, lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
+        if (apart && ref > kNone) {
+            const int e = min(max((int)(__float_as_uint(l) >> 23) - 127, -126), 127);
+            const float d = ref - kTop - sum_ref - (float)e, half = floorf(0.5f * d);
+            inv = __fdiv_rn(ex2(half), times_pow2(l, (float)-e));   // l in [1, 2)
+            inv2 = ex2(d - half);
+            lse2 = log2f(l) + sum_ref;
+        }
         const int64_t out_row = tok * P.q_heads + head;
         const uint32_t out_at = base + Sh::kQ + (uint32_t)(warp - 8) * 32 * 2 * DIM;
 #pragma unroll
@@ -701,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             __syncwarp();
             float* const o = reinterpret_cast<float*>(x);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * inv : 0.0f;
+            for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * inv * inv2 : 0.0f;
             if (P.splits == 1) {   // to shared memory (q's, which no product reads any more): 16-byte pieces, as swizzled as its rows are long
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {

@@ -117,3 +117,49 @@ def test_rows_end_before_the_last_sequence(mx, nq, lens, rows, window):  # noqa:
 def test_windows_without_end(mx, dim, nq, lens, window, causal):  # noqa: F811
     """A window as large as it may be hides nothing, with queries that stand before the first key among the rows."""
     agrees(mx, nq, lens, 2, 3, dim, 32, max(lens), window=window, causal=causal)
+
+
+def zero_values(length, zeros, key_zero, key_rest):
+    """Pages of 32 tokens, all sequences alike: tokens zeros[0] .. zeros[1] - 1 have values of zero (scale 0, as the append leaves them)
+    and keys of the one code, the others the other; all queries are ones."""
+    def setup(cache, q, table):
+        kc, ks, vc, vs = cache.parts
+        q.fill_(1.0)
+        key = torch.tensor([key_zero, key_rest]).to(torch.float8_e4m3fn).view(torch.uint8).tolist()
+        pages = torch.tensor(table, device="cuda")
+        for t in range(0, length, 16):
+            pg, at, zero = pages[:, t // 32], t % 32, zeros[0] <= t < zeros[1]
+            end = at + min(16, length - t)
+            kc[pg, :, at:end] = key[0] if zero else key[1]
+            kc[pg, 0, at:end, 0] ^= (torch.arange(end - at, device="cuda") % 2 * 0x80).to(torch.uint8)   # not all the same score
+            ks[pg, :, at // 16] = 121
+            if zero:
+                vc[pg, :, at:end] = 0
+                vs[pg, :, at // 16] = 0
+    return setup
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,length", [(1, 1100), (4, 1100), (100, 1100), (1, 6000), (60, 1100)])
+@pytest.mark.parametrize("zeros", [(0, 16), (0, 32), (0, 64), (0, 128), (0, 1008), (48, 208), (496, 1100)])
+@pytest.mark.parametrize("key_zero,key_rest", [(0.0, 0.0), (0.0, 40.0), (40.0, 0.0), (-448.0, 448.0), (448.0, -208.0)])
+def test_runs_of_zero_values(mx, dim, nq, length, zeros, key_zero, key_rest):  # noqa: F811
+    """Zero values with scores as large as the others', far below or far above: they count in the softmax's sum, whatever the scale."""
+    check(mx, 4, 2, dim, 32, 16, [nq], [length], seed=dim, setup=zero_values(length, zeros, key_zero, key_rest))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq", [1, 4])
+@pytest.mark.parametrize("zeros", [(0, 32), (0, 128), (48, 208)])
+@pytest.mark.parametrize("key_zero,key_rest", [(0.0, 0.0), (0.0, 40.0), (448.0, -208.0)])
+def test_runs_of_zero_values_in_long_chunks(mx, dim, nq, zeros, key_zero, key_rest):  # noqa: F811
+    """The same where many sequences leave each warp several tiles one after another."""
+    check(mx, 16, 8, dim, 32, 16, [nq] * 80, [400] * 80, seed=dim, setup=zero_values(400, zeros, key_zero, key_rest))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,lens", [([1, 3], [700, 5000]), ([16], [900]), ([50, 100], [300, 2000])])
+@pytest.mark.parametrize("low,high", [(-127, 0), (-127, 100), (-60, 60), (-25, -4), (60, 110)])
+@pytest.mark.parametrize("window", [0, 300])
+def test_value_scales_over_all_of_their_range(mx, dim, nq, lens, low, high, window):  # noqa: F811
+    check(mx, 8, 2, dim, 32, 16, nq, lens, window=window, seed=dim + high, setup=value_scales(low, high))
