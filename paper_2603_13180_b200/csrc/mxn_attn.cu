@@ -158,7 +158,8 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // keys that any row of this tile sees: [lo, hi)
     const int last = min(rows, row0 + Sh::kRows) - 1;
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
-    const int lo = first_seen(shift + P.by_group(row0), P.window) / kTile * kTile;
+    const int seen = first_seen(shift + P.by_group(row0), P.window);   // nothing before it, not even its page, has any influence
+    const int lo = seen / kTile * kTile;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -215,17 +216,17 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     const int mine = tiles > group ? (tiles - group + GROUPS - 1) / GROUPS : 0;
     const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
     // A tile has two runs of 16 tokens, each within one page; lanes 0-15 look after the first, 16-31 after the second.
-    // page_at(i): the table's entry for this lane's run of tile i, -1 behind the last token.  It is looked at a tile later at the
+    // page_at(i): the table's entry for this lane's run of tile i, -1 behind the last token and before the window.  It is looked at a tile later at the
     // earliest, so that nothing waits for it.
     const int run = lane >> 4;
     bool bad_page = false;
     auto tile_at = [&](int i) { return k0 + (group + i * GROUPS) * kTile; };
+    const bool two_boxes = P.page < kTile;   // a page of 16 tokens takes two boxes to a tile
     auto page_at = [&](int i) -> int {
         const int t = tile_at(i) + 16 * run;
-        return i < mine && t < k1 ? __ldg(table + (t >> P.page_shift)) : -1;
+        return i < mine && t < k1 && (t | (two_boxes ? 15 : kTile - 1)) >= seen ? __ldg(table + (t >> P.page_shift)) : -1;
     };
     auto in_pool = [&](int pg) { return (uint32_t)pg < (uint32_t)P.num_pages; };
-    const bool two_boxes = P.page < kTile;   // a page of 16 tokens takes two boxes to a tile
     const uint32_t box_bytes = two_boxes ? Sh::kTileBytes / 2 : Sh::kTileBytes;
     auto request = [&](int i, int st, int pg) {   // by a whole warp, with page_at(i) in hand
         const int pg1 = two_boxes ? __shfl_sync(0xFFFFFFFFu, pg, 16) : -1;
@@ -321,8 +322,9 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
         // tokens of the tile that exist and whose page could be read
         const bool readable = in_pool(pages[0]);
-        const uint32_t there = __ballot_sync(0xFFFFFFFFu, t0 + lane < k1 && readable);
-        bad_page |= t0 + lane < k1 && !readable;
+        const bool wanted = t0 + lane < k1 && t0 + lane >= seen;
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, wanted && readable);
+        bad_page |= wanted && !readable;
         const bool was_apart = apart;
         apart = apart || fabsf(sv[0] - c0) > kApart || fabsf(sv[1] - c0) > kApart;
 
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                     v[x][0] = a.x; v[x][1] = a.y;
                 }
             }
-            if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token, a NaN among it, must not meet the zero weights
+            if (there != 0xFFFFFFFFu) {   // whatever stands behind the last token or before the window, a NaN among it, must not meet the zero weights
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int at = 16 * t + 8 * (x >> 1) + 2 * c + (x & 1);

@@ -241,7 +241,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     if (row0 >= rows) return;
     const bool two = rows - row0 > kTile;   // else nothing is done for the second row tile
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(rows - 1) + 1 : len));
-    const int lo = first_seen(shift + P.by_group(row0), P.window) / kTile * kTile;
+    const int seen = first_seen(shift + P.by_group(row0), P.window);   // nothing before it, not even its page, has any influence
+    const int lo = seen / kTile * kTile;
     const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         auto look_up = [&](int j) {
             const int t = k0 + j * kTile + kRun * (lane & 7);
             int pg = -1;
-            if (j < tiles && lane < 8 && t < k1) {
+            if (j < tiles && lane < 8 && t < k1 && (t | (box - 1)) >= seen) {
                 pg = __ldg(table + (t >> P.page_shift));
                 if (pg < 0 || pg >= P.num_pages) {
                     pg = -1;
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             ok = wait(v_full + 8 * vs, (uint32_t)(j / kValStages) & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const int place = k0 + j * kTile + t;
-            const bool real = place < k1 && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
+            const bool real = place >= seen && place < k1 && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
             if (j >= kHalfStages) ok = wait(h_empty + 8 * hs, (uint32_t)(j / kHalfStages - 1) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const uint32_t src = base + Sh::kV + vs * Sh::kCodes + (uint32_t)t * DIM;

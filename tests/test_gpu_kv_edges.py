@@ -163,3 +163,40 @@ def test_runs_of_zero_values_in_long_chunks(mx, dim, nq, zeros, key_zero, key_re
 @pytest.mark.parametrize("window", [0, 300])
 def test_value_scales_over_all_of_their_range(mx, dim, nq, lens, low, high, window):  # noqa: F811
     check(mx, 8, 2, dim, 32, 16, nq, lens, window=window, seed=dim + high, setup=value_scales(low, high))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page,block", [(16, 16), (32, 16), (64, 32), (128, 64), (256, 16)])
+@pytest.mark.parametrize("nq,lens,window", [
+    ([1], [121], 4), ([1, 1, 4], [1000, 300, 2500], 100), ([4], [9000], 700), ([70], [500], 10), ([90, 200], [800, 3000], 300), ([300], [2000], 1),
+    ([40, 1], [1500, 1400], 33),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_pages_behind_the_window(mx, dim, page, block, nq, lens, window, causal):  # noqa: F811
+    """Pages that lie before every query's window: released (no page of the pool) or full of NaN, they change nothing, and no bad
+    index is counted; the same for NaN values before the window in the page that it begins in."""
+    heads, group = 2, 2
+    table, pool = make_table(lens, -(-max(lens) // page), page, page + dim)
+    cache = Cache(pool, heads, page, dim, block)
+    fill(cache, lens, table, page, block, dim)
+    q = torch.randn(sum(nq), heads * group, dim, generator=torch.Generator().manual_seed(page)).to(torch.bfloat16).cuda()
+    cu = cumulative(nq)
+    call = lambda t: attend(mx, q, cu, lens, t, cache, max(nq), max(lens), dim ** -0.5, causal=causal, window=window)  # noqa: E731
+    mx.device_bad_indices_reset()
+    want = call(table)
+    released = []
+    for s, length in enumerate(lens):
+        first = max(0, length - nq[s] - window + 1)
+        row = list(table[s])
+        for i in range(first // page):
+            cache.parts[0][row[i]] = cache.parts[2][row[i]] = 0x7F
+            cache.parts[1][row[i]] = cache.parts[3][row[i]] = 0xFF
+            row[i] = -1 if i % 2 else pool + i
+        # the page in which the window begins: its tokens before the window, in blocks that are all before it with their scales
+        pg, n = row[first // page], first % page
+        cache.parts[0][pg, :, :n] = cache.parts[2][pg, :, :n] = 0x7F
+        released.append(row)
+    assert all(torch.equal(a, b) for a, b in zip(want, call(table))), "NaN behind the window"
+    assert all(torch.equal(a, b) for a, b in zip(want, call(released))), "released pages behind the window"
+    assert mx.device_bad_indices() == 0
+    assert bool(want[0].isfinite().all())
