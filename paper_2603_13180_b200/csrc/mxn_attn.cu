@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const bool was_apart = apart;
         apart = apart || fabsf(sv[0] - c0) > kApart || fabsf(sv[1] - c0) > kApart;
 
-        if (!mbar_wait_bounded(full + 8 * st, ph)) {
+        // (the warp leaves the loop as a whole: its lanes' polls may end differently)
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(full + 8 * st, ph))) {
             ok = false;
             break;
         }
@@ -507,7 +508,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         if (RW > 1) {
             if (lane == 0) mbar_arrive(empty + 8 * st);
             if (rw == 0 && i + STAGES < mine) {
-                if (!mbar_wait_bounded(empty + 8 * st, ph)) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(empty + 8 * st, ph))) {
                     ok = false;
                     break;
                 }
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         for (int d = 0; d < STAGES + 1; ++d) pages[d] = pages[d + 1];
         pages[STAGES + 1] = page_at(i + STAGES + 2);
     }
-    if (!__all_sync(0xFFFFFFFFu, ok)) {
+    if (!ok) {
         // a wait ran out: no further copies are asked for; those in flight get a second, shorter wait before the shared
         // memory is given up
         if (lane == 0) atomicAdd(&g_attn_timeouts, 1u);
