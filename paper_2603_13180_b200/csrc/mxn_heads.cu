@@ -294,6 +294,10 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
             const uint4 cx[2] = {lds16(at + 2 * PIECE), lds16(at + 3 * PIECE)};
             Lane16 x;
             unpack<PAIRS>(x, cx);
+            if (!good) {   // a token without an angle adds nothing to the gain's gradient, whatever it holds
+                fill(x, 0.0f);
+                fill(d, 0.0f);
+            }
             float2 sd = make_float2(0.0f, 0.0f), se = sd;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -304,12 +308,11 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
             const float ss = head_sum<LP>(dot(x, x)), hx = head_sum<LP>(sd.x + sd.y);
             const float r = head_rcp(ss, P.inv_dim, P.eps);
             const float m = -hx * r * P.inv_dim * r;  // -mean(h n) * r: dx = r * (h + x * m)
-            const float rg = good ? r : 0.0f;         // a token without an angle adds nothing to the gain's gradient
-            const float2 r2 = make_float2(r, r), m2 = make_float2(m, m), rg2 = make_float2(rg, rg);
+            const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                acc.a[j] = __ffma2_rn(__fmul2_rn(d.a[j], x.a[j]), rg2, acc.a[j]);
-                acc.b[j] = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), rg2, acc.b[j]);
+                acc.a[j] = __ffma2_rn(__fmul2_rn(d.a[j], x.a[j]), r2, acc.a[j]);
+                acc.b[j] = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), r2, acc.b[j]);
                 d.a[j] = __fmul2_rn(__ffma2_rn(x.a[j], m2, __fmul2_rn(d.a[j], gamma.a[j])), r2);
                 d.b[j] = __fmul2_rn(__ffma2_rn(x.b[j], m2, __fmul2_rn(d.b[j], gamma.b[j])), r2);
             }
