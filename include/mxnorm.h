@@ -334,7 +334,8 @@ typedef enum { MXN_ROPE_HALVES = 0, MXN_ROPE_PAIRS = 1 } mxn_rope;
  *   zeros stays zero for eps = 0.  normalise == 0: u = x (gains must be NULL).
  *   y = rotation of u by the token's position (cos_sin NULL: y = u); positions int32 [T], NULL = row index.
  *   Outputs bf16, rounded once; they may be the inputs themselves (same pointer and stride), other overlaps are not allowed.
- *   A token whose position lies outside the table gets NaN.  Sums in binary32. */
+ *   A token whose position lies outside the table gets NaN.  The mean of squares is a binary32 sum, of x times a power of two where x^2 would
+ *   leave binary32's range, so heads of any finite size are normalised; 1 / sqrt is rsqrtf (2 units in the last place). */
 mxn_status rmsnorm_rope_fwd(const void* q_bf16, int64_t q_stride, int q_heads, const void* k_bf16, int64_t k_stride, int k_heads,
                             int64_t T, int head_dim, int normalise, const void* q_gain_bf16_or_null,
                             const void* k_gain_bf16_or_null, float eps, const float* cos_sin_or_null, int64_t table_rows, int rot_dim,

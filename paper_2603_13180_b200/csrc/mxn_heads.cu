@@ -104,11 +104,19 @@ __device__ __forceinline__ float head_sum(float v)
     for (int o = LP / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
-// 1 / sqrt(mean + eps); 0 for a head of zeros without eps, which then stays zero
-__device__ __forceinline__ float head_rcp(float sum_sq, float inv_dim, float eps)
+// mean x^2 + eps, and whether binary32 holds it and the squares with all of their digits
+__device__ __forceinline__ float mean_square(float sum_sq, float inv_dim, float eps) { return fmaf(sum_sq, inv_dim, eps); }
+__device__ __forceinline__ bool in_range(float ms) { return ms >= 0x1p-80f && ms <= 0x1p80f; }
+// 1 / sqrt(mean x^2 + eps); 0 for a head of zeros without eps, which then stays zero
+__device__ __forceinline__ float head_rcp(float ms) { return ms != 0.0f ? rsqrtf(ms) : 0.0f; }   // a NaN stays one
+// The same for heads out of range (by a whole warp, whose other heads stay as they are): x is multiplied by a power of two, `unit`, first;
+// the result is that of the new x, so that their product is x / rms all the same.
+template <int LP>
+__device__ __forceinline__ float head_rcp_any(Lane16& x, float ms, float inv_dim, float eps, float& unit)
 {
-    const float ms = fmaf(sum_sq, inv_dim, eps);
-    return ms != 0.0f ? rsqrtf(ms) : 0.0f;   // a NaN stays one
+    unit = ms > 0x1p80f ? 0x1p-80f : ms < 0x1p-80f ? 0x1p80f : 1.0f;
+    scale(x, unit);
+    return head_rcp(mean_square(head_sum<LP>(dot(x, x)), inv_dim, eps * unit * unit));
 }
 
 // a token's row of the rotation's table; rows and tokens are below 2^31
@@ -163,6 +171,7 @@ __global__ void __launch_bounds__(kWarps * 32, tight(LP, PAIRS) ? 5 : 1) rope_fw
     uint4 gw[2];
     Lane16 g;
     int g_of = -1;   // whose gain they hold
+    uint32_t later = 0;   // heads whose squares leave binary32's range: not written here
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int h = h0 + u * G;
@@ -171,7 +180,9 @@ __global__ void __launch_bounds__(kWarps * 32, tight(LP, PAIRS) ? 5 : 1) rope_fw
         unpack<PAIRS>(x, raw[u]);
         float r = 1.0f;
         if (NORM) {
-            r = head_rcp(head_sum<LP>(dot(x, x)), P.inv_dim, P.eps);
+            const float ms = mean_square(head_sum<LP>(dot(x, x)), P.inv_dim, P.eps);
+            if (!in_range(ms)) later |= 1u << u;
+            r = head_rcp(ms);
             const uint16_t* gain = which ? P.gain[1] : P.gain[0];
             if (gain != nullptr && live) {
                 if (g_of != which) {
@@ -189,7 +200,39 @@ __global__ void __launch_bounds__(kWarps * 32, tight(LP, PAIRS) ? 5 : 1) rope_fw
             else if (lp.turns) apply_turn<false, NORM, PAIRS>(x, turn, lp);
         }
         if (NORM) scale(x, r);   // the rotation leaves a common factor alone
-        if (live && h < heads) store<PAIRS>((which ? yk : yq) + h * P.dim + lp.o0, 2 * (lp.o1 - lp.o0), x);
+        if (live && h < heads && !((later >> u) & 1u)) store<PAIRS>((which ? yk : yq) + h * P.dim + lp.o0, 2 * (lp.o1 - lp.o0), x);
+    }
+    if (NORM && __builtin_expect(__any_sync(0xFFFFFFFFu, later != 0u), 0)) {
+        // once more from memory, which still holds them
+#pragma unroll 1
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * G, which = h >= P.heads[0];
+            const uint16_t* const in = (which ? xk : xq) + h * P.dim;
+            const uint16_t* const gain = P.gain[which];
+            const bool mine = live && h < heads && ((later >> u) & 1u);
+            uint4 w[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+            if (mine) {
+                w[0] = ld16(in + lp.o0);
+                w[1] = ld16(in + lp.o1);
+            }
+            Lane16 x;
+            unpack<PAIRS>(x, w);
+            float unit;
+            const float r = head_rcp_any<LP>(x, mean_square(head_sum<LP>(dot(x, x)), P.inv_dim, P.eps), P.inv_dim, P.eps, unit);
+            if (!mine) continue;
+            if (gain != nullptr) {
+                w[0] = __ldg(reinterpret_cast<const uint4*>(gain + lp.o0));
+                w[1] = __ldg(reinterpret_cast<const uint4*>(gain + lp.o1));
+                unpack<PAIRS>(g, w);
+                scale(x, g);
+            }
+            if (P.cos_sin != nullptr) {
+                if (!good) fill(x, __uint_as_float(0x7FC00000u));
+                else if (lp.turns) apply_turn<false, NORM, PAIRS>(x, turn, lp);
+            }
+            scale(x, r);
+            store<PAIRS>((which ? yk : yq) + h * P.dim + lp.o0, 2 * (lp.o1 - lp.o0), x);
+        }
     }
 }
 
@@ -267,6 +310,8 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
         unpack<PAIRS>(gamma, u);
     }
     Turn turn;
+    // a lane's sum of squares from which on, or below which, a head may be out of range
+    const float low = P.eps >= 0x1p-80f ? 0.0f : 0x1p-80f;
     bool good = true, fresh = true;
     int t = (int)first;
     // the token's row of the table, and the next one's: that is on its way to L2 a token ahead of its use
@@ -305,16 +350,32 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
                 se = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), gamma.b[j], se);
             }
             sd = __fadd2_rn(sd, se);
-            const float ss = head_sum<LP>(dot(x, x)), hx = head_sum<LP>(sd.x + sd.y);
-            const float r = head_rcp(ss, P.inv_dim, P.eps);
+            const float sq = dot(x, x);
+            // (asked of the lanes' own sums, ahead of the head's: asked of those the branch below costs 3.5 us of 92)
+            const bool odd = __any_sync(0xFFFFFFFFu, !(sq <= 0x1p80f && sq >= low));
+            const float ms = mean_square(head_sum<LP>(sq), P.inv_dim, P.eps);
+            float hx = head_sum<LP>(sd.x + sd.y), r = head_rcp(ms), r_dx = r;   // r_dx: that of x as it was read
+            if (__builtin_expect(odd, 0)) {
+                float unit;
+                r = head_rcp_any<LP>(x, ms, P.inv_dim, P.eps, unit);
+                r_dx = fminf(r * unit, 3.402823466e+38f);
+                float again = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    again = fmaf(d.a[j].x * x.a[j].x, gamma.a[j].x, fmaf(d.a[j].y * x.a[j].y, gamma.a[j].y, again));
+                    again = fmaf(d.b[j].x * x.b[j].x, gamma.b[j].x, fmaf(d.b[j].y * x.b[j].y, gamma.b[j].y, again));
+                }
+                again = head_sum<LP>(again);
+                if (!in_range(ms)) hx = again;   // the warp's other heads keep their bits
+            }
             const float m = -hx * r * P.inv_dim * r;  // -mean(h n) * r: dx = r * (h + x * m)
-            const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
+            const float2 r2 = make_float2(r, r), dx2 = make_float2(r_dx, r_dx), m2 = make_float2(m, m);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 acc.a[j] = __ffma2_rn(__fmul2_rn(d.a[j], x.a[j]), r2, acc.a[j]);
                 acc.b[j] = __ffma2_rn(__fmul2_rn(d.b[j], x.b[j]), r2, acc.b[j]);
-                d.a[j] = __fmul2_rn(__ffma2_rn(x.a[j], m2, __fmul2_rn(d.a[j], gamma.a[j])), r2);
-                d.b[j] = __fmul2_rn(__ffma2_rn(x.b[j], m2, __fmul2_rn(d.b[j], gamma.b[j])), r2);
+                d.a[j] = __fmul2_rn(__ffma2_rn(x.a[j], m2, __fmul2_rn(d.a[j], gamma.a[j])), dx2);
+                d.b[j] = __fmul2_rn(__ffma2_rn(x.b[j], m2, __fmul2_rn(d.b[j], gamma.b[j])), dx2);
             }
         }
         const bool last = g == groups - 1;
