@@ -192,7 +192,7 @@ __device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
 
 // 2^u of two numbers below 2^21 on the multipliers: u = n + f with n the nearest integer (what is below -126 counts as that: 2^-126 is
 // nothing to a sum whose terms reach 2^-15, and rounds to 0 in f16), and 2^f by a polynomial fitted to the least relative error over
-// [-1/2, 1/2] with 1 as its constant: 9.2e-8, with the roundings 1.6e-7 (2^-22.6)
+// [-1/2, 1/2] with 1 as its constant: 1.09e-7, with the roundings 1.7e-7 (2^-22.4)
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
     const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
