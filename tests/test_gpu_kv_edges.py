@@ -25,8 +25,11 @@ def dense(q, place, k, v, scale, causal, window, limit):
     return p @ v, torch.logsumexp(z, -1), p @ v.abs(), big
 
 
-def near(out, lse, want, want_lse, mag, big):
-    tol = 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * mag + 1e-30
+WIDE = 2.0 ** -8 + 2.0 ** -10
+
+
+def near(out, lse, want, want_lse, mag, big, weight=WIDE):
+    tol = 2.0 ** -8 * want.abs() + weight * mag + 1e-30
     assert bool(((out.double() - want).abs() <= tol).all()), f"out: {float(((out.double() - want).abs() / tol).max()):.3g} tolerances"
     live = want_lse > -math.inf
     assert bool((lse[~live] == -math.inf).all()) and not bool(out[~live].any())
@@ -47,15 +50,15 @@ def attend(mx, q, cu, lens, table, cache, max_q, max_len, scale, **options):  # 
     return out, lse
 
 
-def agrees(mx, nq, lens, heads, group, dim, page, max_len, rows=None, seed=3, **options):  # noqa: F811
+def agrees(mx, nq, lens, heads, group, dim, page, max_len, rows=None, seed=3, scale=None, q_std=1.0, weight=WIDE, **options):  # noqa: F811
     """The call against `dense`, sequence by sequence; `rows`: rows of q that there are (the last sequence may go on behind them)."""
     block, cu = 16, cumulative(nq)
     rows = cu[-1] if rows is None else rows
     table, pool = make_table(lens, -(-max(lens) // page), page, seed)
     cache = Cache(pool, heads, page, dim, block)
     fill(cache, lens, table, page, block, seed)
-    q = torch.randn(rows, heads * group, dim, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda()
-    scale = dim ** -0.5
+    q = (q_std * torch.randn(rows, heads * group, dim, generator=torch.Generator().manual_seed(seed))).to(torch.bfloat16).cuda()
+    scale = dim ** -0.5 if scale is None else scale
     out, lse = attend(mx, q, cu, lens, table, cache, max(nq), max_len, scale, **options)
     for s, length in enumerate(lens):
         a, b = cu[s], min(cu[s + 1], rows)
@@ -64,7 +67,7 @@ def agrees(mx, nq, lens, heads, group, dim, page, max_len, rows=None, seed=3, **
         for h in range(heads * group):
             k, v = (ref.dequantise(c, sc, pages, block, h // group, length) for c, sc in (cache.parts[:2], cache.parts[2:]))
             near(out[a:b, h], lse[a:b, h],
-                 *dense(q[a:b, h], place, k, v, scale, options.get("causal", True), options.get("window", 0), max_len))
+                 *dense(q[a:b, h], place, k, v, scale, options.get("causal", True), options.get("window", 0), max_len), weight)
     assert cache.guards_intact()
 
 
@@ -200,3 +203,92 @@ def test_pages_behind_the_window(mx, dim, page, block, nq, lens, window, causal)
     assert all(torch.equal(a, b) for a, b in zip(want, call(released))), "released pages behind the window"
     assert mx.device_bad_indices() == 0
     assert bool(want[0].isfinite().all())
+
+
+# what test_gpu_kv.py asks of the kernel for few rows, asked of the one for many
+
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -20, 2.0 ** 100])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_query_sizes(mx, size, dim):  # noqa: F811
+    """Queries far from one, against key scales as far the other way."""
+    def setup(cache, q, table):
+        q.mul_(size)
+        ks = cache.parts[1]
+        shift = int(-math.log2(size))
+        ks.copy_(torch.where(ks != 0xFF, (ks.int() + shift).clamp(0, 254), ks.int()).to(torch.uint8))
+    check(mx, 8, 2, dim, 32, 16, [100, 40], [200, 100], seed=12, setup=setup)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_zero_queries(mx, dim):  # noqa: F811
+    def setup(cache, q, table):
+        q[:50] = 0
+        q[50:, :, 3:] = 0
+    check(mx, 8, 2, dim, 32, 16, [100, 20], [200, 100], seed=13, setup=setup)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,height", [(100, 150.0), (100, 20.0), (200, 448.0)])
+def test_prompt_one_token_far_above_the_rest(mx, dim, nq, height):  # noqa: F811
+    """The first key's score above all others', so that the reference comes down by as much as it may afterwards, and the output so far is
+    corrected."""
+    def setup(cache, q, table):
+        kc = cache.parts[0]
+        for h in range(kc.shape[1]):
+            d = q[:, h * (q.shape[1] // kc.shape[1])].float().mean(0)
+            kc[table[0][0], h, 0] = (d * (height / d.abs().max())).to(torch.float8_e4m3fn).view(torch.uint8)
+    check(mx, 2, 2, dim, 64, 16, [nq], [6000], seed=11, q_std=0.3, setup=setup)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_without_keys(mx, dim):  # noqa: F811
+    """Sequences of length zero and queries before the first key: zeros and -infinity."""
+    check(mx, 4, 2, dim, 16, 16, [100, 50, 70], [0, 1, 30], seed=6)
+    check(mx, 4, 2, dim, 16, 16, [100, 50], [0, 0], seed=7)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,lens", [([1], [300]), ([4, 3], [900, 50]), ([100, 30], [150, 700])])
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 3.0])
+def test_scales_of_the_scores(mx, dim, nq, lens, scale):  # noqa: F811
+    agrees(mx, nq, lens, 2, 4, dim, 32, max(lens), scale=scale)
+
+
+# The error of the weights as they are documented: half a step of binary16, 2^-11 each.  The rest, relative to the sum of the weights'
+# magnitudes: a score's binary32 sum, 16 2^-23 of its magnitudes (below 8 here: 2^-16); scale, reference and exponential 2^-19; the binary32
+# sums over up to 2100 tokens in steps of 16, 132 2^-23 < 2^-15; the last product 2^-23: below 2^-14 together, 2^-13 with what
+# the prompt kernel's pair of E4M3 numbers leaves of q's smallest elements (2^-18 of the row's largest, some of 128: below 2^-16).
+# q_std = 0.3 keeps scores and value scales within 13 binades, so that no weight is below binary16's normal range.
+SHARP = 2.0 ** -11 + 2.0 ** -13
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,lens", [([1], [2100]), ([1, 1, 1], [17, 500, 2000]), ([4, 8], [1000, 300]), ([65], [700]), ([150, 300], [2000, 333])])
+@pytest.mark.parametrize("options", [{}, {"window": 200}, {"causal": False}])
+def test_weights_are_as_sharp_as_stated(mx, dim, nq, lens, options):  # noqa: F811
+    agrees(mx, nq, lens, 2, 2, dim, 64, max(lens), q_std=0.3, weight=SHARP, **options)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("nq,length,window", [(1, 2000, 0), (4, 2000, 0), (1, 700, 300), (100, 2000, 0), (100, 700, 0), (200, 900, 250), (4, 20000, 0)])
+def test_each_token_counts_once(mx, dim, page, nq, length, window):  # noqa: F811
+    """Equal scores; one token's value in each dimension, at the ends of runs of 16 tokens (tiles, pages, chunks): its share is one
+    over the number of keys seen."""
+    heads, group = 2, 1
+    table, pool = make_table([length], -(-length // page), page, 1)
+    cache = Cache(pool, heads, page, dim, 16, code=0, scale=121)
+    lo = max(0, length - nq - window + 1) if window else 0
+    ends = [t for t in range(lo, length) if t % 16 in (0, 15) or t >= length - 2]
+    at = [ends[round(i * (len(ends) - 1) / (dim - 1))] for i in range(dim)]
+    for d, t in enumerate(at):
+        cache.parts[2][table[0][t // page], :, t % page, d] = 0x70   # 128 * 2^-6
+    q = torch.zeros(nq, heads * group, dim, dtype=torch.bfloat16, device="cuda")
+    out, lse = attend(mx, q, [0, nq], [length], table, cache, nq, length, 1.0, window=window)
+    place = length - nq + torch.arange(nq, device="cuda")[:, None]
+    key = torch.tensor(at, device="cuda")[None]
+    seen = (key <= place) & (key > place - window if window else key >= 0)
+    count = torch.minimum(place + 1, torch.full_like(place, window)) if window else place + 1
+    want = torch.where(seen, 2.0 / count.double(), 0.0)[:, None].expand(nq, heads, dim)
+    assert bool(((out.double() - want).abs() <= (2.0 ** -8 + SHARP) * want).all())
+    assert bool(((lse.double() - count.double().log()).abs() <= 2.0 ** -19 + 5 * 2.0 ** -23 * count.double().log()).all())
