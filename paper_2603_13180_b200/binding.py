@@ -382,6 +382,15 @@ def _vec(t, dtype, name, shape=None):
     return t.data_ptr()
 
 
+def _workspace(t):
+    """(pointer, bytes) of a workspace; its bytes lie one after another."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _table(cos_sin):
     """(pointer, rows, rotated elements) of a rotation table fp32 [rows, rot]."""
     if cos_sin is None:
@@ -435,12 +444,12 @@ def rmsnorm_rope_bwd(q, k, grad_q, grad_k, q_gain, k_gain, cos_sin, positions, d
     dqp, dqs, _ = _heads(dq, "dq", shape)
     dkp, dks, _ = _heads(dk if kh else None, "dk", k_shape)
     tp, rows, rot = _table(cos_sin)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws, ws_bytes = _workspace(workspace)
     _check(lib.rmsnorm_rope_bwd(qp, qs, qh, kp, ks, kh, gqp, gqs, gkp, gks, T, D, 1 if normalise else 0,
                                 _vec(q_gain, torch.bfloat16, "q_gain", (D,)), _vec(k_gain, torch.bfloat16, "k_gain", (D,)), eps, tp,
                                 rows, rot, 1 if interleaved else 0, _vec(positions, torch.int32, "positions", (T,)), dqp, dqs, dkp, dks,
                                 _vec(q_dgain, torch.float32, "q_dgain", (D,)), _vec(k_dgain, torch.float32, "k_dgain", (D,)),
-                                _ptr(workspace), ws_bytes, raw), "rmsnorm_rope_bwd")
+                                ws, ws_bytes, raw), "rmsnorm_rope_bwd")
 
 
 def alloc_kv_cache(num_pages: int, kv_heads: int, page_size: int, dim: int, block: int = 16, device="cuda"):
@@ -504,7 +513,7 @@ def mxkv_attention(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_s
     op, ost, _ = _heads(out, "out", shape)
     if d != dim:
         raise ValueError("q: dim differs from the cache's")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws, ws_bytes = _workspace(workspace)
     _check(lib.mxkv_attention(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
-                              scale, 1 if causal else 0, window, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), _ptr(workspace),
-                              ws_bytes, raw), "mxkv_attention")
+                              scale, 1 if causal else 0, window, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), ws, ws_bytes,
+                              raw), "mxkv_attention")
