@@ -617,21 +617,29 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             top_all = fmaxf(top_all, utop);
             if (__builtin_expect(apart, 0)) {
                 if (!was_apart && ref > kNone) sum_ref = ref - kTop - c0;
+                // from the scores as they still stand, by the whole warp: apart is the CTA's
                 float ztop = kNone;
+#pragma unroll 1
+                for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t z[16];
+                        tm_load16(z, s_at + 16 * g);
+                        const uint32_t see = visible(g >> 1) >> (16 * (g & 1));
+                        const float f = fmaxf(row_factor * slot.k[4 * buf + g], 1.17549435e-38f);
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) ztop = fmaxf(ztop, __uint_as_float(x[g >> 1][16 * (g & 1) + e]) * fac[g]);
-                if (ztop > sum_ref + kLift) {
-                    const float next = ceilf(ztop);
-                    if (sum_ref > kNone) l = times_pow2(l, sum_ref - next);
-                    sum_ref = next;
+                        for (int e = 0; e < 16; ++e) {
+                            const float s = (see >> e) & 1u ? __uint_as_float(z[e]) * f : kNone;
+                            if (pass == 0) ztop = fmaxf(ztop, s);
+                            else if (sum_ref > kNone) l += ex2(s - sum_ref);
+                        }
+                    }
+                    if (pass == 0 && ztop > sum_ref + kLift) {
+                        const float next = ceilf(ztop);
+                        if (sum_ref > kNone) l = times_pow2(l, sum_ref - next);
+                        sum_ref = next;
+                    }
                 }
-                if (sum_ref > kNone)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) l += ex2(fmaf(__uint_as_float(x[g >> 1][16 * (g & 1) + e]), fac[g], -sum_ref));
             }
             if (__any_sync(0xFFFFFFFFu, utop > ref + kUp || (utop < ref - kDown && utop > kNone))) {
                 float next = ref;   // (ref + kUp is -infinity without a reference)
