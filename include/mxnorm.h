@@ -47,7 +47,7 @@
  *    to MXN_ERR_CUDA.
  *  - Arithmetic contract (what the CPU oracle states and the tests compare):
  *    block absmaxes exact; row statistic accumulated in binary64 and rounded once
- *    to binary32; every element-wise product one IEEE binary32 operation; E8M0
+ *    to binary32 (the entry points around attention sum in binary32, as they state); every element-wise product one IEEE binary32 operation; E8M0
  *    scales by exact exponent tests; element codes round-to-nearest-even,
  *    saturating.  Normalisation factors 1/(r + eps) are 0 for a zero denominator (a row of zeros
  *    stays zero) and saturate at the largest finite binary32 instead of overflowing.
@@ -375,7 +375,10 @@ size_t rmsnorm_rope_bwd_workspace_bytes(int64_t T, int q_heads, int k_heads, int
  *   nothing.  Other tokens' codes and other blocks' scales are left as they were.
  *   The blocks written must belong to one sequence only (pages shared by sequences are full pages, or are copied first).
  *   A block whose page is out of range, or whose tokens lie outside the table, is left out; so are all tokens of a sequence
- *   whose kv_lens is smaller than its number of new tokens. */
+ *   whose kv_lens is smaller than its number of new tokens.  (The values are not rotated: they are written where the keys lie outside
+ *   the table.)
+ *   Inputs are finite.  An infinity sets its block's scale to 2^127, which leaves nothing of the block's other tokens, the earlier ones
+ *   among them; a NaN becomes a NaN code and has no say in the scale.  The scale byte 255 is never written. */
 mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16, int64_t v_stride, int64_t n_tokens, int kv_heads,
                        int head_dim, const int32_t* cu_tokens, int64_t n_seqs, const int32_t* kv_lens, const int32_t* page_table,
                        int64_t max_pages, int64_t num_pages, int page_size, int block, const float* cos_sin_or_null,
@@ -388,13 +391,15 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
  *   causal == 1: it sees the keys up to its own place (causal == 0: all of the sequence); window > 0: of those not more than
  *   `window` places back, its own included.  A row that sees no key gets zeros and lse = -infinity.
  *   max_q_len and max_kv_len bound the sequences' new queries and lengths (host values; they shape the launch: queries past
- *   max_q_len are not computed - their rows may receive undefined values - and keys past max_kv_len are not seen).
+ *   max_q_len are not computed - their rows may receive undefined values - and keys past max_kv_len are not seen; the places of the others
+ *   stay as kv_lens and cu_q give them).
  *   lse_out [n_tokens, q_heads] fp32: the logarithm of the sum of exp(scale q k) over the keys seen.
  *   Products run on the E4M3 codes with binary32 sums.  q enters exactly, but for elements below 2^-10 of their row's largest,
  *   which are kept to 2^-18 of it; the softmax's weights have 11 significant bits (fewer where a weight times its value block's
- *   scale lies below 2^-13 of the row's largest such product), its sums are binary32.
- *   What stands in the cache behind a sequence's last token, or in pages no visible key is in, has no influence.  A page out of
- *   range among the visible ones: its keys are left out.  A query row with an infinity or NaN, or one that sees a NaN key, gets
+ *   scale lies below 2^-13 of the row's largest such product, possibly none below 2^-24 of it), its sums are binary32 and count every weight.
+ *   What stands in the cache behind a sequence's last token, before every query's window, or in pages no visible key is in, has no
+ *   influence: pages behind a sliding window may be released.  A page out of range among the visible ones: its keys are left out.
+ *   Scale bytes of 255 are not expected: a call that sees one gets undefined values.  A query row with an infinity or NaN, or one that sees a NaN key, gets
  *   NaN; so may every row of a sequence one of whose values is NaN (its weight is 0 where it is not seen).
  *   workspace: device memory, 16-byte aligned, at least mxkv_attention_workspace_bytes(...) bytes for the same sizes (0: none
  *   needed); contents irrelevant before and after.  Calls that may overlap need workspaces of their own. */

@@ -12,8 +12,9 @@
 // for the codes, the others are read again from L1.  The run's rows are asked into L2 while the warp looks up its sequence.
 //
 // Bound: HBM, 3 bytes an element (2 read, 1 written); a decode step of a few tokens is bound by the latency of one warp's chain of
-// loads.  Measured, 8 heads of 128 in blocks of 16: six prompts of up to 4096 tokens 31 us, 3.5 TB/s (the shared-memory round trip and
-// the conversions keep half of the issue slots busy); one token for each of 64 sequences 3.7 us.
+// loads.  Measured, 8 heads of 128 in blocks of 16: six prompts of up to 4096 tokens 31 us, 3.5 TB/s, which is no bound: a warp does one
+// block of one head and ends, so that its chain of loads (sequence, length, page, rows, angles) hides behind no other block of its own;
+// half of the issue slots are busy.  One token for each of 64 sequences 4.0 us.
 #include "mxn_async.cuh"
 #include "mxn_internal.h"
 #include "mxn_rope.cuh"
