@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kWarps * 32, tight(LP, PAIRS) ? 5 : 1) rope_fw
         float r = 1.0f;
         if (NORM) {
             const float ms = mean_square(head_sum<LP>(dot(x, x)), P.inv_dim, P.eps);
-            if (!in_range(ms)) later |= 1u << u;
+            if (!in_range(ms) && h < heads) later |= 1u << u;
             r = head_rcp(ms);
             const uint16_t* gain = which ? P.gain[1] : P.gain[0];
             if (gain != nullptr && live) {
@@ -332,6 +332,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
             pos[1] = row_of(t + 2);
         }
         asm volatile("cp.async.wait_group %0;" :: "n"(kRing - 1) : "memory");
+        const bool last = g == groups - 1, mine = live && (!last || grp < in_last);
         const uint4 cg[2] = {lds16(at), lds16(at + PIECE)};
         Lane16 d;
         unpack<PAIRS>(d, cg);
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
             sd = __fadd2_rn(sd, se);
             const float sq = dot(x, x);
             // (asked of the lanes' own sums, ahead of the head's: asked of those the branch below costs 3.5 us of 92)
-            const bool odd = __any_sync(0xFFFFFFFFu, !(sq <= 0x1p80f && sq >= low));
+            const bool odd = __any_sync(0xFFFFFFFFu, !(sq <= 0x1p80f && sq >= low) && mine);
             const float ms = mean_square(head_sum<LP>(sq), P.inv_dim, P.eps);
             float hx = head_sum<LP>(sd.x + sd.y), r = head_rcp(ms), r_dx = r;   // r_dx: that of x as it was read
             if (__builtin_expect(odd, 0)) {
@@ -379,8 +380,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) rope_bwd_kernel(const HeadsPar
                 d.b[j] = __fmul2_rn(__ffma2_rn(x.b[j], m2, __fmul2_rn(d.b[j], gamma.b[j])), dx2);
             }
         }
-        const bool last = g == groups - 1;
-        if (live && (!last || grp < in_last)) {
+        if (mine) {
             if (!good) fill(d, __uint_as_float(0x7FC00000u));
             store<PAIRS>(reinterpret_cast<uint16_t*>(y), second, d);
         }
