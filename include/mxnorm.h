@@ -399,7 +399,8 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
  *   scale lies below 2^-13 of the row's largest such product, possibly none below 2^-24 of it), its sums are binary32 and count every weight.
  *   What stands in the cache behind a sequence's last token, before every query's window, or in pages no visible key is in, has no
  *   influence: pages behind a sliding window may be released.  A page out of range among the visible ones: its keys are left out.
- *   Scale bytes of 255 are not expected: a call that sees one gets undefined values.  A query row with an infinity or NaN, or one that sees a NaN key, gets
+ *   Scale bytes above 247, which the append does not write for finite inputs, are not expected: a call
+ *   that sees one may get infinities or undefined values.  A query row with an infinity or NaN, or one that sees a NaN key, gets
  *   NaN; so may every row of a sequence one of whose values is NaN (its weight is 0 where it is not seen).
  *   workspace: device memory, 16-byte aligned, at least mxkv_attention_workspace_bytes(...) bytes for the same sizes (0: none
  *   needed); contents irrelevant before and after.  Calls that may overlap need workspaces of their own. */

@@ -11,8 +11,8 @@
 //      folded into the softmax's weight, w_t = 2^(s_t + sv_t - R + 1) in f16.  The reference R (an integer, so that corrections of
 //      the sums are exact) is moved when a tile's largest s + sv is 14 above or 16 below it: f16 keeps 11 bits of what is above
 //      2^-14 and drops what is below 2^-25.  The softmax's own sum is l = sum of the unrounded w_t 2^(c0 - sv_t), a factor for each
-//      run of 16 tokens, c0 a constant of the warp; from the first scale on that lies far from c0 it has exponentials and a
-//      reference of its own (see kApart).
+//      run of 16 tokens, c0 near the warp's scales; a tile with scales far from c0, and those after it until the two references have
+//      come near each other, are summed apart (see kApart).
 //
 // A CTA of four warps takes up to 8 * NQ * RW query rows of one sequence and key head, and one chunk of the keys.  4 / RW groups
 // of warps walk over the chunk's tiles of 32 tokens in turn; each group feeds itself through a ring of tiles that the
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // near the value scales: the largest of the first tile; runs without tokens count as one of them
     const uint32_t first_scale = max(__shfl_sync(0xFFFFFFFFu, sc_next, 1), __shfl_sync(0xFFFFFFFFu, sc_next, 17));
     no_scale = min(max(first_scale, 67u), 187u);
-    const float c0 = (float)(int)no_scale - 127.0f;
+    float c0 = (float)(int)no_scale - 127.0f;
     if (!in_pool(pages[0])) sc_next = no_scale;
     bool ok = true, apart = false;   // apart: the sums have references of their own
 
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const uint32_t sc = sc_next;
         sc_next = scale_at(i + 1, pages[1]);
         const float kf[2] = {e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 0)), e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, sc, 16))};
-        const float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
+        float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
         // tokens of the tile that exist and whose page could be read
         const bool readable = in_pool(pages[0]);
         const bool wanted = t0 + lane < k1 && t0 + lane >= seen;
@@ -328,6 +328,28 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         bad_page |= wanted && !readable;
         const bool was_apart = apart;
         apart = apart || fabsf(sv[0] - c0) > kApart || fabsf(sv[1] - c0) > kApart;
+        if (__builtin_expect(was_apart, 0)) {
+            // back to the common unit, with c0 near this tile's scales, if these allow it and the rows' references lie near enough
+            const bool some0 = (there & 0xFFFFu) != 0u, some1 = (there >> 16) != 0u;
+            const float top = fminf(fmaxf(fmaxf(some0 ? sv[0] : -60.0f, some1 ? sv[1] : -60.0f), -60.0f), 60.0f);
+            bool near = !(some0 && fabsf(sv[0] - top) > kApart) && !(some1 && fabsf(sv[1] - top) > kApart);
+            float d[QN];
+#pragma unroll
+            for (int x = 0; x < QN; ++x) {
+                const float r = sum_refs[warp][8 * (x >> 1) + 2 * c + (x & 1)];
+                d[x] = ref[x] == kNone && r == kNone ? 0.0f : ref[x] - kTop - top - r;
+                near = near && fabsf(d[x]) <= kApart;
+            }
+            if (__all_sync(0xFFFFFFFFu, near)) {
+                apart = false;
+                c0 = top;
+                no_scale = (uint32_t)((int)c0 + 127);
+                if (!some0) sv[0] = c0;
+                if (!some1) sv[1] = c0;
+#pragma unroll
+                for (int x = 0; x < QN; ++x) l[x] = times_pow2(l[x], -d[x]);
+            }
+        }
 
         // (the warp leaves the loop as a whole: its lanes' polls may end differently)
         if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(full + 8 * st, ph))) {
@@ -540,8 +562,8 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
 
     // ---- join the groups of warps ----
     // row x of this thread: sum l 2^at, output acc unit 2^at; dimensions g * DIM/8 ... + DIM/8 - 1.  at = ref - kTop - c0 and unit = 2^c0;
-    // with a reference of its own the sum is brought to [1, 2), and acc to the same unit in two steps, since the power may lie outside
-    // binary32's range where the product does not.
+    // with a reference of its own the sum is brought to [1/16, 1/8), and acc to the same unit in two steps, since the power may lie outside
+    // binary32's range where the product does not (it is below a quarter of the largest value then, and the groups' sum in range).
     constexpr int OUT = DIM / 8, PITCH = DIM + 4;
     float* const sm = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
     float2* const stat = reinterpret_cast<float2*>(sm + GROUPS * Sh::kRows * PITCH);   // (at, l)
@@ -558,7 +580,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         for (int x = 0; x < QN; ++x) {
             at[x] = sum_refs[warp][8 * (x >> 1) + 2 * c + (x & 1)];
             if (at[x] == kNone) continue;
-            const int e = min(max((int)(__float_as_uint(l[x]) >> 23) - 127, -126), 127);
+            const int e = min(max((int)(__float_as_uint(l[x]) >> 23) - 127, -126), 127) + 4;
             l[x] = times_pow2(l[x], (float)-e);
             at[x] += (float)e;
             const float d = ref[x] - kTop - at[x], half = floorf(0.5f * d), by1 = ex2(half), by2 = ex2(d - half);

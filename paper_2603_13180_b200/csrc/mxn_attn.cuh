@@ -60,9 +60,9 @@ __device__ __forceinline__ float ex2(float x)
 }
 // The softmax's sum and its range.  While the value scales lie within kApart binades of c0, the sum is in units of 2^(R - 1 - c0): its
 // terms are the weights times 2^(c0 - sv).  R follows the largest s + sv to within 54, so the largest score's term lies between 2^-16
-// and 2^71, and a step of R that is too large for binary32 (the sum so far becomes 0) only drops terms below 2^-39 of it.  From the
-// first tile on whose scales lie farther away (a run of zero values has scale 2^-127) the sum has a reference of its own that follows the
-// scores alone: terms 2^(s - reference), the reference raised where a score lies kLift above it.
+// and 2^71, and a step of R that is too large for binary32 (the sum so far becomes 0) only drops terms below 2^-39 of it.  A tile whose
+// scales lie farther away (a run of zero values has scale 2^-127) is summed apart: with exponentials of its own, terms 2^(s - r), and a
+// reference r of the sum that follows the scores alone, raised where a score lies kLift above it.
 constexpr float kApart = 16.0f, kLift = 60.0f;
 // v 2^d for a whole d whose power may lie outside binary32's range where the product does not
 __device__ __forceinline__ float times_pow2(float v, float d)

@@ -18,8 +18,8 @@
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
 //   is moved only when a step's largest is 14 above or 16 below it, so that the output in tensor memory rarely has to be corrected.
 //   f16 drops what is below 2^-25, i.e. 2^-26 of the weight at R and 2^-10 of the largest of a step at the window's lower end.
-// The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 a constant of the CTA;
-// from the first scale on that lies far from c0 it has exponentials and a reference of its own (see kApart).
+// The softmax's sum is l = sum of w_t 2^(c0 - sv_t) with unrounded w, a factor for each run of 16 tokens, c0 near the scales;
+// a tile with scales far from c0 is summed apart (see kApart), and c0 follows a tile whose scales are all elsewhere.
 // The weights replace their scores in tensor memory and are the second product's first operand from there; the values are its
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
 //
@@ -71,6 +71,7 @@ struct PromptShape {
     static constexpr int kSmem = kEnd + 1024;
 };
 
+constexpr uint32_t kWide = 1, kMoved = 2;
 // one slot of the scales' ring: what the softmax needs to know about a key tile.  The ring is deeper than the keys': a slot is
 // written again once the keys kKeyStages tiles before are free, i.e. when the softmax of both row tiles is past the tile before those.
 struct alignas(16) TileScales {
@@ -78,7 +79,7 @@ struct alignas(16) TileScales {
     float v[kTile / kRun];        // sv - 127
     float l[kTile / kRun];        // 2^(c0 - v): from weights to the softmax's sum
     uint32_t readable;            // bit i: the page of run i could be read
-    uint32_t apart;               // a value scale of this or an earlier tile lies so far from c0 that l is summed apart
+    uint32_t apart;               // kWide: a value scale lies so far from c0 that the tile is summed apart; kMoved: c0 is another than before
     float c0;
 };
 
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
         const int box = min(P.page, kTile), boxes = kTile / box;     // tokens of a box, boxes of a tile
         const int per_page_shift = P.page_shift - P.block_shift;
-        bool any_bad = false, apart = false;
+        bool any_bad = false;
         float c0 = 0.0f;
         int page_next = -1;                                          // lane i: page of run i (lanes 0-7) of the next tile
         auto look_up = [&](int j) {
@@ -386,13 +387,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             TileScales& slot = scales[j % kScaleSlots];
             const float v = (float)(int)sv - 127.0f;
-            if (j == 0) {   // near the value scales: the largest of the first tile
-                c0 = v;
+            // c0, near the value scales: the largest of the first tile, or of the first one whose scales are all elsewhere
+            bool wide = __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - c0) > kApart);
+            const float c0_before = c0;
+            if (j == 0 || wide) {
+                float top = v;   // (a run without tokens has the least)
 #pragma unroll
-                for (int o = 4; o > 0; o >>= 1) c0 = fmaxf(c0, __shfl_xor_sync(0xFFFFFFFFu, c0, o));
-                c0 = fminf(fmaxf(__shfl_sync(0xFFFFFFFFu, c0, 0), -60.0f), 60.0f);
+                for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                top = fminf(fmaxf(__shfl_sync(0xFFFFFFFFu, top, 0), -60.0f), 60.0f);
+                const bool still = __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - top) > kApart);
+                if (j == 0 || !still) {
+                    c0 = top;
+                    wide = still;
+                }
             }
-            apart = apart || __any_sync(0xFFFFFFFFu, pg >= 0 && fabsf(v - c0) > kApart);
             if (lane < 8) {
                 slot.k[lane] = e8m0_to_f32(sk);
                 slot.v[lane] = v;
@@ -400,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             }
             if (lane == 0) {
                 slot.readable = readable;
-                slot.apart = apart;
+                slot.apart = (wide ? kWide : 0u) | (c0 != c0_before ? kMoved : 0u);
                 slot.c0 = c0;
             }
             __syncwarp();
@@ -559,8 +567,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const int see_hi = P.causal ? min(pos + 1, len) : len;
         const int see_lo = first_seen(pos, P.window);
         const float kNone = -INFINITY;
-        float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f, sum_ref = kNone;   // sum_ref: of l, once that is summed apart
-        bool ok = true, apart = false;
+        float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
+        // l's unit is 2^(ref - kTop - c0) until a tile is wide or c0 changes; from then on (`by_own`) 2^sum_ref, and `unit` the former in the
+        // latter.  Where ref lies so far above the scores (a wide tile's larger scales) that weights vanish which the sum has to count, the
+        // warp sums by exponentials of their own (`slow`).
+        float sum_ref = kNone, unit = 1.0f;
+        bool ok = true, by_own = false, slow = false;
         const int steps = 2 * tiles;
         // a row that nothing hides in a step needs no mask: the range that holds for the warp's rows
         const int all_lo = __reduce_max_sync(0xFFFFFFFFu, see_lo), all_hi = __reduce_min_sync(0xFFFFFFFFu, min(see_hi, k1));
@@ -581,9 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                          l4 = *reinterpret_cast<const float4*>(slot.l + 4 * buf);
             const float slot_k[4] = {k4.x, k4.y, k4.z, k4.w}, slot_v[4] = {v4.x, v4.y, v4.z, v4.w}, slot_l[4] = {l4.x, l4.y, l4.z, l4.w};
             const uint32_t readable = (slot.readable >> (4 * buf)) & 0xFu;
-            const bool was_apart = apart;
-            apart = slot.apart != 0;
-            c0 = slot.c0;
+            const uint32_t special = slot.apart & (kWide | (buf ? 0u : kMoved));
             // bit e: the row sees token 32 c + e of the step
             auto visible = [&](int c) -> uint32_t {
                 const int tc = t0 + 32 * c, up = min(max(min(see_hi, k1) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
@@ -616,12 +626,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 utop = max_nan(utop, fmaf(m, fac[g], slot_v[g]));
             }
             top_all = fmaxf(top_all, utop);
-            if (__builtin_expect(apart, 0)) {
-                if (!was_apart && ref > kNone) sum_ref = ref - kTop - c0;
-                // from the scores as they still stand, by the whole warp: apart is the CTA's
+            const bool move = utop > ref + kUp || (utop < ref - kDown && utop > kNone);   // (ref + kUp is -infinity without a reference)
+            float counts = unit;   // what the step's weights count in the sum
+            if (__any_sync(0xFFFFFFFFu, move || special || slow)) {   // one branch for all that is rare
+                const bool summed = slow || (special && (i > 0 || (special & kWide)));
+                if (summed && !by_own) {
+                    by_own = true;
+                    if (ref > kNone) sum_ref = ref - kTop - c0;
+                }
+                c0 = slot.c0;
+                // from the scores as they still stand, by the whole warp
                 float ztop = kNone;
 #pragma unroll 1
-                for (int pass = 0; pass < 2; ++pass) {
+                for (int pass = 0; summed && pass < 2; ++pass) {
 #pragma unroll 1
                     for (int g = 0; g < 4; ++g) {
                         uint32_t z[16];
@@ -641,15 +658,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                         sum_ref = next;
                     }
                 }
-            }
-            if (__any_sync(0xFFFFFFFFu, utop > ref + kUp || (utop < ref - kDown && utop > kNone))) {
-                float next = ref;   // (ref + kUp is -infinity without a reference)
+                float next = ref;
                 if (utop > ref + kUp) next = ceilf(utop);
                 else if (utop < ref - kDown && utop > kNone) next = ceilf(fmaxf(utop, top_all - kDepth));
+                const bool up = next > ref;
                 const float alpha = ref == kNone ? 0.0f : ex2(ref - next);
-                l *= apart ? 1.0f : alpha;
+                l *= by_own ? 1.0f : alpha;
                 ref = next;
-                if (i > 0) {   // the output up to the last step: its end is signalled with the next step's scores
+                if (by_own) {
+                    float d = ref == kNone ? 0.0f : ref - kTop - c0 - sum_ref;
+                    if (d > kApart && up && !(special & kWide)) {   // ref comes from a score of this step within kApart of it
+                        if (sum_ref > kNone) l = times_pow2(l, -d);
+                        sum_ref = ref - kTop - c0;
+                        d = 0.0f;
+                    }
+                    unit = ex2(fminf(d, kApart));
+                    slow = __any_sync(0xFFFFFFFFu, d > kApart);
+                }
+                counts = summed ? 0.0f : unit;
+                if (i > 0 && __any_sync(0xFFFFFFFFu, move)) {   // the output up to the last step: its end is signalled with the next step's scores
                     ok = wait(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u, dead);
                     if (!__all_sync(0xFFFFFFFFu, ok)) break;
                     tc_after();
@@ -688,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 more = fmaf(both.x + both.y, slot_l[g], more);
                 if (g & 1) probe[g >> 1] = mbar_test(s_full + 16 * rt + 8 * (buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u);
             }
-            l += apart && more == more ? 0.0f : more;   // (a NaN among the weights reaches the sum all the same)
+            l = fmaf(more, counts, l);   // (a NaN among the weights reaches the sum all the same)
             tm_store32(s_at, w);
             here = __all_sync(0xFFFFFFFFu, i + 1 < steps && (probe[0] || probe[1]));
             scales_here = __all_sync(0xFFFFFFFFu, probe[2]);
@@ -705,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         // the power in two factors, since it may lie outside binary32's range where the product does not
         const bool some = ref > kNone || l != l;   // (NaN scores set no reference)
         float inv = some ? __fdiv_rn(ex2(c0), l) : 0.0f, inv2 = 1.0f, lse2 = some ? log2f(l) + (ref - kTop - c0) : kNone;
-        if (apart && ref > kNone) {
+        if (by_own && ref > kNone) {
             const int e = min(max((int)(__float_as_uint(l) >> 23) - 127, -126), 127);
             const float d = ref - kTop - sum_ref - (float)e, half = floorf(0.5f * d);
             inv = __fdiv_rn(ex2(half), times_pow2(l, (float)-e));   // l in [1, 2)

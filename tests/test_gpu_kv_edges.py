@@ -292,3 +292,21 @@ def test_each_token_counts_once(mx, dim, page, nq, length, window):  # noqa: F81
     want = torch.where(seen, 2.0 / count.double(), 0.0)[:, None].expand(nq, heads, dim)
     assert bool(((out.double() - want).abs() <= (2.0 ** -8 + SHARP) * want).all())
     assert bool(((lse.double() - count.double().log()).abs() <= 2.0 ** -19 + 5 * 2.0 ** -23 * count.double().log()).all())
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("seqs,nq", [(1, 1), (40, 1), (40, 4), (1, 100), (2, 150)])
+@pytest.mark.parametrize("regions", [(227, 121), (121, 227), (121, 0, 121, 227, 121), (0, 121, 0, 121), (60, 121, 187), (1, 247, 1), (121, 100, 121, 140)])
+@pytest.mark.parametrize("width", [32, 144])
+def test_value_scales_by_region(mx, dim, seqs, nq, regions, width):  # noqa: F811
+    """Regions of tokens whose value scales lie far from their neighbours', and back: each token counts in the softmax's sum.  247 is the
+    largest byte that finite values have; with 254, codes of about 60 are values of 2^133, whose mean no bf16 holds."""
+    length = 900
+
+    def setup(cache, q, table):
+        vc, vs = cache.parts[2:]
+        vc.copy_(torch.where((vc != 0x7F) & ((vc & 0x7F) < 0x38), (vc & 0x80) | 0x38, vc))   # no code below 1: see value_scales
+        pages = torch.tensor(table, device="cuda")[:, :-(-length // 32)]
+        for b in range(-(-length // 16)):
+            vs[pages[:, b // 2], :, b % 2] = regions[16 * b // width % len(regions)]
+    check(mx, 16 if seqs > 2 else 4, 8 if seqs > 2 else 2, dim, 32, 16, [nq] * seqs, [length] * seqs, seed=dim + nq, setup=setup)
