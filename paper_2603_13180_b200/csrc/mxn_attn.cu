@@ -26,7 +26,7 @@
 // cluster, through each other's shared memory; more go to the workspace and are joined in a fixed order by a second kernel.
 //
 // Measured (32 query and 8 key heads of 128; on the device alone, in turn with other work in brackets): 64 sequences of up to 8192 keys
-// 115 us, 5.9 TB/s (123); one of 131072 keys 49 us, 5.4 TB/s with the join; one of 1000 keys 6.2 us, which is a start, two trips to
+// 115 us, 5.9 TB/s (118); one of 131072 keys 49 us, 5.4 TB/s with the join; one of 1000 keys 6.3 us, which is a start, two trips to
 // memory and the join.  32 sequences of four drafted tokens, 32 and 4 heads of 64, window 1024: 20 us, seven times what its bytes
 // take: 256 CTAs whose warps walk over at most five tiles of 32 query rows; how much of it is the start is not known.
 //

@@ -8,9 +8,9 @@
 // works on 32*16/dim heads at a time and keeps the token's cosines and sines in registers over all of its heads.
 // The gradient recomputes r from x, which it reads anyway, instead of loading a saved one.
 //
-// Measured, 32 query and 8 key heads of 128 (on the device alone, in turn with other work in brackets): 16384 tokens forward 62 us (65),
-// 5.4 TB/s; backward with both gains' gradients 88 us (95), 5.7 TB/s; 64 tokens 2.4 us and 5.1 us, the latency of a start and one (two)
-// trips to memory.  4099 tokens of 32 and 4 heads of 64 in pairs, half of each rotated, backward: 16 us (18), 3.6 TB/s, of which 2.6 are
+// Measured, 32 query and 8 key heads of 128 (on the device alone, in turn with other work in brackets): 16384 tokens forward 62 us (62),
+// 5.4 TB/s; backward with both gains' gradients 90 us (91), 5.6 TB/s; 64 tokens 2.5 us and 5.1 us, the latency of a start and one (two)
+// trips to memory.  4099 tokens of 32 and 4 heads of 64 in pairs, half of each rotated, backward: 15 us (18), 3.7 TB/s, of which 2.6 are
 // the second launch that joins the gains' sums and some 3 the start.
 #include <cuda_bf16.h>
 

@@ -24,14 +24,15 @@
 // second operand as they lie ([token][dim] is the "MN-major" form), so nothing is transposed.
 //
 // Bound: at head size 128 the two products of a 256 x 128 tile take 2048 cycles at the tensor cores' rate, its 32768 exponentials
-// 2048 cycles of the special function units.  4096 queries over 8192 keys, 32 query and 8 key heads of 128: 446 us, 924 TFLOP/s, 56 %
-// of a large library product's measured rate (477 us in turn with other work, at lower clocks); a tile takes some 3900 cycles.  Without the softmax's arithmetic the same kernel takes
-// 310 us: what is left is the softmax's chain of loads, maxima, exponentials and stores, two warps for each scheduler, with the special
-// function units busy for half of the time.  Four warps for each scheduler (two for a row) took 595 us: twice the fixed costs
-// of a step.  What shortened the chain: barriers and scales looked at a step ahead, while shared memory is busy with the products'
-// operands (499 -> 478); a rounding of the maximum taken out of it (501 -> 493); q read by rows, 12 warps at it, and the
-// output written by rows through shared memory (464 -> 450), the last units in halves (-> 437).  NaN scores kept as such: 446.  The products alone do not reach their rate either: scores
-// in products of 64 tokens read 6 KB of shared memory in 48 cycles for 32 of the tensor cores.
+// 2048 cycles of the special function units.  4096 queries over 8192 keys, 32 query and 8 key heads of 128: 450 us, 916 TFLOP/s, 55 %
+// of a large library product's measured rate (482 us in turn with other work, at lower clocks); a tile takes some 3900 cycles.  Without
+// the softmax's arithmetic the same kernel takes 310 us: what is left is the softmax's chain of loads, maxima, exponentials and stores,
+// two warps for each scheduler, with the special function units busy for half of the time.  Four warps for each scheduler (two for a
+// row) took 595 us: twice the fixed costs of a step.  What shortened the chain: barriers and scales looked at a step ahead, while
+// shared memory is busy with the products' operands (499 -> 478); a rounding of the maximum taken out of it (501 -> 493); q read by
+// rows, 12 warps at it, and the output written by rows through shared memory (464 -> 450), the last units in halves (-> 437).  NaN
+// scores kept as such: 446, sums apart: 450.  The products alone do not reach their rate either: scores in products of 64 tokens read
+// 6 KB of shared memory in 48 cycles for 32 of the tensor cores.
 //
 // Every wait is bounded; see mxn_device_timeouts.
 #include <cuda_bf16.h>
