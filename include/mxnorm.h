@@ -413,6 +413,69 @@ mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens
 size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads,
                                       int kv_heads, int head_dim);
 
+/* The same with other masks; what is not said here is as in mxkv_attention (workspaces and their sizes too).
+ *   mxkv_attention_sinks: causal, with a window of `window` >= 1 places, beside which a sequence's first `sinks` keys (those up to the query's
+ *   own place) stay visible.  Pages between the first tokens and every query's window have no influence and may be released.
+ *   mxkv_attention_tree: the new tokens of a sequence are drafts that form a tree (or several).  Each sees every key in front of
+ *   the sequence's new tokens, and new token i (place kv_lens - new tokens + i) where bit i % 32 of word i / 32 of its own row of
+ *   mask_u32 [n_tokens, mask_words] is set: as a rule its ancestors and itself.  Bits of tokens that the sequence does not have are
+ *   ignored, tokens past the last word are not seen.  Where drafts stand in the tree, and so their rotation, is the caller's
+ *   (rmsnorm_rope_fwd with positions; mxkv_append without angles). */
+mxn_status mxkv_attention_sinks(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                                const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                                const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                                const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale,
+                                int64_t window, int64_t sinks, void* out_bf16, int64_t out_stride, float* lse_out_or_null, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream);
+mxn_status mxkv_attention_tree(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                               const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                               const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                               const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale,
+                               const void* mask_u32, int64_t mask_words, void* out_bf16, int64_t out_stride, float* lse_out_or_null,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* What each key is given by the softmax: weights[page, head, place in page] = earlier + sum over the call's query rows that see the key, and the
+ *   query heads that share its key head, of exp(scale q k - lse).  It is what eviction goes by.
+ *   q and lse [n_tokens, q_heads] as given to and received from the attention over the same keys, with the same scale, causal,
+ *   window and sinks (sinks > 0 needs causal and a window).  weights and earlier are fp32 [num_pages, kv_heads, page_size]; earlier may
+ *   be weights itself, or NULL (nothing).  A call's own new tokens have nothing from earlier: their places in `earlier` are not read.
+ *   Every token of every sequence up to max_kv_len is written, a sequence without new tokens or keys that no row sees included (earlier + 0);
+ *   places of no token are left as they are.  Rows past max_q_len, and rows whose lse is -infinity, give nothing.  A NaN in a row, its lse or a key that
+ *   it sees makes the sums concerned NaN.  Tokens whose page is out of range are left out.  Sums are binary32 in a fixed order. */
+mxn_status mxkv_attention_weights(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                                  const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                                  const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                                  const void* k_codes_u8, const void* k_scales_u8, float scale, int causal, int64_t window, int64_t sinks,
+                                  const float* lse, const float* earlier_or_null, float* weights, void* cuda_stream);
+
+/* Choice of the tokens that stay in the cache, for each sequence and key head apart: the first `sinks`, the last `recent`, and of those
+ *   between the ones with the largest weights (equal ones by place; a NaN, or a token whose page is out of range, comes last), `keep` in all
+ *   (sinks + recent <= keep).  A sequence of up to `keep` tokens keeps all.  Tokens past max_kv_len do not count.
+ *   kept int32 [n_seqs, kv_heads, keep]: their places, rising; -1 behind a shorter sequence's last.  new_lens int32 [n_seqs]. */
+mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const int32_t* kv_lens, int64_t max_kv_len, const int32_t* page_table,
+                       int64_t max_pages, int64_t num_pages, int page_size, int64_t keep, int64_t sinks, int64_t recent, int32_t* kept,
+                       int32_t* new_lens, void* cuda_stream);
+
+/* Moves listed tokens of a sequence together: token kept[s, h, i] goes to place first[s] + i (first NULL: 0) for the places below
+ *   new_lens[s] (at most max_kept of them).  kept int32 [n_seqs, kept_heads, max_kept], kept_heads = kv_heads or 1 (one list for all heads).
+ *   It closes the gaps that an eviction leaves (with mxkv_select's lists), and those in a tree of drafts of which a path was accepted
+ *   (first = the length in front of the tree, the path as one list).  head_dim is 64 or 128.
+ *   out_page_table NULL (or page_table itself): in place.  The lists then rise and no entry lies below its place.  Needs a workspace (device
+ *   memory, 16-byte aligned, mxkv_compact_workspace_bytes(...) bytes, contents irrelevant before and after; calls that may overlap need
+ *   workspaces of their own).  Otherwise tokens are written to the pages of out_page_table int32 [n_seqs, out_max_pages], which must not be
+ *   pages that the call reads other than for tokens in front of `first`; lists may be in any order.
+ *   Each block that is written gets the scale that its largest value asks for (the append's rule; its tokens in front of `first` included),
+ *   and its codes are rounded on it: exact unless they become subnormal.  A block whose tokens all stay where they are is
+ *   left as it is.  weights fp32 [num_pages, kv_heads, page_size] (or NULL) move along.  Tokens behind new_lens are left as they are, but for their block's scale.
+ *   An entry out of [0, kv_lens[s]), out of order in place, or whose page is out of range: its block is left as it is (in place, an order that does
+ *   not rise leaves the head's tokens undefined).  A `first` out of [0, kv_lens[s]]: the sequence is left as it is. */
+mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, const int32_t* first_or_null, const int32_t* new_lens,
+                        const int32_t* kv_lens, int kv_heads, int head_dim, int64_t n_seqs, const int32_t* page_table, int64_t max_pages,
+                        const int32_t* out_page_table_or_null, int64_t out_max_pages, int64_t num_pages, int page_size, int block,
+                        void* k_codes_u8, void* k_scales_u8, void* v_codes_u8, void* v_scales_u8, float* weights_or_null, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
+size_t mxkv_compact_workspace_bytes(int64_t n_seqs, int kv_heads, int64_t max_kept);
+
 #ifdef __cplusplus
 }
 #endif

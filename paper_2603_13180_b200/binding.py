@@ -27,7 +27,8 @@ EXPORTS = ("mxn_scale_bytes", "mxn_status_string", "mx_cast", "rmsnorm_mxfp8_fwd
            "mx_cast_e5m2", "mx_cast_transposed_e5m2", "mxnorm_postround_fwd",
            "mxnorm_add_fwd", "mx_cast_nvfp4", "mxn_device_bad_indices", "mxn_device_bad_indices_reset",
            "rmsnorm_rope_fwd", "rmsnorm_rope_bwd", "rmsnorm_rope_bwd_workspace_bytes", "mxkv_append", "mxkv_attention",
-           "mxkv_attention_workspace_bytes")
+           "mxkv_attention_workspace_bytes", "mxkv_attention_sinks", "mxkv_attention_tree", "mxkv_attention_weights", "mxkv_select",
+           "mxkv_compact", "mxkv_compact_workspace_bytes")
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -88,12 +89,24 @@ lib.mxkv_attention.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i6
                                _vp, _f32, _i32, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
 lib.mxkv_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i32, _i32, _i32]
 lib.mxkv_attention_workspace_bytes.restype = _sz
+lib.mxkv_attention_sinks.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp,
+                                     _vp, _vp, _f32, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+lib.mxkv_attention_tree.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp,
+                                    _vp, _vp, _f32, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+lib.mxkv_attention_weights.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp,
+                                       _f32, _i32, _i64, _i64, _vp, _vp, _vp, _vp]
+lib.mxkv_select.argtypes = [_vp, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i64, _i64, _i64, _vp, _vp, _vp]
+lib.mxkv_compact.argtypes = [_vp, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                             _vp, _sz, _vp]
+lib.mxkv_compact_workspace_bytes.argtypes = [_i64, _i32, _i64]
+lib.mxkv_compact_workspace_bytes.restype = _sz
 for _name in ("mx_cast", "rmsnorm_mxfp8_fwd", "mxnorm_fwd", "mxnorm_nvfp4_fwd", "mxnorm_bwd", "mxnorm_fwd_host",
               "mxnorm_bwd_noalloc", "mx_cast_fp4", "rmsnorm_mxfp4_fwd", "mxnorm_mxfp4_fwd",
            "mx_cast_transposed", "rmsnorm_nvfp4_fwd", "mxn_selftest_division", "mxn_selftest_dispatch",
            "mx_cast_e5m2", "mx_cast_transposed_e5m2", "mxnorm_postround_fwd",
            "mxnorm_add_fwd", "mx_cast_nvfp4", "mxn_device_bad_indices", "mxn_device_bad_indices_reset", "rmsnorm_rope_fwd",
-           "rmsnorm_rope_bwd", "mxkv_append", "mxkv_attention"):
+           "rmsnorm_rope_bwd", "mxkv_append", "mxkv_attention", "mxkv_attention_sinks", "mxkv_attention_tree", "mxkv_attention_weights",
+              "mxkv_select", "mxkv_compact"):
     getattr(lib, _name).restype = _i32
 
 
@@ -517,3 +530,96 @@ def mxkv_attention(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_s
     _check(lib.mxkv_attention(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
                               scale, 1 if causal else 0, window, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), ws, ws_bytes,
                               raw), "mxkv_attention")
+
+
+def _attention(entry, q, cu_q, kv_lens, page_table, cache, out, max_q_len, max_kv_len, scale, mask_args, lse, workspace, raw):
+    pages, heads, page, dim, block, kc, ks, vc, vs = _cache(*cache)
+    s, width, cup, lp, pt = _sequences(cu_q, kv_lens, page_table)
+    qp, qst, qh = _heads(q, "q")
+    n, _, d = shape = q.shape
+    op, ost, _ = _heads(out, "out", shape)
+    if d != dim:
+        raise ValueError("q: dim differs from the cache's")
+    ws, ws_bytes = _workspace(workspace)
+    _check(getattr(lib, entry)(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
+                               scale, *mask_args, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), ws, ws_bytes, raw), entry)
+
+
+def mxkv_attention_sinks(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, window, sinks,
+                         lse=None, workspace=None, stream=None):
+    """Causal attention over the paged cache in which a query sees the last `window` keys and its sequence's first `sinks`."""
+    raw = _on_current_device(stream, q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, lse, workspace)
+    _attention("mxkv_attention_sinks", q, cu_q, kv_lens, page_table, (k_codes, k_scales, v_codes, v_scales), out, max_q_len, max_kv_len, scale,
+               (window, sinks), lse, workspace, raw)
+
+
+def mxkv_attention_tree(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, tree_mask,
+                        lse=None, workspace=None, stream=None):
+    """Attention of drafted tokens that form a tree.  tree_mask int32 [n, words]: bit i % 32 of word i / 32 of a row tells whether it sees
+    new token i of its sequence (its ancestors and itself); what stands in front of a sequence's new tokens is seen by all of them."""
+    raw = _on_current_device(stream, q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, tree_mask, lse, workspace)
+    if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[0]:
+        raise ValueError("tree_mask: expected int32 [tokens, words]")
+    _attention("mxkv_attention_tree", q, cu_q, kv_lens, page_table, (k_codes, k_scales, v_codes, v_scales), out, max_q_len, max_kv_len, scale,
+               (_vec(tree_mask, torch.int32, "tree_mask"), tree_mask.shape[1]), lse, workspace, raw)
+
+
+def _weights(t, name, codes_shape):
+    """Pointer of the keys' sums fp32 [pages, heads, page] (None stays None)."""
+    return _vec(t, torch.float32, name, codes_shape[:3])
+
+
+def mxkv_attention_weights(q, cu_q, kv_lens, page_table, k_codes, k_scales, lse, weights, max_q_len, max_kv_len, scale, earlier=None,
+                           causal=True, window=0, sinks=0, stream=None):
+    """Sums of the softmax weights that the queries [n, Hq, D] give each key: weights fp32 [pages, heads, page] = earlier + sums; lse
+    [n, Hq] as the attention gave it.  earlier may be weights itself; the call's own new tokens start from nothing."""
+    raw = _on_current_device(stream, q, cu_q, kv_lens, page_table, k_codes, k_scales, lse, weights, earlier)
+    pages, heads, page, dim, block, kc, ks, _, _ = _cache(k_codes, k_scales, k_codes, k_scales)
+    s, width, cup, lp, pt = _sequences(cu_q, kv_lens, page_table)
+    qp, qst, qh = _heads(q, "q")
+    n, _, d = q.shape
+    if d != dim:
+        raise ValueError("q: dim differs from the cache's")
+    _check(lib.mxkv_attention_weights(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, scale,
+                                      1 if causal else 0, window, sinks, _vec(lse, torch.float32, "lse", (n, qh)),
+                                      _weights(earlier, "earlier", k_codes.shape), _weights(weights, "weights", k_codes.shape), raw),
+           "mxkv_attention_weights")
+
+
+def mxkv_select(weights, kv_lens, page_table, kept, new_lens, max_kv_len, sinks=0, recent=0, stream=None):
+    """Chooses the tokens that stay: of each sequence and key head its first `sinks`, its last `recent` and those between with the largest
+    weights, kept.shape[2] in all.  kept int32 [sequences, heads, keep] gets their places, rising (-1 behind a shorter sequence's
+    last), new_lens int32 [sequences] the lengths."""
+    raw = _on_current_device(stream, weights, kv_lens, page_table, kept, new_lens)
+    if weights.dim() != 3 or kept.dim() != 3 or page_table.dim() != 2:
+        raise ValueError("expected weights [pages, heads, page], kept [sequences, heads, keep] and page_table [sequences, pages]")
+    pages, heads, page = weights.shape
+    s, width = page_table.shape
+    keep = kept.shape[2]
+    _check(lib.mxkv_select(_vec(weights, torch.float32, "weights"), heads, s, _vec(kv_lens, torch.int32, "kv_lens", (s,)), max_kv_len,
+                           _vec(page_table, torch.int32, "page_table"), width, pages, page, keep, sinks, recent,
+                           _vec(kept, torch.int32, "kept", (s, heads, keep)), _vec(new_lens, torch.int32, "new_lens", (s,)), raw), "mxkv_select")
+
+
+def mxkv_compact_workspace_bytes(n_seqs: int, kv_heads: int, max_kept: int) -> int:
+    return int(lib.mxkv_compact_workspace_bytes(n_seqs, kv_heads, max_kept))
+
+
+def mxkv_compact(kept, new_lens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out_page_table=None, first=None, weights=None,
+                 workspace=None, stream=None):
+    """Moves listed tokens together: token kept[s, h, i] of sequence s and head h goes to place first[s] + i (None: i) until new_lens[s]
+    places are filled.  kept int32 [sequences, heads or 1, n]; out_page_table: the pages to move to (None: in place, which needs rising lists
+    and a workspace of mxkv_compact_workspace_bytes)."""
+    raw = _on_current_device(stream, kept, new_lens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out_page_table, first, weights,
+                             workspace)
+    pages, heads, page, dim, block, kc, ks, vc, vs = _cache(k_codes, k_scales, v_codes, v_scales)
+    if page_table.dim() != 2 or kept.dim() != 3 or (out_page_table is not None and out_page_table.dim() != 2):
+        raise ValueError("expected kept [sequences, heads or 1, n] and page tables [sequences, pages]")
+    s, width = page_table.shape
+    out_width = width if out_page_table is None else out_page_table.shape[1]
+    ws, ws_bytes = _workspace(workspace)
+    _check(lib.mxkv_compact(_vec(kept, torch.int32, "kept", (s, kept.shape[1], kept.shape[2])), kept.shape[1], kept.shape[2],
+                            _vec(first, torch.int32, "first", (s,)), _vec(new_lens, torch.int32, "new_lens", (s,)),
+                            _vec(kv_lens, torch.int32, "kv_lens", (s,)), heads, dim, s, _vec(page_table, torch.int32, "page_table"), width,
+                            _vec(out_page_table, torch.int32, "out_page_table", (s, out_width)), out_width, pages, page, block, kc, ks, vc, vs,
+                            _weights(weights, "weights", k_codes.shape), ws, ws_bytes, raw), "mxkv_compact")

@@ -106,11 +106,11 @@ const char* mxn_status_string(mxn_status s)
 
 mxn_status mxn_device_timeouts(unsigned int* count_out)
 {
-    unsigned int n = 0, attn = 0, bad = 0;
+    unsigned int n = 0, attn = 0, keep = 0, bad = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_timeouts(&n) != cudaSuccess ||
-        mxn::read_attn_counters(&attn, &bad) != cudaSuccess)
+        mxn::read_attn_counters(&attn, &bad) != cudaSuccess || mxn::read_keep_counters(&keep, &bad) != cudaSuccess)
         return MXN_ERR_CUDA;
-    n += attn;
+    n += attn + keep;
     if (count_out != nullptr) *count_out = n;
     return n == 0 ? MXN_OK : MXN_ERR_TIMEOUT;
 }
@@ -118,17 +118,18 @@ mxn_status mxn_device_timeouts(unsigned int* count_out)
 mxn_status mxn_device_timeouts_reset(void)
 {
     return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_timeouts() == cudaSuccess &&
-                   mxn::reset_attn_timeouts() == cudaSuccess
+                   mxn::reset_attn_timeouts() == cudaSuccess && mxn::reset_keep_counters(true) == cudaSuccess
                ? MXN_OK : MXN_ERR_CUDA;
 }
 
 mxn_status mxn_device_bad_indices(unsigned int* count_out)
 {
-    unsigned int heads = 0, kv = 0, attn = 0, timeouts = 0;
+    unsigned int heads = 0, kv = 0, attn = 0, weights = 0, keep = 0, timeouts = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_heads_bad(&heads) != cudaSuccess ||
-        mxn::read_kv_bad(&kv) != cudaSuccess || mxn::read_attn_counters(&timeouts, &attn) != cudaSuccess)
+        mxn::read_kv_bad(&kv) != cudaSuccess || mxn::read_attn_counters(&timeouts, &attn) != cudaSuccess ||
+        mxn::read_weights_bad(&weights) != cudaSuccess || mxn::read_keep_counters(&timeouts, &keep) != cudaSuccess)
         return MXN_ERR_CUDA;
-    const unsigned int n = heads + kv + attn;
+    const unsigned int n = heads + kv + attn + weights + keep;
     if (count_out != nullptr) *count_out = n;
     return n == 0 ? MXN_OK : MXN_ERR_INDEX;
 }
@@ -136,7 +137,8 @@ mxn_status mxn_device_bad_indices(unsigned int* count_out)
 mxn_status mxn_device_bad_indices_reset(void)
 {
     return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_heads_bad() == cudaSuccess &&
-                   mxn::reset_kv_bad() == cudaSuccess && mxn::reset_attn_bad() == cudaSuccess
+                   mxn::reset_kv_bad() == cudaSuccess && mxn::reset_attn_bad() == cudaSuccess && mxn::reset_weights_bad() == cudaSuccess &&
+                   mxn::reset_keep_counters(false) == cudaSuccess
                ? MXN_OK : MXN_ERR_CUDA;
 }
 
@@ -558,7 +560,8 @@ mxn::HeadsParams rope_params(int64_t T, int q_heads, int k_heads, int dim, int n
 }
 
 mxn_status check_cache(int kv_heads, int dim, int64_t n_seqs, int64_t max_pages, int64_t num_pages, int page_size, int block,
-                       const void* cu, const void* lens, const void* table, const void* kc, const void* ks, const void* vc, const void* vs)
+                       const void* cu, const void* lens, const void* table, const void* kc, const void* ks, const void* vc, const void* vs,
+                       int code_align = 16)
 {
     if (kv_heads < 1 || kv_heads > kMaxHeads || !head_dim_supported(dim) || n_seqs < 0 || n_seqs > kMaxTokens || max_pages < 1 || num_pages < 1)
         return MXN_ERR_SHAPE;
@@ -567,14 +570,14 @@ mxn_status check_cache(int kv_heads, int dim, int64_t n_seqs, int64_t max_pages,
     if (max_pages > kMaxTokens / page_size || num_pages > kMaxTokens / kv_heads) return MXN_ERR_SHAPE;
     if (n_seqs == 0) return MXN_OK;
     if (cu == nullptr || lens == nullptr || table == nullptr || kc == nullptr || ks == nullptr || vc == nullptr || vs == nullptr) return MXN_ERR_NULL;
-    if (misaligned(cu, 4) || misaligned(lens, 4) || misaligned(table, 4) || misaligned(kc, 16) || misaligned(vc, 16)) return MXN_ERR_ALIGN;
+    if (misaligned(cu, 4) || misaligned(lens, 4) || misaligned(table, 4) || misaligned(kc, code_align) || misaligned(vc, code_align)) return MXN_ERR_ALIGN;
     return MXN_OK;
 }
 
 int log2_of(int v)
 {
     int n = 0;
-    while ((1 << n) < v) ++n;
+    while (n < 30 && (1 << n) < v) ++n;
     return n;
 }
 
@@ -583,6 +586,69 @@ bool attention_shape_ok(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int
     return n_tokens >= 0 && n_tokens <= kMaxTokens && n_seqs >= 0 && n_seqs <= kMaxTokens && max_q_len >= 1 && max_q_len <= kMaxTokens &&
            max_kv_len >= 0 && max_kv_len <= kMaxTokens - 511 && kv_heads >= 1 && q_heads >= kv_heads && q_heads <= kMaxHeads &&
            q_heads % kv_heads == 0 && (dim == 64 || dim == 128);
+}
+
+// what attention and the sums of its weights have in common: queries, keys, lists and sizes (not yet checked)
+mxn::AttnParams attention_params(const void* q, int64_t q_stride, int64_t n, int q_heads, int kv_heads, int dim, const int32_t* cu_q, int64_t n_seqs,
+                                 int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len, const int32_t* page_table, int64_t max_pages,
+                                 int64_t num_pages, int page_size, int block, const void* k_codes, const void* k_scales, float scale, int causal,
+                                 int64_t window)
+{
+    mxn::AttnParams P{};
+    P.q = static_cast<const uint16_t*>(q);
+    P.k_codes = static_cast<const uint8_t*>(k_codes);
+    P.k_scales = static_cast<const uint8_t*>(k_scales);
+    P.cu_q = cu_q;
+    P.lens = kv_lens;
+    P.page_table = page_table;
+    P.n = n;
+    P.q_stride = q_stride;
+    P.max_pages = max_pages;
+    P.num_pages = (int)num_pages;
+    P.seqs = (int)n_seqs;
+    P.q_heads = q_heads;
+    P.kv_heads = kv_heads;
+    P.group = kv_heads > 0 ? q_heads / kv_heads : 0;
+    // with s = ceil(log2 group) and mul = ceil(2^(31 + s) / group) the product's error stays below 2^(31 + s) / group for rows < 2^31
+    P.group_shift = P.group > 1 ? (uint32_t)log2_of(P.group) - 1 : 0;
+    P.group_mul = P.group > 1 ? (uint32_t)(((1ull << (32 + P.group_shift)) + P.group - 1) / P.group) : 0;
+    P.dim = dim;
+    P.page = page_size;
+    P.page_shift = log2_of(page_size);
+    P.block_shift = log2_of(block);
+    P.max_q = (int)(max_q_len < n ? max_q_len : n);
+    P.max_len = (int)max_kv_len;
+    P.causal = causal;
+    P.window = (int)window;
+    P.scale = scale;
+    return P;
+}
+
+mxn_status attend(mxn::AttnParams P, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int64_t num_pages, int block, int64_t window, int64_t sinks,
+                  const void* v_codes, const void* v_scales, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,
+                  void* cuda_stream)
+{
+    if (!attention_shape_ok(P.n, n_seqs, max_q_len, max_kv_len, P.q_heads, P.kv_heads, P.dim)) return MXN_ERR_SHAPE;
+    mxn_status st = check_cache(P.kv_heads, P.dim, n_seqs, P.max_pages, num_pages, P.page, block, P.cu_q, P.lens, P.page_table, P.k_codes,
+                                P.k_scales, v_codes, v_scales);
+    if (st != MXN_OK) return st;
+    if (max_kv_len > P.max_pages * P.page || window < 0 || window > kMaxTokens || !(P.scale == P.scale)) return MXN_ERR_SHAPE;
+    if (P.causal != 0 && P.causal != 1) return MXN_ERR_ENUM;
+    if (P.n == 0 || n_seqs == 0) return MXN_OK;
+    if ((st = check_heads(P.q, P.q_stride, P.q_heads, P.dim)) != MXN_OK || (st = check_heads(out, out_stride, P.q_heads, P.dim)) != MXN_OK) return st;
+    if (lse != nullptr && misaligned(lse, 4)) return MXN_ERR_ALIGN;
+    const mxn::AttnPlan plan = mxn::plan_attention(P.n, n_seqs, max_q_len, max_kv_len, P.causal ? window : 0, sinks, P.q_heads, P.kv_heads, P.dim);
+    if (plan.ctas > 0x7FFFFFFF || P.n * P.q_heads > 0x7FFFFFFF) return MXN_ERR_SHAPE;
+    if (plan.splits > 1) {
+        if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
+        if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
+    }
+    P.out = static_cast<uint16_t*>(out);
+    P.out_stride = out_stride;
+    P.lse = lse;
+    P.v_codes = static_cast<const uint8_t*>(v_codes);
+    P.v_scales = static_cast<const uint8_t*>(v_scales);
+    return mxn::launch_attention(P, plan, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
 }
 
 }  // namespace
@@ -718,7 +784,7 @@ size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t 
                                       int head_dim)
 {
     if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim) || n_tokens == 0 || n_seqs == 0) return 0;
-    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, q_heads, kv_heads, head_dim).workspace;
+    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim).workspace;
 }
 
 mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
@@ -728,56 +794,167 @@ mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens
                           void* out_bf16, int64_t out_stride, float* lse_out_or_null, void* workspace, size_t workspace_bytes,
                           void* cuda_stream)
 {
+    const mxn::AttnParams P = attention_params(q_bf16, q_stride, n_tokens, q_heads, kv_heads, head_dim, cu_q, n_seqs, max_q_len, kv_lens, max_kv_len,
+                                               page_table, max_pages, num_pages, page_size, block, k_codes_u8, k_scales_u8, scale, causal, window);
+    return attend(P, n_seqs, max_q_len, max_kv_len, num_pages, block, window, 0, v_codes_u8, v_scales_u8, out_bf16, out_stride, lse_out_or_null, workspace,
+                  workspace_bytes, cuda_stream);
+}
+
+mxn_status mxkv_attention_sinks(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                                const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                                const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                                const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale,
+                                int64_t window, int64_t sinks, void* out_bf16, int64_t out_stride, float* lse_out_or_null, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream)
+{
+    if (window < 1 || sinks < 0 || sinks > kMaxTokens) return MXN_ERR_SHAPE;
+    mxn::AttnParams P = attention_params(q_bf16, q_stride, n_tokens, q_heads, kv_heads, head_dim, cu_q, n_seqs, max_q_len, kv_lens, max_kv_len,
+                                         page_table, max_pages, num_pages, page_size, block, k_codes_u8, k_scales_u8, scale, 1, window);
+    P.sinks = (int)sinks;
+    return attend(P, n_seqs, max_q_len, max_kv_len, num_pages, block, window, sinks, v_codes_u8, v_scales_u8, out_bf16, out_stride, lse_out_or_null,
+                  workspace, workspace_bytes, cuda_stream);
+}
+
+mxn_status mxkv_attention_tree(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                               const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                               const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                               const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale,
+                               const void* mask_u32, int64_t mask_words, void* out_bf16, int64_t out_stride, float* lse_out_or_null,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (mask_words < 1 || mask_words > kMaxTokens / 32) return MXN_ERR_SHAPE;
+    mxn::AttnParams P = attention_params(q_bf16, q_stride, n_tokens, q_heads, kv_heads, head_dim, cu_q, n_seqs, max_q_len, kv_lens, max_kv_len,
+                                         page_table, max_pages, num_pages, page_size, block, k_codes_u8, k_scales_u8, scale, 0, 0);
+    if (n_tokens > 0 && n_seqs > 0) {
+        if (mask_u32 == nullptr) return MXN_ERR_NULL;
+        if (misaligned(mask_u32, 4)) return MXN_ERR_ALIGN;
+    }
+    P.tree = static_cast<const uint32_t*>(mask_u32);
+    P.tree_words = (int)mask_words;
+    return attend(P, n_seqs, max_q_len, max_kv_len, num_pages, block, 0, 0, v_codes_u8, v_scales_u8, out_bf16, out_stride, lse_out_or_null, workspace,
+                  workspace_bytes, cuda_stream);
+}
+
+mxn_status mxkv_attention_weights(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
+                                  const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
+                                  const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
+                                  const void* k_codes_u8, const void* k_scales_u8, float scale, int causal, int64_t window, int64_t sinks,
+                                  const float* lse, const float* earlier_or_null, float* weights, void* cuda_stream)
+{
     if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim)) return MXN_ERR_SHAPE;
     mxn_status st = check_cache(kv_heads, head_dim, n_seqs, max_pages, num_pages, page_size, block, cu_q, kv_lens, page_table, k_codes_u8,
-                                k_scales_u8, v_codes_u8, v_scales_u8);
+                                k_scales_u8, k_codes_u8, k_scales_u8);
     if (st != MXN_OK) return st;
-    if (max_kv_len > max_pages * page_size || window < 0 || window > kMaxTokens || !(scale == scale)) return MXN_ERR_SHAPE;
+    if (max_kv_len > max_pages * page_size || window < 0 || window > kMaxTokens || sinks < 0 || sinks > kMaxTokens || !(scale == scale) ||
+        (sinks > 0 && (window == 0 || causal == 0)) || n_tokens * q_heads > kMaxTokens)
+        return MXN_ERR_SHAPE;
     if (causal != 0 && causal != 1) return MXN_ERR_ENUM;
-    if (n_tokens == 0 || n_seqs == 0) return MXN_OK;
-    if ((st = check_heads(q_bf16, q_stride, q_heads, head_dim)) != MXN_OK || (st = check_heads(out_bf16, out_stride, q_heads, head_dim)) != MXN_OK)
-        return st;
-    if (lse_out_or_null != nullptr && misaligned(lse_out_or_null, 4)) return MXN_ERR_ALIGN;
-    const mxn::AttnPlan plan = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, causal ? window : 0, q_heads, kv_heads,
-                                                    head_dim);
-    if (plan.ctas > 0x7FFFFFFF || n_tokens * q_heads > 0x7FFFFFFF) return MXN_ERR_SHAPE;
-    if (plan.splits > 1) {
-        if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
-        if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
+    if (n_seqs == 0 || max_kv_len == 0) return MXN_OK;
+    if (weights == nullptr) return MXN_ERR_NULL;
+    if (misaligned(weights, 4) || (earlier_or_null != nullptr && misaligned(earlier_or_null, 4))) return MXN_ERR_ALIGN;
+    if (n_tokens > 0) {
+        if ((st = check_heads(q_bf16, q_stride, q_heads, head_dim)) != MXN_OK) return st;
+        if (lse == nullptr) return MXN_ERR_NULL;
+        if (misaligned(lse, 4)) return MXN_ERR_ALIGN;
     }
-    mxn::AttnParams P{};
-    P.q = static_cast<const uint16_t*>(q_bf16);
-    P.out = static_cast<uint16_t*>(out_bf16);
-    P.lse = lse_out_or_null;
-    P.k_codes = static_cast<const uint8_t*>(k_codes_u8);
-    P.k_scales = static_cast<const uint8_t*>(k_scales_u8);
-    P.v_codes = static_cast<const uint8_t*>(v_codes_u8);
-    P.v_scales = static_cast<const uint8_t*>(v_scales_u8);
-    P.cu_q = cu_q;
+    mxn::WeightsParams W{};
+    W.a = attention_params(q_bf16, q_stride, n_tokens, q_heads, kv_heads, head_dim, cu_q, n_seqs, max_q_len, kv_lens, max_kv_len, page_table,
+                           max_pages, num_pages, page_size, block, k_codes_u8, k_scales_u8, scale, causal, window);
+    W.a.sinks = (int)sinks;
+    W.lse = lse;
+    W.earlier = earlier_or_null;
+    W.sums = weights;
+    const int64_t ctas = mxn::plan_weights(W);
+    if (ctas > kMaxTokens) return MXN_ERR_SHAPE;
+    return mxn::launch_weights(W, ctas, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+}
+
+mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const int32_t* kv_lens, int64_t max_kv_len, const int32_t* page_table,
+                       int64_t max_pages, int64_t num_pages, int page_size, int64_t keep, int64_t sinks, int64_t recent, int32_t* kept,
+                       int32_t* new_lens, void* cuda_stream)
+{
+    mxn_status st = check_cache(kv_heads, 64, n_seqs, max_pages, num_pages, page_size, 16, kv_lens, kv_lens, page_table, weights, weights, weights,
+                                weights, 4);
+    if (st != MXN_OK) return st;
+    if (max_kv_len < 0 || max_kv_len > kMaxTokens - 511 || max_kv_len > max_pages * page_size || keep < 0 || keep > kMaxTokens || sinks < 0 ||
+        recent < 0 || sinks > keep || recent > keep - sinks || n_seqs * kv_heads > kMaxTokens / 8)
+        return MXN_ERR_SHAPE;
+    if (n_seqs == 0) return MXN_OK;
+    if (new_lens == nullptr || (kept == nullptr && keep > 0)) return MXN_ERR_NULL;
+    if (misaligned(new_lens, 4) || misaligned(kept, 4)) return MXN_ERR_ALIGN;
+    mxn::SelectParams P{};
+    P.weights = weights;
     P.lens = kv_lens;
     P.page_table = page_table;
-    P.n = n_tokens;
-    P.q_stride = q_stride;
-    P.out_stride = out_stride;
+    P.kept = kept;
+    P.new_lens = new_lens;
     P.max_pages = max_pages;
     P.num_pages = (int)num_pages;
     P.seqs = (int)n_seqs;
-    P.q_heads = q_heads;
-    P.kv_heads = kv_heads;
-    P.group = q_heads / kv_heads;
-    // with s = ceil(log2 group) and mul = ceil(2^(31 + s) / group) the product's error stays below 2^(31 + s) / group for rows < 2^31
-    P.group_shift = P.group > 1 ? (uint32_t)log2_of(P.group) - 1 : 0;
-    P.group_mul = P.group > 1 ? (uint32_t)(((1ull << (32 + P.group_shift)) + P.group - 1) / P.group) : 0;
+    P.heads = kv_heads;
+    P.page_shift = log2_of(page_size);
+    P.max_len = (int)max_kv_len;
+    P.keep = (int)keep;
+    P.sinks = (int)sinks;
+    P.recent = (int)recent;
+    return mxn::launch_select(P, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+}
+
+size_t mxkv_compact_workspace_bytes(int64_t n_seqs, int kv_heads, int64_t max_kept)
+{
+    if (n_seqs <= 0 || kv_heads < 1 || max_kept <= 0 || max_kept > kMaxTokens) return 0;
+    return ((size_t)mxn::compact_units(max_kept) * n_seqs * kv_heads * 2 + 1) * 4;
+}
+
+mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, const int32_t* first_or_null, const int32_t* new_lens,
+                        const int32_t* kv_lens, int kv_heads, int head_dim, int64_t n_seqs, const int32_t* page_table, int64_t max_pages,
+                        const int32_t* out_page_table_or_null, int64_t out_max_pages, int64_t num_pages, int page_size, int block,
+                        void* k_codes_u8, void* k_scales_u8, void* v_codes_u8, void* v_scales_u8, float* weights_or_null, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream)
+{
+    mxn_status st = check_cache(kv_heads, head_dim, n_seqs, max_pages, num_pages, page_size, block, new_lens, kv_lens, page_table, k_codes_u8,
+                                k_scales_u8, v_codes_u8, v_scales_u8);
+    if (st != MXN_OK) return st;
+    const bool in_place = out_page_table_or_null == nullptr || out_page_table_or_null == page_table;
+    if ((head_dim != 64 && head_dim != 128) || (kept_heads != 1 && kept_heads != kv_heads) || max_kept < 0 || max_kept > kMaxTokens ||
+        (!in_place && (out_max_pages < 1 || out_max_pages > kMaxTokens / page_size)))
+        return MXN_ERR_SHAPE;
+    if (n_seqs == 0 || max_kept == 0) return MXN_OK;
+    const int64_t units = mxn::compact_units(max_kept);
+    if (n_seqs * kv_heads > kMaxTokens / 2 / units) return MXN_ERR_SHAPE;
+    if (kept == nullptr) return MXN_ERR_NULL;
+    if (misaligned(kept, 4) || (first_or_null != nullptr && misaligned(first_or_null, 4)) || (!in_place && misaligned(out_page_table_or_null, 4)) ||
+        (weights_or_null != nullptr && misaligned(weights_or_null, 4)))
+        return MXN_ERR_ALIGN;
+    if (in_place) {
+        if (workspace == nullptr || workspace_bytes < mxkv_compact_workspace_bytes(n_seqs, kv_heads, max_kept)) return MXN_ERR_WORKSPACE;
+        if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
+    }
+    mxn::CompactParams P{};
+    P.kept = kept;
+    P.first = first_or_null;
+    P.new_lens = new_lens;
+    P.lens = kv_lens;
+    P.table = page_table;
+    P.out_table = in_place ? page_table : out_page_table_or_null;
+    P.codes[0] = static_cast<uint8_t*>(k_codes_u8);
+    P.codes[1] = static_cast<uint8_t*>(v_codes_u8);
+    P.scales[0] = static_cast<uint8_t*>(k_scales_u8);
+    P.scales[1] = static_cast<uint8_t*>(v_scales_u8);
+    P.weights = weights_or_null;
+    P.work = static_cast<uint32_t*>(workspace);
+    P.max_kept = max_kept;
+    P.width = max_pages;
+    P.out_width = in_place ? max_pages : out_max_pages;
+    P.units = units;
+    P.num_pages = (int)num_pages;
+    P.seqs = (int)n_seqs;
+    P.heads = kv_heads;
+    P.kept_heads = kept_heads;
     P.dim = head_dim;
-    P.page = page_size;
     P.page_shift = log2_of(page_size);
     P.block_shift = log2_of(block);
-    P.max_q = (int)(max_q_len < n_tokens ? max_q_len : n_tokens);
-    P.max_len = (int)max_kv_len;
-    P.causal = causal;
-    P.window = (int)window;
-    P.scale = scale;
-    return mxn::launch_attention(P, plan, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
+    return mxn::launch_compact(P, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MXN_OK : MXN_ERR_CUDA;
 }
 
 }  // extern "C"

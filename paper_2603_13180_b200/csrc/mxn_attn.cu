@@ -128,7 +128,7 @@ __device__ __forceinline__ float4 remote_f4(uint32_t addr, int rank)
 }
 
 // NQ: groups of eight query rows that a warp works on (they share the widened codes); RW: warps that share out the rows
-template <int DIM, int RW, int NQ, int STAGES>
+template <int DIM, int RW, int NQ, int STAGES, int MASK>
 __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
     using Sh = DecodeShape<DIM, RW, NQ, STAGES>;
@@ -159,9 +159,14 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // keys that any row of this tile sees: [lo, hi)
     const int last = min(rows, row0 + Sh::kRows) - 1;
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(last) + 1 : len));
-    const int seen = first_seen(shift + P.by_group(row0), P.window);   // nothing before it, not even its page, has any influence
-    const int lo = seen / kTile * kTile;
-    const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
+    // nothing before it but the first `sinks` tokens, not even a page, has any influence
+    const int seen = MASK == kTree ? 0 : first_seen(shift + P.by_group(row0), P.window);
+    const int lo = seen / kTile * kTile, sinks = MASK == kSinks ? min(P.sinks, hi) : 0;
+    const KeyList list = key_list<kTile>(sinks, lo);
+    // this chunk's part of the keys, or of their list: [k0, k1); no key from `end` on
+    const int from = MASK == kSinks ? 0 : lo, to = MASK == kSinks ? list.head + max(0, hi - lo) : hi;
+    const int k0 = (int)min((int64_t)to, from + (int64_t)split * P.chunk), k1 = (int)min((int64_t)to, (int64_t)k0 + P.chunk);
+    const int end = MASK == kSinks ? hi : k1;
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
     // keys [see_lo, see_hi) of this thread's rows; the tile's rows that every row sees in full
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         const int row = min(row_base + 8 * (x >> 1) + 2 * c + (x & 1), rows - 1);
         const int pos = shift + P.by_group(row);
         see_hi[x] = P.causal ? min(pos + 1, len) : len;
-        see_lo[x] = first_seen(pos, P.window);
+        see_lo[x] = MASK == kTree ? 0 : first_seen(pos, P.window);
     }
     int all_hi = see_hi[0], all_lo = see_lo[0];
 #pragma unroll
@@ -180,7 +185,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         all_hi = min(all_hi, see_hi[x]);
         all_lo = max(all_lo, see_lo[x]);
     }
-    all_hi = min(all_hi, k1);
+    all_hi = min(all_hi, MASK == kTree ? min(shift, end) : end);
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
         all_hi = min(all_hi, __shfl_xor_sync(0xFFFFFFFFu, all_hi, o));
@@ -221,11 +226,15 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
     // earliest, so that nothing waits for it.
     const int run = lane >> 4;
     bool bad_page = false;
-    auto tile_at = [&](int i) { return k0 + (group + i * GROUPS) * kTile; };
+    auto tile_at = [&](int i) {
+        const int u = k0 + (group + i * GROUPS) * kTile;
+        return MASK == kSinks ? list.at(u) : u;
+    };
     const bool two_boxes = P.page < kTile;   // a page of 16 tokens takes two boxes to a tile
     auto page_at = [&](int i) -> int {
         const int t = tile_at(i) + 16 * run;
-        return i < mine && t < k1 && (t | (two_boxes ? 15 : kTile - 1)) >= seen ? __ldg(table + (t >> P.page_shift)) : -1;
+        const int rest = two_boxes ? 15 : kTile - 1;
+        return i < mine && t < end && ((t | rest) >= seen || (MASK == kSinks && (t & ~rest) < sinks)) ? __ldg(table + (t >> P.page_shift)) : -1;
     };
     auto in_pool = [&](int pg) { return (uint32_t)pg < (uint32_t)P.num_pages; };
     const uint32_t box_bytes = two_boxes ? Sh::kTileBytes / 2 : Sh::kTileBytes;
@@ -323,7 +332,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
         float sv[2] = {(float)(int)__shfl_sync(0xFFFFFFFFu, sc, 1) - 127.0f, (float)(int)__shfl_sync(0xFFFFFFFFu, sc, 17) - 127.0f};
         // tokens of the tile that exist and whose page could be read
         const bool readable = in_pool(pages[0]);
-        const bool wanted = t0 + lane < k1 && t0 + lane >= seen;
+        const bool wanted = t0 + lane < end && (t0 + lane >= seen || (MASK == kSinks && t0 + lane < sinks));
         const uint32_t there = __ballot_sync(0xFFFFFFFFu, wanted && readable);
         bad_page |= wanted && !readable;
         const bool was_apart = apart;
@@ -398,7 +407,15 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
 #pragma unroll
                 for (int e = 0; e < 2; ++e) s[t][x >> 1][2 * e + (x & 1)] = fmaf(s[t][x >> 1][2 * e + (x & 1)], f[t][x], apart ? 0.0f : sv[t]);
             }
-        if (there != 0xFFFFFFFFu || t0 < all_lo || t0 + kTile > all_hi) {
+        if (there != 0xFFFFFFFFu || (t0 < all_lo && !(MASK == kSinks && t0 + kTile <= sinks)) || t0 + kTile > all_hi) {
+            uint32_t see[QN];
+            if (MASK == kTree) {
+#pragma unroll
+                for (int x = 0; x < QN; ++x) {
+                    const int row = min(row_base + 8 * (x >> 1) + 2 * c + (x & 1), rows - 1);
+                    see[x] = tree_bits(P.tree + (int64_t)(q0 + P.by_group(row)) * P.tree_words, P.tree_words, (int64_t)t0 - shift);
+                }
+            }
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -406,7 +423,9 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
                     const int at = 16 * t + 8 * e + g, place = t0 + at;
 #pragma unroll
                     for (int x = 0; x < QN; ++x)
-                        if (!((there >> at) & 1u) || place < see_lo[x] || place >= see_hi[x]) s[t][x >> 1][2 * e + (x & 1)] = kNone;
+                        if (!((there >> at) & 1u) || (MASK == kTree && !((see[x] >> at) & 1u)) ||
+                            (place < see_lo[x] && !(MASK == kSinks && place < sinks)) || place >= see_hi[x])
+                            s[t][x >> 1][2 * e + (x & 1)] = kNone;
                 }
         }
         if (__builtin_expect(apart, 0)) {
@@ -852,7 +871,10 @@ bool make_map(CUtensorMap* map, const uint8_t* codes, const AttnParams& P, int b
 template <int DIM, int RW, int NQ, int STAGES>
 cudaError_t launch_decode(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
 {
-    return launch(attn_decode_kernel<DIM, RW, NQ, STAGES>, ctas, P.cluster ? P.splits : 1, kWarps * 32, DecodeShape<DIM, RW, NQ, STAGES>::kSmem, stream, P, M);
+    const int cluster = P.cluster ? P.splits : 1, smem = DecodeShape<DIM, RW, NQ, STAGES>::kSmem;
+    if (P.tree != nullptr) return launch(attn_decode_kernel<DIM, RW, NQ, STAGES, kTree>, ctas, cluster, kWarps * 32, smem, stream, P, M);
+    if (P.sinks > 0) return launch(attn_decode_kernel<DIM, RW, NQ, STAGES, kSinks>, ctas, cluster, kWarps * 32, smem, stream, P, M);
+    return launch(attn_decode_kernel<DIM, RW, NQ, STAGES, kCausal>, ctas, cluster, kWarps * 32, smem, stream, P, M);
 }
 cudaError_t launch_rows(const AttnParams& P, const AttnMaps& M, const AttnPlan& a, cudaStream_t stream)
 {
@@ -873,7 +895,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 namespace {
 
 // wide: heads of 64, 17 to 64 rows: 32 rows a warp (two warps where there are more), else 16 and more CTAs
-AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim, bool wide)
+AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool wide)
 {
     AttnPlan a{};
     const int64_t rows = max_q * (q_heads / kv_heads);
@@ -893,7 +915,8 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
     int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
-    const int64_t span = window > 0 && window + tokens + tile < max_len ? window + tokens + tile : max_len;
+    const int64_t reach = window + tokens + tile + ceil_div(sinks, tile) * tile;
+    const int64_t span = window > 0 && reach < max_len ? reach : max_len;
     const int64_t least = !a.prompt && 2 * units < resident ? 5 : 8;
     auto most = [&](int64_t keys) {
         const int64_t by_least = ceil_div(keys, least * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
@@ -924,15 +947,15 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
 
 }  // namespace
 
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim)
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim)
 {
     if (max_q > n) max_q = n;
-    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, q_heads, kv_heads, dim, true);
+    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, true);
     if (a.prompt || a.row_eights != 4) return a;
     // 32 rows a warp save conversions, 16 hide latency better: taken unless a few chunks of all sequences fit side by side
     // (32 sequences of four drafted tokens, window 1024: 32 rows 19 us, 16 rows 29; 64 sequences of 4100 keys: 83 and 79; 16 of
     // 8000, eight tokens: 75 and 66).  The workspace is that of either, whatever the window.
-    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, q_heads, kv_heads, dim, false);
+    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, false);
     a.workspace = b.workspace = a.workspace > b.workspace ? a.workspace : b.workspace;
     return a.cluster ? a : b;
 }

@@ -42,6 +42,32 @@ __device__ __forceinline__ int first_seen(int pos, int window)
     return window > 0 ? (int)max((int64_t)0, (int64_t)pos - window + 1) : 0;
 }
 
+// What a row may see, apart from its sequence's length: kCausal (places up to its own, from the window's start on), kSinks (the same, and
+// the first tokens), kTree (all in front of the sequence's new tokens, and those of these whose bits its row of the mask has)
+enum { kCausal = 0, kSinks = 1, kTree = 2 };
+
+// The keys of a call as a list of whole tiles of T tokens: with kSinks those of the first tokens, then those from the window on.
+struct KeyList {
+    int head, gap;   // tokens in front of the gap (whole tiles), tokens that the gap leaves out
+    __device__ __forceinline__ int at(int u) const { return u < head ? u : u + gap; }
+};
+template <int T>
+__device__ __forceinline__ KeyList key_list(int sinks, int lo)   // lo: the window's first tile
+{
+    KeyList k;
+    k.head = (int)min((int64_t)lo, ((int64_t)sinks + T - 1) / T * T);
+    k.gap = lo - k.head;
+    return k;
+}
+// 32 bits from bit d of a row of the mask on; all that stands in front of it is seen
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* row, int words, int64_t d)
+{
+    if (d <= -32) return 0xFFFFFFFFu;
+    if (d < 0) return (__ldg(row) << (int)-d) | ((1u << (int)-d) - 1u);
+    const int64_t w = d >> 5;
+    return __funnelshift_r(w < words ? __ldg(row + w) : 0u, w + 1 < words ? __ldg(row + w + 1) : 0u, (uint32_t)d & 31u);
+}
+
 // tiled copy of a box of codes (no multicast); x = 0, y = first token within its page, z = page * heads + head
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar)
 {

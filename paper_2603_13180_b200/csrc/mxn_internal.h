@@ -125,6 +125,9 @@ struct AttnParams {
     int64_t n, q_stride, out_stride, max_pages;
     int num_pages, seqs, q_heads, kv_heads, group, dim, page, page_shift, block_shift, max_q, max_len, causal, window;
     float scale;
+    int sinks;                  // first tokens that stay visible beside the window
+    const uint32_t* tree;       // [n, tree_words]: bit i of a row: it sees its sequence's new token i; or nullptr
+    int tree_words;
     uint32_t group_mul, group_shift;   // row / group = (row * group_mul) >> (32 + group_shift) for rows below 2^31
     __host__ __device__ int by_group(int row) const
     {
@@ -144,10 +147,50 @@ struct AttnPlan {
     bool cluster;               // few chunks, joined by the CTAs as a cluster
     size_t workspace;
 };
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int q_heads, int kv_heads, int dim);
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim);
 cudaError_t launch_attention(AttnParams P, const AttnPlan& plan, void* workspace, cudaStream_t stream);
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad);
 cudaError_t reset_attn_timeouts();
 cudaError_t reset_attn_bad();
+
+// summed attention weights of the keys
+struct WeightsParams {
+    AttnParams a;               // queries, keys, lists, sizes
+    const float* lse;           // [n, q_heads]
+    const float* earlier;       // [num_pages, kv_heads, page] or nullptr
+    float* sums;                // the same
+};
+int64_t plan_weights(WeightsParams& W);   // shares the keys out; returns the number of CTAs
+cudaError_t launch_weights(const WeightsParams& W, int64_t ctas, cudaStream_t stream);
+cudaError_t read_weights_bad(unsigned int* out);
+cudaError_t reset_weights_bad();
+
+// choice of the tokens that stay in the cache
+struct SelectParams {
+    const float* weights;       // [num_pages, heads, page]
+    const int32_t *lens, *page_table;
+    int32_t *kept, *new_lens;   // [seqs, heads, keep], [seqs]
+    int64_t max_pages;
+    int num_pages, seqs, heads, page_shift, max_len, keep, sinks, recent;
+};
+cudaError_t launch_select(const SelectParams& P, cudaStream_t stream);
+
+// moving listed tokens together
+struct CompactParams {
+    const int32_t* kept;        // [seqs, kept_heads, max_kept]
+    const int32_t *first, *new_lens, *lens;   // first: may be nullptr
+    const int32_t *table, *out_table;         // the same one: in place
+    uint8_t* codes[2];
+    uint8_t* scales[2];
+    float* weights;             // or nullptr
+    uint32_t* work;             // in place: a ticket, then a flag for each unit
+    int64_t max_kept, width, out_width;       // pages a sequence in the two tables
+    int64_t units;              // of a sequence, head, keys or values
+    int num_pages, seqs, heads, kept_heads, dim, page_shift, block_shift;
+};
+int64_t compact_units(int64_t max_kept);
+cudaError_t launch_compact(const CompactParams& P, cudaStream_t stream);
+cudaError_t read_keep_counters(unsigned int* timeouts, unsigned int* bad);
+cudaError_t reset_keep_counters(bool timeouts);
 
 }  // namespace mxn

@@ -210,7 +210,7 @@ __device__ __forceinline__ float2 ex2_fma(float2 u)
                        __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
-template <int DIM>
+template <int DIM, int MASK>
 __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
     using Sh = PromptShape<DIM>;
@@ -244,9 +244,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     if (row0 >= rows) return;
     const bool two = rows - row0 > kTile;   // else nothing is done for the second row tile
     const int hi = max(0, min(len, P.causal ? shift + P.by_group(rows - 1) + 1 : len));
-    const int seen = first_seen(shift + P.by_group(row0), P.window);   // nothing before it, not even its page, has any influence
-    const int lo = seen / kTile * kTile;
-    const int k0 = (int)min((int64_t)hi, lo + (int64_t)split * P.chunk), k1 = (int)min((int64_t)hi, (int64_t)k0 + P.chunk);
+    // nothing before it but the first `sinks` tokens, not even a page, has any influence
+    const int seen = MASK == kTree ? 0 : first_seen(shift + P.by_group(row0), P.window);
+    const int lo = seen / kTile * kTile, sinks = MASK == kSinks ? min(P.sinks, hi) : 0;
+    const KeyList list = key_list<kTile>(sinks, lo);
+    // this chunk's part of the keys, or of their list: [k0, k1); no key from `end` on
+    const int from = MASK == kSinks ? 0 : lo, to = MASK == kSinks ? list.head + max(0, hi - lo) : hi;
+    const int k0 = (int)min((int64_t)to, from + (int64_t)split * P.chunk), k1 = (int)min((int64_t)to, (int64_t)k0 + P.chunk);
+    const int end = MASK == kSinks ? hi : k1;
+    auto tile_at = [&](int j) { return MASK == kSinks ? list.at(k0 + j * kTile) : k0 + j * kTile; };
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -352,9 +358,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         float c0 = 0.0f;
         int page_next = -1;                                          // lane i: page of run i (lanes 0-7) of the next tile
         auto look_up = [&](int j) {
-            const int t = k0 + j * kTile + kRun * (lane & 7);
+            const int t = tile_at(j) + kRun * (lane & 7);
             int pg = -1;
-            if (j < tiles && lane < 8 && t < k1 && (t | (box - 1)) >= seen) {
+            if (j < tiles && lane < 8 && t < end && ((t | (box - 1)) >= seen || (MASK == kSinks && (t & ~(box - 1)) < sinks))) {
                 pg = __ldg(table + (t >> P.page_shift));
                 if (pg < 0 || pg >= P.num_pages) {
                     pg = -1;
@@ -368,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         for (int j = 0; j < tiles; ++j) {
             const int pg = page_next;
             page_next = look_up(j + 1);
-            const int t0 = k0 + j * kTile, ks = j % kKeyStages, vs = j % kValStages;
+            const int t0 = tile_at(j), ks = j % kKeyStages, vs = j % kValStages;
             // scales
             uint32_t sk = 0, sv = 0;
             if (pg >= 0) {
@@ -519,8 +525,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             const int vs = j % kValStages, hs = j % kHalfStages;
             ok = wait(v_full + 8 * vs, (uint32_t)(j / kValStages) & 1u, dead) && wait(sc_full + 8 * (j % kScaleSlots), (uint32_t)(j / kScaleSlots) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
-            const int place = k0 + j * kTile + t;
-            const bool real = place >= seen && place < k1 && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
+            const int place = tile_at(j) + t;
+            const bool real = (place >= seen || (MASK == kSinks && place < sinks)) && place < end && ((scales[j % kScaleSlots].readable >> (t / kRun)) & 1u);
             if (j >= kHalfStages) ok = wait(h_empty + 8 * hs, (uint32_t)(j / kHalfStages - 1) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const uint32_t src = base + Sh::kV + vs * Sh::kCodes + (uint32_t)t * DIM;
@@ -566,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         const float row_factor = row_factors[rt * kTile + r_in];
         const int pos = shift + (row_live ? q_tok : nq - 1);
         const int see_hi = P.causal ? min(pos + 1, len) : len;
-        const int see_lo = first_seen(pos, P.window);
+        const int see_lo = MASK == kTree ? 0 : first_seen(pos, P.window);
         const float kNone = -INFINITY;
         float ref = kNone, top_all = kNone, l = 0.0f, c0 = 0.0f;
         // l's unit is 2^(ref - kTop - c0) until a tile is wide or c0 changes; from then on (`by_own`) 2^sum_ref, and `unit` the former in the
@@ -576,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         bool ok = true, by_own = false, slow = false;
         const int steps = 2 * tiles;
         // a row that nothing hides in a step needs no mask: the range that holds for the warp's rows
-        const int all_lo = __reduce_max_sync(0xFFFFFFFFu, see_lo), all_hi = __reduce_min_sync(0xFFFFFFFFu, min(see_hi, k1));
+        const int all_lo = __reduce_max_sync(0xFFFFFFFFu, see_lo), all_hi = __reduce_min_sync(0xFFFFFFFFu, min(MASK == kTree ? shift : see_hi, end));
         bool here = false, scales_here = false;
         for (int i = 0; i < steps; ++i) {
             const int j = i >> 1, buf = i & 1;
@@ -586,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             if (!ok) break;
             tc_after();
             const uint32_t s_at = s_col[rt] + lanes + buf * kStep;
-            const int t0 = k0 + i * kStep;
+            const int t0 = MASK == kSinks ? tile_at(j) + buf * kStep : k0 + i * kStep;
             uint32_t x[2][32];
             tm_request(x[0], s_at);
             tm_request(x[1], s_at + 32);
@@ -597,11 +603,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             const uint32_t special = slot.apart & (kWide | (buf ? 0u : kMoved));
             // bit e: the row sees token 32 c + e of the step
             auto visible = [&](int c) -> uint32_t {
-                const int tc = t0 + 32 * c, up = min(max(min(see_hi, k1) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
-                const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u, above = down == 32 ? 0u : 0xFFFFFFFFu << down;
+                const int tc = t0 + 32 * c, up = min(max(min(see_hi, end) - tc, 0), 32), down = min(max(see_lo - tc, 0), 32);
+                const uint32_t below = up == 32 ? 0xFFFFFFFFu : (1u << up) - 1u;
+                uint32_t above = down == 32 ? 0u : 0xFFFFFFFFu << down;
+                if (MASK == kSinks) {
+                    const int first = min(max(sinks - tc, 0), 32);
+                    above |= first == 32 ? 0xFFFFFFFFu : (1u << first) - 1u;
+                }
+                if (MASK == kTree) above = tree_bits(P.tree + tok * P.tree_words, P.tree_words, (int64_t)tc - shift);
                 return below & above & (((readable >> (2 * c)) & 1u ? 0xFFFFu : 0u) | ((readable >> (2 * c + 1)) & 1u ? 0xFFFF0000u : 0u));
             };
-            const bool all = t0 >= all_lo && t0 + kStep <= all_hi && readable == 0xFu;
+            const bool all = (t0 >= all_lo || (MASK == kSinks && t0 + kStep <= sinks)) && t0 + kStep <= all_hi && readable == 0xFu;
             float fac[4], utop = kNone;
 #pragma unroll
             for (int g = 0; g < 4; ++g) fac[g] = fmaxf(row_factor * slot_k[g], 1.17549435e-38f);
@@ -810,11 +822,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     }
 }
 
-template <int DIM>
+template <int DIM, int MASK>
 cudaError_t launch_dim(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
 {
     const int smem = PromptShape<DIM>::kSmem;
-    const cudaError_t e = cudaFuncSetAttribute(attn_prompt_kernel<DIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = cudaFuncSetAttribute(attn_prompt_kernel<DIM, MASK>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
@@ -826,14 +838,16 @@ cudaError_t launch_dim(const AttnParams& P, const AttnMaps& M, int64_t ctas, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_prompt_kernel<DIM>, P, M);
+    return cudaLaunchKernelEx(&cfg, attn_prompt_kernel<DIM, MASK>, P, M);
 }
 
 }  // namespace
 
 cudaError_t launch_prompt(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream)
 {
-    return P.dim == 128 ? launch_dim<128>(P, M, ctas, stream) : launch_dim<64>(P, M, ctas, stream);
+    if (P.tree != nullptr) return P.dim == 128 ? launch_dim<128, kTree>(P, M, ctas, stream) : launch_dim<64, kTree>(P, M, ctas, stream);
+    if (P.sinks > 0) return P.dim == 128 ? launch_dim<128, kSinks>(P, M, ctas, stream) : launch_dim<64, kSinks>(P, M, ctas, stream);
+    return P.dim == 128 ? launch_dim<128, kCausal>(P, M, ctas, stream) : launch_dim<64, kCausal>(P, M, ctas, stream);
 }
 
 cudaError_t read_prompt_counters(unsigned int* timeouts, unsigned int* bad)

@@ -1,0 +1,292 @@
+// Summed attention weights of the keys of the paged 8-bit cache: what each key has been given by all queries of a call.
+//
+//   w_t = earlier_t + sum over rows i of exp(scale q_i . k_t - lse_i),   k_t = 2^(sk - 127) * code
+//
+// over the rows of t's sequence that see t and the query heads that share the key head; lse is the attention's logarithm of the sum.
+// Every key's sum stands by itself, so that no two warps meet in one and nothing is joined.
+//
+// Few rows (up to kRows a sequence and key head): bound by HBM, dim bytes of codes, 4 (and 4 earlier) of sums a token and head.  A warp
+// takes tiles of 32 tokens.  The order of the dimensions within a product is free: a thread reads one run of dim / 4 bytes of each of
+// its four tokens straight into registers, in which the codes become f16 operands (exact), and asks for the next tile before it works on
+// the one at hand.  q is scaled by a power of two that brings its row's largest to [2^14, 2^15): f16 holds a bf16 value exactly but for
+// elements below 2^-28 of that.
+#include <cuda_fp16.h>
+
+#include "mxn_attn.cuh"
+
+namespace mxn {
+
+namespace {
+
+constexpr int kWarps = 4, kTile = 32, kRows = 64;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ unsigned int g_weights_bad = 0;   // pages out of range within a sequence's length
+
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// what a tile needs from memory
+template <int DIM>
+struct KeyTile {
+    uint4 w[4][DIM / 64];      // codes of tokens g, 8 + g, 16 + g, 24 + g: dimensions c * DIM/4 on
+    uint32_t scale[2];         // of the two runs of 16 tokens
+    float earlier;             // of the token whose sum this thread writes
+    int page[2];               // -1 where there is none to read
+};
+
+// FEW: up to eight rows, held in registers; else up to kRows at a time, in shared memory
+template <int DIM, bool FEW>
+__global__ void __launch_bounds__(kWarps * 32, 4) key_weights_kernel(const WeightsParams W)
+{
+    constexpr int KS = DIM / 16;
+    __shared__ uint2 q_frag[FEW ? 1 : kRows / 8][FEW ? 1 : KS][FEW ? 1 : 32];
+    __shared__ float2 q_row[FEW ? 1 : kRows];   // factor of the scores, -lse in powers of two
+    __shared__ int2 q_see[FEW ? 1 : kRows];     // first and past the last key seen (but for the first `sinks`)
+    pdl_prologue();
+    const AttnParams& P = W.a;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    uint32_t b = blockIdx.x;
+    const int split = (int)(b % (uint32_t)P.splits);
+    b /= (uint32_t)P.splits;
+    const int h = (int)(b % (uint32_t)P.kv_heads), seq = (int)(b / (uint32_t)P.kv_heads);
+    const AttnSequence S = attn_sequence(P, seq);
+    const int G = P.group, rows = S.nq * G, end = S.len;
+    const int k0 = (int)min((int64_t)end, (int64_t)split * P.chunk), k1 = (int)min((int64_t)end, (int64_t)k0 + P.chunk);
+    if (k0 >= k1) return;
+    const int tiles = (k1 - k0 + kTile - 1) / kTile, mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
+    const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
+    const int per_page = P.page_shift - P.block_shift;
+    const bool wide = (reinterpret_cast<uintptr_t>(P.k_codes) & 31u) == 0u;   // (codes are promised to be 16-byte aligned)
+    const int old_end = S.nq > 0 ? S.shift : end;   // tokens in front of the call's own have sums from earlier
+    const int out_at = 16 * (c >> 1) + 8 * (c & 1) + g;   // the token of a tile whose sum this thread writes
+    auto tile_at = [&](int i) { return k0 + (warp + i * kWarps) * kTile; };
+    auto page_at = [&](int i) -> int {   // page of this half warp's run of 16 tokens
+        const int t = tile_at(i) + (lane & 16);
+        return i < mine && t < k1 ? __ldg(table + (t >> P.page_shift)) : -1;
+    };
+    bool bad = false;
+
+    for (int row0 = 0; row0 == 0 || row0 < rows; row0 += kRows) {
+        const int here = min(rows - row0, FEW ? 8 : kRows);   // (may be 0)
+        // keys that any of these rows sees: [lo, hi) and the first `sinks`
+        const int pos0 = S.shift + P.by_group(row0), pos1 = S.shift + P.by_group(max(row0 + here - 1, 0));
+        const int lo = first_seen(pos0, P.window), hi = here > 0 ? (P.causal ? min(pos1 + 1, end) : end) : 0, sinks = min(P.sinks, hi);
+        // ---- the rows: eight at a time by a warp; thread (g, c) reads a quarter of row g ----
+        uint32_t qb[KS][2];
+        float2 my_row = make_float2(0.0f, 0.0f);
+        int2 my_see = make_int2(0, 0);
+        auto prepare = [&](int eight) {
+            const int row = row0 + 8 * eight + g, qt = P.by_group(row);
+            const bool live = 8 * eight + g < here;
+            uint4 raw[DIM / 32];
+            const int64_t head = (int64_t)h * G + row - (int64_t)qt * G, tok = (int64_t)S.q0 + qt;
+            const uint16_t* qp = P.q + tok * P.q_stride + head * DIM + c * (DIM / 4);
+#pragma unroll
+            for (int i = 0; i < DIM / 32; ++i) raw[i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+            const float lse = live ? __ldg(W.lse + tok * P.q_heads + head) : -INFINITY;
+            const uint32_t* u = reinterpret_cast<const uint32_t*>(raw);
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
+            float top = hmax_abs_to_f32(m);
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const uint32_t E = __float_as_uint(top) >> 23, Ec = min(max(E, 15u), 254u);
+            const float up = E == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((268u - Ec) << 23);   // an infinity or NaN: NaN
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                qb[k][0] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
+                qb[k][1] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
+            }
+            my_row = make_float2(P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23), -lse * kLog2e);
+            const int pos = S.shift + qt;
+            // a row that the attention found to see nothing gives nothing
+            my_see = live && lse != -INFINITY ? make_int2(first_seen(pos, P.window), P.causal ? min(pos + 1, end) : end) : make_int2(0, 0);
+        };
+        float2 col_row[2];
+        int2 col_see[2];
+        if constexpr (FEW) {
+            prepare(0);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int from = 8 * c + 4 * e;
+                col_row[e] = make_float2(__shfl_sync(0xFFFFFFFFu, my_row.x, from), __shfl_sync(0xFFFFFFFFu, my_row.y, from));
+                col_see[e] = make_int2(__shfl_sync(0xFFFFFFFFu, my_see.x, from), __shfl_sync(0xFFFFFFFFu, my_see.y, from));
+            }
+        } else {
+            if (row0 > 0) __syncthreads();
+            for (int eight = warp; 8 * eight < here; eight += kWarps) {
+                prepare(eight);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) q_frag[eight][k][lane] = make_uint2(qb[k][0], qb[k][1]);
+                if (c == 0) {
+                    q_row[8 * eight + g] = my_row;
+                    q_see[8 * eight + g] = my_see;
+                }
+            }
+            __syncthreads();
+        }
+        const float* const before = row0 > 0 ? W.sums : W.earlier;   // (a thread reads back only what it wrote itself)
+        const int before_end = row0 > 0 ? end : old_end;
+
+        auto load = [&](KeyTile<DIM>& K, int i, int pg) {   // by a whole warp; pg = page_at(i)
+            const int t0 = tile_at(i);
+            const bool seen = (t0 < hi && t0 + kTile > lo) || t0 < sinks;
+            bad |= row0 == 0 && i < mine && t0 + (lane & 16) < k1 && (uint32_t)pg >= (uint32_t)P.num_pages;
+            if ((uint32_t)pg >= (uint32_t)P.num_pages) pg = -1;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                K.page[t] = __shfl_sync(0xFFFFFFFFu, pg, 16 * t);
+                const int64_t tile = (int64_t)K.page[t] * P.kv_heads + h;
+                const int first = (t0 + 16 * t) & (P.page - 1);
+                K.scale[t] = K.page[t] >= 0 ? __ldg(P.k_scales + (tile << per_page) + (first >> P.block_shift)) : 0u;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int r = 8 * x + g;
+                    if (seen && K.page[t] >= 0 && t0 + 16 * t + r < k1) {
+                        const uint8_t* p = P.k_codes + ((tile << P.page_shift) + first + r) * DIM + c * (DIM / 4);
+                        if (DIM == 128 && wide) {
+                            uint32_t v[8];
+                            ld_v8(p, v);
+#pragma unroll
+                            for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = __ldg(reinterpret_cast<const uint4*>(p) + e);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+            }
+            const int place = t0 + out_at, pw = c < 2 ? K.page[0] : K.page[1];
+            K.earlier = before != nullptr && place < min(k1, before_end) && pw >= 0
+                      ? before[(((int64_t)pw * P.kv_heads + h) << P.page_shift) + (place & (P.page - 1))] : 0.0f;
+        };
+        auto work = [&](const KeyTile<DIM>& K, int i) {
+            const int t0 = tile_at(i);
+            const float kf[2] = {e8m0_to_f32(K.scale[0]), e8m0_to_f32(K.scale[1])};
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // tokens g, 8 + g, 16 + g, 24 + g; this thread's columns
+            if ((t0 < hi && t0 + kTile > lo) || t0 < sinks) {
+                auto eight = [&](const uint2* frag, const float2 (&cr)[2], const int2 (&cs)[2]) {
+                    const bool all = t0 >= max(cs[0].x, cs[1].x) && t0 + kTile <= min(cs[0].y, cs[1].y);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int k = 0; k < KS; ++k) {
+                            uint32_t a0, a1, a2, a3;
+                            widen(word(K.w[2 * t][k / 4], k % 4), a0, a2);
+                            widen(word(K.w[2 * t + 1][k / 4], k % 4), a1, a3);
+                            const uint2 f = FEW ? make_uint2(qb[k][0], qb[k][1]) : frag[k * 32];
+                            mma_f16(s, a0, a1, a2, a3, f.x, f.y);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = ex2(fmaf(s[e], kf[t] * cr[e & 1].x, cr[e & 1].y));
+                            const int place = t0 + 16 * t + 8 * (e >> 1) + g;
+                            const bool sees = all || (place < cs[e & 1].y && (place >= cs[e & 1].x || place < sinks));
+                            sum[2 * t + (e >> 1)] += sees ? p : 0.0f;
+                        }
+                    }
+                };
+                if constexpr (FEW) {
+                    eight(nullptr, col_row, col_see);
+                } else {
+                    for (int y = 0; 8 * y < here; ++y) {
+                        float2 cr[2];
+                        int2 cs[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            cr[e] = q_row[8 * y + 2 * c + e];
+                            cs[e] = q_see[8 * y + 2 * c + e];
+                        }
+                        eight(&q_frag[y][0][lane], cr, cs);
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 1);
+                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 2);
+            }
+            const float all = c < 2 ? (c == 0 ? sum[0] : sum[1]) : (c == 2 ? sum[2] : sum[3]);
+            const int place = t0 + out_at, pw = c < 2 ? K.page[0] : K.page[1];
+            if (place < k1 && pw >= 0) W.sums[(((int64_t)pw * P.kv_heads + h) << P.page_shift) + (place & (P.page - 1))] = K.earlier + all;
+        };
+        KeyTile<DIM> cur, next;
+        int pg = page_at(0);
+        for (int i = -1; i < mine; ++i) {
+            const int pg_next = page_at(i + 2);
+            load(next, i + 1, pg);
+            if (i >= 0) work(cur, i);
+            cur = next;
+            pg = pg_next;
+        }
+    }
+    if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_weights_bad, 1u);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+template <class K>
+cudaError_t launch(K kernel, int64_t ctas, cudaStream_t stream, const WeightsParams& W)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, W);
+}
+
+}  // namespace
+
+int64_t plan_weights(WeightsParams& W)
+{
+    AttnParams& P = W.a;
+    // Chunks of 16 tiles (four for each warp), or of one tile for each warp where CTAs would be fewer than three an SM; nothing is joined,
+    // so a chunk costs no more than its start.
+    const int64_t units = (int64_t)P.seqs * P.kv_heads, least = kWarps * kTile;
+    P.chunk = 4 * least;
+    if (units * ceil_div(P.max_len, P.chunk) < 3 * 148) P.chunk = least;
+    P.splits = (int)ceil_div(P.max_len, P.chunk);
+    return units * P.splits;
+}
+
+cudaError_t launch_weights(const WeightsParams& W, int64_t ctas, cudaStream_t stream)
+{
+    const AttnParams& P = W.a;
+    const bool few = (int64_t)P.max_q * P.group <= 8;
+    if (P.dim == 128) return few ? launch(key_weights_kernel<128, true>, ctas, stream, W) : launch(key_weights_kernel<128, false>, ctas, stream, W);
+    return few ? launch(key_weights_kernel<64, true>, ctas, stream, W) : launch(key_weights_kernel<64, false>, ctas, stream, W);
+}
+
+cudaError_t read_weights_bad(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_weights_bad, sizeof(unsigned int)); }
+cudaError_t reset_weights_bad()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(g_weights_bad, &zero, sizeof(unsigned int));
+}
+
+}  // namespace mxn
