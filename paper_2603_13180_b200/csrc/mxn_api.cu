@@ -106,11 +106,12 @@ const char* mxn_status_string(mxn_status s)
 
 mxn_status mxn_device_timeouts(unsigned int* count_out)
 {
-    unsigned int n = 0, attn = 0, keep = 0, bad = 0;
+    unsigned int n = 0, attn = 0, weights = 0, keep = 0, bad = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_timeouts(&n) != cudaSuccess ||
-        mxn::read_attn_counters(&attn, &bad) != cudaSuccess || mxn::read_keep_counters(&keep, &bad) != cudaSuccess)
+        mxn::read_attn_counters(&attn, &bad) != cudaSuccess || mxn::read_keep_counters(&keep, &bad) != cudaSuccess ||
+        mxn::read_weights_counters(&weights, &bad) != cudaSuccess)
         return MXN_ERR_CUDA;
-    n += attn + keep;
+    n += attn + weights + keep;
     if (count_out != nullptr) *count_out = n;
     return n == 0 ? MXN_OK : MXN_ERR_TIMEOUT;
 }
@@ -118,7 +119,8 @@ mxn_status mxn_device_timeouts(unsigned int* count_out)
 mxn_status mxn_device_timeouts_reset(void)
 {
     return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_timeouts() == cudaSuccess &&
-                   mxn::reset_attn_timeouts() == cudaSuccess && mxn::reset_keep_counters(true) == cudaSuccess
+                   mxn::reset_attn_timeouts() == cudaSuccess && mxn::reset_keep_counters(true) == cudaSuccess &&
+                   mxn::reset_weights_counters(true) == cudaSuccess
                ? MXN_OK : MXN_ERR_CUDA;
 }
 
@@ -127,7 +129,7 @@ mxn_status mxn_device_bad_indices(unsigned int* count_out)
     unsigned int heads = 0, kv = 0, attn = 0, weights = 0, keep = 0, timeouts = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || mxn::read_heads_bad(&heads) != cudaSuccess ||
         mxn::read_kv_bad(&kv) != cudaSuccess || mxn::read_attn_counters(&timeouts, &attn) != cudaSuccess ||
-        mxn::read_weights_bad(&weights) != cudaSuccess || mxn::read_keep_counters(&timeouts, &keep) != cudaSuccess)
+        mxn::read_weights_counters(&timeouts, &weights) != cudaSuccess || mxn::read_keep_counters(&timeouts, &keep) != cudaSuccess)
         return MXN_ERR_CUDA;
     const unsigned int n = heads + kv + attn + weights + keep;
     if (count_out != nullptr) *count_out = n;
@@ -137,7 +139,7 @@ mxn_status mxn_device_bad_indices(unsigned int* count_out)
 mxn_status mxn_device_bad_indices_reset(void)
 {
     return cudaDeviceSynchronize() == cudaSuccess && mxn::reset_heads_bad() == cudaSuccess &&
-                   mxn::reset_kv_bad() == cudaSuccess && mxn::reset_attn_bad() == cudaSuccess && mxn::reset_weights_bad() == cudaSuccess &&
+                   mxn::reset_kv_bad() == cudaSuccess && mxn::reset_attn_bad() == cudaSuccess && mxn::reset_weights_counters(false) == cudaSuccess &&
                    mxn::reset_keep_counters(false) == cudaSuccess
                ? MXN_OK : MXN_ERR_CUDA;
 }

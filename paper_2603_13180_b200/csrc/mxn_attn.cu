@@ -960,6 +960,17 @@ AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len,
     return a.cluster ? a : b;
 }
 
+bool make_query_map(CUtensorMap* map, const AttnParams& P, int heads, int tokens)
+{
+    const EncodeTiled enc = encoder();
+    if (enc == nullptr) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)P.dim, (cuuint64_t)P.q_heads, (cuuint64_t)P.n};
+    const cuuint64_t strides[2] = {(cuuint64_t)P.dim * 2, (cuuint64_t)P.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens}, step[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(P.q), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, cudaStream_t stream)
 {
     P.splits = (int)a.splits;

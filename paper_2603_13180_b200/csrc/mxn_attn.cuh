@@ -13,6 +13,8 @@ struct AttnMaps {
     CUtensorMap k, v;   // codes as [pages * heads, page, dim] bytes
 };
 
+// tensor map of the queries in boxes of 64 dimensions of `heads` heads of `tokens` tokens, 128-byte swizzle
+bool make_query_map(CUtensorMap* map, const AttnParams& P, int heads, int tokens);
 // the kernel for many query rows (mxn_prompt.cu)
 cudaError_t launch_prompt(const AttnParams& P, const AttnMaps& M, int64_t ctas, cudaStream_t stream);
 cudaError_t read_prompt_counters(unsigned int* timeouts, unsigned int* bad);

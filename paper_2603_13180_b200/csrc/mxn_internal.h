@@ -159,11 +159,18 @@ struct WeightsParams {
     const float* lse;           // [n, q_heads]
     const float* earlier;       // [num_pages, kv_heads, page] or nullptr
     float* sums;                // the same
+    // filled by the plan
+    int many;                   // many rows: the tcgen05 kernel, with
+    int tile_heads, tile_tokens, head_parts;   // heads and tokens of a tile of queries, parts of a key head's query heads
+    int key_tiles, ranks;       // of 256 keys; CTAs (a cluster) that share out the queries of a key tile
 };
-int64_t plan_weights(WeightsParams& W);   // shares the keys out; returns the number of CTAs
+int64_t plan_weights(WeightsParams& W);   // shares the work out; returns the number of CTAs
+cudaError_t launch_weights_many(const WeightsParams& W, int64_t ctas, cudaStream_t stream);
+cudaError_t read_weights_many_counters(unsigned int* timeouts, unsigned int* bad);
+cudaError_t reset_weights_many_counters(bool timeouts);
 cudaError_t launch_weights(const WeightsParams& W, int64_t ctas, cudaStream_t stream);
-cudaError_t read_weights_bad(unsigned int* out);
-cudaError_t reset_weights_bad();
+cudaError_t read_weights_counters(unsigned int* timeouts, unsigned int* bad);
+cudaError_t reset_weights_counters(bool timeouts);
 
 // choice of the tokens that stay in the cache
 struct SelectParams {

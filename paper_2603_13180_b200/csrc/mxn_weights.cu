@@ -40,18 +40,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// what a tile needs from memory
-template <int DIM>
-struct KeyTile {
-    uint4 w[4][DIM / 64];      // codes of tokens g, 8 + g, 16 + g, 24 + g: dimensions c * DIM/4 on
-    uint32_t scale[2];         // of the two runs of 16 tokens
-    float earlier;             // of the token whose sum this thread writes
-    int page[2];               // -1 where there is none to read
-};
-
-// FEW: up to eight rows, held in registers; else up to kRows at a time, in shared memory
+// FEW: up to eight rows, whose operands stay in registers; else up to kRows, in shared memory
 template <int DIM, bool FEW>
-__global__ void __launch_bounds__(kWarps * 32, 4) key_weights_kernel(const WeightsParams W)
+__global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(const WeightsParams W)
 {
     constexpr int KS = DIM / 16;
     __shared__ uint2 q_frag[FEW ? 1 : kRows / 8][FEW ? 1 : KS][FEW ? 1 : 32];
@@ -72,173 +63,179 @@ __global__ void __launch_bounds__(kWarps * 32, 4) key_weights_kernel(const Weigh
     const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
     const int per_page = P.page_shift - P.block_shift;
     const bool wide = (reinterpret_cast<uintptr_t>(P.k_codes) & 31u) == 0u;   // (codes are promised to be 16-byte aligned)
-    const int old_end = S.nq > 0 ? S.shift : end;   // tokens in front of the call's own have sums from earlier
-    const int out_at = 16 * (c >> 1) + 8 * (c & 1) + g;   // the token of a tile whose sum this thread writes
+    const int old_end = W.earlier == nullptr ? 0 : S.nq > 0 ? min(S.shift, k1) : k1;   // tokens in front of the call's own have sums from earlier
+    // keys that any row sees: [lo, hi) and the first `sinks`
+    const int pos0 = S.shift, pos1 = S.shift + S.nq - 1;
+    const int lo = first_seen(pos0, P.window), hi = rows > 0 ? (P.causal ? min(pos1 + 1, end) : end) : 0, sinks = min(P.sinks, hi);
     auto tile_at = [&](int i) { return k0 + (warp + i * kWarps) * kTile; };
     auto page_at = [&](int i) -> int {   // page of this half warp's run of 16 tokens
         const int t = tile_at(i) + (lane & 16);
         return i < mine && t < k1 ? __ldg(table + (t >> P.page_shift)) : -1;
     };
+
+    // ---- a tile on its way: codes of tokens g, 8 + g, 16 + g, 24 + g, dimensions c * DIM/4 on; what its sums need ----
+    uint4 w[4][DIM / 64];
+    uint32_t scale[2];   // of the two runs of 16 tokens
+    int64_t at;          // of the sum that this thread writes, -1: of none
+    float earlier;
     bool bad = false;
-
-    for (int row0 = 0; row0 == 0 || row0 < rows; row0 += kRows) {
-        const int here = min(rows - row0, FEW ? 8 : kRows);   // (may be 0)
-        // keys that any of these rows sees: [lo, hi) and the first `sinks`
-        const int pos0 = S.shift + P.by_group(row0), pos1 = S.shift + P.by_group(max(row0 + here - 1, 0));
-        const int lo = first_seen(pos0, P.window), hi = here > 0 ? (P.causal ? min(pos1 + 1, end) : end) : 0, sinks = min(P.sinks, hi);
-        // ---- the rows: eight at a time by a warp; thread (g, c) reads a quarter of row g ----
-        uint32_t qb[KS][2];
-        float2 my_row = make_float2(0.0f, 0.0f);
-        int2 my_see = make_int2(0, 0);
-        auto prepare = [&](int eight) {
-            const int row = row0 + 8 * eight + g, qt = P.by_group(row);
-            const bool live = 8 * eight + g < here;
-            uint4 raw[DIM / 32];
-            const int64_t head = (int64_t)h * G + row - (int64_t)qt * G, tok = (int64_t)S.q0 + qt;
-            const uint16_t* qp = P.q + tok * P.q_stride + head * DIM + c * (DIM / 4);
+    const int out_token = 16 * (c >> 1) + 8 * (c & 1) + g;   // the token of a tile whose sum this thread writes
+    auto load = [&](int i, int pg) {   // by a whole warp; pg = page_at(i)
+        const int t0 = tile_at(i);
+        const bool seen = i < mine && ((t0 < hi && t0 + kTile > lo) || t0 < sinks);
+        bad |= i < mine && t0 + (lane & 16) < k1 && (uint32_t)pg >= (uint32_t)P.num_pages;
+        if ((uint32_t)pg >= (uint32_t)P.num_pages) pg = -1;
+        at = -1;
 #pragma unroll
-            for (int i = 0; i < DIM / 32; ++i) raw[i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
-            const float lse = live ? __ldg(W.lse + tok * P.q_heads + head) : -INFINITY;
-            const uint32_t* u = reinterpret_cast<const uint32_t*>(raw);
-            uint32_t m = 0;
+        for (int t = 0; t < 2; ++t) {
+            const int page = __shfl_sync(0xFFFFFFFFu, pg, 16 * t);
+            const int64_t tile = (int64_t)page * P.kv_heads + h;
+            const int first = (t0 + 16 * t) & (P.page - 1);
+            scale[t] = seen && page >= 0 ? __ldg(P.k_scales + (tile << per_page) + (first >> P.block_shift)) : 0u;
+            if (c >> 1 == t && page >= 0 && t0 + out_token < k1) at = (tile << P.page_shift) + ((t0 + out_token) & (P.page - 1));
 #pragma unroll
-            for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
-            float top = hmax_abs_to_f32(m);
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const uint32_t E = __float_as_uint(top) >> 23, Ec = min(max(E, 15u), 254u);
-            const float up = E == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((268u - Ec) << 23);   // an infinity or NaN: NaN
+            for (int x = 0; x < 2; ++x) {
+                const int r = 8 * x + g;
+                uint4* const y = w[2 * t + x];
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                qb[k][0] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
-                qb[k][1] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
-            }
-            my_row = make_float2(P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23), -lse * kLog2e);
-            const int pos = S.shift + qt;
-            // a row that the attention found to see nothing gives nothing
-            my_see = live && lse != -INFINITY ? make_int2(first_seen(pos, P.window), P.causal ? min(pos + 1, end) : end) : make_int2(0, 0);
-        };
-        float2 col_row[2];
-        int2 col_see[2];
-        if constexpr (FEW) {
-            prepare(0);
+                for (int e = 0; e < DIM / 64; ++e) y[e] = make_uint4(0u, 0u, 0u, 0u);
+                if (seen && page >= 0 && t0 + 16 * t + r < k1) {
+                    const uint8_t* p = P.k_codes + ((tile << P.page_shift) + first + r) * DIM + c * (DIM / 4);
+                    if (DIM == 128 && wide) {
+                        uint32_t v[8];
+                        ld_v8(p, v);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int from = 8 * c + 4 * e;
-                col_row[e] = make_float2(__shfl_sync(0xFFFFFFFFu, my_row.x, from), __shfl_sync(0xFFFFFFFFu, my_row.y, from));
-                col_see[e] = make_int2(__shfl_sync(0xFFFFFFFFu, my_see.x, from), __shfl_sync(0xFFFFFFFFu, my_see.y, from));
-            }
-        } else {
-            if (row0 > 0) __syncthreads();
-            for (int eight = warp; 8 * eight < here; eight += kWarps) {
-                prepare(eight);
-#pragma unroll
-                for (int k = 0; k < KS; ++k) q_frag[eight][k][lane] = make_uint2(qb[k][0], qb[k][1]);
-                if (c == 0) {
-                    q_row[8 * eight + g] = my_row;
-                    q_see[8 * eight + g] = my_see;
-                }
-            }
-            __syncthreads();
-        }
-        const float* const before = row0 > 0 ? W.sums : W.earlier;   // (a thread reads back only what it wrote itself)
-        const int before_end = row0 > 0 ? end : old_end;
-
-        auto load = [&](KeyTile<DIM>& K, int i, int pg) {   // by a whole warp; pg = page_at(i)
-            const int t0 = tile_at(i);
-            const bool seen = (t0 < hi && t0 + kTile > lo) || t0 < sinks;
-            bad |= row0 == 0 && i < mine && t0 + (lane & 16) < k1 && (uint32_t)pg >= (uint32_t)P.num_pages;
-            if ((uint32_t)pg >= (uint32_t)P.num_pages) pg = -1;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                K.page[t] = __shfl_sync(0xFFFFFFFFu, pg, 16 * t);
-                const int64_t tile = (int64_t)K.page[t] * P.kv_heads + h;
-                const int first = (t0 + 16 * t) & (P.page - 1);
-                K.scale[t] = K.page[t] >= 0 ? __ldg(P.k_scales + (tile << per_page) + (first >> P.block_shift)) : 0u;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int r = 8 * x + g;
-                    if (seen && K.page[t] >= 0 && t0 + 16 * t + r < k1) {
-                        const uint8_t* p = P.k_codes + ((tile << P.page_shift) + first + r) * DIM + c * (DIM / 4);
-                        if (DIM == 128 && wide) {
-                            uint32_t v[8];
-                            ld_v8(p, v);
-#pragma unroll
-                            for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = __ldg(reinterpret_cast<const uint4*>(p) + e);
-                        }
+                        for (int e = 0; e < DIM / 64; ++e) y[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < DIM / 64; ++e) K.w[2 * t + x][e] = make_uint4(0u, 0u, 0u, 0u);
+                        for (int e = 0; e < DIM / 64; ++e) y[e] = __ldg(reinterpret_cast<const uint4*>(p) + e);
                     }
                 }
             }
-            const int place = t0 + out_at, pw = c < 2 ? K.page[0] : K.page[1];
-            K.earlier = before != nullptr && place < min(k1, before_end) && pw >= 0
-                      ? before[(((int64_t)pw * P.kv_heads + h) << P.page_shift) + (place & (P.page - 1))] : 0.0f;
-        };
-        auto work = [&](const KeyTile<DIM>& K, int i) {
-            const int t0 = tile_at(i);
-            const float kf[2] = {e8m0_to_f32(K.scale[0]), e8m0_to_f32(K.scale[1])};
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // tokens g, 8 + g, 16 + g, 24 + g; this thread's columns
-            if ((t0 < hi && t0 + kTile > lo) || t0 < sinks) {
-                auto eight = [&](const uint2* frag, const float2 (&cr)[2], const int2 (&cs)[2]) {
-                    const bool all = t0 >= max(cs[0].x, cs[1].x) && t0 + kTile <= min(cs[0].y, cs[1].y);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int k = 0; k < KS; ++k) {
-                            uint32_t a0, a1, a2, a3;
-                            widen(word(K.w[2 * t][k / 4], k % 4), a0, a2);
-                            widen(word(K.w[2 * t + 1][k / 4], k % 4), a1, a3);
-                            const uint2 f = FEW ? make_uint2(qb[k][0], qb[k][1]) : frag[k * 32];
-                            mma_f16(s, a0, a1, a2, a3, f.x, f.y);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = ex2(fmaf(s[e], kf[t] * cr[e & 1].x, cr[e & 1].y));
-                            const int place = t0 + 16 * t + 8 * (e >> 1) + g;
-                            const bool sees = all || (place < cs[e & 1].y && (place >= cs[e & 1].x || place < sinks));
-                            sum[2 * t + (e >> 1)] += sees ? p : 0.0f;
-                        }
-                    }
-                };
-                if constexpr (FEW) {
-                    eight(nullptr, col_row, col_see);
-                } else {
-                    for (int y = 0; 8 * y < here; ++y) {
-                        float2 cr[2];
-                        int2 cs[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            cr[e] = q_row[8 * y + 2 * c + e];
-                            cs[e] = q_see[8 * y + 2 * c + e];
-                        }
-                        eight(&q_frag[y][0][lane], cr, cs);
-                    }
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 1);
-                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 2);
-            }
-            const float all = c < 2 ? (c == 0 ? sum[0] : sum[1]) : (c == 2 ? sum[2] : sum[3]);
-            const int place = t0 + out_at, pw = c < 2 ? K.page[0] : K.page[1];
-            if (place < k1 && pw >= 0) W.sums[(((int64_t)pw * P.kv_heads + h) << P.page_shift) + (place & (P.page - 1))] = K.earlier + all;
-        };
-        KeyTile<DIM> cur, next;
-        int pg = page_at(0);
-        for (int i = -1; i < mine; ++i) {
-            const int pg_next = page_at(i + 2);
-            load(next, i + 1, pg);
-            if (i >= 0) work(cur, i);
-            cur = next;
-            pg = pg_next;
         }
+        earlier = at >= 0 && t0 + out_token < old_end ? W.earlier[at] : 0.0f;
+    };
+    int pg = page_at(0);
+    load(0, pg);
+    pg = page_at(1);
+
+    // ---- the rows: eight at a time by a warp; thread (g, c) reads a quarter of row g ----
+    uint32_t qb[KS][2];
+    float2 my_row = make_float2(0.0f, 0.0f);
+    int2 my_see = make_int2(0, 0);
+    auto prepare = [&](int eight) {
+        const int row = 8 * eight + g, qt = P.by_group(row);
+        const bool live = row < rows;
+        uint4 raw[DIM / 32];
+        const int64_t head = (int64_t)h * G + row - (int64_t)qt * G, tok = (int64_t)S.q0 + qt;
+        const uint16_t* qp = P.q + tok * P.q_stride + head * DIM + c * (DIM / 4);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; ++i) raw[i] = live ? __ldg(reinterpret_cast<const uint4*>(qp) + i) : make_uint4(0, 0, 0, 0);
+        const float lse = live ? __ldg(W.lse + tok * P.q_heads + head) : -INFINITY;
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(raw);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
+        float top = hmax_abs_to_f32(m);
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const uint32_t E = __float_as_uint(top) >> 23, Ec = min(max(E, 15u), 254u);
+        const float up = E == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((268u - Ec) << 23);   // an infinity or NaN: NaN
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            qb[k][0] = pack_f16(bf16_lo(u[2 * k]) * up, bf16_hi(u[2 * k]) * up);
+            qb[k][1] = pack_f16(bf16_lo(u[2 * k + 1]) * up, bf16_hi(u[2 * k + 1]) * up);
+        }
+        my_row = make_float2(P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23), -lse * kLog2e);
+        const int pos = S.shift + qt;
+        // a row that the attention found to see nothing gives nothing
+        my_see = live && lse != -INFINITY ? make_int2(first_seen(pos, P.window), P.causal ? min(pos + 1, end) : end) : make_int2(0, 0);
+    };
+    float2 col_row[2];
+    int2 col_see[2];
+    if constexpr (FEW) {
+        prepare(0);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int from = 8 * c + 4 * e;
+            col_row[e] = make_float2(__shfl_sync(0xFFFFFFFFu, my_row.x, from), __shfl_sync(0xFFFFFFFFu, my_row.y, from));
+            col_see[e] = make_int2(__shfl_sync(0xFFFFFFFFu, my_see.x, from), __shfl_sync(0xFFFFFFFFu, my_see.y, from));
+        }
+    } else {
+        for (int eight = warp; 8 * eight < rows; eight += kWarps) {
+            prepare(eight);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) q_frag[eight][k][lane] = make_uint2(qb[k][0], qb[k][1]);
+            if (c == 0) {
+                q_row[8 * eight + g] = my_row;
+                q_see[8 * eight + g] = my_see;
+            }
+        }
+        __syncthreads();
+    }
+
+    for (int i = 0; i < mine; ++i) {
+        const int t0 = tile_at(i), pg_next = page_at(i + 2);
+        const bool seen = (t0 < hi && t0 + kTile > lo) || t0 < sinks;
+        const float kf[2] = {e8m0_to_f32(scale[0]), e8m0_to_f32(scale[1])};
+        const int64_t out = at;
+        const float before = earlier;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // tokens g, 8 + g, 16 + g, 24 + g; this thread's columns
+        float s[2][4];
+        auto scores = [&](const uint2* frag) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    uint32_t a0, a1, a2, a3;
+                    widen(word(w[2 * t][k / 4], k % 4), a0, a2);
+                    widen(word(w[2 * t + 1][k / 4], k % 4), a1, a3);
+                    const uint2 f = FEW ? make_uint2(qb[k][0], qb[k][1]) : frag[k * 32];
+                    mma_f16(s[t], a0, a1, a2, a3, f.x, f.y);
+                }
+            }
+        };
+        auto add = [&](const float2 (&cr)[2], const int2 (&cs)[2]) {
+            const bool all = t0 >= max(cs[0].x, cs[1].x) && t0 + kTile <= min(cs[0].y, cs[1].y);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = ex2(fmaf(s[t][e], kf[t] * cr[e & 1].x, cr[e & 1].y));
+                    const int place = t0 + 16 * t + 8 * (e >> 1) + g;
+                    const bool sees = all || (place < cs[e & 1].y && (place >= cs[e & 1].x || place < sinks));
+                    sum[2 * t + (e >> 1)] += sees ? p : 0.0f;
+                }
+        };
+        if constexpr (FEW) {
+            scores(nullptr);
+            load(i + 1, pg);   // over the codes at hand: more warps hide more than a second set of registers did
+            if (seen) add(col_row, col_see);
+        } else {
+            if (seen)
+                for (int y = 0; 8 * y < rows; ++y) {
+                    float2 cr[2];
+                    int2 cs[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        cr[e] = q_row[8 * y + 2 * c + e];
+                        cs[e] = q_see[8 * y + 2 * c + e];
+                    }
+                    scores(&q_frag[y][0][lane]);
+                    add(cr, cs);
+                }
+            load(i + 1, pg);
+        }
+        pg = pg_next;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 1);
+            sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 2);
+        }
+        const float all = c < 2 ? (c == 0 ? sum[0] : sum[1]) : (c == 2 ? sum[2] : sum[3]);
+        if (out >= 0) W.sums[out] = before + all;
     }
     if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_weights_bad, 1u);
 }
@@ -265,6 +262,19 @@ cudaError_t launch(K kernel, int64_t ctas, cudaStream_t stream, const WeightsPar
 int64_t plan_weights(WeightsParams& W)
 {
     AttnParams& P = W.a;
+    W.many = (int64_t)P.max_q * P.group > kRows;
+    if (W.many) {
+        // query tiles of up to 128 rows: whole tokens, or one token's heads in parts
+        W.tile_heads = P.group < 128 ? P.group : 128;
+        W.tile_tokens = 128 / W.tile_heads < P.n ? 128 / W.tile_heads : (int)P.n;
+        W.head_parts = (int)ceil_div(P.group, W.tile_heads);
+        W.key_tiles = (int)ceil_div(P.max_len, 256);
+        // CTAs for a key tile: more while the SMs are not filled twice and each still has four query tiles
+        const int64_t units = (int64_t)W.key_tiles * P.seqs * P.kv_heads, tiles = ceil_div(P.max_q, W.tile_tokens) * W.head_parts;
+        W.ranks = 1;
+        while (W.ranks < 8 && units * W.ranks < 2 * 148 && tiles >= 8 * W.ranks) W.ranks *= 2;
+        return units * W.ranks;
+    }
     // Chunks of 16 tiles (four for each warp), or of one tile for each warp where CTAs would be fewer than three an SM; nothing is joined,
     // so a chunk costs no more than its start.
     const int64_t units = (int64_t)P.seqs * P.kv_heads, least = kWarps * kTile;
@@ -277,16 +287,25 @@ int64_t plan_weights(WeightsParams& W)
 cudaError_t launch_weights(const WeightsParams& W, int64_t ctas, cudaStream_t stream)
 {
     const AttnParams& P = W.a;
+    if (W.many) return launch_weights_many(W, ctas, stream);
     const bool few = (int64_t)P.max_q * P.group <= 8;
     if (P.dim == 128) return few ? launch(key_weights_kernel<128, true>, ctas, stream, W) : launch(key_weights_kernel<128, false>, ctas, stream, W);
     return few ? launch(key_weights_kernel<64, true>, ctas, stream, W) : launch(key_weights_kernel<64, false>, ctas, stream, W);
 }
 
-cudaError_t read_weights_bad(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_weights_bad, sizeof(unsigned int)); }
-cudaError_t reset_weights_bad()
+cudaError_t read_weights_counters(unsigned int* timeouts, unsigned int* bad)
+{
+    unsigned int more = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(bad, g_weights_bad, sizeof(unsigned int));
+    if (e == cudaSuccess) e = read_weights_many_counters(timeouts, &more);
+    *bad += more;
+    return e;
+}
+cudaError_t reset_weights_counters(bool timeouts)
 {
     const unsigned int zero = 0;
-    return cudaMemcpyToSymbol(g_weights_bad, &zero, sizeof(unsigned int));
+    const cudaError_t e = timeouts ? cudaSuccess : cudaMemcpyToSymbol(g_weights_bad, &zero, sizeof(unsigned int));
+    return e != cudaSuccess ? e : reset_weights_many_counters(timeouts);
 }
 
 }  // namespace mxn
