@@ -7,10 +7,10 @@
 // after one key, adds its row of scores up in registers, and no sum crosses threads until the end.  The codes become bf16 (exact) once and stay in tensor
 // memory as the first operand; the queries come as they are (bf16), by the tensor copy engine, so that every product is exact; the sums of a score are binary32.
 // Roles, by warp:
-//   0      copies of query tiles
-//   1      issues the products: (query tile, key tile) after (query tile, key tile), into three buffers of tensor memory in turn
-//   2      -lse in powers of two for the columns of a query tile
-//   4-19   keys to tensor memory; then four warpgroups take the products in turn: exponentials and sums
+//   0-15   keys to tensor memory; then exponentials and sums, two warpgroups for a product
+//   16     copies of query tiles
+//   17     issues the products of (query tile, key tile) after (query tile, key tile), into three buffers of tensor memory in turn
+//   18     -lse in powers of two for the columns of a query tile
 // A cluster of CTAs shares out the query tiles of the same keys where there are too few key tiles for the SMs; their sums are added in a fixed order through
 // each other's shared memory.
 //
@@ -28,9 +28,11 @@ namespace mxn {
 
 namespace {
 
-constexpr int kTile = 128, kKeys = 256, kThreads = 640, kBuffers = 3, kGroups = 4, kSlots = 8;
+constexpr int kTile = 128, kHalf = 64, kKeys = 256, kThreads = 608, kBuffers = 3, kGroups = 4, kFull = 4, kSlots = 8;
+constexpr int kCopies = 16, kProducts = 17, kRowSums = 18;   // warps
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kByMultipliers = 5;   // of 16 pairs of exponentials
+static_assert(kFull > kBuffers && kFull % 2 == 0);
+constexpr int kByMultipliers = 3;   // of 16 pairs of exponentials
 
 __device__ unsigned int g_many_timeouts = 0;
 __device__ unsigned int g_many_bad = 0;
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
     using Sh = ManyShape<DIM>;
     constexpr int ST = Sh::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * ST + 2 * kSlots + kGroups + kBuffers + 1];
+    __shared__ uint64_t bars[2 * ST + 2 * kSlots + kFull + kBuffers + 1];
     __shared__ Columns columns[kSlots];
     __shared__ float parts[kGroups][kTile], total[kKeys];
     __shared__ uint32_t tmem_at;
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
 
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, q_empty = q_full + 8 * ST, n_full = q_empty + 8 * ST, n_empty = n_full + 8 * kSlots, d_full = n_empty + 8 * kSlots,
-                   d_empty = d_full + 8 * kGroups, a_full = d_empty + 8 * kBuffers;
+                   d_empty = d_full + 8 * kFull, a_full = d_empty + 8 * kBuffers;
     volatile int* const dead = &dead_flag;
     if (threadIdx.x == 0) {
         dead_flag = 0;
@@ -124,17 +126,17 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
         }
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(n_full + 8 * i, 1);
-            mbar_init(n_empty + 8 * i, 4 * ms);
+            mbar_init(n_empty + 8 * i, 8 * ms);
         }
-        // a product is announced to the warpgroup that takes it, not by its buffer: a group skips uses of a buffer, and would take the
-        // one before for its own
-        for (int i = 0; i < kGroups; ++i) mbar_init(d_full + 8 * i, 1);
-        for (int i = 0; i < kBuffers; ++i) mbar_init(d_empty + 8 * i, 4);
+        // A product is announced by its number, not by its buffer: a warpgroup skips uses of a buffer, and would take the one before for
+        // its own.  Four numbers are more than the buffers, so that none comes round before it has been seen.
+        for (int i = 0; i < kFull; ++i) mbar_init(d_full + 8 * i, 1);
+        for (int i = 0; i < kBuffers; ++i) mbar_init(d_empty + 8 * i, 8);
         mbar_init(a_full, 8 * ms);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
     }
-    if (warp == 1) {
+    if (warp == kProducts) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
     const uint32_t tmem = tmem_at;
     const uint32_t a_col = tmem, d_col = tmem + DIM;   // [key tile][DIM / 2 columns], [buffer][128]
 
-    if (warp == 0) {
+    if (warp == kCopies) {
         bool ok = true;
         const uint32_t bytes = (uint32_t)rows_of_tile * DIM * 2;
         for (int i = 0; i < tiles; ++i) {
@@ -170,12 +172,12 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             }
             __syncwarp();
         }
-    } else if (warp == 1) {
+    } else if (warp == kProducts) {
         const bool one = elect_one();
         bool ok = tiles == 0 || wait(a_full, 0, dead);
         tc_after();
         const uint64_t q_base = operand(base, 1024, 16, 2);
-        uint32_t st = 0, st_par = 0, buf = 0, buf_par = 1, group = 0;   // (the buffers' first use waits for nothing)
+        uint32_t st = 0, st_par = 0, buf = 0, buf_par = 1, number = 0;   // (the buffers' first use waits for nothing)
         for (int i = 0; ok && i < tiles; ++i) {
             ok = wait(q_full + 8 * st, st_par, dead);
             const uint64_t q_desc = q_base + (uint64_t)((st * Sh::kStage) >> 4);
@@ -188,9 +190,9 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                     for (int s = 0; s < DIM / 16; ++s)   // 16 dimensions a step: 8 columns of keys, 32 bytes of the queries' rows
                         mma_values(d_col + buf * kTile, a_col + m * (DIM / 2) + 8 * s, q_desc + (uint64_t)(((s / 4) * kTile * 128 + (s % 4) * 32) >> 4),
                                    idesc_bf16(kTile), s != 0);
-                    mma_commit(d_full + 8 * group);
+                    mma_commit(d_full + 8 * number);
                 }
-                group = (group + 1) % kGroups;
+                number = (number + 1) % kFull;
                 if (++buf == kBuffers) {
                     buf = 0;
                     buf_par ^= 1u;
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             (void)mbar_wait_bounded(q_empty, 0, 1u << 14);
             (void)mbar_wait_bounded(q_empty, 1, 1u << 14);
         }
-    } else if (warp == 2) {
+    } else if (warp == kRowSums) {
         // this lane's columns lane, lane + 32, ...: token and head within a tile
         int tok[4], head[4];
 #pragma unroll
@@ -246,8 +248,8 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             }
             __syncwarp();
         }
-    } else if (warp >= 4) {
-        const int wg = (warp - 4) >> 2, m = ms == 2 ? wg & 1 : 0, r = threadIdx.x & 127;
+    } else {
+        const int wg = warp >> 2, m = ms == 2 ? wg & 1 : 0, r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int key = k0 + m * kTile + r;
         const int32_t page = key < k1 ? __ldg(P.page_table + (int64_t)seq * P.max_pages + (key >> P.page_shift)) : -1;
@@ -283,41 +285,59 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             scale = P.scale * kLog2e * e8m0_to_f32(__ldg(P.k_scales + (tile << (P.page_shift - P.block_shift)) + (in_page >> P.block_shift)));
         const float2 f = f2(scale);
         float2 sum[2] = {f2(0.0f), f2(0.0f)};
-        const int items = tiles * ms;
+        // A product is shared by two warpgroups, half of its columns each: with two key tiles each pair has its own, with one they take turns
+        const int items = tiles * ms, col0 = (ms == 2 ? wg >> 1 : wg & 1) * kHalf;
+        // First tokens of the query tiles all of whose columns see all of this warp's keys: [see0, see1].  (What a key without a page gets is not used.)
+        const int64_t place = (int64_t)key - S.shift;   // of the key, among the call's tokens
+        int see0 = P.causal && real ? (int)max(place, (int64_t)0) : 0, see1 = S.nq - T;
+        if (P.window > 0 && key >= P.sinks && real) see1 = (int)max((int64_t)-1, min((int64_t)see1, place + P.window - T));
+        // ... and those in front of which no column sees any of them, and behind which none does: before none0, from none1 on
+        const int none0 = __reduce_min_sync(0xFFFFFFFFu, P.causal && real ? (int)max(place, (int64_t)0) : 0);
+        const int none1 = __reduce_max_sync(0xFFFFFFFFu, P.window > 0 && key >= P.sinks ? (int)max((int64_t)0, min((int64_t)S.nq, place + P.window)) : S.nq);
+        see0 = __reduce_max_sync(0xFFFFFFFFu, see0);
+        see1 = P.group % GB == 0 ? __reduce_min_sync(0xFFFFFFFFu, see1) : -1;
         bool ok = true;
-        for (int item = wg; item < items; item += kGroups) {
-            const int i = ms == 2 ? item >> 1 : item, buf = item % kBuffers, slot = i % kSlots;
-            // columns [lo, hi) whose rows see this key
-            const At t = tile_at(i);
-            const int valid = min(T, S.nq - t.token) * min(GB, P.group - t.part * GB);
-            const int64_t ahead = (int64_t)key - S.shift - t.token;   // of the tile's first token
-            const int from = P.causal ? (int)max((int64_t)0, min((int64_t)T, ahead)) : 0;
-            const int to = P.window == 0 || key < P.sinks ? T : (int)max((int64_t)0, min((int64_t)T, ahead + P.window));
-            const int lo = from * GB, hi = real ? min(to * GB, valid) : 0;
-            ok = wait(n_full + 8 * slot, (uint32_t)(i / kSlots) & 1u, dead) && wait(d_full + 8 * wg, (uint32_t)(item / kGroups) & 1u, dead);
+        int buf = ms == 2 ? wg & 1 : wg >> 1;
+        for (int item = buf; item < items; item += 2) {
+            const int i = ms == 2 ? item >> 1 : item, slot = i % kSlots;
+            ok = wait(n_full + 8 * slot, (uint32_t)(i / kSlots) & 1u, dead) && wait(d_full + 8 * (item % kFull), (uint32_t)(item / kFull) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_after();
-            const Columns& C = columns[slot];
-            const bool plain = __all_sync(0xFFFFFFFFu, lo == 0 && hi == rows_of_tile) && C.special == 0;
-            const uint32_t at = d_col + buf * kTile + lanes;
+            const uint32_t at = d_col + buf * kTile + col0 + lanes, free_bar = d_empty + 8 * buf;
+            buf = buf > 0 ? buf - 1 : 2;   // two on, of three
             uint32_t x[2][32];
             tm_request(x[0], at);
-            float2 part[2] = {f2(0.0f), f2(0.0f)};
+            tm_request(x[1], at + 32);
+            const Columns& C = columns[slot];
+            const At t = tile_at(i);
+            const bool plain = t.token >= see0 && t.token <= see1 && C.special == 0, none = t.token + T <= none0 || t.token >= none1;
+            uint32_t see[2] = {0u, 0u};   // columns of this half whose rows see this key
+            if (!plain && !none) {
+                const int valid = min(T, S.nq - t.token) * min(GB, P.group - t.part * GB);
+                const int64_t ahead = place - t.token;
+                const int from = P.causal ? (int)max((int64_t)0, min((int64_t)T, ahead)) : 0;
+                const int to = P.window == 0 || key < P.sinks ? T : (int)max((int64_t)0, min((int64_t)T, ahead + P.window));
+                const int lo = from * GB - col0, hi = real ? min(to * GB, valid) - col0 : 0;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tm_arrived(x[c & 1]);
-                if (c < 3) {
-                    tm_request(x[(c + 1) & 1], at + 32 * (c + 1));
-                } else {   // all of the buffer is in registers
-                    tc_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(d_empty + 8 * buf);
+                for (int c = 0; c < 2; ++c) {
+                    const int a = min(max(lo - 32 * c, 0), 32), b = min(max(hi - 32 * c, 0), 32);
+                    see[c] = (b == 32 ? 0xFFFFFFFFu : (1u << b) - 1u) & (a == 32 ? 0u : 0xFFFFFFFFu << a);
                 }
-                const uint32_t* const y = x[c & 1];
+            }
+            float2 part[2] = {f2(0.0f), f2(0.0f)};
+            tm_arrived(x[0]);
+            tm_arrived(x[1]);
+            tc_before();   // the buffer is free again before any arithmetic
+            __syncwarp();
+            if (lane == 0) mbar_arrive(free_bar);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t* const y = x[c];
+                const float* const cl = C.lse + col0 + 32 * c;
                 if (plain) {
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
-                        const float4 n = *reinterpret_cast<const float4*>(C.lse + 32 * c + 2 * e);
+                        const float4 n = *reinterpret_cast<const float4*>(cl + 2 * e);
                         const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, make_float2(n.x, n.y));
                         const float2 v = __ffma2_rn(make_float2(__uint_as_float(y[2 * e + 2]), __uint_as_float(y[2 * e + 3])), f, make_float2(n.z, n.w));
                         // spread over the 16 pairs, so that both kinds run side by side
@@ -326,12 +346,11 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                         part[0] = __fadd2_rn(part[0], mu ? ex2_fma(u) : make_float2(ex2(u.x), ex2(u.y)));
                         part[1] = __fadd2_rn(part[1], mv ? ex2_fma(v) : make_float2(ex2(v.x), ex2(v.y)));
                     }
-                } else {
+                } else if (__any_sync(0xFFFFFFFFu, see[c] != 0u)) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const int col = 32 * c + e;
-                        const float p = ex2(fmaf(__uint_as_float(y[e]), scale, C.lse[col]));
-                        part[e & 1].x += col >= lo && col < hi ? p : 0.0f;
+                        const float p = ex2(fmaf(__uint_as_float(y[e]), scale, cl[e]));
+                        part[e & 1].x += see[c] >> e & 1u ? p : 0.0f;
                     }
                 }
             }
@@ -375,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
         }
     }
     if (W.ranks > 1) cluster_sync();   // nobody leaves while its shared memory is read
-    if (warp == 1) {
+    if (warp == kProducts) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
     }
