@@ -459,7 +459,8 @@ mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const
 /* Moves listed tokens of a sequence together: token kept[s, h, i] goes to place first[s] + i (first NULL: 0) for the places below
  *   new_lens[s] (at most max_kept of them).  kept int32 [n_seqs, kept_heads, max_kept], kept_heads = kv_heads or 1 (one list for all heads).
  *   It closes the gaps that an eviction leaves (with mxkv_select's lists), and those in a tree of drafts of which a path was accepted
- *   (first = the length in front of the tree, the path as one list).  head_dim is 64 or 128.
+ *   (first = the length in front of the tree, the path as one list).  head_dim is 64 or 128; num_pages * kv_heads *
+ *   page_size below 2^31.
  *   out_page_table NULL (or page_table itself): in place.  The lists then rise and no entry lies below its place.  Needs a workspace (device
  *   memory, 16-byte aligned, mxkv_compact_workspace_bytes(...) bytes, contents irrelevant before and after; calls that may overlap need
  *   workspaces of their own).  Otherwise tokens are written to the pages of out_page_table int32 [n_seqs, out_max_pages], which must not be

@@ -639,7 +639,8 @@ mxn_status attend(mxn::AttnParams P, int64_t n_seqs, int64_t max_q_len, int64_t 
     if (P.n == 0 || n_seqs == 0) return MXN_OK;
     if ((st = check_heads(P.q, P.q_stride, P.q_heads, P.dim)) != MXN_OK || (st = check_heads(out, out_stride, P.q_heads, P.dim)) != MXN_OK) return st;
     if (lse != nullptr && misaligned(lse, 4)) return MXN_ERR_ALIGN;
-    const mxn::AttnPlan plan = mxn::plan_attention(P.n, n_seqs, max_q_len, max_kv_len, P.causal ? window : 0, sinks, P.q_heads, P.kv_heads, P.dim);
+    const mxn::AttnPlan plan = mxn::plan_attention(P.n, n_seqs, max_q_len, max_kv_len, P.causal ? window : 0, sinks, P.q_heads, P.kv_heads, P.dim,
+                                                    P.tree != nullptr);
     if (plan.ctas > 0x7FFFFFFF || P.n * P.q_heads > 0x7FFFFFFF) return MXN_ERR_SHAPE;
     if (plan.splits > 1) {
         if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
@@ -786,7 +787,9 @@ size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t 
                                       int head_dim)
 {
     if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim) || n_tokens == 0 || n_seqs == 0) return 0;
-    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim).workspace;
+    const size_t a = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, false).workspace,
+                 b = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, true).workspace;
+    return a > b ? a : b;
 }
 
 mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
@@ -905,7 +908,7 @@ mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const
 size_t mxkv_compact_workspace_bytes(int64_t n_seqs, int kv_heads, int64_t max_kept)
 {
     if (n_seqs <= 0 || kv_heads < 1 || max_kept <= 0 || max_kept > kMaxTokens) return 0;
-    return ((size_t)mxn::compact_units(max_kept) * n_seqs * kv_heads * 2 + 1) * 4;
+    return ((size_t)mxn::compact_units(max_kept, 32) * n_seqs * kv_heads * 2 + 1) * 4;
 }
 
 mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, const int32_t* first_or_null, const int32_t* new_lens,
@@ -919,10 +922,10 @@ mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, c
     if (st != MXN_OK) return st;
     const bool in_place = out_page_table_or_null == nullptr || out_page_table_or_null == page_table;
     if ((head_dim != 64 && head_dim != 128) || (kept_heads != 1 && kept_heads != kv_heads) || max_kept < 0 || max_kept > kMaxTokens ||
-        (!in_place && (out_max_pages < 1 || out_max_pages > kMaxTokens / page_size)))
+        (!in_place && (out_max_pages < 1 || out_max_pages > kMaxTokens / page_size)) || num_pages * kv_heads > kMaxTokens / page_size)
         return MXN_ERR_SHAPE;
     if (n_seqs == 0 || max_kept == 0) return MXN_OK;
-    const int64_t units = mxn::compact_units(max_kept);
+    const int64_t units = mxn::compact_units(max_kept, 32);
     if (n_seqs * kv_heads > kMaxTokens / 2 / units) return MXN_ERR_SHAPE;
     if (kept == nullptr) return MXN_ERR_NULL;
     if (misaligned(kept, 4) || (first_or_null != nullptr && misaligned(first_or_null, 4)) || (!in_place && misaligned(out_page_table_or_null, 4)) ||
@@ -948,7 +951,6 @@ mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, c
     P.max_kept = max_kept;
     P.width = max_pages;
     P.out_width = in_place ? max_pages : out_max_pages;
-    P.units = units;
     P.num_pages = (int)num_pages;
     P.seqs = (int)n_seqs;
     P.heads = kv_heads;

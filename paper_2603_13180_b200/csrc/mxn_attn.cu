@@ -47,6 +47,7 @@ constexpr int kWarps = 4;
 // CTAs an SM that the register allocation makes room for
 __host__ __device__ constexpr int decode_ctas(int dim, int nq) { return nq == 1 ? (dim == 128 ? 3 : 4) : dim == 128 || nq == 4 ? 2 : 3; }
 constexpr int kTile = 32;      // tokens of a tile
+constexpr int kTreeRows = 64, kTreeRounds = 1, kTreeLeast = 4;
 constexpr int kPromptRows = 64;   // more query rows a sequence and key head than this: the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -895,11 +896,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 namespace {
 
 // wide: heads of 64, 17 to 64 rows: 32 rows a warp (two warps where there are more), else 16 and more CTAs
-AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool wide)
+AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool wide, bool tree)
 {
     AttnPlan a{};
     const int64_t rows = max_q * (q_heads / kv_heads);
-    a.prompt = rows > kPromptRows;
+    a.prompt = rows > (tree ? kTreeRows : kPromptRows);
     // a warp holds the output of up to 16 rows of 128 or 32 of 64; more rows are shared out among the CTA's warps
     a.row_eights = rows <= 8 ? 1 : rows <= 16 || dim == 128 || !wide ? 2 : 4;
     a.row_warps = dim == 64 && a.row_eights == 2 ? 1 : (int)(rows <= 8 * a.row_eights ? 1 : rows <= 16 * a.row_eights ? 2 : 4);
@@ -912,12 +913,12 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
     // CTA's start and the join are worth it (64 sequences of up to 2000 keys: 37 us, five steps 40), or five where half of the places
     // would stay empty (16 sequences: eight 20 us, five 16, 14 with the join as it is now), less only where most SMs would be idle.
     const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : decode_ctas(dim, a.row_eights));
-    int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
+    int64_t splits = seqs > 1 && (!a.prompt || tree) ? ceil_div((a.prompt ? kTreeRounds : 4) * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
     const int64_t reach = window + tokens + tile + ceil_div(sinks, tile) * tile;
     const int64_t span = window > 0 && reach < max_len ? reach : max_len;
-    const int64_t least = !a.prompt && 2 * units < resident ? 5 : 8;
+    const int64_t least = a.prompt && tree ? kTreeLeast : !a.prompt && 2 * units < resident ? 5 : 8;
     auto most = [&](int64_t keys) {
         const int64_t by_least = ceil_div(keys, least * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
         return by_least >= idle ? by_least : by_one < idle ? by_one : idle;
@@ -947,15 +948,15 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
 
 }  // namespace
 
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim)
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree)
 {
     if (max_q > n) max_q = n;
-    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, true);
+    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, true, tree);
     if (a.prompt || a.row_eights != 4) return a;
     // 32 rows a warp save conversions, 16 hide latency better: taken unless a few chunks of all sequences fit side by side
     // (32 sequences of four drafted tokens, window 1024: 32 rows 19 us, 16 rows 29; 64 sequences of 4100 keys: 83 and 79; 16 of
     // 8000, eight tokens: 75 and 66).  The workspace is that of either, whatever the window.
-    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, false);
+    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, false, tree);
     a.workspace = b.workspace = a.workspace > b.workspace ? a.workspace : b.workspace;
     return a.cluster ? a : b;
 }

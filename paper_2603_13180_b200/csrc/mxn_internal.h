@@ -147,7 +147,7 @@ struct AttnPlan {
     bool cluster;               // few chunks, joined by the CTAs as a cluster
     size_t workspace;
 };
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim);
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree);
 cudaError_t launch_attention(AttnParams P, const AttnPlan& plan, void* workspace, cudaStream_t stream);
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad);
 cudaError_t reset_attn_timeouts();
@@ -192,11 +192,11 @@ struct CompactParams {
     float* weights;             // or nullptr
     uint32_t* work;             // in place: a ticket, then a flag for each unit
     int64_t max_kept, width, out_width;       // pages a sequence in the two tables
-    int64_t units;              // of a sequence, head, keys or values
+    int64_t units;              // of a sequence, head, keys or values (filled by the launcher)
     int num_pages, seqs, heads, kept_heads, dim, page_shift, block_shift;
 };
-int64_t compact_units(int64_t max_kept);
-cudaError_t launch_compact(const CompactParams& P, cudaStream_t stream);
+int64_t compact_units(int64_t max_kept, int places);
+cudaError_t launch_compact(CompactParams P, cudaStream_t stream);
 cudaError_t read_keep_counters(unsigned int* timeouts, unsigned int* bad);
 cudaError_t reset_keep_counters(bool timeouts);
 
