@@ -908,7 +908,7 @@ mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const
 size_t mxkv_compact_workspace_bytes(int64_t n_seqs, int kv_heads, int64_t max_kept)
 {
     if (n_seqs <= 0 || kv_heads < 1 || max_kept <= 0 || max_kept > kMaxTokens) return 0;
-    return ((size_t)mxn::compact_units(max_kept, 32) * n_seqs * kv_heads * 2 + 1) * 4;
+    return ((size_t)mxn::compact_units(max_kept, 32) * n_seqs * kv_heads + 1) * 4;
 }
 
 mxn_status mxkv_compact(const int32_t* kept, int kept_heads, int64_t max_kept, const int32_t* first_or_null, const int32_t* new_lens,

@@ -192,7 +192,7 @@ struct CompactParams {
     float* weights;             // or nullptr
     uint32_t* work;             // in place: a ticket, then a flag for each unit
     int64_t max_kept, width, out_width;       // pages a sequence in the two tables
-    int64_t units;              // of a sequence, head, keys or values (filled by the launcher)
+    int64_t units;              // of a sequence and head (filled by the launcher)
     int num_pages, seqs, heads, kept_heads, dim, page_shift, block_shift;
 };
 int64_t compact_units(int64_t max_kept, int places);

@@ -6,7 +6,7 @@
 // chosen weight.  Then every warp writes the places that it chose, in order, behind those of the warps before it.  A sequence and head is
 // shared out over a cluster of CTAs, each with a run of tokens whose weights stay in registers; histograms are read across the cluster.
 //
-// Compact: token kept[i] goes to place first + i.  A warp takes 32 places (64 with blocks of as many) of the keys or the values of a head: it reads the listed rows and their blocks' scales,
+// Compact: token kept[i] goes to place first + i.  A warp takes 32 places (64 with blocks of as many) of a head, for keys and values: it reads the listed rows and their blocks' scales,
 // finds for each block of places the scale that its largest value asks for (the append's rule: S = 2^(ceil(log2 absmax) - 8)), rounds the codes
 // on it (exact unless they become subnormal; as they are where the scale stays) and writes them.  In place a row must be read before its place is written.
 // Lists rise and places never lie behind their tokens, so only warps of lower places read what a warp is to overwrite; a warp says so once it
@@ -270,7 +270,7 @@ __device__ __forceinline__ void scale_by(uint4& x, int d)   // -24 <= d <= 15
 
 // K: places of a lane; a warp takes 32 K of them, at least a block
 template <int DIM, bool IN_PLACE, int K>
-__global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kernel(const CompactParams P)
+__global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 4 : 3) compact_kernel(const CompactParams P)
 {
     constexpr int kPlaces = 32 * K;
     constexpr int L = DIM / 16;          // lanes of a row
@@ -286,12 +286,10 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
         __syncthreads();
         cta = ticket;
     }
-    const int64_t unit = (int64_t)cta * kMoveWarps + warp, lists = (int64_t)P.seqs * P.heads * 2;
+    const int64_t unit = (int64_t)cta * kMoveWarps + warp, lists = (int64_t)P.seqs * P.heads;
     if (unit >= P.units * lists) return;
     const int u = (int)(unit / lists);
-    uint32_t rest = (uint32_t)(unit % lists);
-    const int which = (int)(rest & 1u);
-    rest >>= 1;
+    const uint32_t rest = (uint32_t)(unit % lists);
     const int h = (int)(rest % (uint32_t)P.heads), seq = (int)(rest / (uint32_t)P.heads);
     uint32_t* const flags = P.work + 1;   // of the same list: unit u' at u' * lists + (unit % lists)
     const int64_t flag_at = unit - (int64_t)u * lists;
@@ -300,7 +298,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
     const int len = __ldg(P.lens + seq);
     const int64_t asked = (int64_t)__ldg(P.new_lens + seq) - first;
     bool bad = first < 0 || first > len || asked > P.max_kept;
-    if (bad && lane == 0 && u == 0 && h == 0 && which == 0) atomicAdd(&g_keep_bad, 1u);
+    if (bad && lane == 0 && u == 0 && h == 0) atomicAdd(&g_keep_bad, 1u);
     if (first < 0 || first > len) return;   // the sequence is left as it is
     const int end = (int)min(first + min(asked, P.max_kept), (int64_t)0x7FFFFFFF - kPlaces);
     const int from = first / kPlaces * kPlaces, base = (int)min((int64_t)from + (int64_t)u * kPlaces, (int64_t)0x7FFFFFFF - kPlaces);
@@ -311,9 +309,9 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
     const int32_t* const out_table = P.out_table + (int64_t)seq * P.out_width;
     const int page_mask = (1 << P.page_shift) - 1, per_page = P.page_shift - P.block_shift;
 
-    // ---- this lane's two places: where their tokens are (row numbers in the pool, below 2^31; -1: none), where they go ----
+    // ---- this lane's K places: where their tokens are (row numbers in the pool, below 2^31; -1: none), where they go ----
     int src[K], dst[K];
-    int scale[K];
+    int scale[2][K];   // of keys and values
     float moved_weight[K];
     bool stays[K];
 #pragma unroll
@@ -321,7 +319,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
         moved_weight[k] = 0.0f;
         const int place = base + 32 * k + lane;
         src[k] = dst[k] = -1;
-        scale[k] = 0;
+        scale[0][k] = scale[1][k] = 0;
         stays[k] = true;
         if (place >= end) continue;
         bool wrong = false;
@@ -380,19 +378,21 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
             src[k] = -1;
         } else {
             // row / page * (page / block) + block within the page
-            scale[k] = P.scales[which][((src[k] >> P.page_shift) << per_page) + ((src[k] & page_mask) >> P.block_shift)];
-            if (which == 0 && P.weights != nullptr) moved_weight[k] = P.weights[src[k]];
+            const int64_t at = ((int64_t)(src[k] >> P.page_shift) << per_page) + ((src[k] & page_mask) >> P.block_shift);
+            scale[0][k] = P.scales[0][at];
+            scale[1][k] = P.scales[1][at];
+            if (P.weights != nullptr) moved_weight[k] = P.weights[src[k]];
         }
     }
-    uint8_t* const codes = P.codes[which] + 16 * sub;
-    uint4 x[N];
+    uint4 x[2][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int place = i * R + grp;
-        const int row = __shfl_sync(0xFFFFFFFFu, src[i * R / 32], place & 31);
-        x[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (row >= 0) x[i] = *reinterpret_cast<const uint4*>(codes + (int64_t)row * DIM);
-    }
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = __shfl_sync(0xFFFFFFFFu, src[i * R / 32], (i * R + grp) & 31);
+            x[which][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (row >= 0) x[which][i] = *reinterpret_cast<const uint4*>(P.codes[which] + (int64_t)row * DIM + 16 * sub);
+        }
     bool ok = true;
     if (IN_PLACE) {
         // While the rows are on their way: list entries whose tokens lie in this warp's places [base, base + kPlaces).  They stand in front of its own;
@@ -434,71 +434,71 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 6 : 4) compact_kerne
     if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_keep_bad, 1u);
     if (touched[0] == 0u && touched[K - 1] == 0u) return;
 
-    // ---- scales of the blocks: the largest that a token asks for ----
-    // A normal code m asks for ceil(m / 8) - 15 above its token's scale.  Fewer is asked only where all of a token's codes are below 8 (8 itself asks for
-    // as much as the formula gives these), and a NaN (0x7F) has no say: where a piece of 16 codes has its largest among these, all are looked at one by one.
-    int ask[2 * K];   // of 16 places each
-    bool odd = false;
 #pragma unroll
-    for (int q = 0; q < 2 * K; ++q) {
-        int most = -1024;
-#pragma unroll
-        for (int i = q * PER16; i < (q + 1) * PER16; ++i) {
-            const uint32_t m = absmax_codes(x[i]);
-            const int s = __shfl_sync(0xFFFFFFFFu, scale[i * R / 32], (i * R + grp) & 31);
-            odd = odd || m - 8u >= 0x7Fu - 8u;
-            most = max(most, s + (int)((m + 7u) >> 3) - 15);
-        }
-        ask[q] = __reduce_max_sync(0xFFFFFFFFu, most);
+    for (int k = 0; k < K; ++k) {
+        if (!(touched[k] >> lane & 1u)) dst[k] = -1;
+        else if (P.weights != nullptr) P.weights[dst[k]] = moved_weight[k];
     }
-    if (__any_sync(0xFFFFFFFFu, odd)) {
-#pragma unroll 1
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        // ---- scales of the blocks: the largest that a token asks for ----
+        // A normal code m asks for ceil(m / 8) - 15 above its token's scale.  Fewer is asked only where all of a token's codes are below 8 (8 itself asks
+        // for as much as the formula gives these), and a NaN (0x7F) has no say: where a piece of 16 codes has its largest among these, all are looked at one by one.
+        int ask[2 * K];   // of 16 places each
+        bool odd = false;
+#pragma unroll
         for (int q = 0; q < 2 * K; ++q) {
             int most = -1024;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t m = absmax_numbers(x[i]);
-                const int s = __shfl_sync(0xFFFFFFFFu, scale[i * R / 32], (i * R + grp) & 31);
-                if (i / PER16 == q && m != 0u) most = max(most, s + asks(m));
+            for (int i = q * PER16; i < (q + 1) * PER16; ++i) {
+                const uint32_t m = absmax_codes(x[which][i]);
+                const int s = __shfl_sync(0xFFFFFFFFu, scale[which][i * R / 32], (i * R + grp) & 31);
+                odd = odd || m - 8u >= 0x7Fu - 8u;
+                most = max(most, s + (int)((m + 7u) >> 3) - 15);
             }
-            most = __reduce_max_sync(0xFFFFFFFFu, most);
-#pragma unroll
-            for (int y = 0; y < 2 * K; ++y)
-                if (y == q) ask[y] = most;
+            ask[q] = __reduce_max_sync(0xFFFFFFFFu, most);
         }
-    }
-    if (block >= 32) {
+        if (__any_sync(0xFFFFFFFFu, odd)) {
+#pragma unroll 1
+            for (int q = 0; q < 2 * K; ++q) {
+                int most = -1024;
 #pragma unroll
-        for (int k = 0; k < K; ++k) ask[2 * k] = ask[2 * k + 1] = max(ask[2 * k], ask[2 * k + 1]);
-        if (K == 2 && block == 64) ask[0] = ask[1] = ask[2 * K - 2] = ask[2 * K - 1] = max(ask[0], ask[2 * K - 1]);
-    }
+                for (int i = 0; i < N; ++i) {
+                    const uint32_t m = absmax_numbers(x[which][i]);
+                    const int s = __shfl_sync(0xFFFFFFFFu, scale[which][i * R / 32], (i * R + grp) & 31);
+                    if (i / PER16 == q && m != 0u) most = max(most, s + asks(m));
+                }
+                most = __reduce_max_sync(0xFFFFFFFFu, most);
 #pragma unroll
-    for (int q = 0; q < 2 * K; ++q) ask[q] = min(max(ask[q], 0), 254);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (!(touched[k] >> lane & 1u)) {
-            dst[k] = -1;
-            continue;
+                for (int y = 0; y < 2 * K; ++y)
+                    if (y == q) ask[y] = most;
+            }
         }
-        if (which == 0 && P.weights != nullptr) P.weights[dst[k]] = moved_weight[k];
-        const int place = base + 32 * k + lane;
-        // the block's scale: by the block's first place
-        if ((place & (block - 1)) == 0)
-            P.scales[which][((dst[k] >> P.page_shift) << per_page) + ((dst[k] & page_mask) >> P.block_shift)] =
-                (uint8_t)(lane < 16 ? ask[2 * k] : ask[2 * k + 1]);
-    }
+        if (block >= 32) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int from_lane = (i * R + grp) & 31;
-        const int s = __shfl_sync(0xFFFFFFFFu, scale[i * R / 32], from_lane);
-        const int row = __shfl_sync(0xFFFFFFFFu, dst[i * R / 32], from_lane);
-        const int d = max(s - ask[i / PER16], -24);   // at most 17; below -24 nothing is left of any code
-        if (__any_sync(0xFFFFFFFFu, row >= 0 && d != 0)) {
-            const int d1 = min(d, 15);
-            scale_by(x[i], d1);
-            if (__any_sync(0xFFFFFFFFu, d > 15)) scale_by(x[i], min(d, 30) - d1);   // (a power that f16 does not hold; exact in two steps: 1 where it is none)
+            for (int k = 0; k < K; ++k) ask[2 * k] = ask[2 * k + 1] = max(ask[2 * k], ask[2 * k + 1]);
+            if (K == 2 && block == 64) ask[0] = ask[1] = ask[2 * K - 2] = ask[2 * K - 1] = max(ask[0], ask[2 * K - 1]);
         }
-        if (row >= 0) *reinterpret_cast<uint4*>(codes + (int64_t)row * DIM) = x[i];
+#pragma unroll
+        for (int q = 0; q < 2 * K; ++q) ask[q] = min(max(ask[q], 0), 254);
+#pragma unroll
+        for (int k = 0; k < K; ++k)   // the block's scale: by the block's first place
+            if (dst[k] >= 0 && ((base + 32 * k + lane) & (block - 1)) == 0)
+                P.scales[which][((int64_t)(dst[k] >> P.page_shift) << per_page) + ((dst[k] & page_mask) >> P.block_shift)] =
+                    (uint8_t)(lane < 16 ? ask[2 * k] : ask[2 * k + 1]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int from_lane = (i * R + grp) & 31;
+            const int s = __shfl_sync(0xFFFFFFFFu, scale[which][i * R / 32], from_lane);
+            const int row = __shfl_sync(0xFFFFFFFFu, dst[i * R / 32], from_lane);
+            const int d = max(s - ask[i / PER16], -24);   // at most 17; below -24 nothing is left of any code
+            if (__any_sync(0xFFFFFFFFu, row >= 0 && d != 0)) {
+                const int d1 = min(d, 15);
+                scale_by(x[which][i], d1);
+                if (__any_sync(0xFFFFFFFFu, d > 15)) scale_by(x[which][i], min(d, 30) - d1);   // (a power that f16 does not hold; exact in two steps: 1 where it is none)
+            }
+            if (row >= 0) *reinterpret_cast<uint4*>(P.codes[which] + (int64_t)row * DIM + 16 * sub) = x[which][i];
+        }
     }
 }
 
@@ -546,7 +546,7 @@ cudaError_t launch_compact(CompactParams P, cudaStream_t stream)
     // 32 places a warp, 64 where a block has as many: half the registers let more warps hide the chain of loads in front of the rows
     const bool wide = P.block_shift == 6;
     P.units = compact_units(P.max_kept, wide ? 64 : 32);
-    const int64_t units = P.units * P.seqs * P.heads * 2, ctas = ceil_div(units, kMoveWarps);
+    const int64_t units = P.units * P.seqs * P.heads, ctas = ceil_div(units, kMoveWarps);
     const bool in_place = P.out_table == P.table;
     if (in_place) {
         const cudaError_t e = cudaMemsetAsync(P.work, 0, (size_t)(units + 1) * 4, stream);
