@@ -47,7 +47,6 @@ constexpr int kWarps = 4;
 // CTAs an SM that the register allocation makes room for
 __host__ __device__ constexpr int decode_ctas(int dim, int nq) { return nq == 1 ? (dim == 128 ? 3 : 4) : dim == 128 || nq == 4 ? 2 : 3; }
 constexpr int kTile = 32;      // tokens of a tile
-constexpr int kTreeRows = 64, kTreeRounds = 1, kTreeLeast = 4;
 constexpr int kPromptRows = 64;   // more query rows a sequence and key head than this: the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -900,7 +899,7 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
 {
     AttnPlan a{};
     const int64_t rows = max_q * (q_heads / kv_heads);
-    a.prompt = rows > (tree ? kTreeRows : kPromptRows);
+    a.prompt = rows > kPromptRows;
     // a warp holds the output of up to 16 rows of 128 or 32 of 64; more rows are shared out among the CTA's warps
     a.row_eights = rows <= 8 ? 1 : rows <= 16 || dim == 128 || !wide ? 2 : 4;
     a.row_warps = dim == 64 && a.row_eights == 2 ? 1 : (int)(rows <= 8 * a.row_eights ? 1 : rows <= 16 * a.row_eights ? 2 : 4);
@@ -913,17 +912,28 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
     // CTA's start and the join are worth it (64 sequences of up to 2000 keys: 37 us, five steps 40), or five where half of the places
     // would stay empty (16 sequences: eight 20 us, five 16, 14 with the join as it is now), less only where most SMs would be idle.
     const int64_t resident = (int64_t)kSMs * (a.prompt ? 1 : decode_ctas(dim, a.row_eights));
-    int64_t splits = seqs > 1 && (!a.prompt || tree) ? ceil_div((a.prompt ? kTreeRounds : 4) * resident, units) : resident / units;
+    int64_t splits = seqs > 1 && !a.prompt ? ceil_div(4 * resident, units) : resident / units;
     // keys that the rows of a tile can see between them
     const int64_t tokens = ceil_div(tile_rows, q_heads / kv_heads) + 1;
     const int64_t reach = window + tokens + tile + ceil_div(sinks, tile) * tile;
     const int64_t span = window > 0 && reach < max_len ? reach : max_len;
-    const int64_t least = a.prompt && tree ? kTreeLeast : !a.prompt && 2 * units < resident ? 5 : 8;
+    const int64_t least = !a.prompt && 2 * units < resident ? 5 : 8;
     auto most = [&](int64_t keys) {
         const int64_t by_least = ceil_div(keys, least * step), idle = ceil_div(kSMs / 2, units), by_one = ceil_div(keys, step);
         return by_least >= idle ? by_least : by_one < idle ? by_one : idle;
     };
     const int64_t bound = splits < most(max_len) ? splits : most(max_len);   // for the workspace: whatever the window
+    if (a.prompt && tree && units <= resident) {
+        // as many CTAs as run at a time; the longest sequences may have more chunks than their share by number (twice as many and one more at most, which
+        // bounds the workspace)
+        const int64_t tiles = ceil_div(max_len, tile), room = 2 * (resident / units) + 1;
+        a.splits = tiles < 8 || room < 2 ? 1 : ceil_div(tiles, 4) < room ? ceil_div(tiles, 4) : room;
+        a.by_length = a.splits > 1;
+        a.workspace = a.by_length ? (size_t)n * q_heads * a.splits * (dim + 1) * 4 : 0;
+        a.chunk = tiles * tile > 0 ? tiles * tile : tile;
+        a.ctas = a.whole_units = a.by_length ? resident : units;
+        return a;
+    }
     a.workspace = bound > 1 ? (size_t)n * q_heads * bound * (dim + 1) * 4 : 0;
     if (splits > most(span)) splits = most(span);
     if (splits < 1) splits = 1;
@@ -979,6 +989,7 @@ cudaError_t launch_attention(AttnParams P, const AttnPlan& a, void* workspace, c
     P.row_tiles = (int)a.row_tiles;
     P.whole_units = (uint32_t)a.whole_units;
     P.cluster = a.cluster;
+    P.by_length = a.by_length;
     P.part_out = static_cast<float*>(workspace);
     P.part_lse = a.splits > 1 ? P.part_out + P.n * P.q_heads * a.splits * P.dim : nullptr;
     AttnMaps M;

@@ -139,12 +139,14 @@ struct AttnParams {
     int splits, row_tiles;
     int cluster;                // the CTAs of a row tile's chunks are a cluster
     uint32_t whole_units;       // prompts: CTAs of two row tiles; behind them a unit is two CTAs of one
+    int by_length;              // trees: the CTAs share out the keys by the lengths as they are, in up to `splits` chunks
 };
 struct AttnPlan {
     int64_t chunk, splits, row_tiles, whole_units, ctas;
     int row_warps, row_eights;  // warps that share out the query rows of a CTA; groups of eight rows that a warp holds
     bool prompt;                // many query rows: the tcgen05 kernel
     bool cluster;               // few chunks, joined by the CTAs as a cluster
+    bool by_length;
     size_t workspace;
 };
 AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree);

@@ -54,6 +54,7 @@ constexpr int kThreads = 512;
 constexpr int kKeyStages = 3, kValStages = 2, kHalfStages = 2, kScaleSlots = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRun = 16;          // tokens that share a scale at the finest
+constexpr int kLeastTiles = 4;    // of a chunk that is shared out by length
 // Weights: 2^kTop at the reference; the reference is moved when a tile's largest is more than kUp above or kDown below it, but to
 // no more than kDepth below the largest so far (the output's sums must not overflow)
 constexpr float kTop = 1.0f, kUp = 14.0f, kDown = 16.0f, kDepth = 40.0f;
@@ -85,6 +86,69 @@ struct alignas(16) TileScales {
     float c0;
 };
 
+// Trees: which rows and keys a CTA takes, by the lengths as they are.  A grid of no more CTAs than run at a time shares out all sequences' key
+// tiles in chunks of the same size, the smallest that gives no more chunks than CTAs (64 drafts of 32 + 8 heads a sequence, one of 8192 keys beside
+// seven of 300: the same number of chunks for each 103 us, by length 61; beside seven of 4000: 111 and 79).  By one warp.
+struct Share {
+    int seq, h, block, split, splits, chunk;   // seq -1: nothing
+};
+__device__ __forceinline__ Share share_out(const AttnParams& P)
+{
+    const int lane = threadIdx.x & 31, slots = (int)gridDim.x;
+    auto work = [&](int s, int& tiles) -> int {   // key tiles of a sequence; returns its blocks of rows over all heads
+        tiles = 0;
+        if (s >= P.seqs) return 0;
+        const AttnSequence S = attn_sequence(P, s);
+        if (S.nq == 0) return 0;
+        tiles = max(1, (S.len + kTile - 1) / kTile);
+        return (S.nq * P.group + 2 * kTile - 1) / (2 * kTile) * P.kv_heads;
+    };
+    int most = 1;
+    for (int s0 = 0; s0 < P.seqs; s0 += 32) {
+        int tiles;
+        (void)work(s0 + lane, tiles);
+        most = max(most, __reduce_max_sync(0xFFFFFFFFu, tiles));
+    }
+    // the smallest chunk, at least kLeastTiles: [lo, hi]
+    int lo = max(kLeastTiles, (most + P.splits - 1) / P.splits), hi = max(lo, most);
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        int chunks = 0;
+        for (int s0 = 0; s0 < P.seqs; s0 += 32) {
+            int tiles;
+            const int blocks = work(s0 + lane, tiles);
+            chunks += __reduce_add_sync(0xFFFFFFFFu, blocks * ((tiles + mid - 1) / mid));
+        }
+        if (chunks <= slots) hi = mid;
+        else lo = mid + 1;
+    }
+    Share w = {-1, 0, 0, 0, 1, lo * kTile};
+    int before = 0;
+    for (int s0 = 0; s0 < P.seqs && w.seq < 0; s0 += 32) {
+        int tiles;
+        const int blocks = work(s0 + lane, tiles), splits = (tiles + lo - 1) / lo;
+        int upto = blocks * splits;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const int at = (int)blockIdx.x - before;
+        const unsigned here = __ballot_sync(0xFFFFFFFFu, at < upto);
+        if (here) {
+            const int l = __ffs(here) - 1;
+            w.seq = s0 + l;
+            w.splits = __shfl_sync(0xFFFFFFFFu, splits, l);
+            const int r = at - __shfl_sync(0xFFFFFFFFu, upto - blocks * splits, l), unit = r / w.splits;
+            w.split = r - unit * w.splits;
+            w.h = unit % P.kv_heads;
+            w.block = unit / P.kv_heads;
+        }
+        before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    return w;
+}
+
 template <int DIM, int MASK>
 __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnParams P, const __grid_constant__ AttnMaps M)
 {
@@ -106,12 +170,29 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
         half = (int)((b - P.whole_units) & 1u);
         b = P.whole_units + (b - P.whole_units) / 2;
     }
-    const int split = (int)(b % (uint32_t)P.splits);
+    int split = (int)(b % (uint32_t)P.splits), last_split = P.splits - 1;
     b /= (uint32_t)P.splits;
-    const int seq = (int)(b % (uint32_t)P.seqs);
+    int seq = (int)(b % (uint32_t)P.seqs);
     b /= (uint32_t)P.seqs;
-    const int h = (int)(b % (uint32_t)P.kv_heads);
-    const int block = P.row_tiles - 1 - (int)(b / (uint32_t)P.kv_heads);   // the rows that see most keys first
+    int h = (int)(b % (uint32_t)P.kv_heads);
+    int block = P.row_tiles - 1 - (int)(b / (uint32_t)P.kv_heads);   // the rows that see most keys first
+    int64_t chunk = P.chunk;
+    if (MASK == kTree && P.by_length) {
+        __shared__ Share share;
+        if (warp == 0) {
+            const Share w = share_out(P);
+            if (lane == 0) share = w;
+        }
+        __syncthreads();
+        if (share.seq < 0) return;
+        seq = share.seq;
+        h = share.h;
+        block = share.block;
+        split = share.split;
+        last_split = share.splits - 1;
+        chunk = share.chunk;
+        half = -1;
+    }
 
     const AttnSequence S = attn_sequence(P, seq);
     const int q0 = S.q0, len = S.len, shift = S.shift, nq = S.nq;
@@ -125,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
     const KeyList list = key_list<kTile>(sinks, lo);
     // this chunk's part of the keys, or of their list: [k0, k1); no key from `end` on
     const int from = MASK == kSinks ? 0 : lo, to = MASK == kSinks ? list.head + max(0, hi - lo) : hi;
-    const int k0 = (int)min((int64_t)to, from + (int64_t)split * P.chunk), k1 = (int)min((int64_t)to, (int64_t)k0 + P.chunk);
+    const int k0 = (int)min((int64_t)to, from + (int64_t)split * chunk), k1 = (int)min((int64_t)to, (int64_t)k0 + chunk);
     const int end = MASK == kSinks ? hi : k1;
     auto tile_at = [&](int j) { return MASK == kSinks ? list.at(k0 + j * kTile) : k0 + j * kTile; };
     const int tiles = (k1 - k0 + kTile - 1) / kTile;
@@ -673,8 +754,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
             }
         }
         if (row_live) {
-            if (P.splits > 1) P.part_lse[out_row * P.splits + split] = lse2;
-            else if (P.lse != nullptr) P.lse[out_row] = lse2 * kLn2;
+            if (P.splits > 1) {
+                P.part_lse[out_row * P.splits + split] = lse2;
+                if (MASK == kTree && split == last_split)   // chunks that the workspace has room for and this sequence has not
+                    for (int i = split + 1; i < P.splits; ++i) P.part_lse[out_row * P.splits + i] = kNone;
+            }
+            if (P.splits == 1 && P.lse != nullptr) P.lse[out_row] = lse2 * kLn2;
         }
         tc_before();
     } else {

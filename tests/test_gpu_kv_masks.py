@@ -176,14 +176,46 @@ def test_tree_more_drafts_than_the_cache_has(mx, qh):  # noqa: F811
 
 
 def test_a_chain_has_the_causal_masks_bits(mx):  # noqa: F811
-    for qh, nq in ((4, 6), (8, 40)):
-        cu, table, cache, q, buf, out, lse, max_q, max_len, ws = job(mx, qh, 1, 128, 64, 16, [nq], [900], 1)
-        args = (q, dev(cu), dev([900]), dev(table), *cache.parts)
+    # (few rows; many rows in calls whose keys neither of the two entry points shares out)
+    for qh, h, nq, length in ((4, 1, 6, 900), (320, 40, 40, 800)):
+        cu, table, cache, q, buf, out, lse, max_q, max_len, ws = job(mx, qh, h, 128, 64, 16, [nq], [length], 1)
+        args = (q, dev(cu), dev([length]), dev(table), *cache.parts)
         other = torch.empty_like(out)
         mask = kr.words([(2 << i) - 1 for i in range(nq)] + [0] * 3, 2).cuda()
         mx.mxkv_attention_tree(*args, out, max_q, max_len, 0.1, mask, lse=lse, workspace=ws)
         mx.mxkv_attention(*args, other, max_q, max_len, 0.1, workspace=ws)
         assert torch.equal(out[:nq], other[:nq])
+
+
+@pytest.mark.parametrize("qh,h,dim,nq,lens", [
+    (16, 1, 64, [9] * 40, [1 + 37 * i for i in range(40)]), (8, 2, 128, [0, 40, 3, 0, 64], [5, 3000, 700, 9000, 64]),
+    (20, 4, 64, [20, 70], [20, 5000]), (32, 2, 128, [5] * 70, [500] * 70), (5, 1, 128, [50, 20], [0, 4000]),
+])
+@pytest.mark.parametrize("max_q,max_len", [(None, None), (33, 900)])
+def test_trees_shared_out_by_length(mx, qh, h, dim, nq, lens, max_q, max_len):  # noqa: F811
+    """Many sequences of very different lengths, sequences without drafts, drafts without keys, bounds below the lists: rows past max_q_len are
+    undefined, all others as ever."""
+    pick = random.Random(len(nq))
+    rows = [random_tree(n, pick) for n in nq]
+    cu, table, cache, q, buf, out, lse, _, _, ws = job(mx, qh, h, dim, 32, 16, nq, lens, 3)
+    scale, count = dim ** -0.5, -(-max(nq) // 32)
+    max_q = max(nq) if max_q is None else max_q
+    max_len = max(lens) if max_len is None else min(max_len, max(lens))
+    mask = kr.words([r for sequence in rows for r in sequence] + [0] * 3, count).cuda()
+    masks = [kr.tree_mask(sequence, length, device="cuda") & (torch.arange(length, device="cuda") < max_len) for sequence, length in zip(rows, lens)]
+    need = mx.mxkv_attention_workspace_bytes(q.shape[0], len(lens), max_q, max_len, qh, h, dim)
+    ws = torch.full((max(16, need),), 0xFF, dtype=torch.uint8, device="cuda")
+    mx.mxkv_attention_tree(q, dev(cu), dev(lens), dev(table), *cache.parts, out, max_q, max_len, scale, mask, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    want, want_lse, mag, big = kr.attention(q[:cu[-1]], cu, lens, table, *cache.parts, scale, masks)
+    done = torch.cat([torch.arange(n) < max_q for n in nq]).cuda()
+    got, want, mag = out[:cu[-1]][done].double(), want[done], mag[done]
+    assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * mag + 1e-30).all())
+    e, live = (lse[:cu[-1]][done].double() - want_lse[done]), want_lse[done] > -math.inf
+    assert bool((lse[:cu[-1]][done][~live] == -math.inf).all())
+    assert bool((e[live].abs() <= (16 * 2.0 ** -23 * big[done] + 2.0 ** -19 + 5 * 2.0 ** -23 * want_lse[done].abs())[live]).all())
+    assert bool((lse[cu[-1]:] == 7).all()) and bool((buf[cu[-1]:] == 7).all()) and bool((buf[:, -1] == 7).all())
+    assert mx.device_timeouts() == 0 and cache.guards_intact()
 
 
 def test_masks_on_streams_and_in_graphs(mx):  # noqa: F811
