@@ -25,7 +25,7 @@ __device__ unsigned int g_keep_timeouts = 0;
 __device__ unsigned int g_keep_bad = 0;   // entries, pages or lengths out of range
 
 constexpr int kBins = 2048;
-constexpr int kHeld = 16;   // tokens of a thread that are held in registers; with more all are read again
+constexpr int kHeld = 4;   // runs of four tokens of a thread that are held in registers; with more all are read again
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cluster_sync()
@@ -79,30 +79,48 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
         for (int64_t i = rank * WARPS * 32 + threadIdx.x; i < P.keep; i += cluster * WARPS * 32) out[i] = i < len ? (int)i : -1;
         return;
     }
-    // this warp's tokens: whole groups of 32, kHeld of them at a time in registers
-    const int groups = (len + 31) >> 5, per_warp = (groups + cluster * WARPS - 1) / (cluster * WARPS);
+    // this warp's tokens: whole groups of 128, four a lane, kHeld groups of them at a time in registers
+    const int groups = (len + 127) >> 7, per_warp = (groups + cluster * WARPS - 1) / (cluster * WARPS);
     const int g0 = (int)min((int64_t)groups, (int64_t)(rank * WARPS + warp) * per_warp), g1 = min(groups, g0 + per_warp);
     const bool once = per_warp <= kHeld;   // else the weights are read again for each step
     const int tail = len - P.recent;
     const int32_t* const table = P.page_table + (int64_t)seq * P.max_pages;
     const float* const weights = P.weights + ((int64_t)h << P.page_shift);
     const int page_mask = (1 << P.page_shift) - 1;
+    const bool wide = (reinterpret_cast<uintptr_t>(P.weights) & 15u) == 0u;   // (weights are promised to be 4-byte aligned)
     bool bad = false;
-    uint32_t k[kHeld];   // of token (g + x) * 32 + lane; 0 where there is none, kSure for the first and the last ones
-    auto fetch = [&](int g) {   // all pages, then all weights on their way at once
+    uint32_t k[kHeld][4];   // of tokens 128 (g + x) + 4 lane + j; 0 where there is none, kSure for the first and the last ones
+    auto fetch = [&](int g) {   // all pages, then all weights on their way at once.  Four tokens lie in one page.
         int32_t pg[kHeld];
+        float4 w[kHeld];
 #pragma unroll
         for (int x = 0; x < kHeld; ++x) {
-            const int t = (g + x) * 32 + lane;
-            pg[x] = g + x < g1 && t < len ? __ldg(table + (t >> P.page_shift)) : 0;
+            const int t = (g + x) * 128 + lane * 4;
+            pg[x] = g + x < g1 && t < len ? __ldg(table + (t >> P.page_shift)) : -1;
         }
 #pragma unroll
         for (int x = 0; x < kHeld; ++x) {
-            const int t = (g + x) * 32 + lane;
+            const int t = (g + x) * 128 + lane * 4;
+            w[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if ((uint32_t)pg[x] < (uint32_t)P.num_pages) {
+                const float* const at = weights + (((int64_t)pg[x] * P.heads) << P.page_shift) + (t & page_mask);
+                w[x] = wide ? __ldg(reinterpret_cast<const float4*>(at)) : make_float4(__ldg(at), __ldg(at + 1), __ldg(at + 2), __ldg(at + 3));
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kHeld; ++x) {
+            const int t = (g + x) * 128 + lane * 4;
             const bool real = g + x < g1 && t < len, fits = (uint32_t)pg[x] < (uint32_t)P.num_pages;
             bad |= real && !fits;
-            const float w = real && fits ? __ldg(weights + (((int64_t)pg[x] * P.heads) << P.page_shift) + (t & page_mask)) : 0.0f;
-            k[x] = !real ? 0u : t < P.sinks || t >= tail ? kSure : fits ? ordered(w) : 1u;
+            const float v[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[x][j] = fits ? ordered(v[j]) : 1u;
+            if (!real || t < P.sinks || t + 4 > tail) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!real || t + j >= len) k[x][j] = 0u;
+                    else if (t + j < P.sinks || t + j >= tail) k[x][j] = kSure;
+            }
         }
     };
     for (int i = threadIdx.x; i < 3 * kBins; i += WARPS * 32) (&hist[0][0])[i] = 0u;
@@ -117,8 +135,10 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
             if (!once) fetch(g);
 #pragma unroll
             for (int x = 0; x < kHeld; ++x)
-                if (k[x] - 1u < kSure - 1u && (pass == 0 || k[x] >> (kUp[pass] & 31) == prefix))
-                    atomicAdd(&hist[pass][(k[x] >> kShift[pass]) & (pass == 2 ? 1023u : 2047u)], 1u);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k[x][j] - 1u < kSure - 1u && (pass == 0 || k[x][j] >> (kUp[pass] & 31) == prefix))
+                        atomicAdd(&hist[pass][(k[x][j] >> kShift[pass]) & (pass == 2 ? 1023u : 2047u)], 1u);
         }
         if (cluster > 1) cluster_sync();
         else __syncthreads();
@@ -172,10 +192,12 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
     for (int g = g0; g < g1; g += kHeld) {
         if (!once) fetch(g);
 #pragma unroll
-        for (int x = 0; x < kHeld; ++x) {
-            n_above += k[x] > least;
-            n_equal += k[x] == least;
-        }
+        for (int x = 0; x < kHeld; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                n_above += k[x][j] > least;
+                n_equal += k[x][j] == least;
+            }
     }
     n_above = warp_sum_u32(n_above);
     n_equal = warp_sum_u32(n_equal);
@@ -198,18 +220,32 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
         a_before += warp_sum_u32(other_a);
         e_before += warp_sum_u32(other_e);
     }
-    const uint32_t below = (1u << lane) - 1u;
     for (int g = g0; g < g1; g += kHeld) {
         if (!once) fetch(g);
 #pragma unroll
         for (int x = 0; x < kHeld; ++x) {
-            const uint32_t ua = __ballot_sync(0xFFFFFFFFu, k[x] > least), ue = __ballot_sync(0xFFFFFFFFu, k[x] == least);
-            const uint32_t e_mine = e_before + __popc(ue & below);   // equal ones in front of this token
-            const bool chosen = k[x] > least || (k[x] == least && e_mine < need);
-            const uint32_t at = a_before + __popc(ua & below) + min(e_mine, need);
-            if (chosen && at < (uint32_t)P.keep) out[at] = (g + x) * 32 + lane;
-            a_before += __popc(ua);
-            e_before += __popc(ue);
+            // above in the low half, equal in the high half, of this lane's four and of the lanes before it
+            uint32_t mine = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += (k[x][j] > least ? 1u : 0u) + (k[x][j] == least ? 0x10000u : 0u);
+            uint32_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const uint32_t all = __shfl_sync(0xFFFFFFFFu, upto, 31), front = upto - mine;
+            uint32_t a_front = a_before + (front & 0xFFFFu), e_front = e_before + (front >> 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool is_above = k[x][j] > least, is_equal = k[x][j] == least;
+                const uint32_t at = a_front + min(e_front, need);
+                if ((is_above || (is_equal && e_front < need)) && at < (uint32_t)P.keep) out[at] = (g + x) * 128 + lane * 4 + j;
+                a_front += is_above;
+                e_front += is_equal;
+            }
+            a_before += all & 0xFFFFu;
+            e_before += all >> 16;
         }
     }
     if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_keep_bad, 1u);
@@ -534,7 +570,7 @@ cudaError_t launch_select(const SelectParams& P, cudaStream_t stream)
     const int64_t lists = (int64_t)P.seqs * P.heads;
     int cluster = 1;
     while (cluster < 8 && lists * cluster * 2 <= 148 && P.max_len > 1024 * cluster) cluster *= 2;
-    if (P.max_len > (int64_t)cluster * 16 * 32 * kHeld) return launch(select_kernel<32>, lists * cluster, cluster, 1024, 0, stream, P, cluster);
+    if (P.max_len > (int64_t)cluster * 16 * 128 * kHeld) return launch(select_kernel<32>, lists * cluster, cluster, 1024, 0, stream, P, cluster);
     return launch(select_kernel<16>, lists * cluster, cluster, 512, 0, stream, P, cluster);
 }
 
