@@ -291,9 +291,6 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
         const int64_t place = (int64_t)key - S.shift;   // of the key, among the call's tokens
         int see0 = P.causal && real ? (int)max(place, (int64_t)0) : 0, see1 = S.nq - T;
         if (P.window > 0 && key >= P.sinks && real) see1 = (int)max((int64_t)-1, min((int64_t)see1, place + P.window - T));
-        // ... and those in front of which no column sees any of them, and behind which none does: before none0, from none1 on
-        const int none0 = __reduce_min_sync(0xFFFFFFFFu, P.causal && real ? (int)max(place, (int64_t)0) : 0);
-        const int none1 = __reduce_max_sync(0xFFFFFFFFu, P.window > 0 && key >= P.sinks ? (int)max((int64_t)0, min((int64_t)S.nq, place + P.window)) : S.nq);
         see0 = __reduce_max_sync(0xFFFFFFFFu, see0);
         see1 = P.group % GB == 0 ? __reduce_min_sync(0xFFFFFFFFu, see1) : -1;
         bool ok = true;
@@ -305,39 +302,25 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             tc_after();
             const uint32_t at = d_col + buf * kTile + col0 + lanes, free_bar = d_empty + 8 * buf;
             buf = buf > 0 ? buf - 1 : 2;   // two on, of three
-            uint32_t x[2][32];
-            tm_request(x[0], at);
-            tm_request(x[1], at + 32);
             const Columns& C = columns[slot];
             const At t = tile_at(i);
-            const bool plain = t.token >= see0 && t.token <= see1 && C.special == 0, none = t.token + T <= none0 || t.token >= none1;
-            uint32_t see[2] = {0u, 0u};   // columns of this half whose rows see this key
-            if (!plain && !none) {
-                const int valid = min(T, S.nq - t.token) * min(GB, P.group - t.part * GB);
-                const int64_t ahead = place - t.token;
-                const int from = P.causal ? (int)max((int64_t)0, min((int64_t)T, ahead)) : 0;
-                const int to = P.window == 0 || key < P.sinks ? T : (int)max((int64_t)0, min((int64_t)T, ahead + P.window));
-                const int lo = from * GB - col0, hi = real ? min(to * GB, valid) - col0 : 0;
+            const float* const cl = C.lse + col0;
+            float2 part[2] = {f2(0.0f), f2(0.0f)};
+            if (t.token >= see0 && t.token <= see1 && C.special == 0) {
+                uint32_t x[2][32];
+                tm_request(x[0], at);
+                tm_request(x[1], at + 32);
+                tm_arrived(x[0]);
+                tm_arrived(x[1]);
+                tc_before();   // the buffer is free again before any arithmetic
+                __syncwarp();
+                if (lane == 0) mbar_arrive(free_bar);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int a = min(max(lo - 32 * c, 0), 32), b = min(max(hi - 32 * c, 0), 32);
-                    see[c] = (b == 32 ? 0xFFFFFFFFu : (1u << b) - 1u) & (a == 32 ? 0u : 0xFFFFFFFFu << a);
-                }
-            }
-            float2 part[2] = {f2(0.0f), f2(0.0f)};
-            tm_arrived(x[0]);
-            tm_arrived(x[1]);
-            tc_before();   // the buffer is free again before any arithmetic
-            __syncwarp();
-            if (lane == 0) mbar_arrive(free_bar);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const uint32_t* const y = x[c];
-                const float* const cl = C.lse + col0 + 32 * c;
-                if (plain) {
+                    const uint32_t* const y = x[c];
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
-                        const float4 n = *reinterpret_cast<const float4*>(cl + 2 * e);
+                        const float4 n = *reinterpret_cast<const float4*>(cl + 32 * c + 2 * e);
                         const float2 u = __ffma2_rn(make_float2(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), f, make_float2(n.x, n.y));
                         const float2 v = __ffma2_rn(make_float2(__uint_as_float(y[2 * e + 2]), __uint_as_float(y[2 * e + 3])), f, make_float2(n.z, n.w));
                         // spread over the 16 pairs, so that both kinds run side by side
@@ -346,13 +329,30 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                         part[0] = __fadd2_rn(part[0], mu ? ex2_fma(u) : make_float2(ex2(u.x), ex2(u.y)));
                         part[1] = __fadd2_rn(part[1], mv ? ex2_fma(v) : make_float2(ex2(v.x), ex2(v.y)));
                     }
-                } else if (__any_sync(0xFFFFFFFFu, see[c] != 0u)) {
+                }
+            } else {
+                // Columns [lo, hi) of these see this key.  In a short loop with loads of its own: with the registers of the common path that one carried
+                // 32 moves for each 32 columns along.
+                const int valid = min(T, S.nq - t.token) * min(GB, P.group - t.part * GB);
+                const int64_t ahead = place - t.token;
+                const int from = P.causal ? (int)max((int64_t)0, min((int64_t)T, ahead)) : 0;
+                const int to = P.window == 0 || key < P.sinks ? T : (int)max((int64_t)0, min((int64_t)T, ahead + P.window));
+                const int lo = max(from * GB - col0, 0), hi = min((real ? min(to * GB, valid) : 0) - col0, kHalf);
+                if (__any_sync(0xFFFFFFFFu, lo < hi)) {
+#pragma unroll 1
+                    for (int c = 0; c < kHalf; c += 16) {
+                        uint32_t z[16];
+                        tm_load16(z, at + c);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float p = ex2(fmaf(__uint_as_float(y[e]), scale, cl[e]));
-                        part[e & 1].x += see[c] >> e & 1u ? p : 0.0f;
+                        for (int e = 0; e < 16; ++e) {
+                            const float p = ex2(fmaf(__uint_as_float(z[e]), scale, cl[c + e]));
+                            part[e & 1].x += c + e >= lo && c + e < hi ? p : 0.0f;
+                        }
                     }
                 }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(free_bar);
             }
             sum[0] = __fadd2_rn(sum[0], part[0]);
             sum[1] = __fadd2_rn(sum[1], part[1]);
