@@ -307,17 +307,16 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             const float* const cl = C.lse + col0;
             float2 part[2] = {f2(0.0f), f2(0.0f)};
             if (t.token >= see0 && t.token <= see1 && C.special == 0) {
-                uint32_t x[2][32];
-                tm_request(x[0], at);
-                tm_request(x[1], at + 32);
-                tm_arrived(x[0]);
-                tm_arrived(x[1]);
-                tc_before();   // the buffer is free again before any arithmetic
-                __syncwarp();
-                if (lane == 0) mbar_arrive(free_bar);
+                // 32 columns at a time: with 64 in registers the polynomial's constants found no room (263 us, so 259)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const uint32_t* const y = x[c];
+                    uint32_t y[32];
+                    tm_load(y, at + 32 * c);
+                    if (c == 1) {   // the buffer is free again before the rest of the arithmetic
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(free_bar);
+                    }
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
                         const float4 n = *reinterpret_cast<const float4*>(cl + 32 * c + 2 * e);
