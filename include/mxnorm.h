@@ -441,7 +441,8 @@ mxn_status mxkv_attention_tree(const void* q_bf16, int64_t q_stride, int64_t n_t
  *   be weights itself, or NULL (nothing).  A call's own new tokens have nothing from earlier: their places in `earlier` are not read.
  *   Every token of every sequence up to max_kv_len is written, a sequence without new tokens or keys that no row sees included (earlier + 0);
  *   places of no token are left as they are.  Rows past max_q_len, and rows whose lse is -infinity, give nothing.  A NaN in a row, its lse or a key that
- *   it sees makes the sums concerned NaN.  Tokens whose page is out of range are left out.  Sums are binary32 in a fixed order. */
+ *   it sees makes the sums concerned NaN.  Tokens whose page is out of range are left out.  Sums are binary32 in a fixed order.
+ *   A page in which sums are written belongs to one sequence of the call (of a page shared by several the sums are one of theirs). */
 mxn_status mxkv_attention_weights(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
                                   const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
                                   const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
@@ -465,6 +466,7 @@ mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const
  *   memory, 16-byte aligned, mxkv_compact_workspace_bytes(...) bytes, contents irrelevant before and after; calls that may overlap need
  *   workspaces of their own).  Otherwise tokens are written to the pages of out_page_table int32 [n_seqs, out_max_pages], which must not be
  *   pages that the call reads other than for tokens in front of `first`; lists may be in any order.
+ *   The blocks written belong to one sequence only, as in the append.
  *   Each block that is written gets the scale that its largest value asks for (the append's rule; its tokens in front of `first` included),
  *   and its codes are rounded on it: exact unless they become subnormal.  A block whose tokens all stay where they are is
  *   left as it is.  weights fp32 [num_pages, kv_heads, page_size] (or NULL) move along.  Tokens behind new_lens are left as they are, but for their block's scale.

@@ -7,9 +7,14 @@
 //
 // Few rows (up to kRows a sequence and key head): bound by HBM, dim bytes of codes, 4 (and 4 earlier) of sums a token and head.  A warp
 // takes tiles of 32 tokens.  The order of the dimensions within a product is free: a thread reads one run of dim / 4 bytes of each of
-// its four tokens straight into registers, in which the codes become f16 operands (exact), and asks for the next tile before it works on
-// the one at hand.  q is scaled by a power of two that brings its row's largest to [2^14, 2^15): f16 holds a bf16 value exactly but for
-// elements below 2^-28 of that.
+// its four tokens straight into registers, in which the codes become f16 operands (exact), and asks for the next tile's over them once the
+// products have read them.  q is scaled by a power of two that brings its row's largest to [2^14, 2^15): f16 holds a bf16 value exactly but
+// for elements below 2^-28 of that.
+//
+// Measured, 32 query and 8 key heads of 128, 64 sequences of up to 8192 keys, one token each, added to earlier sums: 70 us, 5.1 TB/s, 0.79
+// of a copy's rate.  Two sets of registers and four CTAs an SM took 94 us, one set and five 74, with fewer instructions beside the products 70 (some 490 a
+// tile now, of which 145 are products, conversions and exponentials: half of the issue slots).  A ring of tiles filled by the tensor copy
+// engine took 73 with two stages a warp and 80 with three (fewer warps fit beside more shared memory), six CTAs an SM 78 (spills).
 #include <cuda_fp16.h>
 
 #include "mxn_attn.cuh"
@@ -75,32 +80,32 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
 
     // ---- a tile on its way: codes of tokens g, 8 + g, 16 + g, 24 + g, dimensions c * DIM/4 on; what its sums need ----
     uint4 w[4][DIM / 64];
-    uint32_t scale[2];   // of the two runs of 16 tokens
+    uint32_t scale;      // of this half warp's run of 16 tokens
     int64_t at;          // of the sum that this thread writes, -1: of none
     float earlier;
     bool bad = false;
-    const int out_token = 16 * (c >> 1) + 8 * (c & 1) + g;   // the token of a tile whose sum this thread writes
+    const int page_mask = P.page - 1, out_token = 16 * (c >> 1) + 8 * (c & 1) + g;   // the token of a tile whose sum this thread writes
+    auto seen = [&](int t0) { return (t0 < hi && t0 + kTile > lo) || t0 < sinks; };
     auto load = [&](int i, int pg) {   // by a whole warp; pg = page_at(i)
-        const int t0 = tile_at(i);
-        const bool seen = i < mine && ((t0 < hi && t0 + kTile > lo) || t0 < sinks);
-        bad |= i < mine && t0 + (lane & 16) < k1 && (uint32_t)pg >= (uint32_t)P.num_pages;
-        if ((uint32_t)pg >= (uint32_t)P.num_pages) pg = -1;
-        at = -1;
+        const int t0 = tile_at(i), run = t0 + (lane & 16);
+        const bool wanted = i < mine && run < k1;
+        bad |= wanted && (uint32_t)pg >= (uint32_t)P.num_pages;
+        const int tile = wanted && (uint32_t)pg < (uint32_t)P.num_pages ? pg * P.kv_heads + h : -1;   // (fewer than 2^31)
+        scale = tile >= 0 ? __ldg(P.k_scales + ((int64_t)tile << per_page) + ((run & page_mask) >> P.block_shift)) : 0u;
+        const int out_tile = __shfl_sync(0xFFFFFFFFu, tile, 8 * (c & 2)), place = t0 + out_token;
+        at = out_tile >= 0 && place < k1 ? ((int64_t)out_tile << P.page_shift) + (place & page_mask) : -1;
+        earlier = at >= 0 && place < old_end ? W.earlier[at] : 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int page = __shfl_sync(0xFFFFFFFFu, pg, 16 * t);
-            const int64_t tile = (int64_t)page * P.kv_heads + h;
-            const int first = (t0 + 16 * t) & (P.page - 1);
-            scale[t] = seen && page >= 0 ? __ldg(P.k_scales + (tile << per_page) + (first >> P.block_shift)) : 0u;
-            if (c >> 1 == t && page >= 0 && t0 + out_token < k1) at = (tile << P.page_shift) + ((t0 + out_token) & (P.page - 1));
+            const int from = __shfl_sync(0xFFFFFFFFu, tile, 16 * t);
+            const uint8_t* const p0 = P.k_codes + (((int64_t)from << P.page_shift) + ((t0 + 16 * t) & page_mask) + g) * DIM + c * (DIM / 4);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int r = 8 * x + g;
                 uint4* const y = w[2 * t + x];
+                const uint8_t* const p = p0 + 8 * x * DIM;
 #pragma unroll
                 for (int e = 0; e < DIM / 64; ++e) y[e] = make_uint4(0u, 0u, 0u, 0u);
-                if (seen && page >= 0 && t0 + 16 * t + r < k1) {
-                    const uint8_t* p = P.k_codes + ((tile << P.page_shift) + first + r) * DIM + c * (DIM / 4);
+                if (from >= 0 && t0 + 16 * t + 8 * x + g < k1 && seen(t0)) {
                     if (DIM == 128 && wide) {
                         uint32_t v[8];
                         ld_v8(p, v);
@@ -113,7 +118,6 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
                 }
             }
         }
-        earlier = at >= 0 && t0 + out_token < old_end ? W.earlier[at] : 0.0f;
     };
     int pg = page_at(0);
     load(0, pg);
@@ -176,8 +180,8 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
 
     for (int i = 0; i < mine; ++i) {
         const int t0 = tile_at(i), pg_next = page_at(i + 2);
-        const bool seen = (t0 < hi && t0 + kTile > lo) || t0 < sinks;
-        const float kf[2] = {e8m0_to_f32(scale[0]), e8m0_to_f32(scale[1])};
+        const bool any = seen(t0);
+        const float kf[2] = {e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, scale, 0)), e8m0_to_f32(__shfl_sync(0xFFFFFFFFu, scale, 16))};
         const int64_t out = at;
         const float before = earlier;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // tokens g, 8 + g, 16 + g, 24 + g; this thread's columns
@@ -198,23 +202,28 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
             }
         };
         auto add = [&](const float2 (&cr)[2], const int2 (&cs)[2]) {
-            const bool all = t0 >= max(cs[0].x, cs[1].x) && t0 + kTile <= min(cs[0].y, cs[1].y);
+            if (__all_sync(0xFFFFFFFFu, t0 >= max(cs[0].x, cs[1].x) && t0 + kTile <= min(cs[0].y, cs[1].y))) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = ex2(fmaf(s[t][e], kf[t] * cr[e & 1].x, cr[e & 1].y));
-                    const int place = t0 + 16 * t + 8 * (e >> 1) + g;
-                    const bool sees = all || (place < cs[e & 1].y && (place >= cs[e & 1].x || place < sinks));
-                    sum[2 * t + (e >> 1)] += sees ? p : 0.0f;
-                }
+                    for (int e = 0; e < 4; ++e) sum[2 * t + (e >> 1)] += ex2(fmaf(s[t][e], kf[t] * cr[e & 1].x, cr[e & 1].y));
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = ex2(fmaf(s[t][e], kf[t] * cr[e & 1].x, cr[e & 1].y));
+                        const int place = t0 + 16 * t + 8 * (e >> 1) + g;
+                        sum[2 * t + (e >> 1)] += place < cs[e & 1].y && (place >= cs[e & 1].x || place < sinks) ? p : 0.0f;
+                    }
+            }
         };
         if constexpr (FEW) {
             scores(nullptr);
             load(i + 1, pg);   // over the codes at hand: more warps hide more than a second set of registers did
-            if (seen) add(col_row, col_see);
+            if (any) add(col_row, col_see);
         } else {
-            if (seen)
+            if (any)
                 for (int y = 0; 8 * y < rows; ++y) {
                     float2 cr[2];
                     int2 cs[2];
@@ -229,12 +238,11 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
             load(i + 1, pg);
         }
         pg = pg_next;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 1);
-            sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 2);
-        }
-        const float all = c < 2 ? (c == 0 ? sum[0] : sum[1]) : (c == 2 ? sum[2] : sum[3]);
+        // over the four threads of a token's columns; thread c keeps sum[c]
+        const bool up = c & 2, odd = c & 1;
+        const float a0 = (up ? sum[2] : sum[0]) + __shfl_xor_sync(0xFFFFFFFFu, up ? sum[0] : sum[2], 2);
+        const float a1 = (up ? sum[3] : sum[1]) + __shfl_xor_sync(0xFFFFFFFFu, up ? sum[1] : sum[3], 2);
+        const float all = (odd ? a1 : a0) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a0 : a1, 1);
         if (out >= 0) W.sums[out] = before + all;
     }
     if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_weights_bad, 1u);
@@ -275,10 +283,10 @@ int64_t plan_weights(WeightsParams& W)
         while (W.ranks < 8 && units * W.ranks < 2 * 148 && tiles >= 8 * W.ranks) W.ranks *= 2;
         return units * W.ranks;
     }
-    // Chunks of 16 tiles (four for each warp), or of one tile for each warp where CTAs would be fewer than three an SM; nothing is joined,
+    // Chunks of 32 tiles (eight for each warp), or of one tile for each warp where CTAs would be fewer than three an SM; nothing is joined,
     // so a chunk costs no more than its start.
     const int64_t units = (int64_t)P.seqs * P.kv_heads, least = kWarps * kTile;
-    P.chunk = 4 * least;
+    P.chunk = 8 * least;
     if (units * ceil_div(P.max_len, P.chunk) < 3 * 148) P.chunk = least;
     P.splits = (int)ceil_div(P.max_len, P.chunk);
     return units * P.splits;
