@@ -472,3 +472,90 @@ def test_compact_many_at_once_in_place(mx):  # noqa: F811
     for _, cache, _, _, _, got in jobs:
         assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other)) and cache.guards_intact()
     assert mx.device_timeouts() == 0
+
+
+def test_weights_without_rows(mx):  # noqa: F811
+    """No new tokens at all, or none in some sequences: earlier sums are passed on; sequences without tokens; nothing else is written."""
+    heads, dim, page = 2, 64, 32
+    lens = [70, 0, 5]
+    table, pool = make_table(lens, 4, page, 2)
+    cache = Cache(pool, heads, page, dim, 16)
+    fill(cache, lens, table, page, 16, 1)
+    before = torch.rand(pool, heads, page, generator=torch.Generator().manual_seed(1)).cuda()
+    full, sums = sums_buffer(pool, heads, page)
+    q, lse = torch.empty(0, 4, dim, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 4, device="cuda")
+    want = sums.clone()
+    for s, length in enumerate(lens):
+        for t in range(length):
+            want[table[s][t // page], :, t % page] = before[table[s][t // page], :, t % page]
+    for max_q in (1, 500):
+        mx.mxkv_attention_weights(q, dev([0, 0, 0, 0]), dev(lens), dev(table), cache.parts[0], cache.parts[1], lse, sums, max_q, 70, 0.1, earlier=before)
+        assert torch.equal(sums, want) and bool((full[:64] == -3).all())
+        sums.fill_(7.0)
+    # one sequence has a row, by the kernels for few and for many rows
+    for max_q in (1, 500):
+        q = torch.zeros(1, 4, dim, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((1, 4), math.log(70.0), device="cuda")   # scores of zero: 1 / 70 for each of 70 keys and head
+        mx.mxkv_attention_weights(q, dev([0, 1, 1, 1]), dev(lens), dev(table), cache.parts[0], cache.parts[1], lse, sums, max_q, 70, 0.1, earlier=before)
+        key = torch.arange(70, device="cuda")
+        pages = torch.tensor(table[0], device="cuda")[key // page]
+        old = torch.where(key < 69, 1.0, 0.0)[:, None] * before[pages, :, key % page]
+        assert bool(((sums[pages, :, key % page] - old - 2 / 70).abs() < 1e-6).all())
+        assert torch.equal(sums[table[2][0], :, :5], before[table[2][0], :, :5])
+        sums.fill_(7.0)
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_select_weights_of_any_alignment(mx, offset):  # noqa: F811
+    lens, heads, page = [900, 64], 2, 32
+    table, pool = make_table(lens, 30, page, 5)
+    room = torch.rand(pool * heads * page + 8, generator=torch.Generator().manual_seed(3)).cuda()
+    w = room[offset:offset + pool * heads * page].view(pool, heads, page)
+    kept, new_lens = run_select(mx, w, lens, table, heads, 100, 4, 20, 900)
+    other, _ = run_select(mx, w.clone(), lens, table, heads, 100, 4, 20, 900)
+    assert torch.equal(kept, other) and new_lens.tolist() == [100, 64]
+
+
+def test_keeping_on_streams(mx):  # noqa: F811
+    """Summed weights (few rows, prompts in both head sizes), choice and attention on four streams at once: the bits of a call alone."""
+    jobs = []
+    for seed, (qh, heads, dim, nq, lens) in enumerate(((8, 2, 128, [1, 1], [9000, 400]), (8, 2, 128, [700, 90], [2000, 700]), (8, 4, 64, [600], [3000]),
+                                                       (16, 2, 64, [9, 9], [700, 300]))):
+        cu, n = cumulative(nq), sum(nq)
+        table, pool = make_table(lens, 150, 64, seed)
+        cache = Cache(pool, heads, 64, dim, 16)
+        fill(cache, lens, table, 64, 16, seed)
+        q = torch.randn(n, qh, dim, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda()
+        lists = (dev(cu), dev(lens), dev(table))
+        out, lse = torch.empty_like(q), torch.empty(n, qh, device="cuda")
+        ws = torch.empty(max(16, mx.mxkv_attention_workspace_bytes(n, len(nq), max(nq), max(lens), qh, heads, dim)), dtype=torch.uint8, device="cuda")
+
+        def call(sums, kept, q=q, lists=lists, cache=cache, out=out, lse=lse, ws=ws, a=(max(nq), max(lens), dim ** -0.5)):
+            mx.mxkv_attention(q, *lists, *cache.parts, out, *a, lse=lse, workspace=ws)
+            mx.mxkv_attention_weights(q, *lists, cache.parts[0], cache.parts[1], lse, sums, *a)
+            mx.mxkv_select(sums, lists[1], lists[2], kept[0], kept[1], a[1], sinks=2, recent=9)
+        new = lambda n=len(nq), h=heads, p=pool: (torch.zeros(p, h, 64, device="cuda"),  # noqa: E731
+                                                  (torch.zeros(n, h, 100, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")))
+        alone, again = new(), new()
+        call(*alone)
+        jobs.append((call, alone, again, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for call, _, again, stream in jobs:
+            with torch.cuda.stream(stream):
+                call(*again)
+    torch.cuda.synchronize()
+    for _, alone, again, _ in jobs:
+        assert torch.equal(alone[0], again[0]) and torch.equal(alone[1][0], again[1][0])
+    assert mx.device_timeouts() == 0
+
+
+def test_compact_a_list_for_each_head_behind_a_part_that_stays(mx):  # noqa: F811
+    """Different tokens for each head, in place, with a first place inside a block; lists as long as the row of the table allows."""
+    pick = random.Random(8)
+    first = [37, 64, 500]
+    lens = [400, 64 + 300, 501]
+    n = [90, 299, 1]
+    lists = [[[f + t for t in rising(pick, length - f, k)] for _ in range(3)] for f, length, k in zip(first, lens, n)]
+    for dim, page, block in ((128, 64, 16), (64, 32, 32), (128, 64, 64)):
+        check_compact(mx, 3, dim, page, block, lens, lists, first=first, seed=dim + block)
