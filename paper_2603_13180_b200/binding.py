@@ -355,6 +355,9 @@ def device_bad_indices_reset() -> None:
     _check(lib.mxn_device_bad_indices_reset(), "mxn_device_bad_indices_reset")
 
 
+_uint8, _int32, _float32, _bfloat16 = torch.uint8, torch.int32, torch.float32, torch.bfloat16
+
+
 def _on_current_device(stream, first, *tensors):
     """Every tensor lies on the current device (calls enqueue there); returns the raw stream to enqueue on."""
     if not first.is_cuda:
@@ -373,7 +376,7 @@ def _heads(t, name, like=None):
     if t is None:
         return None, 0, 0
     shape = t.shape
-    if t.dtype is not torch.bfloat16 or len(shape) != 3:
+    if t.dtype is not _bfloat16 or len(shape) != 3:
         raise ValueError(f"{name}: expected a bf16 tensor [tokens, heads, dim]")
     if like is not None and shape != like:
         raise ValueError(f"{name}: shape {tuple(shape)}, expected {tuple(like)}")
@@ -477,11 +480,19 @@ def alloc_kv_cache(num_pages: int, kv_heads: int, page_size: int, dim: int, bloc
 def _cache(k_codes, k_scales, v_codes, v_scales):
     """(pages, heads, page size, dim, block) of a cache's four tensors and their pointers."""
     cs, ss = k_codes.shape, k_scales.shape
-    if len(cs) != 4 or len(ss) != 3 or ss[2] < 1 or ss[:2] != cs[:2]:
+    if len(cs) != 4 or len(ss) != 3:
         raise ValueError("cache: expected codes [pages, heads, page, dim] and scales [pages, heads, page / block]")
     pages, heads, page, dim = cs
-    return (pages, heads, page, dim, page // ss[2] if page % ss[2] == 0 else 0, _vec(k_codes, torch.uint8, "k_codes"),
-            _vec(k_scales, torch.uint8, "k_scales"), _vec(v_codes, torch.uint8, "v_codes", cs), _vec(v_scales, torch.uint8, "v_scales", ss))
+    sp, sh, blocks = ss
+    if blocks < 1 or sp != pages or sh != heads:
+        raise ValueError("cache: expected codes [pages, heads, page, dim] and scales [pages, heads, page / block]")
+    block = page // blocks if page % blocks == 0 else 0
+    # one expression where all is well (the calls below say what is not)
+    if (k_codes.dtype is _uint8 and k_scales.dtype is _uint8 and v_codes.dtype is _uint8 and v_scales.dtype is _uint8 and v_codes.shape == cs and v_scales.shape == ss
+            and k_codes.is_contiguous() and k_scales.is_contiguous() and v_codes.is_contiguous() and v_scales.is_contiguous()):
+        return pages, heads, page, dim, block, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr()
+    return (pages, heads, page, dim, block, _vec(k_codes, _uint8, "k_codes"), _vec(k_scales, _uint8, "k_scales"), _vec(v_codes, _uint8, "v_codes", cs),
+            _vec(v_scales, _uint8, "v_scales", ss))
 
 
 def _sequences(cu, lens, page_table):
@@ -490,8 +501,10 @@ def _sequences(cu, lens, page_table):
     if len(shape) != 2:
         raise ValueError("page_table: expected int32 [sequences, pages]")
     s, width = shape
-    return (s, width, _vec(cu, torch.int32, "cu", (s + 1,)), _vec(lens, torch.int32, "kv_lens", (s,)),
-            _vec(page_table, torch.int32, "page_table"))
+    if (cu.dtype is _int32 and lens.dtype is _int32 and page_table.dtype is _int32 and cu.dim() == 1 and lens.dim() == 1 and cu.numel() == s + 1
+            and lens.numel() == s and cu.is_contiguous() and lens.is_contiguous() and page_table.is_contiguous()):
+        return s, width, cu.data_ptr(), lens.data_ptr(), page_table.data_ptr()
+    return s, width, _vec(cu, _int32, "cu", (s + 1,)), _vec(lens, _int32, "kv_lens", (s,)), _vec(page_table, _int32, "page_table")
 
 
 def mxkv_append(k, v, cu_tokens, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, cos_sin=None, interleaved=False, stream=None):
@@ -542,7 +555,7 @@ def _attention(entry, q, cu_q, kv_lens, page_table, cache, out, max_q_len, max_k
         raise ValueError("q: dim differs from the cache's")
     ws, ws_bytes = _workspace(workspace)
     _check(getattr(lib, entry)(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, vc, vs,
-                               scale, *mask_args, op, ost, _vec(lse, torch.float32, "lse", (n, qh)), ws, ws_bytes, raw), entry)
+                               scale, *mask_args, op, ost, _vec(lse, _float32, "lse", (n, qh)), ws, ws_bytes, raw), entry)
 
 
 def mxkv_attention_sinks(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, window, sinks,
@@ -561,12 +574,12 @@ def mxkv_attention_tree(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes
     if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[0]:
         raise ValueError("tree_mask: expected int32 [tokens, words]")
     _attention("mxkv_attention_tree", q, cu_q, kv_lens, page_table, (k_codes, k_scales, v_codes, v_scales), out, max_q_len, max_kv_len, scale,
-               (_vec(tree_mask, torch.int32, "tree_mask"), tree_mask.shape[1]), lse, workspace, raw)
+               (_vec(tree_mask, _int32, "tree_mask"), tree_mask.shape[1]), lse, workspace, raw)
 
 
 def _weights(t, name, codes_shape):
     """Pointer of the keys' sums fp32 [pages, heads, page] (None stays None)."""
-    return _vec(t, torch.float32, name, codes_shape[:3])
+    return _vec(t, _float32, name, codes_shape[:3])
 
 
 def mxkv_attention_weights(q, cu_q, kv_lens, page_table, k_codes, k_scales, lse, weights, max_q_len, max_kv_len, scale, earlier=None,
@@ -581,7 +594,7 @@ def mxkv_attention_weights(q, cu_q, kv_lens, page_table, k_codes, k_scales, lse,
     if d != dim:
         raise ValueError("q: dim differs from the cache's")
     _check(lib.mxkv_attention_weights(qp, qst, n, qh, heads, dim, cup, s, max_q_len, lp, max_kv_len, pt, width, pages, page, block, kc, ks, scale,
-                                      1 if causal else 0, window, sinks, _vec(lse, torch.float32, "lse", (n, qh)),
+                                      1 if causal else 0, window, sinks, _vec(lse, _float32, "lse", (n, qh)),
                                       _weights(earlier, "earlier", k_codes.shape), _weights(weights, "weights", k_codes.shape), raw),
            "mxkv_attention_weights")
 
@@ -596,9 +609,9 @@ def mxkv_select(weights, kv_lens, page_table, kept, new_lens, max_kv_len, sinks=
     pages, heads, page = weights.shape
     s, width = page_table.shape
     keep = kept.shape[2]
-    _check(lib.mxkv_select(_vec(weights, torch.float32, "weights"), heads, s, _vec(kv_lens, torch.int32, "kv_lens", (s,)), max_kv_len,
-                           _vec(page_table, torch.int32, "page_table"), width, pages, page, keep, sinks, recent,
-                           _vec(kept, torch.int32, "kept", (s, heads, keep)), _vec(new_lens, torch.int32, "new_lens", (s,)), raw), "mxkv_select")
+    _check(lib.mxkv_select(_vec(weights, _float32, "weights"), heads, s, _vec(kv_lens, _int32, "kv_lens", (s,)), max_kv_len,
+                           _vec(page_table, _int32, "page_table"), width, pages, page, keep, sinks, recent,
+                           _vec(kept, _int32, "kept", (s, heads, keep)), _vec(new_lens, _int32, "new_lens", (s,)), raw), "mxkv_select")
 
 
 def mxkv_compact_workspace_bytes(n_seqs: int, kv_heads: int, max_kept: int) -> int:
@@ -618,8 +631,8 @@ def mxkv_compact(kept, new_lens, kv_lens, page_table, k_codes, k_scales, v_codes
     s, width = page_table.shape
     out_width = width if out_page_table is None else out_page_table.shape[1]
     ws, ws_bytes = _workspace(workspace)
-    _check(lib.mxkv_compact(_vec(kept, torch.int32, "kept", (s, kept.shape[1], kept.shape[2])), kept.shape[1], kept.shape[2],
-                            _vec(first, torch.int32, "first", (s,)), _vec(new_lens, torch.int32, "new_lens", (s,)),
-                            _vec(kv_lens, torch.int32, "kv_lens", (s,)), heads, dim, s, _vec(page_table, torch.int32, "page_table"), width,
-                            _vec(out_page_table, torch.int32, "out_page_table", (s, out_width)), out_width, pages, page, block, kc, ks, vc, vs,
+    _check(lib.mxkv_compact(_vec(kept, _int32, "kept", (s, kept.shape[1], kept.shape[2])), kept.shape[1], kept.shape[2],
+                            _vec(first, _int32, "first", (s,)), _vec(new_lens, _int32, "new_lens", (s,)),
+                            _vec(kv_lens, _int32, "kv_lens", (s,)), heads, dim, s, _vec(page_table, _int32, "page_table"), width,
+                            _vec(out_page_table, _int32, "out_page_table", (s, out_width)), out_width, pages, page, block, kc, ks, vc, vs,
                             _weights(weights, "weights", k_codes.shape), ws, ws_bytes, raw), "mxkv_compact")
