@@ -12,6 +12,11 @@
 // Lists rise and places never lie behind their tokens, so only warps of lower places read what a warp is to overwrite; a warp says so once it
 // has read, and waits for those (two at most) whose tokens lie in its places.  Work is handed out by a ticket in the order of the places, so that whoever is
 // waited for has started, and nobody waits before it has read: every wait ends.  (All waits are bounded; see mxn_device_timeouts.)
+//
+// Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 70 us
+// (the move 55: 0.27 GB, 4.9 TB/s; without its arithmetic it takes 50, so that rows of 128 bytes read from all over are what bounds it); one of 131072
+// brought to 32768, 56 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16 CTAs a cluster
+// took twice that.  In place the two moves take 1.3 and 1.4 times what they take to other pages.
 #include <cuda_fp16.h>
 
 #include "mxn_device.cuh"

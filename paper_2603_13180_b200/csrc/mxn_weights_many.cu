@@ -14,8 +14,16 @@
 // A cluster of CTAs shares out the query tiles of the same keys where there are too few key tiles for the SMs; their sums are added in a fixed order through
 // each other's shared memory.
 //
-// Bound: at head size 128 a product of 128 keys and 128 rows takes 512 cycles, its 16384 exponentials 1024 cycles of the special function units;
-// some of them are computed on the multipliers instead.
+// Bound: at head size 128 a product of 128 keys and 128 rows takes 512 cycles of the tensor cores, its 16384 exponentials 1024 of the special
+// function units; three pairs of exponentials in 16 are computed on the multipliers instead.  4096 queries over 8192 keys, 32 query and 8 key heads
+// of 128: 257 us, 0.49 of a large library product's measured rate, the special function units busy for two thirds of the time, issue slots for 53 %.
+// Eight prompts of up to 1000 queries over up to 1500 keys, 32 and 4 heads of 64: 56 us, of which some 10 are starts and ends of CTAs.
+// What mattered (4096 queries): products announced by number and two warpgroups for a product, 64 columns each, instead of whole products in turn
+// (280 us); the products that a mask touches in a loop of their own with loads of their own (280 -> 263: the common path had carried 32 moves for
+// each 32 columns along); 32 columns in registers at a time (-> 259).  What did not: six buffers of 64 columns (305: the products are issued one
+// every 50 cycles), the next product's columns loaded ahead (276-303), more exponentials on the multipliers (five in 16: 262, seven: 287, in part
+// because its constants find no room in registers), three warpgroups for a product of 96 columns (286-302), eight or one CTA for a key tile (340, 328).
+// The copies of queries cost nothing (the same time without them).
 // Every wait is bounded; see mxn_device_timeouts.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
