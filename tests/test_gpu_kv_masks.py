@@ -252,3 +252,29 @@ def test_masks_on_streams_and_in_graphs(mx):  # noqa: F811
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for _, a, b, _, _ in jobs)
     assert mx.device_timeouts() == 0
+
+
+@pytest.mark.parametrize("dim,block", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("length", [1030, 1100, 2047, 4096, 5000])
+def test_trees_of_up_to_128_rows(mx, dim, block, length):  # noqa: F811
+    """Up to 128 rows for a key head, in chunks: odd and even numbers of tiles, value scales far apart within and between tiles, runs of zero values."""
+    qh, h, nq = 16, 2, [16, 9, 12]
+    lens = [length, 1025, 300]
+    pick = random.Random(length)
+    rows = [random_tree(n, pick) for n in nq]
+    for spread in (0, 40):
+        cu, table, cache, q, buf, out, lse, max_q, max_len, ws = job(mx, qh, h, dim, 64, block, nq, lens, 5)
+        if spread:
+            g = torch.Generator(device="cuda").manual_seed(length)
+            for s, n in enumerate(lens):
+                for i in range(-(-n // 64)):
+                    v = cache.parts[3][table[s][i]]
+                    v.copy_(torch.randint(90, 90 + spread, v.shape, generator=g, device="cuda").to(torch.uint8))
+                    if i % 3 == 1:
+                        v.zero_()
+                        cache.parts[2][table[s][i]].zero_()
+        scale, mask = dim ** -0.5, kr.words([r for sequence in rows for r in sequence] + [0] * 3, 1).cuda()
+        masks = [kr.tree_mask(sequence, n, device="cuda") for sequence, n in zip(rows, lens)]
+        # weights are rounded beside the largest product of weight and value scale of their tile: the bound goes by the softmax |v| as ever
+        compare(mx, lambda: mx.mxkv_attention_tree(q, dev(cu), dev(lens), dev(table), *cache.parts, out, max_q, max_len, scale, mask, lse=lse, workspace=ws),
+                q, cu, lens, table, cache, scale, masks, out, lse, buf)
