@@ -599,6 +599,16 @@ def mxkv_attention_weights(q, cu_q, kv_lens, page_table, k_codes, k_scales, lse,
            "mxkv_attention_weights")
 
 
+def _kept_lists(kept, new_lens, kv_lens, page_table, s):
+    """Pointers of the lists that choice and move share: kept [s, heads, n], new_lens and kv_lens [s], page_table [s, pages]."""
+    if (kept.dtype is _int32 and new_lens.dtype is _int32 and kv_lens.dtype is _int32 and page_table.dtype is _int32 and new_lens.dim() == 1
+            and kv_lens.dim() == 1 and new_lens.numel() == s and kv_lens.numel() == s and kept.shape[0] == s and kept.is_contiguous()
+            and new_lens.is_contiguous() and kv_lens.is_contiguous() and page_table.is_contiguous()):
+        return kept.data_ptr(), new_lens.data_ptr(), kv_lens.data_ptr(), page_table.data_ptr()
+    return (_vec(kept, _int32, "kept", (s, kept.shape[1], kept.shape[2])), _vec(new_lens, _int32, "new_lens", (s,)),
+            _vec(kv_lens, _int32, "kv_lens", (s,)), _vec(page_table, _int32, "page_table"))
+
+
 def mxkv_select(weights, kv_lens, page_table, kept, new_lens, max_kv_len, sinks=0, recent=0, stream=None):
     """Chooses the tokens that stay: of each sequence and key head its first `sinks`, its last `recent` and those between with the largest
     weights, kept.shape[2] in all.  kept int32 [sequences, heads, keep] gets their places, rising (-1 behind a shorter sequence's
@@ -608,10 +618,12 @@ def mxkv_select(weights, kv_lens, page_table, kept, new_lens, max_kv_len, sinks=
         raise ValueError("expected weights [pages, heads, page], kept [sequences, heads, keep] and page_table [sequences, pages]")
     pages, heads, page = weights.shape
     s, width = page_table.shape
-    keep = kept.shape[2]
-    _check(lib.mxkv_select(_vec(weights, _float32, "weights"), heads, s, _vec(kv_lens, _int32, "kv_lens", (s,)), max_kv_len,
-                           _vec(page_table, _int32, "page_table"), width, pages, page, keep, sinks, recent,
-                           _vec(kept, _int32, "kept", (s, heads, keep)), _vec(new_lens, _int32, "new_lens", (s,)), raw), "mxkv_select")
+    _, kept_heads, keep = kept.shape
+    if kept_heads != heads:
+        raise ValueError(f"kept: {kept_heads} heads, expected {heads}")
+    kp, np_, lp, pt = _kept_lists(kept, new_lens, kv_lens, page_table, s)
+    _check(lib.mxkv_select(_vec(weights, _float32, "weights"), heads, s, lp, max_kv_len, pt, width, pages, page, keep, sinks, recent, kp, np_, raw),
+           "mxkv_select")
 
 
 def mxkv_compact_workspace_bytes(n_seqs: int, kv_heads: int, max_kept: int) -> int:
@@ -631,8 +643,8 @@ def mxkv_compact(kept, new_lens, kv_lens, page_table, k_codes, k_scales, v_codes
     s, width = page_table.shape
     out_width = width if out_page_table is None else out_page_table.shape[1]
     ws, ws_bytes = _workspace(workspace)
-    _check(lib.mxkv_compact(_vec(kept, _int32, "kept", (s, kept.shape[1], kept.shape[2])), kept.shape[1], kept.shape[2],
-                            _vec(first, _int32, "first", (s,)), _vec(new_lens, _int32, "new_lens", (s,)),
-                            _vec(kv_lens, _int32, "kv_lens", (s,)), heads, dim, s, _vec(page_table, _int32, "page_table"), width,
+    _, kept_heads, max_kept = kept.shape
+    kp, np_, lp, pt = _kept_lists(kept, new_lens, kv_lens, page_table, s)
+    _check(lib.mxkv_compact(kp, kept_heads, max_kept, _vec(first, _int32, "first", (s,)), np_, lp, heads, dim, s, pt, width,
                             _vec(out_page_table, _int32, "out_page_table", (s, out_width)), out_width, pages, page, block, kc, ks, vc, vs,
                             _weights(weights, "weights", k_codes.shape), ws, ws_bytes, raw), "mxkv_compact")

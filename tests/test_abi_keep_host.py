@@ -98,3 +98,16 @@ def test_binding_refuses_other_tensors(binding):  # noqa: F811
     for call in (lambda: binding.mxkv_select(torch.zeros(3, 2, 32), q, q, q, q, 5), lambda: binding.mxkv_attention_tree(*[q] * 9, 1, 1, 1.0, q)):
         with pytest.raises(ValueError):      # not on a GPU
             call()
+
+
+def test_lists_of_choice_and_move(binding):  # noqa: F811
+    """Every list's type, shape and layout is looked at, whichever way the check takes."""
+    good = dict(kept=torch.zeros(3, 2, 5, dtype=torch.int32), new_lens=torch.zeros(3, dtype=torch.int32), kv_lens=torch.zeros(3, dtype=torch.int32),
+                page_table=torch.zeros(3, 4, dtype=torch.int32))
+    assert binding._kept_lists(**good, s=3) == tuple(t.data_ptr() for t in good.values())
+    wide = torch.zeros(3, 2, 10, dtype=torch.int32)
+    for name, bad in (("kept", good["kept"].long()), ("kept", good["kept"][:2]), ("kept", wide[..., ::2]), ("new_lens", good["new_lens"][:2]),
+                      ("new_lens", torch.zeros(3, 1, dtype=torch.int32)), ("kv_lens", torch.zeros(6, dtype=torch.int32)[::2]),
+                      ("kv_lens", good["kv_lens"].float()), ("page_table", good["page_table"].long()), ("page_table", torch.zeros(4, 3, dtype=torch.int32).t())):
+        with pytest.raises(ValueError):
+            binding._kept_lists(**dict(good, **{name: bad}), s=3)
