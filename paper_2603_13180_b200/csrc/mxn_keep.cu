@@ -13,9 +13,9 @@
 // has read, and waits for those (two at most) whose tokens lie in its places.  Work is handed out by a ticket in the order of the places, so that whoever is
 // waited for has started, and nobody waits before it has read: every wait ends.  (All waits are bounded; see mxn_device_timeouts.)
 //
-// Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 70 us
-// (the move 55: 0.27 GB, 4.9 TB/s; without its arithmetic it takes 50, so that rows of 128 bytes read from all over are what bounds it); one of 131072
-// brought to 32768, 56 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16 CTAs a cluster
+// Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 66 us
+// (the move 51: 0.27 GB, 5.2 TB/s; rows of 128 bytes read from all over bound it: without its arithmetic it took 55 where it took 61; four CTAs an SM
+// in place of five 55); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16 CTAs a cluster
 // took twice that.  In place the two moves take 1.3 and 1.4 times what they take to other pages.
 #include <cuda_fp16.h>
 
@@ -311,7 +311,7 @@ __device__ __forceinline__ void scale_by(uint4& x, int d)   // -24 <= d <= 15
 
 // K: places of a lane; a warp takes 32 K of them, at least a block
 template <int DIM, bool IN_PLACE, int K>
-__global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 4 : 3) compact_kernel(const CompactParams P)
+__global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 5 : 3) compact_kernel(const CompactParams P)
 {
     constexpr int kPlaces = 32 * K;
     constexpr int L = DIM / 16;          // lanes of a row
