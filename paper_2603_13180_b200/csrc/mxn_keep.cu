@@ -2,20 +2,22 @@
 //
 // Select: of a sequence's tokens the first `sinks`, the last `recent`, and of those between the largest by weight, equal ones by place, until
 // `keep` are chosen; for each key head apart.  A weight's bits, turned so that they order as unsigned numbers, are looked at in three digits
-// (11, 11, 10 bits) from the top: a histogram of the digit among what agrees with the digits before gives the next digit of the smallest
-// chosen weight.  Then every warp writes the places that it chose, in order, behind those of the warps before it.  A sequence and head is
-// shared out over a cluster of CTAs, each with a run of tokens whose weights stay in registers; histograms are read across the cluster.
+// (11, 11, 10 bits) from the top: a histogram of the digit among what agrees with the digits before gives the next digit of the smallest chosen
+// weight.  Then every warp writes the places that it chose, in order, behind those of the warps before it.  A sequence and head is shared out
+// over a cluster of CTAs, each with a run of tokens whose weights stay in registers; histograms are read across the cluster.
 //
-// Compact: token kept[i] goes to place first + i.  A warp takes 32 places (64 with blocks of as many) of a head, for keys and values: it reads the listed rows and their blocks' scales,
-// finds for each block of places the scale that its largest value asks for (the append's rule: S = 2^(ceil(log2 absmax) - 8)), rounds the codes
-// on it (exact unless they become subnormal; as they are where the scale stays) and writes them.  In place a row must be read before its place is written.
-// Lists rise and places never lie behind their tokens, so only warps of lower places read what a warp is to overwrite; a warp says so once it
-// has read, and waits for those (two at most) whose tokens lie in its places.  Work is handed out by a ticket in the order of the places, so that whoever is
-// waited for has started, and nobody waits before it has read: every wait ends.  (All waits are bounded; see mxn_device_timeouts.)
+// Compact: token kept[i] goes to place first + i.  A warp takes 32 places (64 with blocks of as many) of a head, for keys and values: it reads
+// the listed rows and their blocks' scales, finds for each block of places the scale that its largest value asks for (the append's rule: S =
+// 2^(ceil(log2 absmax) - 8)), rounds the codes on it (exact unless they become subnormal; as they are where the scale stays) and writes them.
+// In place a row must be read before its place is written. Lists rise and places never lie behind their tokens, so only warps of lower places
+// read what a warp is to overwrite; a warp says so once it has read, and waits for those (two at most) whose tokens lie in its places.  Work is
+// handed out by a ticket in the order of the places, so that whoever is waited for has started, and nobody waits before it has read: every wait
+// ends.  (All waits are bounded; see mxn_device_timeouts.)
 //
 // Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 66 us
-// (the move 50: 0.27 GB, 5.4 TB/s; rows of 128 bytes read from all over bound it: with four CTAs an SM it took 55, and without its arithmetic 50); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16 CTAs a cluster
-// took twice that.  In place the two moves take 1.3 and 1.4 times what they take to other pages.
+// (the move 50: 0.27 GB, 5.4 TB/s; rows of 128 bytes read from all over bound it: with four CTAs an SM it took 55, and without its arithmetic
+// 50); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16
+// CTAs a cluster took twice that.  In place the two moves take 1.3 and 1.4 times what they take to other pages.
 #include <cuda_fp16.h>
 
 #include "mxn_device.cuh"
