@@ -17,7 +17,7 @@
 // Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 66 us
 // (the move 50: 0.27 GB, 5.4 TB/s; rows of 128 bytes read from all over bound it: with four CTAs an SM it took 55, and without its arithmetic
 // 50); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16
-// CTAs a cluster took twice that.  In place the two moves take 1.3 and 1.4 times what they take to other pages.
+// CTAs a cluster took twice that.  In place either move takes 1.4 times what it takes to other pages.
 #include <cuda_fp16.h>
 
 #include "mxn_device.cuh"
