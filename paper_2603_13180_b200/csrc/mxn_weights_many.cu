@@ -6,6 +6,8 @@
 // (whole tokens of the query heads that share the key head).  Keys are the rows of the products and queries their columns: a thread looks
 // after one key, adds its row of scores up in registers, and no sum crosses threads until the end.  The codes become bf16 (exact) once and stay in tensor
 // memory as the first operand; the queries come as they are (bf16), by the tensor copy engine, so that every product is exact; the sums of a score are binary32.
+// A key enters with most of its scale (a power of two): a product's sum then lies within binary32's range wherever the score does, also where very large
+// queries stand over very small keys or the other way round.
 // Roles, by warp:
 //   0-15   keys to tensor memory; then exponentials and sums, two warpgroups for a product
 //   16     copies of query tiles
@@ -74,12 +76,12 @@ __device__ __forceinline__ void tma_load_queries(uint32_t dst, const CUtensorMap
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar) : "memory");
 }
-// two E4M3 codes -> two bf16
-__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t two)
+// two E4M3 codes times a power of two -> two bf16
+__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t two, float power)
 {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xFFFFu), __NV_E4M3);
     const float2 f = __half22float2(__half2(h));
-    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x, f.y);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x * power, f.y * power);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
@@ -280,6 +282,11 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
         const bool real = (uint32_t)page < (uint32_t)P.num_pages;
         const int64_t tile = (int64_t)page * P.kv_heads + h;
         const int in_page = key & (P.page - 1);
+        // The key's scale is 2^(byte - 127).  2^in of it enters the operand: 2^16 below the scale, so that a sum has room above the largest score, but no
+        // lower than 2^-110, so that the smallest code (2^-9) stays a normal bf16; the largest (448) is one up to byte 254.  2^(byte - 127 - in) is left.
+        const int byte = real ? (int)__ldg(P.k_scales + (tile << (P.page_shift - P.block_shift)) + (in_page >> P.block_shift)) : 0;
+        const int in = max(byte - 127 - 16, -110);
+        auto pow2 = [](int e) { return __uint_as_float((uint32_t)(e + 127) << 23); };
         // ---- keys to tensor memory: half of a row's dimensions a thread (with one key tile the other warpgroups rest) ----
         if (ms == 2 || !(wg & 1)) {
             const int half = wg >> 1;
@@ -291,8 +298,8 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                 const uint32_t c[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    w[8 * i + 2 * e] = bf16_of_codes(c[e]);
-                    w[8 * i + 2 * e + 1] = bf16_of_codes(c[e] >> 16);
+                    w[8 * i + 2 * e] = bf16_of_codes(c[e], pow2(in));
+                    w[8 * i + 2 * e + 1] = bf16_of_codes(c[e] >> 16, pow2(in));
                 }
             }
             const uint32_t at = a_col + m * (DIM / 2) + half * (DIM / 4) + lanes;
@@ -304,9 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             if (lane == 0) mbar_arrive(a_full);
         }
         if (rank == 0 && wg < ms && __any_sync(0xFFFFFFFFu, key < k1 && !real) && lane == 0) atomicAdd(&g_many_bad, 1u);
-        float scale = 0.0f;
-        if (real)
-            scale = P.scale * kLog2e * e8m0_to_f32(__ldg(P.k_scales + (tile << (P.page_shift - P.block_shift)) + (in_page >> P.block_shift)));
+        const float scale = real ? P.scale * kLog2e * pow2(byte - 127 - in) : 0.0f;
         const float2 f = f2(scale);
         float2 sum[2] = {f2(0.0f), f2(0.0f)};
         // A product is shared by two warpgroups, half of its columns each: with two key tiles each pair has its own, with one they take turns

@@ -1,0 +1,57 @@
+"""Summed weights at the ends of binary32's range, on both sides of 64 query rows for a key head, on the GPU against 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests import keep_ref as kr
+from tests.test_gpu_kv import Cache, cumulative, dev, fill, make_table, mx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+FEW, MANY = (4, 2, 3), (8, 2, 130)   # query heads, key heads, new queries
+
+
+def setting(qh, h, dim, nq, length, page=32, block=16, seed=0, binades=0):
+    """Queries times 2^binades over keys times 2^-binades."""
+    table, pool = make_table([length], -(-length // page) + 1, page, seed)
+    cache = Cache(pool, h, page, dim, block)
+    fill(cache, [length], table, page, block, seed)
+    scales = cache.parts[1]
+    scales.copy_(torch.where(scales == 255, scales, (scales.int() - binades).to(torch.uint8)))
+    q = 2 * torch.randn(nq, qh, dim, generator=torch.Generator().manual_seed(seed + 1)).to(torch.bfloat16).double()
+    return table, cache, (q * 2.0 ** binades).to(torch.bfloat16).cuda()
+
+
+def summed(mx, q, lse, table, cache, length, earlier=None, causal=True):  # noqa: F811
+    out = torch.full(cache.parts[1].shape[:2] + cache.parts[0].shape[2:3], 7.0, device="cuda")
+    mx.mxkv_attention_weights(q, dev([0, q.shape[0]]), dev([length]), dev(table), cache.parts[0], cache.parts[1], lse, out, q.shape[0], length,
+                              q.shape[2] ** -0.5, earlier=earlier, causal=causal)
+    torch.cuda.synchronize()
+    assert mx.device_timeouts() == 0 and cache.guards_intact()
+    return out
+
+
+def of_tokens(sums, table, length):
+    key = torch.arange(length, device="cuda")
+    page = sums.shape[2]
+    return sums[torch.tensor(table[0], device="cuda")[key // page], :, key % page]   # [length, heads]
+
+
+@pytest.mark.parametrize("qh,h,nq", [FEW, MANY])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("binades", [118, 60, -60, -118, -124])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_queries_of_any_size(mx, qh, h, nq, dim, binades, mixed):  # noqa: F811
+    """Very large queries over very small keys and the other way round: the scores are ordinary ones.  Mixed: every other query is an ordinary one, whose
+    scores are next to nothing (over small keys; over large ones it would have to see one key only)."""
+    length, scale = 400, dim ** -0.5
+    table, cache, q = setting(qh, h, dim, nq, length, seed=dim + nq, binades=binades)
+    if mixed:
+        q[::2] = (q[::2].double() * 2.0 ** -max(binades, 0)).to(torch.bfloat16) if binades > 0 else 0.0
+    masks = [kr.sinks_mask(nq, length, 0, 0, device="cuda")]
+    lse = kr.attention(q, [0, nq], [length], table, *cache.parts[:2], *cache.parts[:2], scale, masks)[1].float()
+    sums = summed(mx, q, lse, table, cache, length)
+    want = torch.full_like(sums, 7.0).double()
+    slack = kr.weights(q, lse, [0, nq], [length], table, *cache.parts[:2], scale, masks, want, None)
+    err = (sums.double() - want).abs()
+    assert bool((err <= slack).all()), f"off by {float((err / slack.clamp(min=1e-30)).nan_to_num(math.inf).max()):.3g} tolerances"
