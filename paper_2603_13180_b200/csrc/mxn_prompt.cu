@@ -86,12 +86,13 @@ struct alignas(16) TileScales {
     float c0;
 };
 
-// 2^u of two numbers below 2^21 on the multipliers: u = n + f with n the nearest integer (what is below -126 counts as that: 2^-126 is
-// nothing to a sum whose terms reach 2^-15, and rounds to 0 in f16), and 2^f by a polynomial fitted to the least relative error over
-// [-1/2, 1/2] with 1 as its constant: 1.09e-7, with the roundings 1.7e-7 (2^-22.4)
+// 2^u of two numbers below 2^21 on the multipliers: u = n + f with n the nearest integer (from u = -127 down it is exactly 0, since n = -127 takes
+// the whole exponent of p = 1; between -127 and -126 it is off by up to 2^-127, which is nothing to a sum whose terms reach 2^-15 and rounds
+// to 0 in f16), and 2^f by a polynomial fitted to the least relative error over [-1/2, 1/2] with 1
+// as its constant: 1.09e-7, with the roundings 1.7e-7 (2^-22.4)
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
-    const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
+    const float2 v = make_float2(fmaxf(u.x, -127.0f), fmaxf(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
     const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
     float2 p = f2(0.00132647273f);
     p = __ffma2_rn(p, f, f2(0.00967151299f));

@@ -54,9 +54,10 @@ struct ManyShape {
     static constexpr int kSmem = kStages * kStage + 1024;
 };
 
+enum { kNan = 1, kUnseeing = 2 };
 struct alignas(16) Columns {
     float lse[kTile];     // -lse in powers of two; -infinity for columns without a row
-    int special;          // a NaN is among them
+    int special;          // kNan: a NaN is among them; kUnseeing: a row that saw nothing
 };
 
 __device__ __forceinline__ void cluster_sync()
@@ -86,10 +87,11 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t two, float power)
 }
 
 // 2^u of two numbers below 2^21 on the multipliers: the polynomial of the prompt attention (mxn_prompt.cu), whose relative error is 1.7e-7 with the
-// roundings.  What is below -126 counts as that: 2^-126 is nothing to a sum of weights.
+// roundings.  From u = -127 down it is exactly 0 (n = -127 takes the whole exponent of p = 1), so that what gives nothing adds nothing; between
+// -127 and -126 it is off by up to 2^-127.
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
-    const float2 v = make_float2(fmaxf(u.x, -126.0f), fmaxf(u.y, -126.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
+    const float2 v = make_float2(fmaxf(u.x, -127.0f), fmaxf(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
     const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
     float2 p = f2(0.00132647273f);
     p = __ffma2_rn(p, f, f2(0.00967151299f));
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bool live = i < tiles && tok[e] < S.nq - t.token && t.part * GB + head[e] < P.group;
-                v[e] = live ? __ldg(W.lse + (int64_t)(S.q0 + t.token + tok[e]) * P.q_heads + h * P.group + t.part * GB + head[e]) : -INFINITY;
+                v[e] = live ? __ldg(W.lse + (int64_t)(S.q0 + t.token + tok[e]) * P.q_heads + h * P.group + t.part * GB + head[e]) : INFINITY;
             }
         };
         float v[4], next[4];
@@ -259,17 +261,18 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             const int slot = i % kSlots;
             const bool ok = i < kSlots || wait(n_empty + 8 * slot, (uint32_t)(i / kSlots - 1) & 1u, dead);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
-            bool nan = false;
+            bool nan = false, unseeing = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 nan = nan || v[e] != v[e];
+                unseeing = unseeing || v[e] == -INFINITY;
                 columns[slot].lse[lane + 32 * e] = v[e] == -INFINITY ? -INFINITY : -v[e] * kLog2e;   // (a row that saw nothing gives nothing)
                 v[e] = next[e];
             }
-            nan = __any_sync(0xFFFFFFFFu, nan);
+            const int special = (__any_sync(0xFFFFFFFFu, nan) ? kNan : 0) | (__any_sync(0xFFFFFFFFu, unseeing) ? kUnseeing : 0);
             __syncwarp();
             if (lane == 0) {
-                columns[slot].special = nan;
+                columns[slot].special = special;
                 mbar_arrive(n_full + 8 * slot);
             }
             __syncwarp();
@@ -367,14 +370,20 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                 const int to = P.window == 0 || key < P.sinks ? T : (int)max((int64_t)0, min((int64_t)T, ahead + P.window));
                 const int lo = max(from * GB - col0, 0), hi = min((real ? min(to * GB, valid) : 0) - col0, kHalf);
                 if (__any_sync(0xFFFFFFFFu, lo < hi)) {
+                    const bool unseeing = C.special & kUnseeing;
 #pragma unroll 1
                     for (int c = 0; c < kHalf; c += 16) {
                         uint32_t z[16];
                         tm_load16(z, at + c);
+                        uint32_t in = ((1u << min(max(hi - c, 0), 16)) - 1u) & (0xFFFFFFFFu << min(max(lo - c, 0), 16));   // bit: the column counts
+                        if (unseeing) {   // a row that saw nothing gives nothing, also where its score is a NaN
+#pragma unroll 1
+                            for (int e = 0; e < 16; ++e) in &= ~((cl[c + e] == -INFINITY ? 1u : 0u) << e);
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const float p = ex2(fmaf(__uint_as_float(z[e]), scale, cl[c + e]));
-                            part[e & 1].x += c + e >= lo && c + e < hi ? p : 0.0f;
+                            part[e & 1].x += (in >> e) & 1u ? p : 0.0f;
                         }
                     }
                 }

@@ -55,3 +55,31 @@ def test_queries_of_any_size(mx, qh, h, nq, dim, binades, mixed):  # noqa: F811
     slack = kr.weights(q, lse, [0, nq], [length], table, *cache.parts[:2], scale, masks, want, None)
     err = (sums.double() - want).abs()
     assert bool((err <= slack).all()), f"off by {float((err / slack.clamp(min=1e-30)).nan_to_num(math.inf).max()):.3g} tolerances"
+
+
+@pytest.mark.parametrize("qh,h,nq", [FEW, MANY, (6, 1, 90), (3, 1, 200), (7, 1, 8), (1, 1, 300)])
+@pytest.mark.parametrize("lse_of_all", [-math.inf, 300.0])
+@pytest.mark.parametrize("causal", [True, False])
+def test_nothing_is_exactly_nothing(mx, qh, h, nq, lse_of_all, causal):  # noqa: F811
+    """Rows that saw nothing, and weights below 2^-400: exactly 0, and exactly the earlier sums, whatever rows a tile of queries has."""
+    length = 500
+    table, cache, q = setting(qh, h, 64, nq, length, seed=nq)
+    q = (q.double() / 16).to(torch.bfloat16)   # scores below some 20
+    lse = torch.full((nq, qh), lse_of_all, device="cuda")
+    assert bool((of_tokens(summed(mx, q, lse, table, cache, length, causal=causal), table, length) == 0).all())
+    shape = cache.parts[1].shape[:2] + (32,)
+    before = torch.exp(torch.randn(shape, generator=torch.Generator().manual_seed(1)) - 85).cuda()   # some 2^-123
+    got, old = (of_tokens(x, table, length) for x in (summed(mx, q, lse, table, cache, length, earlier=before, causal=causal), before))
+    assert torch.equal(got[:length - nq], old[:length - nq]) and bool((got[length - nq:] == 0).all())
+
+
+@pytest.mark.parametrize("qh,h,nq", [(2, 2, 5), (2, 2, 128)])
+def test_nan_that_gives_nothing(mx, qh, h, nq):  # noqa: F811
+    """A row whose lse is -infinity gives nothing, a NaN in it or not."""
+    length = 300
+    table, cache, q = setting(qh, h, 64, nq, length, seed=nq)
+    lse = torch.full((nq, qh), -math.inf, device="cuda")
+    q[nq // 2] = math.nan
+    assert bool((of_tokens(summed(mx, q, lse, table, cache, length, causal=False), table, length) == 0).all())
+    q[0] = math.inf
+    assert bool((of_tokens(summed(mx, q, lse, table, cache, length, causal=False), table, length) == 0).all())
