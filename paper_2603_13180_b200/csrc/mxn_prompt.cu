@@ -92,7 +92,7 @@ struct alignas(16) TileScales {
 // as its constant: 1.09e-7, with the roundings 1.7e-7 (2^-22.4)
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
-    const float2 v = make_float2(fmaxf(u.x, -127.0f), fmaxf(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
+    const float2 v = make_float2(max_nan(u.x, -127.0f), max_nan(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
     const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
     float2 p = f2(0.00132647273f);
     p = __ffma2_rn(p, f, f2(0.00967151299f));
@@ -678,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const AttnPara
                 }
             }
             // weights, over their scores
-            // a NaN among the scores reaches all of the step's weights: the polynomial below would take it for a small number
+            // a NaN among the scores reaches all of the step's weights: the polynomial below would take it for a number
             const float shift_by = utop != utop ? utop : ref == kNone ? 0.0f : kTop - ref;
             uint32_t w[32];
             float more = 0.0f;

@@ -43,6 +43,9 @@ constexpr int kCopies = 16, kProducts = 17, kRowSums = 18;   // warps
 constexpr float kLog2e = 1.4426950408889634f;
 static_assert(kFull > kBuffers && kFull % 2 == 0);
 constexpr int kByMultipliers = 3;   // of 16 pairs of exponentials
+// A weight is at most about 1 and a sum of them at most about the number of rows, so a sum that is not below this holds a NaN that went through the
+// polynomial.  (A NaN looked for among the exponents themselves took a register and 6 % of the prompts' time.)
+constexpr float kMost = 1.70141183e38f;   // 2^127
 
 __device__ unsigned int g_many_timeouts = 0;
 __device__ unsigned int g_many_bad = 0;
@@ -88,10 +91,10 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t two, float power)
 
 // 2^u of two numbers below 2^21 on the multipliers: the polynomial of the prompt attention (mxn_prompt.cu), whose relative error is 1.7e-7 with the
 // roundings.  From u = -127 down it is exactly 0 (n = -127 takes the whole exponent of p = 1), so that what gives nothing adds nothing; between
-// -127 and -126 it is off by up to 2^-127.
+// -127 and -126 it is off by up to 2^-127.  A NaN becomes a NaN or, by the exponent that is added to its bits, a number of 2^127 or more (see kMost).
 __device__ __forceinline__ float2 ex2_fma(float2 u)
 {
-    const float2 v = make_float2(fmaxf(u.x, -127.0f), fmaxf(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
+    const float2 v = make_float2(max_nan(u.x, -127.0f), max_nan(u.y, -127.0f)), t = __fadd2_rn(v, f2(12582912.0f));   // 1.5 * 2^23
     const float2 n = __fadd2_rn(t, f2(-12582912.0f)), f = __fadd2_rn(v, make_float2(-n.x, -n.y));
     float2 p = f2(0.00132647273f);
     p = __ffma2_rn(p, f, f2(0.00967151299f));
@@ -397,7 +400,8 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
             if (lane == 0) mbar_arrive(n_empty + 8 * slot);
         }
         const float2 both = __fadd2_rn(sum[0], sum[1]);
-        parts[wg][r] = both.x + both.y;
+        const float all = both.x + both.y;
+        parts[wg][r] = all < kMost ? all : __uint_as_float(0x7FC00000u);
         tc_before();
     }
     __syncthreads();

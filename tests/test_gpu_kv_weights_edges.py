@@ -83,3 +83,22 @@ def test_nan_that_gives_nothing(mx, qh, h, nq):  # noqa: F811
     assert bool((of_tokens(summed(mx, q, lse, table, cache, length, causal=False), table, length) == 0).all())
     q[0] = math.inf
     assert bool((of_tokens(summed(mx, q, lse, table, cache, length, causal=False), table, length) == 0).all())
+
+
+@pytest.mark.parametrize("qh,h,nq", [(2, 2, 5), (2, 2, 128)])
+@pytest.mark.parametrize("where", ["query", "lse"])
+def test_nan_in_any_row(mx, qh, h, nq, where):  # noqa: F811
+    """A NaN in a query or in its lse alone (the attention gives such a query an lse of NaN) makes the sums of its head's keys NaN and no other,
+    whichever row it is."""
+    length = 300
+    table, cache, q = setting(qh, h, 64, nq, length, seed=nq)
+    masks = [kr.sinks_mask(nq, length, 0, 0, causal=False, device="cuda")]
+    lse = kr.attention(q, [0, nq], [length], table, *cache.parts[:2], *cache.parts[:2], 0.125, masks)[1].float()
+    for row in range(nq):
+        x, y = q.clone(), lse.clone()
+        if where == "query":
+            x[row, 1, 7 * row % 64] = math.nan
+        else:
+            y[row, 1] = math.nan
+        got = of_tokens(summed(mx, x, y, table, cache, length, causal=False), table, length)
+        assert bool(got[:, 1].isnan().all()) and not bool(got[:, 0].isnan().any()), row
