@@ -65,7 +65,7 @@ extern "C" {
 typedef enum {
     MXN_OK = 0,
     MXN_ERR_NULL = 1,      /* a required pointer is NULL */
-    MXN_ERR_SHAPE = 2,     /* T < 0, D <= 0, D % B != 0, unsupported B or D, bad p */
+    MXN_ERR_SHAPE = 2,     /* T < 0, D <= 0, D % B != 0, unsupported B or D, bad p; tensors that must not share memory and do */
     MXN_ERR_ALIGN = 3,     /* a pointer misses the alignment stated above */
     MXN_ERR_ENUM = 4,      /* unknown rounding mode / layout */
     MXN_ERR_WORKSPACE = 5, /* workspace NULL or smaller than the query says */
@@ -452,7 +452,8 @@ mxn_status mxkv_attention_weights(const void* q_bf16, int64_t q_stride, int64_t 
 /* Choice of the tokens that stay in the cache, for each sequence and key head apart: the first `sinks`, the last `recent`, and of those
  *   between the ones with the largest weights (equal ones by place; a NaN, or a token whose page is out of range, comes last), `keep` in all
  *   (sinks + recent <= keep).  A sequence of up to `keep` tokens keeps all.  Tokens past max_kv_len do not count.
- *   kept int32 [n_seqs, kv_heads, keep]: their places, rising; -1 behind a shorter sequence's last.  new_lens int32 [n_seqs]. */
+ *   kept int32 [n_seqs, kv_heads, keep]: their places, rising; -1 behind a shorter sequence's last.  new_lens int32 [n_seqs].  Neither may share
+ *   memory with the other or with what is read (kv_lens among it: MXN_ERR_SHAPE). */
 mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const int32_t* kv_lens, int64_t max_kv_len, const int32_t* page_table,
                        int64_t max_pages, int64_t num_pages, int page_size, int64_t keep, int64_t sinks, int64_t recent, int32_t* kept,
                        int32_t* new_lens, void* cuda_stream);

@@ -612,7 +612,7 @@ def _kept_lists(kept, new_lens, kv_lens, page_table, s):
 def mxkv_select(weights, kv_lens, page_table, kept, new_lens, max_kv_len, sinks=0, recent=0, stream=None):
     """Chooses the tokens that stay: of each sequence and key head its first `sinks`, its last `recent` and those between with the largest
     weights, kept.shape[2] in all.  kept int32 [sequences, heads, keep] gets their places, rising (-1 behind a shorter sequence's
-    last), new_lens int32 [sequences] the lengths."""
+    last), new_lens int32 [sequences] the lengths; both are tensors of their own (not kv_lens)."""
     raw = _on_current_device(stream, weights, kv_lens, page_table, kept, new_lens)
     if weights.dim() != 3 or kept.dim() != 3 or page_table.dim() != 2:
         raise ValueError("expected weights [pages, heads, page], kept [sequences, heads, keep] and page_table [sequences, pages]")

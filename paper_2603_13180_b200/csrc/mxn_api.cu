@@ -576,6 +576,12 @@ mxn_status check_cache(int kv_heads, int dim, int64_t n_seqs, int64_t max_pages,
     return MXN_OK;
 }
 
+bool share_memory(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes > 0 && b_bytes > 0 && (x < y ? (uint64_t)(y - x) < (uint64_t)a_bytes : (uint64_t)(x - y) < (uint64_t)b_bytes);
+}
+
 int log2_of(int v)
 {
     int n = 0;
@@ -887,6 +893,14 @@ mxn_status mxkv_select(const float* weights, int kv_heads, int64_t n_seqs, const
     if (n_seqs == 0) return MXN_OK;
     if (new_lens == nullptr || (kept == nullptr && keep > 0)) return MXN_ERR_NULL;
     if (misaligned(new_lens, 4) || misaligned(kept, 4)) return MXN_ERR_ALIGN;
+    // Some CTAs write while others still read.  A length read after it was written would leave its head with the wrong tokens, or one CTA of a cluster
+    // waiting for another that has left.  (The counts' products stay below 2^62.)
+    const int64_t kept_bytes = n_seqs * kv_heads * keep * 4, lens_bytes = n_seqs * 4;
+    const struct { const void* at; int64_t bytes; } read[] = {{weights, num_pages * kv_heads * page_size * 4}, {kv_lens, lens_bytes},
+                                                              {page_table, n_seqs * max_pages * 4}};
+    if (share_memory(kept, kept_bytes, new_lens, lens_bytes)) return MXN_ERR_SHAPE;
+    for (const auto& r : read)
+        if (share_memory(kept, kept_bytes, r.at, r.bytes) || share_memory(new_lens, lens_bytes, r.at, r.bytes)) return MXN_ERR_SHAPE;
     mxn::SelectParams P{};
     P.weights = weights;
     P.lens = kv_lens;
