@@ -413,14 +413,17 @@ mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens
 size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads,
                                       int kv_heads, int head_dim);
 
-/* The same with other masks; what is not said here is as in mxkv_attention (workspaces and their sizes too).
+/* The same with other masks; what is not said here is as in mxkv_attention (workspaces and their sizes too, but for what is said of trees).
  *   mxkv_attention_sinks: causal, with a window of `window` >= 1 places, beside which a sequence's first `sinks` keys (those up to the query's
  *   own place) stay visible.  Pages between the first tokens and every query's window have no influence and may be released.
  *   mxkv_attention_tree: the new tokens of a sequence are drafts that form a tree (or several).  Each sees every key in front of
  *   the sequence's new tokens, and new token i (place kv_lens - new tokens + i) where bit i % 32 of word i / 32 of its own row of
  *   mask_u32 [n_tokens, mask_words] is set: as a rule its ancestors and itself.  Bits of tokens that the sequence does not have are
  *   ignored, tokens past the last word are not seen.  Where drafts stand in the tree, and so their rotation, is the caller's
- *   (rmsnorm_rope_fwd with positions; mxkv_append without angles). */
+ *   (rmsnorm_rope_fwd with positions; mxkv_append without angles).
+ *   Trees of more than 64 query rows for a key head share out the keys by the sequences' lengths as they are.  For that they can use up to
+ *   mxkv_attention_tree_workspace_bytes(...) bytes; with a workspace of mxkv_attention_workspace_bytes(...), which may be smaller, they
+ *   take fewer chunks (slower where lengths differ, and other roundings).  For fewer rows both are the same. */
 mxn_status mxkv_attention_sinks(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,
                                 const int32_t* cu_q, int64_t n_seqs, int64_t max_q_len, const int32_t* kv_lens, int64_t max_kv_len,
                                 const int32_t* page_table, int64_t max_pages, int64_t num_pages, int page_size, int block,
@@ -433,6 +436,8 @@ mxn_status mxkv_attention_tree(const void* q_bf16, int64_t q_stride, int64_t n_t
                                const void* k_codes_u8, const void* k_scales_u8, const void* v_codes_u8, const void* v_scales_u8, float scale,
                                const void* mask_u32, int64_t mask_words, void* out_bf16, int64_t out_stride, float* lse_out_or_null,
                                void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t mxkv_attention_tree_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads, int kv_heads,
+                                           int head_dim);
 
 /* What each key is given by the softmax: weights[page, head, place in page] = earlier + sum over the call's query rows that see the key, and the
  *   query heads that share its key head, of exp(scale q k - lse).  It is what eviction goes by.

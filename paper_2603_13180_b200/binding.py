@@ -28,7 +28,7 @@ EXPORTS = ("mxn_scale_bytes", "mxn_status_string", "mx_cast", "rmsnorm_mxfp8_fwd
            "mxnorm_add_fwd", "mx_cast_nvfp4", "mxn_device_bad_indices", "mxn_device_bad_indices_reset",
            "rmsnorm_rope_fwd", "rmsnorm_rope_bwd", "rmsnorm_rope_bwd_workspace_bytes", "mxkv_append", "mxkv_attention",
            "mxkv_attention_workspace_bytes", "mxkv_attention_sinks", "mxkv_attention_tree", "mxkv_attention_weights", "mxkv_select",
-           "mxkv_compact", "mxkv_compact_workspace_bytes")
+           "mxkv_compact", "mxkv_compact_workspace_bytes", "mxkv_attention_tree_workspace_bytes")
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -89,6 +89,8 @@ lib.mxkv_attention.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i6
                                _vp, _f32, _i32, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
 lib.mxkv_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i32, _i32, _i32]
 lib.mxkv_attention_workspace_bytes.restype = _sz
+lib.mxkv_attention_tree_workspace_bytes.argtypes = lib.mxkv_attention_workspace_bytes.argtypes
+lib.mxkv_attention_tree_workspace_bytes.restype = _sz
 lib.mxkv_attention_sinks.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp,
                                      _vp, _vp, _f32, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
 lib.mxkv_attention_tree.argtypes = [_vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp,
@@ -528,6 +530,10 @@ def mxkv_attention_workspace_bytes(n_tokens: int, n_seqs: int, max_q_len: int, m
     return int(lib.mxkv_attention_workspace_bytes(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, dim))
 
 
+def mxkv_attention_tree_workspace_bytes(n_tokens: int, n_seqs: int, max_q_len: int, max_kv_len: int, q_heads: int, kv_heads: int, dim: int) -> int:
+    return int(lib.mxkv_attention_tree_workspace_bytes(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, dim))
+
+
 def mxkv_attention(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, causal=True,
                    window=0, lse=None, workspace=None, stream=None):
     """Attention of the queries [n, Hq, D] over the paged cache; see mxkv_attention in include/mxnorm.h."""
@@ -569,7 +575,8 @@ def mxkv_attention_sinks(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_code
 def mxkv_attention_tree(q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, max_q_len, max_kv_len, scale, tree_mask,
                         lse=None, workspace=None, stream=None):
     """Attention of drafted tokens that form a tree.  tree_mask int32 [n, words]: bit i % 32 of word i / 32 of a row tells whether it sees
-    new token i of its sequence (its ancestors and itself); what stands in front of a sequence's new tokens is seen by all of them."""
+    new token i of its sequence (its ancestors and itself); what stands in front of a sequence's new tokens is seen by all of them.
+    workspace: of mxkv_attention_tree_workspace_bytes (one of mxkv_attention_workspace_bytes will do, with fewer chunks)."""
     raw = _on_current_device(stream, q, cu_q, kv_lens, page_table, k_codes, k_scales, v_codes, v_scales, out, tree_mask, lse, workspace)
     if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[0]:
         raise ValueError("tree_mask: expected int32 [tokens, words]")

@@ -1,4 +1,5 @@
 // extern "C" entry points of libmxnorm: argument checks and dispatch only.
+#include <cstdint>
 #include <mutex>
 
 #include "../../include/mxnorm.h"
@@ -645,11 +646,18 @@ mxn_status attend(mxn::AttnParams P, int64_t n_seqs, int64_t max_q_len, int64_t 
     if (P.n == 0 || n_seqs == 0) return MXN_OK;
     if ((st = check_heads(P.q, P.q_stride, P.q_heads, P.dim)) != MXN_OK || (st = check_heads(out, out_stride, P.q_heads, P.dim)) != MXN_OK) return st;
     if (lse != nullptr && misaligned(lse, 4)) return MXN_ERR_ALIGN;
-    const mxn::AttnPlan plan = mxn::plan_attention(P.n, n_seqs, max_q_len, max_kv_len, P.causal ? window : 0, sinks, P.q_heads, P.kv_heads, P.dim,
-                                                    P.tree != nullptr);
+    const size_t room = workspace == nullptr ? 0 : workspace_bytes;
+    auto plan_for = [&](bool tree, size_t bytes) {
+        return mxn::plan_attention(P.n, n_seqs, max_q_len, max_kv_len, P.causal ? window : 0, sinks, P.q_heads, P.kv_heads, P.dim, tree, bytes);
+    };
+    if (P.tree != nullptr) {   // keys shared out by length make do with the workspace that the other masks ask for, not with less
+        const mxn::AttnPlan full = plan_for(true, SIZE_MAX);
+        if (full.by_length && room < full.workspace && room < plan_for(false, 0).workspace) return MXN_ERR_WORKSPACE;
+    }
+    const mxn::AttnPlan plan = plan_for(P.tree != nullptr, room);
     if (plan.ctas > 0x7FFFFFFF || P.n * P.q_heads > 0x7FFFFFFF) return MXN_ERR_SHAPE;
     if (plan.splits > 1) {
-        if (workspace == nullptr || workspace_bytes < plan.workspace) return MXN_ERR_WORKSPACE;
+        if (room < plan.workspace) return MXN_ERR_WORKSPACE;
         if (misaligned(workspace, 16)) return MXN_ERR_ALIGN;
     }
     P.out = static_cast<uint16_t*>(out);
@@ -793,9 +801,14 @@ size_t mxkv_attention_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t 
                                       int head_dim)
 {
     if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim) || n_tokens == 0 || n_seqs == 0) return 0;
-    const size_t a = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, false).workspace,
-                 b = mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, true).workspace;
-    return a > b ? a : b;
+    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, false, 0).workspace;
+}
+
+size_t mxkv_attention_tree_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int64_t max_q_len, int64_t max_kv_len, int q_heads, int kv_heads,
+                                           int head_dim)
+{
+    if (!attention_shape_ok(n_tokens, n_seqs, max_q_len, max_kv_len, q_heads, kv_heads, head_dim) || n_tokens == 0 || n_seqs == 0) return 0;
+    return mxn::plan_attention(n_tokens, n_seqs, max_q_len, max_kv_len, 0, 0, q_heads, kv_heads, head_dim, true, SIZE_MAX).workspace;
 }
 
 mxn_status mxkv_attention(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,

@@ -895,7 +895,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 namespace {
 
 // wide: heads of 64, 17 to 64 rows: 32 rows a warp (two warps where there are more), else 16 and more CTAs
-AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool wide, bool tree)
+AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool wide, bool tree,
+                   size_t room)
 {
     AttnPlan a{};
     const int64_t rows = max_q * (q_heads / kv_heads);
@@ -925,9 +926,10 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
     const int64_t bound = splits < most(max_len) ? splits : most(max_len);   // for the workspace: whatever the window
     if (a.prompt && tree && units <= resident) {
         // as many CTAs as run at a time; the longest sequences may have more chunks than their share by number (twice as many and one more at most, which
-        // bounds the workspace)
-        const int64_t tiles = ceil_div(max_len, tile), room = 2 * (resident / units) + 1;
-        a.splits = tiles < 8 || room < 2 ? 1 : ceil_div(tiles, 4) < room ? ceil_div(tiles, 4) : room;
+        // bounds the workspace), but no more than the workspace at hand has room for
+        const int64_t tiles = ceil_div(max_len, tile), most_chunks = 2 * (resident / units) + 1, by_room = (int64_t)(room / ((size_t)n * q_heads * (dim + 1) * 4));
+        a.splits = tiles < 8 ? 1 : ceil_div(tiles, 4) < most_chunks ? ceil_div(tiles, 4) : most_chunks;
+        if (a.splits > by_room) a.splits = by_room > 1 ? by_room : 1;
         a.by_length = a.splits > 1;
         a.workspace = a.by_length ? (size_t)n * q_heads * a.splits * (dim + 1) * 4 : 0;
         a.chunk = tiles * tile > 0 ? tiles * tile : tile;
@@ -958,15 +960,16 @@ AttnPlan plan_rows(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int6
 
 }  // namespace
 
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree)
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree,
+                        size_t room)
 {
     if (max_q > n) max_q = n;
-    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, true, tree);
+    AttnPlan a = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, true, tree, room);
     if (a.prompt || a.row_eights != 4) return a;
     // 32 rows a warp save conversions, 16 hide latency better: taken unless a few chunks of all sequences fit side by side
     // (32 sequences of four drafted tokens, window 1024: 32 rows 19 us, 16 rows 29; 64 sequences of 4100 keys: 83 and 79; 16 of
     // 8000, eight tokens: 75 and 66).  The workspace is that of either, whatever the window.
-    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, false, tree);
+    AttnPlan b = plan_rows(n, seqs, max_q, max_len, window, sinks, q_heads, kv_heads, dim, false, tree, room);
     a.workspace = b.workspace = a.workspace > b.workspace ? a.workspace : b.workspace;
     return a.cluster ? a : b;
 }

@@ -149,7 +149,9 @@ struct AttnPlan {
     bool by_length;
     size_t workspace;
 };
-AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree);
+// room: bytes of workspace at hand, for trees of many rows, which take more of it where there is more (any other plan asks for what it needs)
+AttnPlan plan_attention(int64_t n, int64_t seqs, int64_t max_q, int64_t max_len, int64_t window, int64_t sinks, int q_heads, int kv_heads, int dim, bool tree,
+                        size_t room);
 cudaError_t launch_attention(AttnParams P, const AttnPlan& plan, void* workspace, cudaStream_t stream);
 cudaError_t read_attn_counters(unsigned int* timeouts, unsigned int* bad);
 cudaError_t reset_attn_timeouts();
