@@ -398,8 +398,8 @@ def _run_own(c):
         b.mxkv_compact(c["kept"], c["new_lens"], c["lens"], c["page_table"], c["k_codes"], c["k_scales"], c["v_codes"], c["v_scales"],
                        out_page_table=c["out_table"], weights=c["weights"])
         return _evicted(c)
-    ws = _workspace(c, lambda: b.mxkv_attention_workspace_bytes(c["n"], c["seqs"], c["q_max"], c["len_max"], c["q_heads"], c["kv_heads"],
-                                                                c["dim"]))
+    size = b.mxkv_attention_tree_workspace_bytes if c["op"] == "tree" else b.mxkv_attention_workspace_bytes
+    ws = _workspace(c, lambda: size(c["n"], c["seqs"], c["q_max"], c["len_max"], c["q_heads"], c["kv_heads"], c["dim"]))
     cache = (c["k_codes"], c["k_scales"], c["v_codes"], c["v_scales"])
     if c["op"] == "sinks":
         b.mxkv_attention_sinks(c["q"], c["cu"], c["lens"], c["page_table"], *cache, c["out"], c["q_max"], c["len_max"], c["scale"],
