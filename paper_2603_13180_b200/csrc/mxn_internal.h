@@ -166,7 +166,7 @@ struct WeightsParams {
     // filled by the plan
     int many;                   // many rows: the tcgen05 kernel, with
     int tile_heads, tile_tokens, head_parts;   // heads and tokens of a tile of queries, parts of a key head's query heads
-    int key_tiles, ranks;       // of 256 keys; CTAs (a cluster) that share out the queries of a key tile
+    int ranks;                  // CTAs (a cluster) that share out the queries of a tile of 256 keys
 };
 int64_t plan_weights(WeightsParams& W);   // shares the work out; returns the number of CTAs
 cudaError_t launch_weights_many(const WeightsParams& W, int64_t ctas, cudaStream_t stream);

@@ -547,16 +547,11 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 5 : 3) compact_kerne
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <class K, class... Args>
-cudaError_t launch(K kernel, int64_t ctas, int cluster, int threads, int smem, cudaStream_t stream, const Args&... args)
+cudaError_t launch(K kernel, int64_t ctas, int cluster, int threads, cudaStream_t stream, const Args&... args)
 {
-    if (smem > 16 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -576,8 +571,8 @@ cudaError_t launch_select(const SelectParams& P, cudaStream_t stream)
     const int64_t lists = (int64_t)P.seqs * P.heads;
     int cluster = 1;
     while (cluster < 8 && lists * cluster * 2 <= 148 && P.max_len > 1024 * cluster) cluster *= 2;
-    if (P.max_len > (int64_t)cluster * 16 * 128 * kHeld) return launch(select_kernel<32>, lists * cluster, cluster, 1024, 0, stream, P, cluster);
-    return launch(select_kernel<16>, lists * cluster, cluster, 512, 0, stream, P, cluster);
+    if (P.max_len > (int64_t)cluster * 16 * 128 * kHeld) return launch(select_kernel<32>, lists * cluster, cluster, 1024, stream, P, cluster);
+    return launch(select_kernel<16>, lists * cluster, cluster, 512, stream, P, cluster);
 }
 
 // units of places that max_kept entries reach into, wherever the first stands
@@ -594,7 +589,7 @@ cudaError_t launch_compact(CompactParams P, cudaStream_t stream)
         const cudaError_t e = cudaMemsetAsync(P.work, 0, (size_t)(units + 1) * 4, stream);
         if (e != cudaSuccess) return e;
     }
-    auto go = [&](auto kernel) { return launch(kernel, ctas, 1, kMoveWarps * 32, 0, stream, P); };
+    auto go = [&](auto kernel) { return launch(kernel, ctas, 1, kMoveWarps * 32, stream, P); };
     if (P.dim == 128) return wide ? (in_place ? go(compact_kernel<128, true, 2>) : go(compact_kernel<128, false, 2>))
                                   : (in_place ? go(compact_kernel<128, true, 1>) : go(compact_kernel<128, false, 1>));
     return wide ? (in_place ? go(compact_kernel<64, true, 2>) : go(compact_kernel<64, false, 2>))

@@ -276,9 +276,8 @@ int64_t plan_weights(WeightsParams& W)
         W.tile_heads = P.group < 128 ? P.group : 128;
         W.tile_tokens = 128 / W.tile_heads < P.n ? 128 / W.tile_heads : (int)P.n;
         W.head_parts = (int)ceil_div(P.group, W.tile_heads);
-        W.key_tiles = (int)ceil_div(P.max_len, 256);
         // CTAs for a key tile: more while the SMs are not filled twice and each still has four query tiles
-        const int64_t units = (int64_t)W.key_tiles * P.seqs * P.kv_heads, tiles = ceil_div(P.max_q, W.tile_tokens) * W.head_parts;
+        const int64_t units = ceil_div(P.max_len, 256) * P.seqs * P.kv_heads, tiles = ceil_div(P.max_q, W.tile_tokens) * W.head_parts;
         W.ranks = 1;
         while (W.ranks < 8 && units * W.ranks < 2 * 148 && tiles >= 8 * W.ranks) W.ranks *= 2;
         return units * W.ranks;
