@@ -1,4 +1,4 @@
-// Shared-memory barriers and bulk copies used by the kernels that feed themselves through a ring of stages.
+// Shared-memory barriers and bulk copies used by the kernels that feed themselves through a ring of stages; clusters of CTAs.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -40,6 +40,35 @@ __device__ __forceinline__ uint4 lds_v4(uint32_t addr)
     uint4 r;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
     return r;
+}
+
+// ---- clusters: a barrier of all threads of the cluster's CTAs; shared memory of the CTA of that rank, at the address that it has in this one ----
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote_address(uint32_t addr, int rank)
+{
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ uint32_t remote_u32(uint32_t addr, int rank)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(remote_address(addr, rank)));
+    return v;
+}
+__device__ __forceinline__ uint4 remote_v4(uint32_t addr, int rank)
+{
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote_address(addr, rank)));
+    return v;
+}
+__device__ __forceinline__ float4 remote_f4(uint32_t addr, int rank)
+{
+    const uint4 v = remote_v4(addr, rank);
+    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
 }
 
 }  // namespace mxn

@@ -42,7 +42,6 @@ namespace mxn {
 
 namespace {
 
-constexpr int kSMs = 148;
 constexpr int kWarps = 4;
 // CTAs an SM that the register allocation makes room for
 __host__ __device__ constexpr int decode_ctas(int dim, int nq) { return nq == 1 ? (dim == 128 ? 3 : 4) : dim == 128 || nq == 4 ? 2 : 3; }
@@ -53,21 +52,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ unsigned int g_attn_timeouts = 0;
 __device__ unsigned int g_attn_bad = 0;   // pages out of range within a sequence's length
 
-__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// the four E4M3 codes of a word -> two f16 pairs
-__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi)
-{
-    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 // transposes an 8 x 8 matrix of f16: row g, columns 2c, 2c + 1 in a thread's register
 __device__ __forceinline__ uint32_t turn8x8(uint32_t v)
 {
@@ -105,27 +89,6 @@ struct DecodeShape {
     static constexpr int kJoinBytes = kGroups * kRows * ((DIM + 4) * 4 + 8);
     static constexpr int kSmem = (kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes) + 1024;
 };
-
-// ---- clusters: the CTAs that hold the chunks of the same rows ----
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t remote_u32(uint32_t addr, int rank)
-{
-    uint32_t at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at));
-    return v;
-}
-__device__ __forceinline__ float4 remote_f4(uint32_t addr, int rank)
-{
-    uint32_t at;
-    float4 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
-    return v;
-}
 
 // NQ: groups of eight query rows that a warp works on (they share the widened codes); RW: warps that share out the rows
 template <int DIM, int RW, int NQ, int STAGES, int MASK>
@@ -886,8 +849,6 @@ cudaError_t launch_rows(const AttnParams& P, const AttnMaps& M, const AttnPlan& 
          : a.row_eights == 2 ? launch_decode<64, 1, 2, 3>(P, M, a.ctas, stream)
          : a.row_warps == 1  ? launch_decode<64, 1, 4, 3>(P, M, a.ctas, stream) : launch_decode<64, 2, 4, 3>(P, M, a.ctas, stream);
 }
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 

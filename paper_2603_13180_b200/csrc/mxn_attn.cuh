@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_fp16.h>
 
 #include "mxn_async.cuh"
 #include "mxn_device.cuh"
@@ -97,6 +98,22 @@ __device__ __forceinline__ float times_pow2(float v, float d)
 {
     const float h = floorf(0.5f * d);
     return v * ex2(h) * ex2(d - h);
+}
+// a product of 16 x 16 by 16 x 8, binary32 sums
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the four E4M3 codes of a word -> two f16 pairs
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 // 2^(byte - 127), the value of an E8M0 byte
 __device__ __forceinline__ float e8m0_to_f32(uint32_t b) { return __uint_as_float(b == 0 ? 0x00400000u : b << 23); }

@@ -27,7 +27,6 @@
 
 namespace mxn {
 
-constexpr int kSMs = 148;          // B200
 
 __device__ unsigned int g_bwd_timeouts = 0;
 

@@ -21,7 +21,6 @@ namespace mxn {
 
 namespace {
 
-constexpr int kSMs = 148;   // B200
 constexpr int kWarps = 4;   // per CTA
 
 __device__ unsigned int g_heads_bad = 0;   // tokens whose position lies outside the table

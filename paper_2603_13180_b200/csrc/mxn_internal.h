@@ -6,6 +6,9 @@
 
 namespace mxn {
 
+constexpr int kSMs = 148;   // B200
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 enum { STAT_NONE = 0, STAT_RMS = 1, STAT_MX = 2, STAT_POSTROUND = 3 };
 enum { ELEM_E4M3 = 0, ELEM_E2M1 = 1, ELEM_E5M2 = 2 };
 

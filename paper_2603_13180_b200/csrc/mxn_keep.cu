@@ -20,6 +20,7 @@
 // CTAs a cluster took twice that.  In place either move takes 1.4 times what it takes to other pages.
 #include <cuda_fp16.h>
 
+#include "mxn_async.cuh"
 #include "mxn_device.cuh"
 #include "mxn_internal.h"
 
@@ -33,19 +34,6 @@ __device__ unsigned int g_keep_bad = 0;   // entries, pages or lengths out of ra
 constexpr int kBins = 2048;
 constexpr int kHeld = 4;   // runs of four tokens of a thread that are held in registers; with more all are read again
 
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t remote_u32(uint32_t addr, int rank)
-{
-    uint32_t at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
-}
-
 // Orders as unsigned numbers: -infinity ... -0 = 0 ... infinity; NaN below all.  0 and kSure are no weight's.
 constexpr uint32_t kSure = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t ordered(float w)
@@ -53,14 +41,6 @@ __device__ __forceinline__ uint32_t ordered(float w)
     if (w != w) return 1u;
     const uint32_t b = __float_as_uint(w + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ uint4 remote_v4(uint32_t addr, int rank)
-{
-    uint32_t at;
-    uint4 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
 }
 __device__ __forceinline__ uint32_t warp_sum_u32(uint32_t v) { return __reduce_add_sync(0xFFFFFFFFu, v); }
 
@@ -151,7 +131,7 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
         // thread i: bins BINS i ... from the top, of all CTAs; an inclusive sum from the top over the block
         const int b0 = kBins - BINS * (1 + (int)threadIdx.x);
         uint32_t n[4] = {0u, 0u, 0u, 0u};   // bins b0 ...
-        const uint32_t quad = smem_at(&hist[pass][b0 & ~3]);
+        const uint32_t quad = smem_u32(&hist[pass][b0 & ~3]);
 #pragma unroll
         for (int r = 0; r < 8; ++r)
             if (r < cluster) {
@@ -222,7 +202,7 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 2 : 1) select_kernel
             counts[1] = all_e;
         }
         cluster_sync();
-        const uint32_t other_a = lane < rank ? remote_u32(smem_at(&counts[0]), lane) : 0u, other_e = lane < rank ? remote_u32(smem_at(&counts[1]), lane) : 0u;
+        const uint32_t other_a = lane < rank ? remote_u32(smem_u32(&counts[0]), lane) : 0u, other_e = lane < rank ? remote_u32(smem_u32(&counts[1]), lane) : 0u;
         a_before += warp_sum_u32(other_a);
         e_before += warp_sum_u32(other_e);
     }
@@ -544,8 +524,6 @@ __global__ void __launch_bounds__(kMoveWarps * 32, K == 1 ? 5 : 3) compact_kerne
     }
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 template <class K, class... Args>
 cudaError_t launch(K kernel, int64_t ctas, int cluster, int threads, cudaStream_t stream, const Args&... args)
 {
@@ -570,7 +548,7 @@ cudaError_t launch_select(const SelectParams& P, cudaStream_t stream)
     // CTAs of a sequence and head: more while one an SM is not reached and each still has 1024 tokens; of 32 warps where 16 would not hold their tokens
     const int64_t lists = (int64_t)P.seqs * P.heads;
     int cluster = 1;
-    while (cluster < 8 && lists * cluster * 2 <= 148 && P.max_len > 1024 * cluster) cluster *= 2;
+    while (cluster < 8 && lists * cluster * 2 <= kSMs && P.max_len > 1024 * cluster) cluster *= 2;
     if (P.max_len > (int64_t)cluster * 16 * 128 * kHeld) return launch(select_kernel<32>, lists * cluster, cluster, 1024, stream, P, cluster);
     return launch(select_kernel<16>, lists * cluster, cluster, 512, stream, P, cluster);
 }

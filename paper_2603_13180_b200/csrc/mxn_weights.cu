@@ -15,8 +15,6 @@
 // of a copy's rate.  Two sets of registers and four CTAs an SM took 94 us, one set and five 74, with fewer instructions beside the products 70 (some 490 a
 // tile now, of which 145 are products, conversions and exponentials: half of the issue slots).  A ring of tiles filled by the tensor copy
 // engine took 73 with two stages a warp and 80 with three (fewer warps fit beside more shared memory), six CTAs an SM 78 (spills).
-#include <cuda_fp16.h>
-
 #include "mxn_attn.cuh"
 
 namespace mxn {
@@ -27,21 +25,6 @@ constexpr int kWarps = 4, kTile = 32, kRows = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ unsigned int g_weights_bad = 0;   // pages out of range within a sequence's length
-
-__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi)
-{
-    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
@@ -248,8 +231,6 @@ __global__ void __launch_bounds__(kWarps * 32, FEW ? 5 : 4) key_weights_kernel(c
     if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicAdd(&g_weights_bad, 1u);
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 template <class K>
 cudaError_t launch(K kernel, int64_t ctas, cudaStream_t stream, const WeightsParams& W)
 {
@@ -279,14 +260,14 @@ int64_t plan_weights(WeightsParams& W)
         // CTAs for a key tile: more while the SMs are not filled twice and each still has four query tiles
         const int64_t units = ceil_div(P.max_len, 256) * P.seqs * P.kv_heads, tiles = ceil_div(P.max_q, W.tile_tokens) * W.head_parts;
         W.ranks = 1;
-        while (W.ranks < 8 && units * W.ranks < 2 * 148 && tiles >= 8 * W.ranks) W.ranks *= 2;
+        while (W.ranks < 8 && units * W.ranks < 2 * kSMs && tiles >= 8 * W.ranks) W.ranks *= 2;
         return units * W.ranks;
     }
     // Chunks of 32 tiles (eight for each warp), or of one tile for each warp where CTAs would be fewer than three an SM; nothing is joined,
     // so a chunk costs no more than its start.
     const int64_t units = (int64_t)P.seqs * P.kv_heads, least = kWarps * kTile;
     P.chunk = 8 * least;
-    if (units * ceil_div(P.max_len, P.chunk) < 3 * 148) P.chunk = least;
+    if (units * ceil_div(P.max_len, P.chunk) < 3 * kSMs) P.chunk = least;
     P.splits = (int)ceil_div(P.max_len, P.chunk);
     return units * P.splits;
 }

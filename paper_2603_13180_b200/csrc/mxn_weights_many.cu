@@ -63,18 +63,6 @@ struct alignas(16) Columns {
     int special;          // kNan: a NaN is among them; kUnseeing: a row that saw nothing
 };
 
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ float remote_f32(uint32_t addr, int rank)
-{
-    uint32_t at;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
-}
 __device__ __forceinline__ void tma_load_queries(uint32_t dst, const CUtensorMap* map, int x, int head, int token, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -424,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
     if ((int)threadIdx.x < share && key < k1) {
         float w = 0.0f;
         if (W.ranks > 1)
-            for (int i = 0; i < W.ranks; ++i) w += remote_f32(smem_u32(total + at), i);
+            for (int i = 0; i < W.ranks; ++i) w += __uint_as_float(remote_u32(smem_u32(total + at), i));
         else
             w = total[at];
         const int page = __ldg(P.page_table + (int64_t)seq * P.max_pages + (key >> P.page_shift));
