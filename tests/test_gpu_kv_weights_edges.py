@@ -102,3 +102,21 @@ def test_nan_in_any_row(mx, qh, h, nq, where):  # noqa: F811
             y[row, 1] = math.nan
         got = of_tokens(summed(mx, x, y, table, cache, length, causal=False), table, length)
         assert bool(got[:, 1].isnan().all()) and not bool(got[:, 0].isnan().any()), row
+
+
+@pytest.mark.parametrize("qh,h,nq", [FEW, (8, 2, 12), MANY])
+@pytest.mark.parametrize("binades", [-116, -100, 0, 100])
+def test_small_scales_of_the_scores(mx, qh, h, nq, binades):  # noqa: F811
+    """The scores' scale far below 1 / sqrt(dim), over keys that are larger by as much: a factor of small queries and the scale has to keep its bits."""
+    length, dim, scale = 400, 64, 2.0 ** -10
+    table, cache, q = setting(qh, h, dim, nq, length, seed=nq, binades=binades)
+    scales = cache.parts[1]
+    scales.copy_(torch.where(scales == 255, scales, scales + 7))
+    masks = [kr.sinks_mask(nq, length, 0, 0, device="cuda")]
+    lse = kr.attention(q, [0, nq], [length], table, *cache.parts[:2], *cache.parts[:2], scale, masks)[1].float()
+    sums = torch.full(cache.parts[1].shape[:2] + (32,), 7.0, device="cuda")
+    mx.mxkv_attention_weights(q, dev([0, nq]), dev([length]), dev(table), cache.parts[0], cache.parts[1], lse, sums, nq, length, scale)
+    want = torch.full_like(sums, 7.0).double()
+    slack = kr.weights(q, lse, [0, nq], [length], table, *cache.parts[:2], scale, masks, want, None)
+    err = (sums.double() - want).abs()
+    assert bool((err <= slack).all()), f"off by {float((err / slack.clamp(min=1e-30)).nan_to_num(math.inf).max()):.3g} tolerances"
