@@ -6,7 +6,8 @@
 // is exact, two at a time in registers, and multiplied there with binary32 sums (mma m16n8k16), keys and values as the 16-row
 // operand, so that the query rows are the 8 columns: eight query heads that share a key head fill a product.
 //   q  is scaled by a power of two that brings the row's largest magnitude to [2^14, 2^15), so that f16 holds a bf16 value exactly
-//      but for elements below 2^-28 of the row's largest (to 2^-39 of it).
+//      but for elements below 2^-28 of the row's largest (to 2^-39 of it).  The power is at most 2^110, by which f16 still holds the smallest bf16
+//      (2^-133 times it is 2^-23): the factor that takes it back, with the scores' scale, then stays a normal number for scales down to 2^-16.
 //   The scales of the cache never touch the codes: a key block's scale multiplies the finished product, a value block's is
 //      folded into the softmax's weight, w_t = 2^(s_t + sv_t - R + 1) in f16.  The reference R (an integer, so that corrections of
 //      the sums are exact) is moved when a tile's largest s + sv is 14 above or 16 below it: f16 keeps 11 bits of what is above
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kWarps * 32, decode_ctas(DIM, NQ)) attn_decode
 #pragma unroll
         for (int i = 0; i < DIM / 8; ++i) m = absmax_bf16x2(m, u[i]);
         const uint32_t E = __float_as_uint(quad_max(hmax_abs_to_f32(m))) >> 23;
-        const uint32_t Ec = min(max(E, 15u), 254u);
+        const uint32_t Ec = min(max(E, 31u), 254u);
         // 2^(14 - (E - 127)); with an infinity or NaN in the row its result is NaN
         const float up = E == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((268u - Ec) << 23);
         const float factor = P.scale * kLog2e * __uint_as_float((Ec - 14u) << 23);          // ... and its inverse
