@@ -394,8 +394,8 @@ mxn_status mxkv_append(const void* k_bf16, int64_t k_stride, const void* v_bf16,
  *   max_q_len are not computed - their rows may receive undefined values - and keys past max_kv_len are not seen; the places of the others
  *   stay as kv_lens and cu_q give them).
  *   lse_out [n_tokens, q_heads] fp32: the logarithm of the sum of exp(scale q k) over the keys seen.
- *   Products run on the E4M3 codes with binary32 sums.  q enters exactly, but for elements below 2^-10 of their row's largest,
- *   which are kept to 2^-18 of it; the softmax's weights have 11 significant bits (fewer where a weight times its value block's
+ *   Products run on the E4M3 codes with binary32 sums.  q enters exactly, but for elements below 2^-9 of their row's largest,
+ *   which are kept to 2^-17 of it; the softmax's weights have 11 significant bits (fewer where a weight times its value block's
  *   scale lies below 2^-13 of the row's largest such product, possibly none below 2^-24 of it), its sums are binary32 and count every weight.
  *   What stands in the cache behind a sequence's last token, before every query's window, or in pages no visible key is in, has no
  *   influence: pages behind a sliding window may be released.  A page out of range among the visible ones: its keys are left out.
@@ -445,7 +445,7 @@ size_t mxkv_attention_tree_workspace_bytes(int64_t n_tokens, int64_t n_seqs, int
  *   window and sinks (sinks > 0 needs causal and a window).  weights and earlier are fp32 [num_pages, kv_heads, page_size]; earlier may
  *   be weights itself, or NULL (nothing).  A call's own new tokens have nothing from earlier: their places in `earlier` are not read.
  *   Every token of every sequence up to max_kv_len is written, a sequence without new tokens or keys that no row sees included (earlier + 0);
- *   places of no token are left as they are.  Rows past max_q_len, and rows whose lse is -infinity, give nothing.  A NaN in a row, its lse or a key that
+ *   places of no token are left as they are.  Rows past max_q_len, and rows whose lse is -infinity, give exactly nothing.  A NaN in a row, its lse or a key that
  *   it sees makes the sums concerned NaN.  Tokens whose page is out of range are left out.  Sums are binary32 in a fixed order.
  *   A page in which sums are written belongs to one sequence of the call (of a page shared by several the sums are one of theirs). */
 mxn_status mxkv_attention_weights(const void* q_bf16, int64_t q_stride, int64_t n_tokens, int q_heads, int kv_heads, int head_dim,

@@ -15,9 +15,9 @@
 // ends.  (All waits are bounded; see mxn_device_timeouts.)
 //
 // Measured, 8 heads of 128 in blocks of 16, choice and move to other pages together: 32 sequences of up to 8192 tokens brought to 2048, 66 us
-// (the move 50: 0.27 GB, 5.4 TB/s; rows of 128 bytes read from all over bound it: with four CTAs an SM it took 55, and without its arithmetic
-// 50); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16
-// CTAs a cluster took twice that.  In place either move takes 1.4 times what it takes to other pages.
+// (the move 50: 0.27 GB, 5.4 TB/s, HBM busy for 55 %: what its warps wait for is loads that follow one another, list, page, then rows and scales;
+// with four CTAs an SM in place of five it took 55); one of 131072 brought to 32768, 55 us, of which the choice takes some 25: 64 CTAs, instructions and three trips across the cluster; 16
+// CTAs a cluster took twice that.  In place either move takes 1.4 times what it takes to other pages (74 and 53 us by replays).
 #include <cuda_fp16.h>
 
 #include "mxn_async.cuh"

@@ -12,8 +12,8 @@
 // The two row tiles alternate: while one's scores are in the softmax, the other's products run.
 //
 // Scores: E4M3 x E4M3 products on the key codes as they are; q is scaled by a power of two to [128, 256) at its row's largest
-//   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-10 of the row's largest (to 2^-18
-//   of it).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
+//   and written as a sum of two E4M3 numbers, hi + lo, which is exact but for elements below 2^-9 of the row's largest (to 2^-17
+//   of it: below 1/4 a bf16 reaches under the smallest code, 2^-9).  Two products of twice f16's rate cost what one in f16 would, and the keys need no conversion.
 // Weights: w_t = 2^(s_t + sv_t - R + 1) in f16 (11 significant bits): the value block's scale is folded into the weight, so that the
 //   codes enter the second product without a scale.  R (an integer: corrections are exact) is the first tile's largest s + sv and
 //   is moved only when a step's largest is 14 above or 16 below it, so that the output in tensor memory rarely has to be corrected.

@@ -18,11 +18,11 @@
 //
 // Bound: at head size 128 a product of 128 keys and 128 rows takes 512 cycles of the tensor cores, its 16384 exponentials 1024 of the special
 // function units; three pairs of exponentials in 16 are computed on the multipliers instead.  4096 queries over 8192 keys, 32 query and 8 key heads
-// of 128: 257 us, 0.49 of a large library product's measured rate, the special function units busy for two thirds of the time, issue slots for 53 %.
+// of 128: 255 us, 0.49 of a large library product's measured rate, the special function units busy for two thirds of the time, issue slots for 53 %.
 // Eight prompts of up to 1000 queries over up to 1500 keys, 32 and 4 heads of 64: 56 us, of which some 10 are starts and ends of CTAs.
 // What mattered (4096 queries): products announced by number and two warpgroups for a product, 64 columns each, instead of whole products in turn
-// (280 us); the products that a mask touches in a loop of their own with loads of their own (280 -> 263: the common path had carried 32 moves for
-// each 32 columns along); 32 columns in registers at a time (-> 259).  What did not: six buffers of 64 columns (305: the products are issued one
+// (280 us); the products that a mask touches in a loop of their own with loads of their own (280 -> 263);
+// 32 columns in registers at a time (-> 259).  What did not: six buffers of 64 columns (305: the products are issued one
 // every 50 cycles), the next product's columns loaded ahead (276-303), more exponentials on the multipliers (five in 16: 262, seven: 287, in part
 // because its constants find no room in registers), three warpgroups for a product of 96 columns (286-302), eight or one CTA for a key tile (340, 328).
 // The copies of queries cost nothing (the same time without them).
@@ -353,8 +353,8 @@ __global__ void __launch_bounds__(kThreads, 1) key_weights_many_kernel(const Wei
                     }
                 }
             } else {
-                // Columns [lo, hi) of these see this key.  In a short loop with loads of its own: with the registers of the common path that one carried
-                // 32 moves for each 32 columns along.
+                // Columns [lo, hi) of these see this key.  In a short loop with loads of its own: as a branch over the common path's registers it cost
+                // that path 17 of 280 us.
                 const int valid = min(T, S.nq - t.token) * min(GB, P.group - t.part * GB);
                 const int64_t ahead = place - t.token;
                 const int from = P.causal ? (int)max((int64_t)0, min((int64_t)T, ahead)) : 0;
