@@ -120,3 +120,17 @@ def test_small_scales_of_the_scores(mx, qh, h, nq, binades):  # noqa: F811
     slack = kr.weights(q, lse, [0, nq], [length], table, *cache.parts[:2], scale, masks, want, None)
     err = (sums.double() - want).abs()
     assert bool((err <= slack).all()), f"off by {float((err / slack.clamp(min=1e-30)).nan_to_num(math.inf).max()):.3g} tolerances"
+
+
+@pytest.mark.parametrize("qh,h,nq", [(2, 2, 5), (2, 2, 128), (6, 2, 100)])
+def test_nan_in_a_key(mx, qh, h, nq):  # noqa: F811
+    """A NaN code makes its own key's sum NaN and no other, with an lse that knows nothing of it."""
+    length = 300
+    table, cache, q = setting(qh, h, 64, nq, length, seed=nq)
+    masks = [kr.sinks_mask(nq, length, 0, 0, causal=False, device="cuda")]
+    lse = kr.attention(q, [0, nq], [length], table, *cache.parts[:2], *cache.parts[:2], 0.125, masks)[1].float()
+    bad = [0, 31, 128, 255, 299]
+    for t in bad:
+        cache.parts[0][table[0][t // 32], 1, t % 32, t % 64] = 0x7F
+    got = of_tokens(summed(mx, q, lse, table, cache, length, causal=False), table, length)
+    assert got[:, 1].isnan().nonzero().flatten().tolist() == bad and not bool(got[:, 0].isnan().any())
